@@ -27,8 +27,8 @@
  *     launch error after enqueueing returns VP_ERR_HIP; vp_last_error() then
  *     gives the message (thread-local).
  *   - Q, K, V, Y are [N, H, d] row-major (token-major; the d values of one
- *     head of one token are contiguous).  Supported: 1 <= H <= 16, d = 64,
- *     router/surrogate hidden size L = 64, dtype fp32 or bf16 (fp32
+ *     head of one token are contiguous).  Supported: 1 <= H <= 16 (the paged
+ *     cache has limits of its own), d = 64, router/surrogate hidden size L = 64, dtype fp32 or bf16 (fp32
  *     accumulation everywhere).
  *   - Numeric anomalies never fail a call: a NaN routing score sends its head
  *     to FULL and sets bit 0 of the flags word of `buckets`.
@@ -383,6 +383,117 @@ vp_status vp_tome_merge_qkv(const vp_shape *shape, const void *Q, const void *K,
                             void *Qm, void *Km, void *Vm, void *stream);
 vp_status vp_tome_unmerge(const vp_shape *shape, const void *Ym, int64_t nrows,
                           const int32_t *row, void *Y, void *stream);
+
+/* ---------------------------------------------------------------------------
+ * Paged key-value cache: exact attention of views (or tokens) that arrive one
+ * chunk after another, for several sequences at once.  Keys and values of the
+ * tokens seen so far lie in pages of a common pool; per slot the pool also
+ * holds the attention weight its key has gathered and its token's number.
+ *
+ * Layout: K, V [npages, Hkv, page, 64] in `dtype` (bf16 or fp32); weight fp32 and
+ * stamp int32 [npages, Hkv, page].  Slot s of sequence b is slot s % page of
+ * page table[b][s / page]; entries past a sequence's last slot are not read, a
+ * number outside [0, npages) makes its slots invisible.  A page belongs to one
+ * sequence.  1 <= Hkv <= Hq <= 128, Hq a multiple of Hkv (query heads h of the
+ * G = Hq / Hkv from hk G on share key head hk); page a power of two, 16 to 4096.
+ *
+ * A call serves B sequences; sequence b's new tokens are rows q_start[b] ..
+ * q_start[b + 1] - 1 of the call's T tokens (none is allowed), and lie in its
+ * last slots: length[b] counts all slots in use, the chunk's included, and
+ * seen[b] all tokens so far, the chunk's included (length without evictions).  The
+ * arrays are on the device; the host gives bounds: no chunk has more than
+ * max_q tokens and no sequence more than max_len <= max_pages * page slots.
+ * Values beyond a bound are cut to it; rows from q_start[B] on are left alone.
+ * Rows of Q, K, V are [H, 64] contiguous, tokens *_stride elements apart (16-byte
+ * multiples), so slices of one projection's output serve as they are. */
+typedef struct {
+    void *K, *V;
+    float *weight;   /* may be NULL where an operator does not need it */
+    int32_t *stamp;
+    int64_t npages;
+    int32_t page, Hkv, d;
+    vp_dtype dtype;
+} vp_cache;
+
+typedef struct {
+    const int32_t *table;    /* [B, max_pages] */
+    const int32_t *length;   /* [B] */
+    const int32_t *seen;     /* [B]; append with stamps, evict */
+    const int32_t *q_start;  /* [B + 1]; append, attend */
+    int32_t B, max_pages, T, max_q, max_len;
+} vp_cache_batch;
+
+/* Rotary positions: the first `dim` (even, 0 to 64) features of a head form
+ * `axes` (1 to 4) equal sections, section a turned by pos[t][a].  HALF pairs feature j of
+ * a section with j + half the section, INTERLEAVED 2j with 2j + 1.  A pair (x0, x1)
+ * becomes mag (x0 cos - x1 sin, x1 cos + x0 sin) of the angle 2 pi pos freq / 2^64, freq
+ * per pair in the order of the sections; pos * freq is taken modulo a
+ * revolution exactly, for any int32 position. */
+typedef enum { VP_ROT_INTERLEAVED = 0, VP_ROT_HALF = 1 } vp_rot_layout;
+typedef struct {
+    const int32_t *pos;      /* device [T, axes] */
+    const uint64_t *freq;    /* device [dim / 2]; 8-byte aligned */
+    int32_t dim, axes;
+    vp_rot_layout layout;
+    float mag;               /* 1 when 0 */
+} vp_rotary_spec;
+
+/* Frequencies base^(-2j / section) of every section, in host memory, and the
+ * factor on the rotated features.  NONE: as they are.  LINEAR: divided by `factor`.
+ * PARTS (for contexts `factor` times the `original` one): a pair that turns at most
+ * `low` times over `original` positions is divided by `factor`, one that turns at
+ * least `high` times is kept, linearly blended between; *mag = 0.1 ln factor + 1 (1
+ * for the others).  base > 1, factor >= 1, 0 <= low < high, original > 0 (PARTS). */
+typedef enum { VP_ROT_SCALE_NONE = 0, VP_ROT_SCALE_LINEAR = 1, VP_ROT_SCALE_PARTS = 2 } vp_rot_scaling;
+vp_status vp_rotary_frequencies(int32_t dim, int32_t axes, double base, vp_rot_scaling scaling,
+                                double factor, double original, double low, double high,
+                                uint64_t *freq, float *mag);
+
+/* y = rotated x, or with `transpose` the transposed map (the gradient of x from
+ * that of y).  [T, H, 64] in `dtype`, arithmetic in fp32, one rounding; y may be x. */
+vp_status vp_rotary(const vp_rotary_spec *rot, vp_dtype dtype, int32_t T, int32_t H,
+                    const void *x, int64_t x_stride, void *y, int64_t y_stride,
+                    int32_t transpose, void *stream);
+
+/* Append: K rotated and V as it is into the sequences' last slots, Q rotated
+ * into Q_out [T, Hq, 64] (Q may be NULL, or Q_out the same contiguous tensor); the
+ * slots' weight becomes 0, their stamp the token's number, 0 for a sequence's
+ * first.  rot may be NULL: no rotation. */
+vp_status vp_cache_append(const vp_cache *cache, const vp_cache_batch *batch, int32_t Hq,
+                          const void *Q, int64_t q_stride, const void *K, int64_t k_stride,
+                          const void *V, int64_t v_stride, const vp_rotary_spec *rot,
+                          void *Q_out, void *stream);
+
+/* Attend: row (t, h) sees the first `length` slots of its sequence, with `causal`
+ * the first length - n + i + 1 (token i of n in the chunk).  With x_j = scale q . k_j
+ * (1/8 when 0; positive), O = sum_j e^(x_j - lse) v_j [T, Hq, 64] in the cache's dtype and
+ * lse = log sum_j e^x_j [T, Hq] fp32.  A row that sees no slot, or only
+ * logits of -inf, gives zeros and -inf; slots a row does not see never reach it,
+ * whatever they hold.  With weight_out (fp32, laid out as cache->weight, which may be
+ * the same array), weight_out = weight + the sum over the chunk's tokens and the key head's query
+ * heads of e^(x_j - lse), for every slot in use of the sequences with new tokens.
+ * Logits, sums and results in fp32; bf16 caches round the probabilities of the
+ * value product to bf16.  Deterministic (no atomics; the work's division follows from
+ * the host's sizes). */
+size_t vp_cache_attend_workspace_bytes(const vp_cache *cache, const vp_cache_batch *batch,
+                                       int32_t Hq);
+vp_status vp_cache_attend(const vp_cache *cache, const vp_cache_batch *batch, int32_t Hq,
+                          const void *Q, int64_t q_stride, int32_t causal, float scale, void *O,
+                          float *lse, float *weight_out, void *ws, size_t ws_bytes,
+                          void *stream);
+
+/* Evict: of every sequence and key head, n = min(length, keep) slots stay: first
+ * the protected ones (stamp < sink, or stamp >= seen - recent), then by weight, the
+ * largest first (NaN before all numbers), the lower slot first among equals.
+ * Kept slots past n move into the freed ones below, both in ascending
+ * order; key, value, weight and stamp go together.  weight_out and stamp_out
+ * (laid out as the cache's arrays, which they may be) get the n slots' values, length_out
+ * [B] (may be batch->length) n.  K and V are changed in place.  The freed pages are the
+ * table's entries from ceil(n / page) on.  keep >= 1, sink, recent >= 0. */
+size_t vp_cache_evict_workspace_bytes(int32_t B, int32_t Hkv, int32_t max_len);
+vp_status vp_cache_evict(const vp_cache *cache, const vp_cache_batch *batch, int32_t keep,
+                         int32_t sink, int32_t recent, float *weight_out, int32_t *stamp_out,
+                         int32_t *length_out, void *ws, size_t ws_bytes, void *stream);
 
 /* Static description of a status code. */
 const char *vp_status_string(vp_status s);

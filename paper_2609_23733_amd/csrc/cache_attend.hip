@@ -1,0 +1,844 @@
+// Softmax attention of a chunk of new tokens over a paged key-value cache, and the gathering of
+// the attention weights that fall on every slot.
+//
+// Row (i, h) of a sequence, token i of the chunk and query head h = hk G + g, sees the first
+// vis_i slots of key head hk:
+//   x_j = scale q . k_j,  lse = log sum_{j < vis_i} e^{x_j},  O = sum_{j < vis_i} e^{x_j - lse} v_j.
+// The G heads that share a key head are rows of one matrix product (row r = i G + g), so their
+// keys and values are read once.
+#include <type_traits>
+
+#include "cache_device.hpp"
+
+namespace vp {
+
+typedef __attribute__((address_space(3))) char lds_char;
+typedef short s16x4 __attribute__((__vector_size__(8)));
+
+__device__ __forceinline__ float maximum(float a, float b) {
+    return __builtin_elementwise_maximum(a, b);   // IEEE maximum: a NaN stays one
+}
+
+// ------------------------------------------------------------------------
+// Geometry of the two kernel variants.  Narrow: 32 rows per workgroup, its four waves split the
+// slots and each streams tiles of its own (no barrier until the end).  Wide: 256 rows, 64 per
+// wave, the waves share every tile.
+// ------------------------------------------------------------------------
+template <typename T, bool WIDE>
+struct Geo {
+    static constexpr bool kBf = sizeof(T) == 2;
+    static constexpr int NB = WIDE ? 2 : 1;                     // 32-row blocks per wave
+    static constexpr int TK = WIDE && kBf ? 64 : 32;            // slots per tile
+    static constexpr int KB = TK / 32;
+    static constexpr int RT = WIDE ? 256 : 32;                  // rows per workgroup
+    static constexpr int ROWB = kD * sizeof(T);                 // bytes of a slot's K or V
+    static constexpr int kTile = 2 * TK * ROWB;                 // K, then V
+    static constexpr int NST = WIDE ? 3 : 2;                    // tiles in LDS
+    static constexpr int kRing = NST * kTile;
+    static constexpr int kLds = WIDE ? kRing : 4 * kRing;
+    static constexpr int UC = 16 * ROWB / 1024;                 // 1 KB copies per 16 slots
+    static constexpr int PPW = (TK / 16) * 2 / (WIDE ? 4 : 1);  // (16 slots of K or V) per wave
+    static constexpr int CPT = PPW * UC;                        // copies per wave and tile
+    // Slot within a 32-slot block that result register r of lane half hh belongs to.
+    static __device__ __forceinline__ constexpr int key(int r, int hh) {
+        return kBf ? 16 * (r >> 3) + 8 * hh + (r & 7) : 8 * (r >> 2) + 4 * hh + (r & 3);
+    }
+};
+
+// Page numbers of a run of slots: lane i holds the page of the table's entry first + i.  Numbers
+// outside the pool count as page 0 here and clear `sane`; the slots on such pages are masked.
+struct PageWindow {
+    const int32_t* row;   // the sequence's table row
+    int last;             // last entry that may be read
+    int64_t npages;
+    int first, cur, next;
+    bool sane;
+
+    __device__ __forceinline__ int load(int at, int lane) const {
+        const int i = at + lane;
+        return row[i < last ? i : last];
+    }
+    __device__ __forceinline__ bool valid(int id) const { return id >= 0 && id < npages; }
+    __device__ __forceinline__ int settle(int id) {
+        if (__builtin_amdgcn_ballot_w64(!valid(id))) sane = false;
+        return valid(id) ? id : 0;
+    }
+    __device__ __forceinline__ void start(const CacheArgs& a, int b, int lo, int last_slot, int lane) {
+        row = a.table + (int64_t)b * a.max_pages;
+        last = last_slot >> a.page_log2;
+        npages = a.npages;
+        sane = true;
+        first = lo >> a.page_log2;
+        const int id = load(first, lane);
+        next = load(first + 64, lane);
+        cur = settle(id);
+    }
+    // Page of table entry `at` (uniform, never falling from call to call).
+    __device__ __forceinline__ int page(int at, int lane) {
+        if (at - first >= 64) {
+            const int hop = (at - first) >> 6;
+            first += hop * 64;
+            if (hop > 1) next = load(first, lane);
+            cur = settle(next);
+            next = load(first + 64, lane);
+        }
+        return __builtin_amdgcn_readlane(cur, at - first);
+    }
+};
+
+template <int CPT>
+__device__ __forceinline__ void wait_tiles(int behind) {
+    // Copies are counted in the order of their issue: all but the `behind` youngest tiles' have
+    // arrived.  Earlier LDS reads of this wave have returned, too.
+    if (behind <= 0) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    else if (behind == 1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"i"(CPT) : "memory");
+    else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"i"(2 * CPT) : "memory");
+}
+
+// ------------------------------------------------------------------------
+// The attention of one tile by one wave.  S^T = K Q^T, so that a lane owns one query row (lane %
+// 32) and its registers run over slots: the softmax's maximum and sum are per lane, and the
+// probabilities are already the B operand of O^T += V^T P^T.  For that K's rows enter the MFMA
+// with index bits 2 and 3 swapped (bf16), which puts eight consecutive slots into each lane half.
+// V^T comes from the row-major tile by transposing LDS reads (bf16) or as it lies (fp32: one
+// slot and 32 features per 32x32x2 MFMA and half).
+//
+// The running reference m (in log2 units) moves only when a logit passes it by 8: until then
+// probabilities grow to at most 2^8, which neither the fp32 sums nor the bf16 probabilities
+// (rounded to 8 bits, as their values are; the sum l takes them unrounded) mind.
+// ------------------------------------------------------------------------
+template <typename T, bool WIDE>
+struct WaveState {
+    typedef Geo<T, WIDE> G;
+    bf16x8 qb[G::kBf ? G::NB : 1][4];
+    float qf[G::kBf ? 1 : G::NB][32];
+    f32x16 o[G::NB][2];
+    float m[G::NB], l[G::NB];
+    int vis[G::NB];
+};
+
+template <typename T, bool WIDE, bool MASK>
+__device__ __forceinline__ void attend_tile(WaveState<T, WIDE>& w, lds_char* tile, float c2, int k0,
+                                            int klim, uint32_t units, int lane) {
+    typedef Geo<T, WIDE> G;
+    const int l31 = lane & 31, hh = lane >> 5;
+    f32x16 s[G::NB][G::KB];
+#pragma unroll
+    for (int nb = 0; nb < G::NB; ++nb)
+#pragma unroll
+        for (int kb = 0; kb < G::KB; ++kb) s[nb][kb] = zero_f32x16();
+    // ---- logits
+    if constexpr (G::kBf) {
+        typedef __attribute__((address_space(3))) const bf16x8 lds_frag;
+        const int row = swap23(l31);
+        const int a0 = row * 128 + ((hh ^ ((row & 3) | ((row >> 3) & 1) << 2)) << 4);
+#pragma unroll
+        for (int kb = 0; kb < G::KB; ++kb)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const bf16x8 k = *(lds_frag*)(tile + kb * 4096 + (a0 ^ (i << 5)));
+#pragma unroll
+                for (int nb = 0; nb < G::NB; ++nb) s[nb][kb] = mfma_bf16(k, w.qb[nb][i], s[nb][kb]);
+            }
+    } else {
+        typedef __attribute__((address_space(3))) const f32x4 lds_frag;
+        const int a0 = l31 * 256 + ((hh ^ (l31 & 15)) << 4);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const f32x4 k = *(lds_frag*)(tile + (a0 ^ (i << 5)));
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int nb = 0; nb < G::NB; ++nb)
+                    s[nb][0] = mfma_f32(k[e], w.qf[nb][4 * i + e], s[nb][0]);
+        }
+    }
+    // ---- probabilities
+    bf16x8 p[G::NB][G::KB][2];
+#pragma unroll
+    for (int nb = 0; nb < G::NB; ++nb) {
+        if constexpr (MASK) {
+#pragma unroll
+            for (int kb = 0; kb < G::KB; ++kb)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int k = 32 * kb + G::key(r, hh);
+                    const bool ok = k0 + k < w.vis[nb] && ((units >> (k >> 4)) & 1);
+                    s[nb][kb][r] = ok ? s[nb][kb][r] : -INFINITY;
+                }
+        }
+        float mx[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) mx[j] = maximum(s[nb][0][4 * j], s[nb][0][4 * j + 1]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) mx[j] = maximum(maximum(mx[j], s[nb][0][4 * j + 2]), s[nb][0][4 * j + 3]);
+#pragma unroll
+        for (int kb = 1; kb < G::KB; ++kb)
+#pragma unroll
+            for (int r = 0; r < 16; r += 2)
+                mx[(r >> 1) & 3] = maximum(maximum(mx[(r >> 1) & 3], s[nb][kb][r]), s[nb][kb][r + 1]);
+        float top = maximum(maximum(mx[0], mx[1]), maximum(mx[2], mx[3]));
+        {
+            const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+            top = maximum(__uint_as_float(x[0]), __uint_as_float(x[1])) * c2;
+        }
+        if (__builtin_amdgcn_ballot_w64(top > w.m[nb] + 8.f)) {
+            const float mn = top > w.m[nb] + 8.f ? top : w.m[nb];
+            const float f = w.m[nb] == mn ? 1.f : exp2f_fast(w.m[nb] - mn);   // 0 from -inf
+            w.l[nb] *= f;
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) w.o[nb][m][r] *= f;
+            w.m[nb] = mn;
+        }
+        const float ref = w.m[nb] == -INFINITY ? 0.f : w.m[nb];
+        float ls[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kb = 0; kb < G::KB; ++kb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const float e = exp2f_fast(fmaf(s[nb][kb][r], c2, -ref));
+                s[nb][kb][r] = e;
+                ls[r & 3] += e;
+            }
+        w.l[nb] += (ls[0] + ls[1]) + (ls[2] + ls[3]);
+    }
+    // ---- values.  Slots that no row sees (past klim, or on no page) may hold anything: their
+    // values are cleared.  Slots that some rows see and others do not may hold infinities or
+    // NaN, which a product with 0 would carry into the rows that do not see them: then
+    // the matrix product runs without these values, and they are added one slot at a time where seen.
+    bool odd = false;
+    if constexpr (G::kBf) {
+        const int i16 = lane & 15, dq = (lane >> 4) & 1;
+        const int v0 = (8 * hh + (i16 >> 2)) * 128 +
+                       (((2 * dq + ((i16 & 3) >> 1)) ^ (2 * (i16 >> 2))) << 4) + (i16 & 1) * 8;
+        typedef __attribute__((address_space(3))) s16x4 lds_tr;
+        lds_char* vt = tile + G::TK * G::ROWB;
+        auto frag = [&](int kb, int st, int m) {
+            lds_char* a = vt + (v0 ^ (m << 6)) + kb * 4096 + st * 2048;
+            const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr*)a);
+            const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr*)(a + 512));
+            typedef uint32_t u32x2 __attribute__((__vector_size__(8)));
+            const u32x2 xx = __builtin_bit_cast(u32x2, x), yy = __builtin_bit_cast(u32x2, y);
+            u32x4 f = {xx[0], xx[1], yy[0], yy[1]};
+            if constexpr (MASK) {
+                const int k = 32 * kb + 16 * st + 8 * hh;   // eight slots from here
+                int left = klim - (k0 + k);
+                if (!((units >> (k >> 4)) & 1)) left = 0;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    f[j] &= left > 2 * j + 1 ? 0xffffffffu : left == 2 * j + 1 ? 0xffffu : 0u;
+            }
+            return f;
+        };
+        if constexpr (MASK) {
+            typedef unsigned short u16x2 __attribute__((__vector_size__(4)));
+            u16x2 top = {0, 0};
+#pragma unroll
+            for (int kb = 0; kb < G::KB; ++kb)
+#pragma unroll
+                for (int st = 0; st < 2; ++st)
+#pragma unroll
+                    for (int m = 0; m < 2; ++m) {
+                        const u32x4 f = frag(kb, st, m);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            top = __builtin_elementwise_max(
+                                top, __builtin_bit_cast(u16x2, f[j] & 0x7fff7fffu));
+                    }
+            odd = __builtin_amdgcn_ballot_w64(top[0] >= 0x7f80 || top[1] >= 0x7f80) != 0;
+            if (odd) {
+#pragma unroll 1
+                for (int it = 0; it < 16 * G::KB; ++it) {
+                    const int r = it & 15, kb = it >> 4;
+#pragma unroll 1
+                    for (int hx = 0; hx < 2; ++hx) {
+                        const int k = 32 * kb + G::key(r, hx);
+                        if (k0 + k >= klim || !((units >> (k >> 4)) & 1)) continue;
+                        lds_char* vr = vt + k * 128;
+#pragma unroll
+                        for (int nb = 0; nb < G::NB; ++nb) {
+                            const float mine = s[nb][0][0];
+                            const float other = __shfl_xor(mine, 32);
+                            const float pk = hh == hx ? mine : other;
+                            if (k0 + k >= w.vis[nb]) continue;
+#pragma unroll
+                            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                                for (int q = 0; q < 16; ++q) {
+                                    const int d = 32 * m + 8 * (q >> 2) + 4 * hh + (q & 3);
+                                    const unsigned short x =
+                                        *(__attribute__((address_space(3))) const unsigned short*)(
+                                            vr + (((d >> 3) ^ (2 * (k & 3))) << 4) + (d & 7) * 2);
+                                    if ((x & 0x7f80) == 0x7f80)
+                                        w.o[nb][m][q] += pk * __uint_as_float((uint32_t)x << 16);
+                                }
+                        }
+                    }
+                    // the next register's probabilities come to the front
+#pragma unroll
+                    for (int nb = 0; nb < G::NB; ++nb) {
+                        const float head = s[nb][0][0];
+#pragma unroll
+                        for (int j = 0; j < 16 * G::KB - 1; ++j)
+                            s[nb][j >> 4][j & 15] = s[nb][(j + 1) >> 4][(j + 1) & 15];
+                        s[nb][G::KB - 1][15] = head;
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int nb = 0; nb < G::NB; ++nb)
+#pragma unroll
+            for (int kb = 0; kb < G::KB; ++kb)
+#pragma unroll
+                for (int st = 0; st < 2; ++st)
+                    p[nb][kb][st] = pack_bf16x8(
+                        s[nb][kb][8 * st], s[nb][kb][8 * st + 1], s[nb][kb][8 * st + 2],
+                        s[nb][kb][8 * st + 3], s[nb][kb][8 * st + 4], s[nb][kb][8 * st + 5],
+                        s[nb][kb][8 * st + 6], s[nb][kb][8 * st + 7]);
+#pragma unroll
+        for (int kb = 0; kb < G::KB; ++kb)
+#pragma unroll
+            for (int st = 0; st < 2; ++st)
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                    u32x4 f = frag(kb, st, m);
+                    if (MASK && odd) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            if ((f[j] & 0x7f80u) == 0x7f80u) f[j] &= 0xffff0000u;
+                            if ((f[j] & 0x7f800000u) == 0x7f800000u) f[j] &= 0xffffu;
+                        }
+                    }
+#pragma unroll
+                    for (int nb = 0; nb < G::NB; ++nb)
+                        w.o[nb][m] = mfma_bf16(__builtin_bit_cast(bf16x8, f), p[nb][kb][st], w.o[nb][m]);
+                }
+    } else {
+        typedef __attribute__((address_space(3))) const float lds_f32;
+        lds_char* vt = tile + G::TK * G::ROWB + hh * 1024 + l31 * 4;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int kr = G::key(r, 0);
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                float v = *(lds_f32*)(vt + kr * 256 + m * 128);
+                if constexpr (MASK) {
+                    const int k = kr + 4 * hh;
+                    const bool live = k0 + k < klim && ((units >> (k >> 4)) & 1);
+                    v = live ? v : 0.f;
+                    // a value that is not finite, seen by some rows: see above
+                    const bool bad = !(fabsf(v) <= 3.4028235e38f);
+                    uint64_t who = __builtin_amdgcn_ballot_w64(bad);
+                    if (who) {
+#pragma unroll 1
+                        for (; who; who &= who - 1) {
+                            const int from = __builtin_ctzll(who);        // lane of the value
+                            const float x = __shfl(v, from);
+                            const int fk = kr + 4 * (from >> 5), fd = from & 31;
+#pragma unroll
+                            for (int nb = 0; nb < G::NB; ++nb) {
+                                const float pk = __shfl(s[nb][0][r], l31 + (from & 32));
+                                const bool sees = k0 + fk < w.vis[nb];
+#pragma unroll
+                                for (int q = 0; q < 16; ++q)
+                                    if (8 * (q >> 2) + 4 * hh + (q & 3) == fd && sees)
+                                        w.o[nb][m][q] += pk * x;
+                            }
+                        }
+                        v = bad ? 0.f : v;
+                    }
+                }
+#pragma unroll
+                for (int nb = 0; nb < G::NB; ++nb) w.o[nb][m] = mfma_f32(v, s[nb][0][r], w.o[nb][m]);
+            }
+        }
+    }
+}
+
+// Factor 1 / l of a row and its log-sum-exp from (m, l).  No key seen, or only
+// logits of -inf: zeros and -inf.  A reference of +inf stands for an infinite logit: NaN.
+__device__ __forceinline__ void row_result(float m, float l, float* inv, float* lse) {
+    if (m == INFINITY) l = __builtin_nanf("");
+    *inv = l == 0.f ? 0.f : 1.f / l;
+    *lse = l == 0.f ? -INFINITY : (m + __log2f(l)) * kLn2;
+}
+
+template <typename T, bool WIDE>
+__global__ __launch_bounds__(256, 2) void k_cache_attend(AttendArgs a) {
+    typedef Geo<T, WIDE> G;
+    __shared__ __attribute__((aligned(1024))) char smem[G::kLds];
+    const int tid = threadIdx.x, lane = tid & 63, l31 = lane & 31, hh = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    // Work item: row tiles of one key head and slot range next to each other, on one XCD (they
+    // read the same keys and values).
+    int x = xcd_remap(blockIdx.x, gridDim.x);
+    const int rt = x % a.row_tiles;
+    x /= a.row_tiles;
+    const int split = x % a.nsplit;
+    x /= a.nsplit;
+    const int hk = x % a.c.Hkv, b = x / a.c.Hkv;
+
+    const CacheSeq sq = cache_seq(a.c, b);
+    const int nrows = sq.nq * a.G, row0 = rt * G::RT + (WIDE ? wave * 64 : 0);
+    if (rt * G::RT >= nrows) return;
+    const int tile_last = rt * G::RT + G::RT - 1 < nrows ? rt * G::RT + G::RT - 1 : nrows - 1;
+    const int klim = cache_visible(sq, a.causal, tile_last / a.G);
+    const int c0 = split * a.chunk, c1 = c0 + a.chunk < klim ? c0 + a.chunk : klim;
+    if (split > 0 && c0 >= klim) return;
+
+    // ---- this wave's rows
+    WaveState<T, WIDE> w;
+    const bool alive = row0 < nrows;
+    int64_t orow[G::NB];   // row of O
+#pragma unroll
+    for (int nb = 0; nb < G::NB; ++nb) {
+        int r = row0 + 32 * nb + l31;
+        r = r < nrows ? r : nrows - 1;
+        const int i = r / a.G, head = hk * a.G + r - i * a.G;
+        w.vis[nb] = cache_visible(sq, a.causal, i);
+        w.m[nb] = -INFINITY;
+        w.l[nb] = 0.f;
+        w.o[nb][0] = w.o[nb][1] = zero_f32x16();
+        orow[nb] = (int64_t)(sq.q0 + i) * a.Hq + head;
+        const T* q = (const T*)a.Q + (int64_t)(sq.q0 + i) * a.q_stride + head * kD;
+        if constexpr (G::kBf) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w.qb[nb][k] = load_bf16x8(q + 16 * k + 8 * hh);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const f32x4 v = *(const f32x4*)(q + 8 * k + 4 * hh);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w.qf[nb][4 * k + e] = v[e];
+            }
+        }
+    }
+    const int wave_last = row0 + 32 * G::NB - 1 < nrows ? row0 + 32 * G::NB - 1 : nrows - 1;
+    const int wlim = alive ? cache_visible(sq, a.causal, wave_last / a.G) : 0;
+    const int wfull = alive ? cache_visible(sq, a.causal, row0 / a.G) : 0;
+
+    // ---- the tiles
+    const int nt_all = (c1 - c0 + G::TK - 1) / G::TK;
+    const int tstep = WIDE ? 1 : 4, tfirst = WIDE ? 0 : wave;
+    const int nt = nt_all > tfirst ? (nt_all - tfirst + tstep - 1) / tstep : 0;
+    if (nt > 0) {
+        PageWindow pw;
+        pw.start(a.c, b, c0, c1 - 1, lane);
+        const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)smem + (WIDE ? 0 : wave * G::kRing);
+        lds_char* ring = (lds_char*)smem + (WIDE ? 0 : wave * G::kRing);
+        const int page_mask = (1 << a.c.page_log2) - 1;
+        const int last_unit = (c1 - 1) & ~15;
+        // Per lane: byte within a 1 KB copy.  K's and V's 16-byte pieces are exchanged within
+        // their row so that the tile's readers meet no bank twice: K's piece p of slot s lies at p ^
+        // (s & 3 | s bit 3 << 2) (bf16) or p ^ (s & 15) (fp32), V's at p ^ 2 (s & 3) (bf16).
+        uint32_t kv, vv;
+        if constexpr (G::kBf) {
+            const int r = lane >> 3, pc = lane & 7;
+            kv = r * 128 + ((pc ^ (r & 3)) << 4);
+            vv = r * 128 + ((pc ^ (2 * (r & 3))) << 4);
+        } else {
+            const int r = lane >> 4, pc = lane & 15;
+            kv = r * 256 + ((pc ^ r) << 4);
+            vv = lane * 16;
+        }
+        auto issue = [&](int t) {
+            const int k0 = c0 + (tfirst + t * tstep) * G::TK;
+            const uint32_t stage = lds0 + (t % G::NST) * G::kTile;
+#pragma unroll
+            for (int j = 0; j < G::PPW; ++j) {
+                const int part = WIDE ? wave * G::PPW + j : j, unit = part >> 1;
+                const bool isv = part & 1;
+                int slot = k0 + 16 * unit;
+                slot = slot < last_unit ? slot : last_unit;
+                const int id = pw.page(slot >> a.c.page_log2, lane);
+                const int64_t at = ((((int64_t)id * a.c.Hkv + hk) << a.c.page_log2) + (slot & page_mask)) * G::ROWB;
+                const char* src = (const char*)(isv ? a.c.V : a.c.K) + at;
+                const uint32_t dst = stage + (isv ? G::TK * G::ROWB : 0) + unit * 16 * G::ROWB;
+#pragma unroll
+                for (int u = 0; u < G::UC; ++u)
+                    copy_to_lds(dst + u * 1024, src + u * 1024, isv ? vv : kv ^ (64 * u));
+            }
+        };
+#pragma unroll
+        for (int t = 0; t < G::NST - 1; ++t)
+            if (t < nt) issue(t);
+        for (int t = 0; t < nt; ++t) {
+            const int more = nt - 1 - t;
+            if constexpr (WIDE) {
+                wait_tiles<G::CPT>(more < G::NST - 2 ? more : G::NST - 2);
+                __builtin_amdgcn_s_barrier();
+                if (t + G::NST - 1 < nt) issue(t + G::NST - 1);
+            } else {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the tile before is read
+                if (t + G::NST - 1 < nt) issue(t + G::NST - 1);
+                wait_tiles<G::CPT>(more < G::NST - 1 ? more : G::NST - 1);
+            }
+            const int k0 = c0 + (tfirst + t * tstep) * G::TK;
+            if (k0 >= wlim) continue;   // (wide: keeps to the barriers)
+            lds_char* tile = ring + (t % G::NST) * G::kTile;
+            if (pw.sane && k0 + G::TK <= wfull && k0 + G::TK <= c1) {
+                attend_tile<T, WIDE, false>(w, tile, a.c2, k0, 0, 0, lane);
+            } else {
+                uint32_t units = ~0u;
+                if (!pw.sane) {
+                    units = 0;
+#pragma unroll
+                    for (int u = 0; u < G::TK / 16; ++u) {
+                        const int at = (k0 + 16 * u) >> a.c.page_log2;
+                        if (at <= pw.last && pw.valid(pw.row[at])) units |= 1u << u;
+                    }
+                }
+                const int lim = wlim < c1 ? wlim : c1;
+                attend_tile<T, WIDE, true>(w, tile, a.c2, k0, lim, units, lane);
+            }
+        }
+    }
+#pragma unroll
+    for (int nb = 0; nb < G::NB; ++nb) w.l[nb] += __shfl_xor(w.l[nb], 32);
+
+    const int64_t all_rows = (int64_t)a.c.T * a.Hq;
+    if constexpr (WIDE) {
+#pragma unroll
+        for (int nb = 0; nb < G::NB; ++nb) {
+            if (row0 + 32 * nb + l31 >= nrows) continue;
+            if (a.nsplit > 1) {
+                float* po = a.part + (split * all_rows + orow[nb]) * kD;
+                if (hh == 0) {
+                    f32x2 ml = {w.m[nb], w.l[nb]};
+                    *(f32x2*)(a.part_ml + (split * all_rows + orow[nb]) * 2) = ml;
+                }
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        f32x4 v;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v[e] = w.o[nb][m][4 * g + e];
+                        *(f32x4*)(po + 32 * m + 8 * g + 4 * hh) = v;
+                    }
+                continue;
+            }
+            float inv, lse;
+            row_result(w.m[nb], w.l[nb], &inv, &lse);
+            if (hh == 0) a.lse[orow[nb]] = lse;
+            T* out = (T*)a.O + orow[nb] * kD;
+            if constexpr (G::kBf) {
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int g = 0; g < 2; ++g) {
+                        uint32_t d[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            bf16x2 pr = {(bf16)(w.o[nb][m][8 * g + 2 * e] * inv),
+                                         (bf16)(w.o[nb][m][8 * g + 2 * e + 1] * inv)};
+                            d[e] = __builtin_bit_cast(uint32_t, pr);
+                        }
+                        swap_halves(d[0], d[2]);
+                        swap_halves(d[1], d[3]);
+                        u32x4 v = {d[0], d[1], d[2], d[3]};
+                        *(u32x4*)(out + 32 * m + 16 * g + 8 * hh) = v;
+                    }
+            } else {
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        f32x4 v;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v[e] = w.o[nb][m][4 * g + e] * inv;
+                        *(f32x4*)(out + 32 * m + 8 * g + 4 * hh) = v;
+                    }
+            }
+        }
+    } else {
+        // The four waves' partial results meet in LDS (the ring is free then).
+        constexpr int kRow = 68;
+        float* sml = (float*)smem;                 // [4][32][2]
+        float* so = (float*)smem + 256;            // [4][32][68]
+        static_assert((256 + 4 * 32 * kRow) * 4 <= G::kLds, "partial results fit the ring");
+        __syncthreads();
+        if (hh == 0) {
+            sml[(wave * 32 + l31) * 2] = w.m[0];
+            sml[(wave * 32 + l31) * 2 + 1] = w.l[0];
+        }
+        __syncthreads();
+        float M = -INFINITY;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) M = maximum(M, sml[(v * 32 + l31) * 2]);
+        const float f = w.m[0] == -INFINITY ? 0.f : w.m[0] == M ? 1.f : exp2f_fast(w.m[0] - M);
+        if (row0 + l31 < nrows) {
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    f32x4 v;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = w.o[0][m][4 * g + e] * f;
+                    *(f32x4*)(so + (wave * 32 + l31) * kRow + 32 * m + 8 * g + 4 * hh) = v;
+                }
+        }
+        __syncthreads();
+        const int rr = tid >> 3, d0 = (tid & 7) * 8, r = row0 + rr;
+        if (r < nrows) {
+            const int i = r / a.G;
+            const int64_t at = (int64_t)(sq.q0 + i) * a.Hq + hk * a.G + r - i * a.G;
+            float mm[4], MM = -INFINITY, L = 0.f;
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                mm[v] = sml[(v * 32 + rr) * 2];
+                MM = maximum(MM, mm[v]);
+            }
+            float acc[8] = {};
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const float g = mm[v] == -INFINITY ? 0.f : mm[v] == MM ? 1.f : exp2f_fast(mm[v] - MM);
+                L += g * sml[(v * 32 + rr) * 2 + 1];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) acc[e] += so[(v * 32 + rr) * kRow + d0 + e];
+            }
+            if (a.nsplit > 1) {
+                float* po = a.part + (split * all_rows + at) * kD + d0;
+                *(f32x4*)po = f32x4{acc[0], acc[1], acc[2], acc[3]};
+                *(f32x4*)(po + 4) = f32x4{acc[4], acc[5], acc[6], acc[7]};
+                if (d0 == 0) *(f32x2*)(a.part_ml + (split * all_rows + at) * 2) = f32x2{MM, L};
+            } else {
+                float inv, lse;
+                row_result(MM, L, &inv, &lse);
+                if (d0 == 0) a.lse[at] = lse;
+                T* out = (T*)a.O + at * kD + d0;
+                if constexpr (G::kBf) {
+                    *(bf16x8*)out = pack_bf16x8(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv,
+                                                acc[4] * inv, acc[5] * inv, acc[6] * inv, acc[7] * inv);
+                } else {
+                    *(f32x4*)out = f32x4{acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
+                    *(f32x4*)(out + 4) = f32x4{acc[4] * inv, acc[5] * inv, acc[6] * inv, acc[7] * inv};
+                }
+            }
+        }
+    }
+}
+
+// ------------------------------------------------------------------------
+// Join of the split results, one wave per row: the splits whose slot range the row sees.
+// ------------------------------------------------------------------------
+template <typename T>
+__global__ __launch_bounds__(256) void k_cache_join(AttendArgs a) {
+    const int lane = threadIdx.x & 63;
+    const int b = blockIdx.y;
+    const CacheSeq sq = cache_seq(a.c, b);
+    const int r = blockIdx.x * 4 + (threadIdx.x >> 6);   // (token, head) of the sequence
+    const int i = r / a.Hq;
+    if (i >= sq.nq) return;
+    const int64_t at = (int64_t)sq.q0 * a.Hq + r, all_rows = (int64_t)a.c.T * a.Hq;
+    const int vis = cache_visible(sq, a.causal, i);
+    int ns = (vis + a.chunk - 1) / a.chunk;
+    ns = ns < 1 ? 1 : ns < a.nsplit ? ns : a.nsplit;
+    float M = -INFINITY;
+    for (int s = lane; s < ns; s += 64) M = maximum(M, a.part_ml[(s * all_rows + at) * 2]);
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) M = maximum(M, __shfl_xor(M, o));
+    float L = 0.f, acc = 0.f;
+    for (int s0 = 0; s0 < ns; s0 += 64) {
+        float f = 0.f;
+        if (s0 + lane < ns) {
+            const f32x2 ml = *(const f32x2*)(a.part_ml + ((s0 + lane) * all_rows + at) * 2);
+            f = ml[0] == -INFINITY ? 0.f : ml[0] == M ? 1.f : exp2f_fast(ml[0] - M);
+            L += f * ml[1];
+        }
+        const int n = ns - s0 < 64 ? ns - s0 : 64;
+        const float* po = a.part + (s0 * all_rows + at) * kD + lane;
+#pragma unroll 8
+        for (int s = 0; s < n; ++s) acc += __shfl(f, s) * po[s * all_rows * kD];
+    }
+    L = wave_sum(L);
+    float inv, lse;
+    row_result(M, L, &inv, &lse);
+    if (lane == 0) a.lse[at] = lse;
+    ((T*)a.O)[at * kD + lane] = (T)(acc * inv);
+}
+
+// ------------------------------------------------------------------------
+// Attention weights that fall on every slot, weight_out = weight + sum over the group's rows of
+// e^{x_j - lse}.  Keys stay in registers as the MFMA's B operand (a lane owns one slot of the
+// wave's 32), the rows stream through LDS as A with -lse in the accumulator's input, so that
+// a result is the exponent itself.  Every slot is written by one wave: no atomics, one order.
+// ------------------------------------------------------------------------
+constexpr int kWRows = 64;    // rows per step
+
+template <typename T>
+__global__ __launch_bounds__(256, 2) void k_cache_weight(AttendArgs a) {
+    constexpr bool kBf = sizeof(T) == 2;
+    constexpr int ROW = kBf ? 144 : 272;   // LDS bytes per row: 16 beyond a multiple of 128
+    __shared__ __attribute__((aligned(16))) char sq_[2][kWRows * ROW];
+    __shared__ __attribute__((aligned(16))) float so[2][kWRows];
+    const int tid = threadIdx.x, lane = tid & 63, l31 = lane & 31, hh = lane >> 5, wave = tid >> 6;
+    const int hk = blockIdx.y % a.c.Hkv, b = blockIdx.y / a.c.Hkv;
+    const CacheSeq sq = cache_seq(a.c, b);
+    const int k0 = blockIdx.x * 128;
+    if (k0 >= sq.len || sq.nq == 0) return;
+    const int slot = k0 + 32 * wave + l31;
+    int page = -1;
+    if (slot < sq.len) page = a.c.table[(int64_t)b * a.c.max_pages + (slot >> a.c.page_log2)];
+    const bool live = page >= 0 && page < a.c.npages;
+    const int64_t at = (((int64_t)(live ? page : 0) * a.c.Hkv + hk) << a.c.page_log2) +
+                       (slot & ((1 << a.c.page_log2) - 1));
+    bf16x8 kb[4];
+    float kf[kBf ? 1 : 32];
+    if constexpr (kBf) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            kb[i] = zero_bf16x8();
+            if (live) kb[i] = load_bf16x8((const T*)a.c.K + at * kD + 16 * i + 8 * hh);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            f32x4 v = {0.f, 0.f, 0.f, 0.f};
+            if (live) v = *(const f32x4*)((const T*)a.c.K + at * kD + 8 * i + 4 * hh);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) kf[4 * i + e] = v[e];
+        }
+    }
+    // Rows that see the workgroup's first slot: causal rows before them add nothing.
+    const int nrows = sq.nq * a.G;
+    int first = 0;
+    if (a.causal) first = clampi(k0 - (sq.len - sq.n), 0, sq.nq) * a.G;
+    first &= ~(kWRows - 1);
+    const float noff = -kLog2e / a.c2;
+    constexpr int EPT = kBf ? 8 : 4;                   // elements per 16 bytes
+    constexpr int LPR = kD / EPT;                      // 16-byte pieces per row
+    constexpr int NP = kWRows * LPR / 256;             // pieces per thread
+    u32x4 piece[NP];
+    float off = 0.f;
+    auto fetch = [&](int r0) {
+#pragma unroll
+        for (int j = 0; j < NP; ++j) {
+            const int p = tid + 256 * j, rr = p / LPR, r = r0 + rr < nrows ? r0 + rr : nrows - 1;
+            const int i = r / a.G;
+            piece[j] = *(const u32x4*)((const T*)a.Q + (int64_t)(sq.q0 + i) * a.q_stride +
+                                       (hk * a.G + r - i * a.G) * kD + (p % LPR) * EPT);
+        }
+        if (tid < kWRows) {
+            off = -INFINITY;
+            const int r = r0 + tid;
+            if (r < nrows) {
+                const int i = r / a.G;
+                const float lse = a.lse[(int64_t)(sq.q0 + i) * a.Hq + hk * a.G + r - i * a.G];
+                off = lse == -INFINITY ? -INFINITY : lse * noff;   // a row without weights adds none
+            }
+        }
+    };
+    auto put = [&](int buf) {
+#pragma unroll
+        for (int j = 0; j < NP; ++j) {
+            const int p = tid + 256 * j;
+            *(u32x4*)(sq_[buf] + (p / LPR) * ROW + (p % LPR) * 16) = piece[j];
+        }
+        if (tid < kWRows) so[buf][tid] = off;
+    };
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    if (first < nrows) {
+        fetch(first);
+        put(0);
+    }
+    int buf = 0;
+    for (int r0 = first; r0 < nrows; r0 += kWRows, buf ^= 1) {
+        __syncthreads();
+        if (r0 + kWRows < nrows) fetch(r0 + kWRows);
+        // slots that row r0 sees all rows of the step see
+        const bool mask = a.causal && k0 + 128 > cache_visible(sq, 1, r0 / a.G);
+#pragma unroll
+        for (int rb = 0; rb < kWRows / 32; ++rb) {
+            f32x16 s;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const f32x4 v = *(const f32x4*)(so[buf] + 32 * rb + 8 * g + 4 * hh);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[4 * g + e] = v[e];
+            }
+            const char* qr = sq_[buf] + (32 * rb + l31) * ROW;
+            if constexpr (kBf) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s = mfma_bf16(*(const bf16x8*)(qr + 32 * i + 16 * hh), kb[i], s);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const f32x4 q = *(const f32x4*)(qr + 32 * i + 16 * hh);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s = mfma_f32(q[e], kf[4 * i + e], s);
+                }
+            }
+            if (mask) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int row = r0 + 32 * rb + 8 * (r >> 2) + 4 * hh + (r & 3);
+                    const int i = row / a.G;
+                    if (slot >= cache_visible(sq, 1, i)) s[r] = -INFINITY;
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sum[r & 3] += exp2f_fast(s[r] * a.c2);
+        }
+        if (r0 + kWRows < nrows) put(buf ^ 1);
+    }
+    float t = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    t += __shfl_xor(t, 32);
+    if (live && hh == 0) a.weight_out[at] = a.c.weight[at] + t;
+}
+
+// ------------------------------------------------------------------ launchers
+
+// Variant and split of a call, from the host's sizes alone (so that results do not depend on
+// the lengths' values on the device).
+void attend_plan(AttendArgs* a) {
+    const int64_t rows = (int64_t)a->c.max_q * a->G;
+    a->wide = rows > 64;
+    const int rt = a->wide ? 256 : 32;
+    a->row_tiles = (int)((rows + rt - 1) / rt);
+    const int64_t items = (int64_t)a->c.B * a->c.Hkv * a->row_tiles;
+    const int64_t slots = 512;                       // workgroups that run together
+    const int64_t least = a->wide ? 512 : 1024;      // slots per split at least
+    const int64_t most = (a->c.max_len + least - 1) / least;
+    int64_t best = 1;
+    double best_t = 0;
+    for (int64_t ns = 1; ns <= most && ns <= 256; ++ns) {
+        const double rounds = (double)((items * ns + slots - 1) / slots);
+        const double t = rounds * ((double)a->c.max_len / ns + (a->wide ? 256 : 512)) + 8.0 * ns;
+        if (ns == 1 || t < best_t) best = ns, best_t = t;
+    }
+    const int64_t ch = (a->c.max_len + best - 1) / best;
+    a->chunk = (int)((ch + 63) / 64 * 64);
+    if (a->chunk < 64) a->chunk = 64;
+    a->nsplit = (int)((a->c.max_len + a->chunk - 1) / a->chunk);
+    if (a->nsplit < 1) a->nsplit = 1;
+}
+
+size_t attend_part_rows(const AttendArgs& a) {
+    return a.nsplit > 1 ? (size_t)a.nsplit * a.c.T * a.Hq : 0;
+}
+
+template <typename T>
+static void attend_go(const AttendArgs& a, hipStream_t st) {
+    const int64_t grid = (int64_t)a.c.B * a.c.Hkv * a.row_tiles * a.nsplit;
+    if (a.wide)
+        hipLaunchKernelGGL((k_cache_attend<T, true>), dim3(grid), dim3(256), 0, st, a);
+    else
+        hipLaunchKernelGGL((k_cache_attend<T, false>), dim3(grid), dim3(256), 0, st, a);
+    if (a.nsplit > 1)
+        hipLaunchKernelGGL(k_cache_join<T>, dim3(((int64_t)a.c.max_q * a.Hq + 3) / 4, a.c.B), dim3(256), 0,
+                           st, a);
+    if (a.weight_out && a.c.max_len > 0)
+        hipLaunchKernelGGL(k_cache_weight<T>, dim3((a.c.max_len + 127) / 128, a.c.B * a.c.Hkv), dim3(256), 0,
+                           st, a);
+}
+
+void launch_cache_attend(const AttendArgs& a, hipStream_t st) {
+    if (a.c.dtype == DT_BF16) attend_go<bf16>(a, st);
+    else attend_go<float>(a, st);
+}
+
+}  // namespace vp

@@ -1,0 +1,347 @@
+// Eviction from a paged key-value cache by gathered attention weight.
+//
+// Of the len slots of a sequence and key head, n = min(len, keep) stay: protected ones first
+// (stamp below `sink`, or among the latest `recent` of the sequence's `seen` tokens), then
+// by weight, the larger first, NaN before all numbers; among equals the lower slot.  Kept slots below n
+// stay where they are; the j-th kept slot from n on moves into the j-th slot below n that is not kept.
+// (Attention does not depend on the order of the slots, and sources and destinations never
+// overlap: every move runs at once, in place, and slots that need not move are not
+// touched.)
+//
+// Selection: each slot's rank as a 32-bit key, the n-th largest key by counting digits (11, 11
+// and 10 bits) over the slots, in the order of the keys' top digits; then, with `above` the slots
+// whose key is larger and `ties` those whose key is equal, slot s is kept if it is above or one of
+// the first n - #above ties.  The kept slots before s, kb(s), follow from prefix counts, and so
+// do both lists: hole s is number s - kb(s), mover s number kb(s) - kb(n).
+#include "cache_device.hpp"
+
+namespace vp {
+
+constexpr int kEvChunk = 4096;          // slots per workgroup of the counting passes
+constexpr int kEvBins = 2048;
+
+struct EvictWs {
+    uint32_t* key;      // [B * Hkv, cap]
+    int32_t *hist;      // [B * Hkv, 3, kEvBins]
+    int32_t *count;     // [B * Hkv, chunks, 2]: above, ties
+    int32_t *hole, *mover;   // [B * Hkv, cap]
+    int32_t *kbn, *left;     // [B * Hkv]: kept slots below n; n
+    int cap, chunks;
+};
+
+__host__ __device__ inline size_t ev_up(size_t x) { return (x + 255) & ~(size_t)255; }
+
+static EvictWs evict_layout(int B, int Hkv, int max_len, void* ws, size_t* total) {
+    EvictWs w;
+    const size_t bh = (size_t)B * Hkv;
+    w.chunks = max_len > 0 ? (max_len + kEvChunk - 1) / kEvChunk : 1;
+    w.cap = w.chunks * kEvChunk;
+    size_t off = 0;
+    char* p = (char*)ws;
+    auto take = [&](size_t bytes) {
+        char* at = p + off;
+        off = ev_up(off + bytes);
+        return at;
+    };
+    w.hist = (int32_t*)take(bh * 3 * kEvBins * 4);
+    w.key = (uint32_t*)take(bh * w.cap * 4);
+    w.count = (int32_t*)take(bh * w.chunks * 8);
+    w.hole = (int32_t*)take(bh * w.cap * 4);
+    w.mover = (int32_t*)take(bh * w.cap * 4);
+    w.kbn = (int32_t*)take(bh * 4);
+    w.left = (int32_t*)take(bh * 4);
+    if (total) *total = off;
+    return w;
+}
+
+size_t evict_ws_bytes(int B, int Hkv, int max_len) {
+    size_t n;
+    evict_layout(B, Hkv, max_len, nullptr, &n);
+    return n;
+}
+
+// Larger keys are kept first.  Weights keep their order as integers (-0 counts as 0).
+__device__ __forceinline__ uint32_t evict_key(float w, int stamp, int sink, int64_t latest) {
+    if (stamp < sink || stamp >= latest) return 0xffffffffu;
+    if (w != w) return 0xfffffffeu;
+    const uint32_t u = __float_as_uint(w + 0.f);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+__device__ __forceinline__ int64_t slot_at(const CacheArgs& c, int b, int hk, int slot) {
+    const int page = c.table[(int64_t)b * c.max_pages + (slot >> c.page_log2)];
+    if (page < 0 || page >= c.npages) return -1;
+    return (((int64_t)page * c.Hkv + hk) << c.page_log2) + (slot & ((1 << c.page_log2) - 1));
+}
+
+__global__ __launch_bounds__(256) void k_evict_clear(int32_t* hist, int64_t n) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i < n) hist[i] = 0;
+}
+
+// Digit that holds the need-th largest key of a histogram, and how many of that digit are still
+// wanted.  All 256 threads; s: 256 + 2 ints of LDS.
+__device__ __forceinline__ void find_digit(const int32_t* hist, int bins, int need, int* digit, int* left,
+                                           int* s) {
+    const int t = threadIdx.x, per = bins / 256, lane = t & 63, wv = t >> 6;
+    int own[kEvBins / 256], sum = 0;
+#pragma unroll
+    for (int j = 0; j < kEvBins / 256; ++j) {
+        own[j] = j < per ? hist[bins - 1 - (t * per + j)] : 0;   // from the largest digit down
+        sum += own[j];
+    }
+    int inc = sum;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int v = __shfl_up(inc, o);
+        if (lane >= o) inc += v;
+    }
+    __syncthreads();
+    if (lane == 63) s[wv] = inc;
+    __syncthreads();
+    int before = inc - sum;
+    for (int v = 0; v < wv; ++v) before += s[v];
+    if (before < need && before + sum >= need) {
+#pragma unroll
+        for (int j = 0; j < kEvBins / 256; ++j) {
+            if (before < need && before + own[j] >= need) {
+                s[8] = bins - 1 - (t * per + j);
+                s[9] = need - before;
+            }
+            before += own[j];
+        }
+    }
+    __syncthreads();
+    *digit = s[8];
+    *left = s[9];
+    __syncthreads();
+}
+
+// Counting pass PASS (0: keys made, top 11 bits; 1: next 11; 2: last 10).
+template <int PASS>
+__global__ __launch_bounds__(256) void k_evict_digit(EvictArgs a, EvictWs w) {
+    const int bh = blockIdx.y, hk = bh % a.c.Hkv, b = bh / a.c.Hkv;
+    const int len = cache_length(a.c, b), n = len < a.keep ? len : a.keep;
+    const int s0 = blockIdx.x * kEvChunk, s1 = s0 + kEvChunk < len ? s0 + kEvChunk : len;
+    if (s0 >= len || n == len) return;
+    __shared__ int bins[kEvBins];
+    __shared__ int tmp[16];
+    int32_t* hist = w.hist + (int64_t)bh * 3 * kEvBins;
+    uint32_t prefix = 0;
+    int need = n, d;
+    if (PASS >= 1) {
+        find_digit(hist, 2048, need, &d, &need, tmp);
+        prefix = d;
+    }
+    if (PASS >= 2) {
+        find_digit(hist + kEvBins, 2048, need, &d, &need, tmp);
+        prefix = prefix << 11 | d;
+    }
+    for (int i = threadIdx.x; i < kEvBins; i += 256) bins[i] = 0;
+    __syncthreads();
+    uint32_t* key = w.key + (int64_t)bh * w.cap;
+    const int64_t latest = PASS == 0 ? (int64_t)a.c.seen[b] - a.recent : 0;
+#pragma unroll 4
+    for (int s = s0 + threadIdx.x; s < s1; s += 256) {
+        uint32_t k;
+        if (PASS == 0) {
+            const int64_t at = slot_at(a.c, b, hk, s);
+            k = at >= 0 ? evict_key(a.c.weight[at], a.c.stamp[at], a.sink, latest) : 0;
+            key[s] = k;
+            atomicAdd(&bins[k >> 21], 1);
+        } else {
+            k = key[s];
+            if (PASS == 1 && k >> 21 == prefix) atomicAdd(&bins[(k >> 10) & 2047], 1);
+            if (PASS == 2 && k >> 10 == prefix) atomicAdd(&bins[k & 1023], 1);
+        }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < kEvBins; i += 256)
+        if (bins[i]) atomicAdd(hist + PASS * kEvBins + i, bins[i]);
+}
+
+// The n-th largest key and the number of its ties that are kept.
+__device__ __forceinline__ uint32_t evict_bound(const int32_t* hist, int n, int* ties, int* tmp) {
+    int d, need = n;
+    uint32_t k;
+    find_digit(hist, 2048, need, &d, &need, tmp);
+    k = d;
+    find_digit(hist + kEvBins, 2048, need, &d, &need, tmp);
+    k = k << 11 | d;
+    find_digit(hist + 2 * kEvBins, 1024, need, &d, &need, tmp);
+    *ties = need;
+    return k << 10 | d;
+}
+
+// Per chunk: slots above the bound, and ties.
+__global__ __launch_bounds__(256) void k_evict_count(EvictArgs a, EvictWs w) {
+    const int bh = blockIdx.y, b = bh / a.c.Hkv;
+    const int len = cache_length(a.c, b), n = len < a.keep ? len : a.keep;
+    const int s0 = blockIdx.x * kEvChunk, s1 = s0 + kEvChunk < len ? s0 + kEvChunk : len;
+    if (s0 >= len || n == len) return;
+    __shared__ int tmp[16];
+    int ties;
+    const uint32_t bound = evict_bound(w.hist + (int64_t)bh * 3 * kEvBins, n, &ties, tmp);
+    const uint32_t* key = w.key + (int64_t)bh * w.cap;
+    int above = 0, tie = 0;
+#pragma unroll 4
+    for (int s = s0 + threadIdx.x; s < s1; s += 256) {
+        const uint32_t k = key[s];
+        above += k > bound;
+        tie += k == bound;
+    }
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) {
+        above += __shfl_xor(above, o);
+        tie += __shfl_xor(tie, o);
+    }
+    if ((threadIdx.x & 63) == 0) {
+        tmp[threadIdx.x >> 6] = above;
+        tmp[4 + (threadIdx.x >> 6)] = tie;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        int32_t* c = w.count + ((int64_t)bh * w.chunks + blockIdx.x) * 2;
+        c[0] = tmp[0] + tmp[1] + tmp[2] + tmp[3];
+        c[1] = tmp[4] + tmp[5] + tmp[6] + tmp[7];
+    }
+}
+
+// The lists of holes and movers, and the weights and stamps of the slots that stay.
+__global__ __launch_bounds__(256) void k_evict_lists(EvictArgs a, EvictWs w) {
+    const int bh = blockIdx.y, hk = bh % a.c.Hkv, b = bh / a.c.Hkv;
+    const int len = cache_length(a.c, b), n = len < a.keep ? len : a.keep;
+    const int s0 = blockIdx.x * kEvChunk, s1 = s0 + kEvChunk < len ? s0 + kEvChunk : len;
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        w.left[bh] = n;
+        if (n == len) w.kbn[bh] = n;   // nothing moves
+    }
+    if (s0 >= len) return;
+    const bool same = a.weight_out == a.c.weight && a.stamp_out == a.c.stamp;
+    if (n < len) {
+        __shared__ int tmp[16];
+        const int t = threadIdx.x, lane = t & 63, wv = t >> 6;
+        int ties;
+        const uint32_t bound = evict_bound(w.hist + (int64_t)bh * 3 * kEvBins, n, &ties, tmp);
+        const uint32_t* key = w.key + (int64_t)bh * w.cap;
+        // counts of the chunks before
+        int above = 0, tie = 0;
+        const int32_t* cnt = w.count + (int64_t)bh * w.chunks * 2;
+        for (int c = t; c < (int)blockIdx.x; c += 256) above += cnt[2 * c], tie += cnt[2 * c + 1];
+#pragma unroll
+        for (int o = 32; o >= 1; o >>= 1) {
+            above += __shfl_xor(above, o);
+            tie += __shfl_xor(tie, o);
+        }
+        if (lane == 0) tmp[wv] = above, tmp[4 + wv] = tie;
+        __syncthreads();
+        above = tmp[0] + tmp[1] + tmp[2] + tmp[3];
+        tie = tmp[4] + tmp[5] + tmp[6] + tmp[7];
+        __syncthreads();
+        // sixteen slots in a row per thread
+        constexpr int kPer = kEvChunk / 256;
+        const int p0 = s0 + t * kPer;
+        uint32_t k[kPer];
+        int ma = 0, mt = 0;
+#pragma unroll
+        for (int j = 0; j < kPer; j += 4) {
+            u32x4 v = *(const u32x4*)(key + p0 + j);    // (cap is whole chunks)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const bool in = p0 + j + e < s1;
+                k[j + e] = v[e];
+                ma += in && v[e] > bound;
+                mt += in && v[e] == bound;
+            }
+        }
+        int ia = ma, it = mt;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int va = __shfl_up(ia, o), vt = __shfl_up(it, o);
+            if (lane >= o) ia += va, it += vt;
+        }
+        if (lane == 63) tmp[wv] = ia, tmp[4 + wv] = it;
+        __syncthreads();
+        above += ia - ma;
+        tie += it - mt;
+        for (int v = 0; v < wv; ++v) above += tmp[v], tie += tmp[4 + v];
+        int32_t* hole = w.hole + (int64_t)bh * w.cap;
+        int32_t* mover = w.mover + (int64_t)bh * w.cap;
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            const int s = p0 + j;
+            if (s >= s1) break;
+            const int kb = above + (tie < ties ? tie : ties);
+            const bool up = k[j] > bound, eq = k[j] == bound;
+            const bool kept = up || (eq && tie < ties);
+            above += up;
+            tie += eq;
+            if (s == n) w.kbn[bh] = kb;
+            if (s < n && !kept) hole[s - kb] = s;
+            if (s >= n && kept) mover[kb] = s;
+        }
+    }
+    if (same) return;
+    const int e1 = s1 < n ? s1 : n;
+    for (int s = s0 + threadIdx.x; s < e1; s += 256) {
+        const int64_t at = slot_at(a.c, b, hk, s);
+        if (at < 0) continue;
+        a.weight_out[at] = a.c.weight[at];
+        a.stamp_out[at] = a.c.stamp[at];
+    }
+}
+
+// The moves: eight threads per move and tensor row.
+template <typename T>
+__global__ __launch_bounds__(256) void k_evict_move(EvictArgs a, EvictWs w) {
+    const int bh = blockIdx.y, hk = bh % a.c.Hkv, b = bh / a.c.Hkv;
+    // (`length` may be `length_out`: it is not read here.)
+    const int n = w.left[bh], kbn = w.kbn[bh], moves = n - kbn;
+    if (blockIdx.x == 0 && hk == 0 && threadIdx.x == 0) a.length_out[b] = n;
+    const int c = threadIdx.x & 7;
+    constexpr int kE = 16 / sizeof(T), kV = 8 * sizeof(T) / 16;
+    for (int j = blockIdx.x * 32 + (threadIdx.x >> 3); j < moves; j += gridDim.x * 32) {
+        const int s = w.mover[(int64_t)bh * w.cap + kbn + j], d = w.hole[(int64_t)bh * w.cap + j];
+        const int64_t src = slot_at(a.c, b, hk, s), dst = slot_at(a.c, b, hk, d);
+        if (src < 0 || dst < 0) continue;
+        u32x4 k[kV], v[kV];
+#pragma unroll
+        for (int e = 0; e < kV; ++e) {
+            k[e] = *(const u32x4*)((const T*)a.c.K + src * kD + (8 * e + c) * kE);
+            v[e] = *(const u32x4*)((const T*)a.c.V + src * kD + (8 * e + c) * kE);
+        }
+#pragma unroll
+        for (int e = 0; e < kV; ++e) {
+            *(u32x4*)((T*)a.c.K + dst * kD + (8 * e + c) * kE) = k[e];
+            *(u32x4*)((T*)a.c.V + dst * kD + (8 * e + c) * kE) = v[e];
+        }
+        if (c == 0) {
+            a.weight_out[dst] = a.c.weight[src];
+            a.stamp_out[dst] = a.c.stamp[src];
+        }
+    }
+}
+
+void launch_cache_evict(const EvictArgs& a, hipStream_t st) {
+    EvictWs w = evict_layout(a.c.B, a.c.Hkv, a.c.max_len, a.ws, nullptr);
+    const int bh = a.c.B * a.c.Hkv;
+    const int64_t nh = (int64_t)bh * 3 * kEvBins;
+    const dim3 grid(w.chunks, bh);
+    hipLaunchKernelGGL(k_evict_clear, dim3((nh + 255) / 256), dim3(256), 0, st, w.hist, nh);
+    hipLaunchKernelGGL(k_evict_digit<0>, grid, dim3(256), 0, st, a, w);
+    hipLaunchKernelGGL(k_evict_digit<1>, grid, dim3(256), 0, st, a, w);
+    hipLaunchKernelGGL(k_evict_digit<2>, grid, dim3(256), 0, st, a, w);
+    hipLaunchKernelGGL(k_evict_count, grid, dim3(256), 0, st, a, w);
+    hipLaunchKernelGGL(k_evict_lists, grid, dim3(256), 0, st, a, w);
+    // A move for every slot past the first `keep` at most.
+    int64_t most = a.c.max_len - a.keep;
+    most = most < 1 ? 1 : most < a.keep ? most : a.keep;
+    int64_t gx = (most + 31) / 32, cap = 8192 / bh + 1;
+    if (gx > cap) gx = cap;
+    if (a.c.dtype == DT_BF16)
+        hipLaunchKernelGGL(k_evict_move<bf16>, dim3(gx, bh), dim3(256), 0, st, a, w);
+    else
+        hipLaunchKernelGGL(k_evict_move<float>, dim3(gx, bh), dim3(256), 0, st, a, w);
+}
+
+}  // namespace vp

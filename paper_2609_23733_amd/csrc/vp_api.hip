@@ -10,6 +10,7 @@
 #include <mutex>
 
 #include "../../include/vggt_prime.h"
+#include "cache_device.hpp"
 #include "vp_internal.hpp"
 
 namespace {
@@ -806,3 +807,235 @@ vp_status vp_tome_unmerge(const vp_shape* shape, const void* Ym, int64_t nrows,
     return hip_status("vp_tome_unmerge");
 }
 
+// ------------------------------------------------------- paged key-value cache
+
+namespace {
+
+constexpr int32_t kMaxCacheHeads = 128;
+constexpr int32_t kMaxCacheTokens = 1 << 23;        // of one call
+constexpr int64_t kMaxCacheSlots = (int64_t)1 << 30;   // of one sequence
+
+int log2_of(int32_t x) {
+    int n = 0;
+    while (n < 31 && ((int32_t)1 << n) < x) ++n;
+    return ((int32_t)1 << n) == x ? n : -1;
+}
+
+// Elements between tokens: whole 16-byte units, rows that do not overlap.
+bool stride_ok(int64_t stride, int32_t heads, vp_dtype dt) {
+    return stride >= (int64_t)heads * VP_HEAD_DIM && stride % (dt == VP_BF16 ? 8 : 4) == 0;
+}
+
+vp_status check_cache(const vp_cache* c, const vp_cache_batch* b, bool chunk, vp::CacheArgs* a) {
+    if (!c || !b) return VP_ERR_INVALID_ARG;
+    if (c->dtype != VP_F32 && c->dtype != VP_BF16) return VP_ERR_INVALID_ARG;
+    if (!c->K || !c->V || !aligned16(c->K) || !aligned16(c->V) || !aligned4(c->weight) ||
+        !aligned4(c->stamp) || c->npages < 1 || c->Hkv < 1 || c->page < 1)
+        return VP_ERR_INVALID_ARG;
+    if (!b->table || !aligned4(b->table) || !b->length || !aligned4(b->length) ||
+        !aligned4(b->seen) || !aligned4(b->q_start) || (chunk && !b->q_start))
+        return VP_ERR_INVALID_ARG;
+    if (b->B < 1 || b->max_pages < 1 || b->max_len < 0) return VP_ERR_INVALID_ARG;
+    if (chunk && (b->T < 0 || b->max_q < 0 || b->max_q > b->T)) return VP_ERR_INVALID_ARG;
+    if (c->d != VP_HEAD_DIM || c->Hkv > kMaxCacheHeads) return VP_ERR_UNSUPPORTED;
+    const int lg = log2_of(c->page);
+    if (lg < 4 || lg > 12 || c->npages > INT32_MAX) return VP_ERR_UNSUPPORTED;
+    if ((int64_t)b->max_pages * c->page > kMaxCacheSlots) return VP_ERR_UNSUPPORTED;
+    if (b->max_len > b->max_pages * c->page) return VP_ERR_INVALID_ARG;
+    if ((int64_t)b->B * c->Hkv > 65535 || (chunk && b->T > kMaxCacheTokens)) return VP_ERR_UNSUPPORTED;
+    memset(a, 0, sizeof(*a));
+    a->dtype = c->dtype;
+    a->K = c->K; a->V = c->V; a->weight = c->weight; a->stamp = c->stamp;
+    a->npages = c->npages;
+    a->page_log2 = lg;
+    a->Hkv = c->Hkv;
+    a->table = b->table; a->max_pages = b->max_pages;
+    a->length = b->length; a->seen = b->seen; a->q_start = b->q_start;
+    a->B = b->B;
+    a->max_len = b->max_len;
+    if (chunk) { a->T = b->T; a->max_q = b->max_q; }
+    return VP_OK;
+}
+
+bool heads_ok(int32_t Hq, int32_t Hkv) { return Hq >= Hkv && Hq % Hkv == 0; }
+
+// `tokens`: there are any, so positions have to be given.
+vp_status check_rotary(const vp_rotary_spec* r, bool transpose, bool tokens, vp::RotArgs* a) {
+    memset(a, 0, sizeof(*a));
+    a->axes = 1;
+    a->mag = 1.f;
+    a->sign = transpose ? -1.f : 1.f;
+    if (!r) return VP_OK;
+    if (r->dim < 0 || r->axes < 1 || (r->layout != VP_ROT_INTERLEAVED && r->layout != VP_ROT_HALF) ||
+        !isfinite(r->mag))
+        return VP_ERR_INVALID_ARG;
+    if (r->dim > VP_HEAD_DIM || r->axes > 4 || r->dim % (2 * r->axes)) return VP_ERR_UNSUPPORTED;
+    if (r->dim > 0 && ((tokens && !r->pos) || !aligned4(r->pos) || !r->freq || ((uintptr_t)r->freq & 7u)))
+        return VP_ERR_INVALID_ARG;
+    a->pos = r->pos;
+    a->freq = r->freq;
+    a->dim = r->dim;
+    a->axes = r->axes;
+    a->layout = r->layout;
+    if (r->mag != 0.f) a->mag = r->mag;
+    return VP_OK;
+}
+
+vp_status attend_args(const vp_cache* cache, const vp_cache_batch* batch, int32_t Hq,
+                      vp::AttendArgs* a) {
+    memset(a, 0, sizeof(*a));
+    vp_status st = check_cache(cache, batch, true, &a->c);
+    if (st != VP_OK) return st;
+    if (Hq < 1 || !heads_ok(Hq, cache->Hkv)) return VP_ERR_INVALID_ARG;
+    if (Hq > kMaxCacheHeads) return VP_ERR_UNSUPPORTED;
+    a->Hq = Hq;
+    a->G = Hq / cache->Hkv;
+    vp::attend_plan(a);
+    if ((int64_t)a->c.B * a->c.Hkv * a->row_tiles * a->nsplit > INT32_MAX) return VP_ERR_UNSUPPORTED;
+    return VP_OK;
+}
+
+size_t attend_ws(const vp::AttendArgs& a) {
+    const size_t rows = vp::attend_part_rows(a);
+    return kAlign + align_up(rows * VP_HEAD_DIM * sizeof(float)) + align_up(rows * 2 * sizeof(float));
+}
+
+}  // namespace
+
+vp_status vp_rotary_frequencies(int32_t dim, int32_t axes, double base, vp_rot_scaling scaling,
+                                double factor, double original, double low, double high,
+                                uint64_t* freq, float* mag) {
+    if (!freq || !mag || dim < 2 || axes < 1 || !(base > 1) || !isfinite(base)) return VP_ERR_INVALID_ARG;
+    if (scaling != VP_ROT_SCALE_NONE && scaling != VP_ROT_SCALE_LINEAR && scaling != VP_ROT_SCALE_PARTS)
+        return VP_ERR_INVALID_ARG;
+    if (scaling != VP_ROT_SCALE_NONE && (!(factor >= 1) || !isfinite(factor))) return VP_ERR_INVALID_ARG;
+    if (scaling == VP_ROT_SCALE_PARTS &&
+        (!(original > 0) || !isfinite(original) || !(low >= 0) || !(high > low) || !isfinite(high)))
+        return VP_ERR_INVALID_ARG;
+    if (dim > VP_HEAD_DIM || axes > 4 || dim % (2 * axes)) return VP_ERR_UNSUPPORTED;
+    const int n = dim / axes / 2;
+    const long double turn = 6.283185307179586476925286766559L;
+    for (int j = 0; j < n; ++j) {
+        long double f = powl((long double)base, -(long double)j / n);
+        if (scaling == VP_ROT_SCALE_LINEAR) f /= factor;
+        if (scaling == VP_ROT_SCALE_PARTS) {
+            long double k = (original * f / turn - low) / (high - low);
+            k = k < 0 ? 0 : k > 1 ? 1 : k;
+            f *= k + (1 - k) / factor;
+        }
+        // below 2^62: a pair turns by at most one radian per position
+        const uint64_t fixed = (uint64_t)(f / turn * 18446744073709551616.0L + 0.5L);
+        for (int a = 0; a < axes; ++a) freq[a * n + j] = fixed;
+    }
+    *mag = scaling == VP_ROT_SCALE_PARTS ? (float)(0.1 * log(factor) + 1) : 1.f;
+    return VP_OK;
+}
+
+vp_status vp_rotary(const vp_rotary_spec* rot, vp_dtype dtype, int32_t T, int32_t H, const void* x,
+                    int64_t x_stride, void* y, int64_t y_stride, int32_t transpose, void* stream) {
+    vp::RotArgs r;
+    if (!rot) return VP_ERR_INVALID_ARG;
+    vp_status st = check_rotary(rot, transpose != 0, T > 0, &r);
+    if (st != VP_OK) return st;
+    if (dtype != VP_F32 && dtype != VP_BF16) return VP_ERR_INVALID_ARG;
+    if (T < 0 || H < 1) return VP_ERR_INVALID_ARG;
+    if (T > kMaxTokens || H > kMaxCacheHeads) return VP_ERR_UNSUPPORTED;
+    if (T == 0) return VP_OK;
+    if (!x || !y || !aligned16(x) || !aligned16(y) || !stride_ok(x_stride, H, dtype) ||
+        !stride_ok(y_stride, H, dtype) || (x == y && x_stride != y_stride))
+        return VP_ERR_INVALID_ARG;
+    (void)hipGetLastError();
+    vp::launch_rotary(dtype == VP_BF16 ? 1 : 0, x, x_stride, y, y_stride, T, H, r, (hipStream_t)stream);
+    return hip_status("vp_rotary");
+}
+
+vp_status vp_cache_append(const vp_cache* cache, const vp_cache_batch* batch, int32_t Hq,
+                          const void* Q, int64_t q_stride, const void* K, int64_t k_stride,
+                          const void* V, int64_t v_stride, const vp_rotary_spec* rot, void* Q_out,
+                          void* stream) {
+    vp::AppendArgs a;
+    memset(&a, 0, sizeof(a));
+    vp::RotArgs r;
+    vp_status st = check_cache(cache, batch, true, &a.c);
+    if (st == VP_OK) st = check_rotary(rot, false, batch->T > 0, &r);
+    if (st != VP_OK) return st;
+    if (Q && (Hq < 1 || !heads_ok(Hq, cache->Hkv))) return VP_ERR_INVALID_ARG;
+    if (Q && Hq > kMaxCacheHeads) return VP_ERR_UNSUPPORTED;
+    if (cache->stamp && !batch->seen) return VP_ERR_INVALID_ARG;
+    if (batch->T == 0 || batch->max_q == 0) return VP_OK;
+    if (!K || !V || !aligned16(K) || !aligned16(V) || !stride_ok(k_stride, cache->Hkv, cache->dtype) ||
+        !stride_ok(v_stride, cache->Hkv, cache->dtype))
+        return VP_ERR_INVALID_ARG;
+    if (Q && (!Q_out || !aligned16(Q) || !aligned16(Q_out) || !stride_ok(q_stride, Hq, cache->dtype) ||
+              (Q == Q_out && q_stride != (int64_t)Hq * VP_HEAD_DIM)))
+        return VP_ERR_INVALID_ARG;
+    a.Hq = Q ? Hq : 0;
+    a.Q = Q; a.Kn = K; a.Vn = V; a.Qo = Q_out;
+    a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride;
+    (void)hipGetLastError();
+    vp::launch_cache_append(a, r, (hipStream_t)stream);
+    return hip_status("vp_cache_append");
+}
+
+size_t vp_cache_attend_workspace_bytes(const vp_cache* cache, const vp_cache_batch* batch, int32_t Hq) {
+    vp::AttendArgs a;
+    return attend_args(cache, batch, Hq, &a) == VP_OK ? attend_ws(a) : 0;
+}
+
+vp_status vp_cache_attend(const vp_cache* cache, const vp_cache_batch* batch, int32_t Hq,
+                          const void* Q, int64_t q_stride, int32_t causal, float scale, void* O,
+                          float* lse, float* weight_out, void* ws, size_t ws_bytes, void* stream) {
+    vp::AttendArgs a;
+    vp_status st = attend_args(cache, batch, Hq, &a);
+    if (st != VP_OK) return st;
+    if (!isfinite(scale) || scale < 0.f) return VP_ERR_INVALID_ARG;
+    if (weight_out && (!cache->weight || !aligned4(weight_out))) return VP_ERR_INVALID_ARG;
+    if (!ws || ((uintptr_t)ws & (kAlign - 1))) return VP_ERR_INVALID_ARG;
+    if (ws_bytes < attend_ws(a)) return VP_ERR_WORKSPACE;
+    if (batch->T == 0 || batch->max_q == 0) return VP_OK;
+    if (!Q || !O || !lse || !aligned16(Q) || !aligned16(O) || !aligned4(lse) ||
+        !stride_ok(q_stride, Hq, cache->dtype))
+        return VP_ERR_INVALID_ARG;
+    a.Q = Q;
+    a.q_stride = q_stride;
+    a.causal = causal != 0;
+    a.c2 = (scale > 0.f ? scale : 0.125f) * 1.4426950408889634f;
+    a.O = O;
+    a.lse = lse;
+    a.weight_out = weight_out;
+    const size_t rows = vp::attend_part_rows(a);
+    a.part = (float*)((char*)ws + kAlign);
+    a.part_ml = (float*)((char*)ws + kAlign + align_up(rows * VP_HEAD_DIM * sizeof(float)));
+    (void)hipGetLastError();
+    vp::launch_cache_attend(a, (hipStream_t)stream);
+    return hip_status("vp_cache_attend");
+}
+
+size_t vp_cache_evict_workspace_bytes(int32_t B, int32_t Hkv, int32_t max_len) {
+    if (B < 1 || Hkv < 1 || Hkv > kMaxCacheHeads || (int64_t)B * Hkv > 65535 || max_len < 0 ||
+        max_len > kMaxCacheSlots)
+        return 0;
+    return align_up(vp::evict_ws_bytes(B, Hkv, max_len));
+}
+
+vp_status vp_cache_evict(const vp_cache* cache, const vp_cache_batch* batch, int32_t keep,
+                         int32_t sink, int32_t recent, float* weight_out, int32_t* stamp_out,
+                         int32_t* length_out, void* ws, size_t ws_bytes, void* stream) {
+    vp::EvictArgs a;
+    memset(&a, 0, sizeof(a));
+    vp_status st = check_cache(cache, batch, false, &a.c);
+    if (st != VP_OK) return st;
+    if (!cache->weight || !cache->stamp || !batch->seen || !weight_out || !stamp_out || !length_out ||
+        !aligned4(weight_out) || !aligned4(stamp_out) || !aligned4(length_out) || keep < 1 || sink < 0 ||
+        recent < 0)
+        return VP_ERR_INVALID_ARG;
+    if (!ws || ((uintptr_t)ws & (kAlign - 1))) return VP_ERR_INVALID_ARG;
+    if (ws_bytes < vp_cache_evict_workspace_bytes(batch->B, cache->Hkv, batch->max_len))
+        return VP_ERR_WORKSPACE;
+    a.keep = keep; a.sink = sink; a.recent = recent;
+    a.weight_out = weight_out; a.stamp_out = stamp_out; a.length_out = length_out;
+    a.ws = ws;
+    (void)hipGetLastError();
+    vp::launch_cache_evict(a, (hipStream_t)stream);
+    return hip_status("vp_cache_evict");
+}

@@ -35,7 +35,9 @@ EXPORTS = ("vp_workspace_bytes", "vp_router_score", "vp_router_score_noalloc",
            "vp_block_qkv", "vp_block_out", "vp_teacher_workspace_bytes", "vp_loss_workspace_bytes",
            "vp_teacher_targets", "vp_router_loss", "vp_latent_loss", "vp_tome_split",
            "vp_tome_workspace_bytes", "vp_tome_plan", "vp_tome_merge", "vp_tome_merge_qkv",
-           "vp_tome_unmerge")
+           "vp_tome_unmerge", "vp_rotary_frequencies", "vp_rotary", "vp_cache_append",
+           "vp_cache_attend_workspace_bytes", "vp_cache_attend",
+           "vp_cache_evict_workspace_bytes", "vp_cache_evict")
 TOME_SPECIAL = 5   # special tokens per view (camera + registers), never merged
 MODEL_DIM = MAX_HEADS * HEAD_DIM
 BLOCK_VECS = ("ln1_w", "ln1_b", "b_qkv", "b_o", "ls1", "ln2_w", "ln2_b", "b_fc1", "b_fc2", "ls2")
@@ -72,6 +74,23 @@ class vp_block_weights(ctypes.Structure):
                 ("w_fc1", ctypes.c_void_p), ("b_fc1", ctypes.c_void_p),
                 ("w_fc2", ctypes.c_void_p), ("b_fc2", ctypes.c_void_p), ("ls2", ctypes.c_void_p),
                 ("ln_eps", ctypes.c_float), ("rope_base", ctypes.c_float)]
+
+
+class vp_cache(ctypes.Structure):
+    _fields_ = [("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("weight", ctypes.c_void_p),
+                ("stamp", ctypes.c_void_p), ("npages", ctypes.c_int64), ("page", ctypes.c_int32),
+                ("Hkv", ctypes.c_int32), ("d", ctypes.c_int32), ("dtype", ctypes.c_int)]
+
+
+class vp_cache_batch(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("length", ctypes.c_void_p), ("seen", ctypes.c_void_p),
+                ("q_start", ctypes.c_void_p), ("B", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+                ("T", ctypes.c_int32), ("max_q", ctypes.c_int32), ("max_len", ctypes.c_int32)]
+
+
+class vp_rotary_spec(ctypes.Structure):
+    _fields_ = [("pos", ctypes.c_void_p), ("freq", ctypes.c_void_p), ("dim", ctypes.c_int32),
+                ("axes", ctypes.c_int32), ("layout", ctypes.c_int), ("mag", ctypes.c_float)]
 
 
 _lib = None
@@ -135,6 +154,20 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.vp_tome_unmerge.argtypes = [ctypes.POINTER(vp_shape), P, i64, P, P, P]
     for f in ("vp_tome_split", "vp_tome_plan", "vp_tome_merge", "vp_tome_merge_qkv",
               "vp_tome_unmerge"):
+        getattr(lib, f).restype = ctypes.c_int
+    f64, cch, cba = ctypes.c_double, ctypes.POINTER(vp_cache), ctypes.POINTER(vp_cache_batch)
+    rsp = ctypes.POINTER(vp_rotary_spec)
+    lib.vp_rotary_frequencies.argtypes = [i32, i32, f64, ctypes.c_int, f64, f64, f64, f64, P, P]
+    lib.vp_rotary.argtypes = [rsp, ctypes.c_int, i32, i32, P, i64, P, i64, i32, P]
+    lib.vp_cache_append.argtypes = [cch, cba, i32, P, i64, P, i64, P, i64, rsp, P, P]
+    lib.vp_cache_attend_workspace_bytes.argtypes = [cch, cba, i32]
+    lib.vp_cache_attend_workspace_bytes.restype = ctypes.c_size_t
+    lib.vp_cache_attend.argtypes = [cch, cba, i32, P, i64, i32, f32, P, P, P, P, ctypes.c_size_t, P]
+    lib.vp_cache_evict_workspace_bytes.argtypes = [i32, i32, i32]
+    lib.vp_cache_evict_workspace_bytes.restype = ctypes.c_size_t
+    lib.vp_cache_evict.argtypes = [cch, cba, i32, i32, i32, P, P, P, P, ctypes.c_size_t, P]
+    for f in ("vp_rotary_frequencies", "vp_rotary", "vp_cache_append", "vp_cache_attend",
+              "vp_cache_evict"):
         getattr(lib, f).restype = ctypes.c_int
     for f in ("vp_router_score", "vp_router_score_noalloc", "vp_router_logits", "vp_assign_heads",
               "vp_routed_global_attention", "vp_gather_full_heads", "vp_full_head_attention",
