@@ -97,15 +97,18 @@ __device__ __forceinline__ void wait_tiles(int behind) {
 
 // ------------------------------------------------------------------------
 // The attention of one tile by one wave.  S^T = K Q^T, so that a lane owns one query row (lane %
-// 32) and its registers run over slots: the softmax's maximum and sum are per lane, and the
+// 32) and its registers run over slots: the softmax's sum is per lane, and the
 // probabilities are already the B operand of O^T += V^T P^T.  For that K's rows enter the MFMA
 // with index bits 2 and 3 swapped (bf16), which puts eight consecutive slots into each lane half.
 // V^T comes from the row-major tile by transposing LDS reads (bf16) or as it lies (fp32: one
 // slot and 32 features per 32x32x2 MFMA and half).
 //
-// The running reference m (in log2 units) moves only when a logit passes it by 8: until then
-// probabilities grow to at most 2^8, which neither the fp32 sums nor the bf16 probabilities
-// (rounded to 8 bits, as their values are; the sum l takes them unrounded) mind.
+// Probabilities are 2^(x - m) with a reference m (in log2 units) that is the row's maximum over its
+// first tile and moves only when a tile's sum passes 2^16: fp32 sums and bf16 probabilities
+// (rounded to 8 bits, as their values are; the sum l takes them unrounded) keep their relative
+// precision at any scale, so ordinary tiles need no maximum.  When a tile passes the bound (and at
+// a row's first slots, where m = -inf makes the sum inf or NaN) its logits are formed again, m becomes
+// the maximum so far and O and l are scaled to it.
 // ------------------------------------------------------------------------
 template <typename T, bool WIDE>
 struct WaveState {
@@ -116,18 +119,17 @@ struct WaveState {
     float m[G::NB], l[G::NB];
     int vis[G::NB];
 };
+constexpr float kMoveAt = 65536.f;
 
-template <typename T, bool WIDE, bool MASK>
-__device__ __forceinline__ void attend_tile(WaveState<T, WIDE>& w, lds_char* tile, float c2, int k0,
-                                            int klim, uint32_t units, int lane) {
+template <typename T, bool WIDE>
+__device__ __forceinline__ void tile_logits(const WaveState<T, WIDE>& w, lds_char* tile, int lane,
+                                            f32x16 (&s)[Geo<T, WIDE>::NB][Geo<T, WIDE>::KB]) {
     typedef Geo<T, WIDE> G;
     const int l31 = lane & 31, hh = lane >> 5;
-    f32x16 s[G::NB][G::KB];
 #pragma unroll
     for (int nb = 0; nb < G::NB; ++nb)
 #pragma unroll
         for (int kb = 0; kb < G::KB; ++kb) s[nb][kb] = zero_f32x16();
-    // ---- logits
     if constexpr (G::kBf) {
         typedef __attribute__((address_space(3))) const bf16x8 lds_frag;
         const int row = swap23(l31);
@@ -153,37 +155,68 @@ __device__ __forceinline__ void attend_tile(WaveState<T, WIDE>& w, lds_char* til
                     s[nb][0] = mfma_f32(k[e], w.qf[nb][4 * i + e], s[nb][0]);
         }
     }
-    // ---- probabilities
-    bf16x8 p[G::NB][G::KB][2];
+}
+
+// Slots that a row does not see: logits of -inf.  `units`: which groups of 16 slots exist.
+template <typename T, bool WIDE>
+__device__ __forceinline__ void tile_mask(const WaveState<T, WIDE>& w, int k0, uint32_t units, int lane,
+                                          f32x16 (&s)[Geo<T, WIDE>::NB][Geo<T, WIDE>::KB]) {
+    typedef Geo<T, WIDE> G;
+#pragma unroll
+    for (int nb = 0; nb < G::NB; ++nb)
+#pragma unroll
+        for (int kb = 0; kb < G::KB; ++kb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int k = 32 * kb + G::key(r, lane >> 5);
+                const bool ok = k0 + k < w.vis[nb] && ((units >> (k >> 4)) & 1);
+                s[nb][kb][r] = ok ? s[nb][kb][r] : -INFINITY;
+            }
+}
+
+// Logits to probabilities and their sum.
+template <int KB>
+__device__ __forceinline__ float tile_exp(f32x16 (&s)[KB], float c2, float ref) {
+    float ls[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            s[kb][r] = exp2f_fast(fmaf(s[kb][r], c2, -ref));
+            ls[r & 3] += s[kb][r];
+        }
+    return (ls[0] + ls[1]) + (ls[2] + ls[3]);
+}
+
+template <typename T, bool WIDE>
+__device__ __forceinline__ void attend_tile(WaveState<T, WIDE>& w, lds_char* tile, float c2, int k0,
+                                            bool partial, uint32_t units, int lane) {
+    typedef Geo<T, WIDE> G;
+    const int l31 = lane & 31, hh = lane >> 5;
+    f32x16 s[G::NB][G::KB];
+    float sum[G::NB];
+    tile_logits<T, WIDE>(w, tile, lane, s);
+    if (partial) tile_mask<T, WIDE>(w, k0, units, lane, s);
+    bool far = false;
 #pragma unroll
     for (int nb = 0; nb < G::NB; ++nb) {
-        if constexpr (MASK) {
+        sum[nb] = tile_exp<G::KB>(s[nb], c2, w.m[nb]);   // inf or NaN while m is -inf
+        far = far || !(sum[nb] < kMoveAt);
+    }
+    if (__builtin_amdgcn_ballot_w64(far)) {
+        tile_logits<T, WIDE>(w, tile, lane, s);
+        if (partial) tile_mask<T, WIDE>(w, k0, units, lane, s);
+#pragma unroll
+        for (int nb = 0; nb < G::NB; ++nb) {
+            float top = s[nb][0][0];
 #pragma unroll
             for (int kb = 0; kb < G::KB; ++kb)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int k = 32 * kb + G::key(r, hh);
-                    const bool ok = k0 + k < w.vis[nb] && ((units >> (k >> 4)) & 1);
-                    s[nb][kb][r] = ok ? s[nb][kb][r] : -INFINITY;
-                }
-        }
-        float mx[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) mx[j] = maximum(s[nb][0][4 * j], s[nb][0][4 * j + 1]);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) mx[j] = maximum(maximum(mx[j], s[nb][0][4 * j + 2]), s[nb][0][4 * j + 3]);
-#pragma unroll
-        for (int kb = 1; kb < G::KB; ++kb)
-#pragma unroll
-            for (int r = 0; r < 16; r += 2)
-                mx[(r >> 1) & 3] = maximum(maximum(mx[(r >> 1) & 3], s[nb][kb][r]), s[nb][kb][r + 1]);
-        float top = maximum(maximum(mx[0], mx[1]), maximum(mx[2], mx[3]));
-        {
+                for (int r = 0; r < 16; r += 2)
+                    top = maximum(maximum(top, s[nb][kb][r]), s[nb][kb][r + 1]);
             const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
             top = maximum(__uint_as_float(x[0]), __uint_as_float(x[1])) * c2;
-        }
-        if (__builtin_amdgcn_ballot_w64(top > w.m[nb] + 8.f)) {
-            const float mn = top > w.m[nb] + 8.f ? top : w.m[nb];
+            const float mn = top > w.m[nb] ? top : w.m[nb];
             const float f = w.m[nb] == mn ? 1.f : exp2f_fast(w.m[nb] - mn);   // 0 from -inf
             w.l[nb] *= f;
 #pragma unroll
@@ -191,103 +224,13 @@ __device__ __forceinline__ void attend_tile(WaveState<T, WIDE>& w, lds_char* til
 #pragma unroll
                 for (int r = 0; r < 16; ++r) w.o[nb][m][r] *= f;
             w.m[nb] = mn;
+            sum[nb] = tile_exp<G::KB>(s[nb], c2, mn == -INFINITY ? 0.f : mn);
         }
-        const float ref = w.m[nb] == -INFINITY ? 0.f : w.m[nb];
-        float ls[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int kb = 0; kb < G::KB; ++kb)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const float e = exp2f_fast(fmaf(s[nb][kb][r], c2, -ref));
-                s[nb][kb][r] = e;
-                ls[r & 3] += e;
-            }
-        w.l[nb] += (ls[0] + ls[1]) + (ls[2] + ls[3]);
     }
-    // ---- values.  Slots that no row sees (past klim, or on no page) may hold anything: their
-    // values are cleared.  Slots that some rows see and others do not may hold infinities or
-    // NaN, which a product with 0 would carry into the rows that do not see them: then
-    // the matrix product runs without these values, and they are added one slot at a time where seen.
-    bool odd = false;
+#pragma unroll
+    for (int nb = 0; nb < G::NB; ++nb) w.l[nb] += sum[nb];
     if constexpr (G::kBf) {
-        const int i16 = lane & 15, dq = (lane >> 4) & 1;
-        const int v0 = (8 * hh + (i16 >> 2)) * 128 +
-                       (((2 * dq + ((i16 & 3) >> 1)) ^ (2 * (i16 >> 2))) << 4) + (i16 & 1) * 8;
-        typedef __attribute__((address_space(3))) s16x4 lds_tr;
-        lds_char* vt = tile + G::TK * G::ROWB;
-        auto frag = [&](int kb, int st, int m) {
-            lds_char* a = vt + (v0 ^ (m << 6)) + kb * 4096 + st * 2048;
-            const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr*)a);
-            const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr*)(a + 512));
-            typedef uint32_t u32x2 __attribute__((__vector_size__(8)));
-            const u32x2 xx = __builtin_bit_cast(u32x2, x), yy = __builtin_bit_cast(u32x2, y);
-            u32x4 f = {xx[0], xx[1], yy[0], yy[1]};
-            if constexpr (MASK) {
-                const int k = 32 * kb + 16 * st + 8 * hh;   // eight slots from here
-                int left = klim - (k0 + k);
-                if (!((units >> (k >> 4)) & 1)) left = 0;
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    f[j] &= left > 2 * j + 1 ? 0xffffffffu : left == 2 * j + 1 ? 0xffffu : 0u;
-            }
-            return f;
-        };
-        if constexpr (MASK) {
-            typedef unsigned short u16x2 __attribute__((__vector_size__(4)));
-            u16x2 top = {0, 0};
-#pragma unroll
-            for (int kb = 0; kb < G::KB; ++kb)
-#pragma unroll
-                for (int st = 0; st < 2; ++st)
-#pragma unroll
-                    for (int m = 0; m < 2; ++m) {
-                        const u32x4 f = frag(kb, st, m);
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            top = __builtin_elementwise_max(
-                                top, __builtin_bit_cast(u16x2, f[j] & 0x7fff7fffu));
-                    }
-            odd = __builtin_amdgcn_ballot_w64(top[0] >= 0x7f80 || top[1] >= 0x7f80) != 0;
-            if (odd) {
-#pragma unroll 1
-                for (int it = 0; it < 16 * G::KB; ++it) {
-                    const int r = it & 15, kb = it >> 4;
-#pragma unroll 1
-                    for (int hx = 0; hx < 2; ++hx) {
-                        const int k = 32 * kb + G::key(r, hx);
-                        if (k0 + k >= klim || !((units >> (k >> 4)) & 1)) continue;
-                        lds_char* vr = vt + k * 128;
-#pragma unroll
-                        for (int nb = 0; nb < G::NB; ++nb) {
-                            const float mine = s[nb][0][0];
-                            const float other = __shfl_xor(mine, 32);
-                            const float pk = hh == hx ? mine : other;
-                            if (k0 + k >= w.vis[nb]) continue;
-#pragma unroll
-                            for (int m = 0; m < 2; ++m)
-#pragma unroll
-                                for (int q = 0; q < 16; ++q) {
-                                    const int d = 32 * m + 8 * (q >> 2) + 4 * hh + (q & 3);
-                                    const unsigned short x =
-                                        *(__attribute__((address_space(3))) const unsigned short*)(
-                                            vr + (((d >> 3) ^ (2 * (k & 3))) << 4) + (d & 7) * 2);
-                                    if ((x & 0x7f80) == 0x7f80)
-                                        w.o[nb][m][q] += pk * __uint_as_float((uint32_t)x << 16);
-                                }
-                        }
-                    }
-                    // the next register's probabilities come to the front
-#pragma unroll
-                    for (int nb = 0; nb < G::NB; ++nb) {
-                        const float head = s[nb][0][0];
-#pragma unroll
-                        for (int j = 0; j < 16 * G::KB - 1; ++j)
-                            s[nb][j >> 4][j & 15] = s[nb][(j + 1) >> 4][(j + 1) & 15];
-                        s[nb][G::KB - 1][15] = head;
-                    }
-                }
-            }
-        }
+        bf16x8 p[G::NB][G::KB][2];
 #pragma unroll
         for (int nb = 0; nb < G::NB; ++nb)
 #pragma unroll
@@ -298,20 +241,22 @@ __device__ __forceinline__ void attend_tile(WaveState<T, WIDE>& w, lds_char* til
                         s[nb][kb][8 * st], s[nb][kb][8 * st + 1], s[nb][kb][8 * st + 2],
                         s[nb][kb][8 * st + 3], s[nb][kb][8 * st + 4], s[nb][kb][8 * st + 5],
                         s[nb][kb][8 * st + 6], s[nb][kb][8 * st + 7]);
+        const int i16 = lane & 15, dq = (lane >> 4) & 1;
+        const int v0 = (8 * hh + (i16 >> 2)) * 128 +
+                       (((2 * dq + ((i16 & 3) >> 1)) ^ (2 * (i16 >> 2))) << 4) + (i16 & 1) * 8;
+        typedef __attribute__((address_space(3))) s16x4 lds_tr;
+        lds_char* vt = tile + G::TK * G::ROWB;
 #pragma unroll
         for (int kb = 0; kb < G::KB; ++kb)
 #pragma unroll
             for (int st = 0; st < 2; ++st)
 #pragma unroll
                 for (int m = 0; m < 2; ++m) {
-                    u32x4 f = frag(kb, st, m);
-                    if (MASK && odd) {
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            if ((f[j] & 0x7f80u) == 0x7f80u) f[j] &= 0xffff0000u;
-                            if ((f[j] & 0x7f800000u) == 0x7f800000u) f[j] &= 0xffffu;
-                        }
-                    }
+                    lds_char* a = vt + (v0 ^ (m << 6)) + kb * 4096 + st * 2048;
+                    typedef uint32_t u32x2 __attribute__((__vector_size__(8)));
+                    const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr*)a));
+                    const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr*)(a + 512)));
+                    const u32x4 f = {x[0], x[1], y[0], y[1]};
 #pragma unroll
                     for (int nb = 0; nb < G::NB; ++nb)
                         w.o[nb][m] = mfma_bf16(__builtin_bit_cast(bf16x8, f), p[nb][kb][st], w.o[nb][m]);
@@ -320,40 +265,85 @@ __device__ __forceinline__ void attend_tile(WaveState<T, WIDE>& w, lds_char* til
         typedef __attribute__((address_space(3))) const float lds_f32;
         lds_char* vt = tile + G::TK * G::ROWB + hh * 1024 + l31 * 4;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int kr = G::key(r, 0);
+        for (int r = 0; r < 16; ++r)
 #pragma unroll
             for (int m = 0; m < 2; ++m) {
-                float v = *(lds_f32*)(vt + kr * 256 + m * 128);
-                if constexpr (MASK) {
-                    const int k = kr + 4 * hh;
-                    const bool live = k0 + k < klim && ((units >> (k >> 4)) & 1);
-                    v = live ? v : 0.f;
-                    // a value that is not finite, seen by some rows: see above
-                    const bool bad = !(fabsf(v) <= 3.4028235e38f);
-                    uint64_t who = __builtin_amdgcn_ballot_w64(bad);
-                    if (who) {
-#pragma unroll 1
-                        for (; who; who &= who - 1) {
-                            const int from = __builtin_ctzll(who);        // lane of the value
-                            const float x = __shfl(v, from);
-                            const int fk = kr + 4 * (from >> 5), fd = from & 31;
-#pragma unroll
-                            for (int nb = 0; nb < G::NB; ++nb) {
-                                const float pk = __shfl(s[nb][0][r], l31 + (from & 32));
-                                const bool sees = k0 + fk < w.vis[nb];
-#pragma unroll
-                                for (int q = 0; q < 16; ++q)
-                                    if (8 * (q >> 2) + 4 * hh + (q & 3) == fd && sees)
-                                        w.o[nb][m][q] += pk * x;
-                            }
-                        }
-                        v = bad ? 0.f : v;
-                    }
-                }
+                const float v = *(lds_f32*)(vt + G::key(r, 0) * 256 + m * 128);
 #pragma unroll
                 for (int nb = 0; nb < G::NB; ++nb) w.o[nb][m] = mfma_f32(v, s[nb][0][r], w.o[nb][m]);
             }
+    }
+}
+
+// Values of a tile that is seen in part, `rows` slots from slot k of the cache at `v` in LDS, before any
+// wave multiplies with them.  Slots from `end` on or on no page may hold anything: cleared.
+// Slots that some rows see and others do not may hold infinities or NaN, which a product with a
+// probability of 0 would carry into the rows that do not see them: cleared too, and true returned for
+// add_odd_values() to give them to their rows.
+template <typename T>
+__device__ __forceinline__ bool clean_values(lds_char* v, int rows, int k, int end, uint32_t units, int lane) {
+    constexpr int kPieces = kD * sizeof(T) / 16;   // per slot
+    typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+    bool odd = false;
+    for (int c = lane; c < rows * kPieces; c += 64) {
+        const int slot = c / kPieces;
+        u32x4 x = *(lds_u32x4*)(v + c * 16);
+        const bool live = k + slot < end && ((units >> (slot >> 4)) & 1);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if constexpr (sizeof(T) == 2) {
+                const bool lo = (x[j] & 0x7f80u) == 0x7f80u, hi = (x[j] & 0x7f800000u) == 0x7f800000u;
+                odd = odd || (live && (lo || hi));
+                x[j] = !live ? 0u : x[j] & (lo ? 0xffff0000u : 0xffffffffu) & (hi ? 0xffffu : 0xffffffffu);
+            } else {
+                const bool inf = (x[j] & 0x7f800000u) == 0x7f800000u;
+                odd = odd || (live && inf);
+                x[j] = live && !inf ? x[j] : 0u;
+            }
+        }
+        *(lds_u32x4*)(v + c * 16) = x;
+    }
+    const bool any = __builtin_amdgcn_ballot_w64(odd) != 0;
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    return any;
+}
+
+// Values that are not finite in slots [k0, k1) of a tile seen in part, which clean_values() took
+// out, for the rows that see them.  Rare: slot by slot from memory, logits by plain sums.
+template <typename T, bool WIDE>
+__device__ __forceinline__ void add_odd_values(const AttendArgs& a, WaveState<T, WIDE>& w, int b, int hk,
+                                               int k0, int k1, int lane) {
+    typedef Geo<T, WIDE> G;
+    const int hh = lane >> 5;
+#pragma unroll 1
+    for (int k = k0; k < k1; ++k) {
+        const int page = a.c.table[(int64_t)b * a.c.max_pages + (k >> a.c.page_log2)];
+        if (page < 0 || page >= a.c.npages) continue;
+        const int64_t at = ((((int64_t)page * a.c.Hkv + hk) << a.c.page_log2) +
+                            (k & ((1 << a.c.page_log2) - 1))) * kD;
+        const T *kr = (const T*)a.c.K + at, *vr = (const T*)a.c.V + at;
+#pragma unroll
+        for (int nb = 0; nb < G::NB; ++nb) {
+            float x = 0.f;
+            if constexpr (G::kBf) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) x = fmaf((float)kr[16 * i + 8 * hh + j], (float)w.qb[nb][i][j], x);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) x = fmaf(kr[8 * (i >> 2) + 4 * hh + (i & 3)], w.qf[nb][i], x);
+            }
+            x += __shfl_xor(x, 32);
+            const float p = exp2f_fast(fmaf(x, a.c2, -w.m[nb]));
+            const bool sees = k < w.vis[nb];
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const float v = (float)vr[32 * m + 8 * (r >> 2) + 4 * hh + (r & 3)];
+                    if (sees && !(fabsf(v) <= 3.4028235e38f)) w.o[nb][m][r] += p * v;
+                }
         }
     }
 }
@@ -418,7 +408,8 @@ __global__ __launch_bounds__(256, 2) void k_cache_attend(AttendArgs a) {
     }
     const int wave_last = row0 + 32 * G::NB - 1 < nrows ? row0 + 32 * G::NB - 1 : nrows - 1;
     const int wlim = alive ? cache_visible(sq, a.causal, wave_last / a.G) : 0;
-    const int wfull = alive ? cache_visible(sq, a.causal, row0 / a.G) : 0;
+    // slots of this range that every row of the workgroup sees
+    const int all = cache_visible(sq, a.causal, rt * G::RT / a.G), seen_by_all = all < c1 ? all : c1;
 
     // ---- the tiles
     const int nt_all = (c1 - c0 + G::TK - 1) / G::TK;
@@ -465,24 +456,21 @@ __global__ __launch_bounds__(256, 2) void k_cache_attend(AttendArgs a) {
 #pragma unroll
         for (int t = 0; t < G::NST - 1; ++t)
             if (t < nt) issue(t);
+        bool odd = false;
         for (int t = 0; t < nt; ++t) {
             const int more = nt - 1 - t;
+            const int k0 = c0 + (tfirst + t * tstep) * G::TK;
+            lds_char* tile = ring + (t % G::NST) * G::kTile;
             if constexpr (WIDE) {
                 wait_tiles<G::CPT>(more < G::NST - 2 ? more : G::NST - 2);
-                __builtin_amdgcn_s_barrier();
-                if (t + G::NST - 1 < nt) issue(t + G::NST - 1);
             } else {
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the tile before is read
                 if (t + G::NST - 1 < nt) issue(t + G::NST - 1);
                 wait_tiles<G::CPT>(more < G::NST - 1 ? more : G::NST - 1);
             }
-            const int k0 = c0 + (tfirst + t * tstep) * G::TK;
-            if (k0 >= wlim) continue;   // (wide: keeps to the barriers)
-            lds_char* tile = ring + (t % G::NST) * G::kTile;
-            if (pw.sane && k0 + G::TK <= wfull && k0 + G::TK <= c1) {
-                attend_tile<T, WIDE, false>(w, tile, a.c2, k0, 0, 0, lane);
-            } else {
-                uint32_t units = ~0u;
+            const bool partial = !pw.sane || k0 + G::TK > seen_by_all;
+            uint32_t units = ~0u;
+            if (partial) {
                 if (!pw.sane) {
                     units = 0;
 #pragma unroll
@@ -491,10 +479,35 @@ __global__ __launch_bounds__(256, 2) void k_cache_attend(AttendArgs a) {
                         if (at <= pw.last && pw.valid(pw.row[at])) units |= 1u << u;
                     }
                 }
-                const int lim = wlim < c1 ? wlim : c1;
-                attend_tile<T, WIDE, true>(w, tile, a.c2, k0, lim, units, lane);
+                // this wave's own copies have arrived: no barrier in between
+                if constexpr (G::kBf && WIDE)
+                    odd |= clean_values<T>(tile + (G::TK + 16 * wave) * G::ROWB, 16, k0 + 16 * wave, c1,
+                                           units >> wave, lane);
+                else if constexpr (WIDE) {
+                    if (wave & 1)
+                        odd |= clean_values<T>(tile + (G::TK + 8 * (wave - 1)) * G::ROWB, 16, k0 + 8 * (wave - 1),
+                                               c1, units >> (wave >> 1), lane);
+                } else
+                    odd |= clean_values<T>(tile + G::TK * G::ROWB, G::TK, k0, c1, units, lane);
             }
+            if constexpr (WIDE) {
+                __builtin_amdgcn_s_barrier();
+                if (t + G::NST - 1 < nt) issue(t + G::NST - 1);
+            }
+            if (k0 < wlim) attend_tile<T, WIDE>(w, tile, a.c2, k0, partial, units, lane);
         }
+        if constexpr (WIDE) {   // what one wave took out, all see to
+            __shared__ int s_odd[4];
+            if (lane == 0) s_odd[wave] = odd;
+            __syncthreads();
+            odd = s_odd[0] | s_odd[1] | s_odd[2] | s_odd[3];
+        }
+        if (odd && alive)
+            for (int t = 0; t < nt; ++t) {
+                const int k0 = c0 + (tfirst + t * tstep) * G::TK;
+                if (!pw.sane || k0 + G::TK > seen_by_all)
+                    add_odd_values<T, WIDE>(a, w, b, hk, k0, k0 + G::TK < c1 ? k0 + G::TK : c1, lane);
+            }
     }
 #pragma unroll
     for (int nb = 0; nb < G::NB; ++nb) w.l[nb] += __shfl_xor(w.l[nb], 32);
