@@ -21,16 +21,17 @@ __device__ __forceinline__ float maximum(float a, float b) {
 
 // ------------------------------------------------------------------------
 // Geometry of the two kernel variants.  Narrow: 32 rows per workgroup, its four waves split the
-// slots and each streams tiles of its own (no barrier until the end).  Wide: 256 rows, 64 per
-// wave, the waves share every tile.
+// slots and each streams tiles of its own (no barrier until the end).  Wide: 64 rows per wave (bf16;
+// a tile's LDS reads serve two MFMA blocks) or 32 (fp32, whose MFMAs take 16 times the cycles: one
+// block keeps its registers within bounds), the waves share every tile.
 // ------------------------------------------------------------------------
 template <typename T, bool WIDE>
 struct Geo {
     static constexpr bool kBf = sizeof(T) == 2;
-    static constexpr int NB = WIDE ? 2 : 1;                     // 32-row blocks per wave
+    static constexpr int NB = WIDE && kBf ? 2 : 1;              // 32-row blocks per wave
     static constexpr int TK = WIDE && kBf ? 64 : 32;            // slots per tile
     static constexpr int KB = TK / 32;
-    static constexpr int RT = WIDE ? 256 : 32;                  // rows per workgroup
+    static constexpr int RT = WIDE ? 128 * NB : 32;             // rows per workgroup
     static constexpr int ROWB = kD * sizeof(T);                 // bytes of a slot's K or V
     static constexpr int kTile = 2 * TK * ROWB;                 // K, then V
     static constexpr int NST = WIDE ? 3 : 2;                    // tiles in LDS
@@ -362,17 +363,18 @@ __global__ __launch_bounds__(256, 2) void k_cache_attend(AttendArgs a) {
     __shared__ __attribute__((aligned(1024))) char smem[G::kLds];
     const int tid = threadIdx.x, lane = tid & 63, l31 = lane & 31, hh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    // Work item: row tiles of one key head and slot range next to each other, on one XCD (they
-    // read the same keys and values).
-    int x = xcd_remap(blockIdx.x, gridDim.x);
-    const int rt = x % a.row_tiles;
-    x /= a.row_tiles;
+    // The row tiles of one key head and slot range read the same keys and values: they go to
+    // one XCD (workgroup i runs on XCD i % 8).  Ranges are dealt to the XCDs in turn, so that one long
+    // sequence of a batch fills them all.
+    const int turn = (blockIdx.x >> 3) / a.row_tiles, rt = (blockIdx.x >> 3) - turn * a.row_tiles;
+    int x = turn * 8 + (blockIdx.x & 7);
     const int split = x % a.nsplit;
     x /= a.nsplit;
     const int hk = x % a.c.Hkv, b = x / a.c.Hkv;
+    if (b >= a.c.B) return;
 
     const CacheSeq sq = cache_seq(a.c, b);
-    const int nrows = sq.nq * a.G, row0 = rt * G::RT + (WIDE ? wave * 64 : 0);
+    const int nrows = sq.nq * a.G, row0 = rt * G::RT + (WIDE ? wave * 32 * G::NB : 0);
     if (rt * G::RT >= nrows) return;
     const int tile_last = rt * G::RT + G::RT - 1 < nrows ? rt * G::RT + G::RT - 1 : nrows - 1;
     const int klim = cache_visible(sq, a.causal, tile_last / a.G);
@@ -810,17 +812,19 @@ __global__ __launch_bounds__(256, 2) void k_cache_weight(AttendArgs a) {
 void attend_plan(AttendArgs* a) {
     const int64_t rows = (int64_t)a->c.max_q * a->G;
     a->wide = rows > 64;
-    const int rt = a->wide ? 256 : 32;
+    const int rt = !a->wide ? 32 : a->c.dtype == DT_BF16 ? 256 : 128;
     a->row_tiles = (int)((rows + rt - 1) / rt);
+    if (a->row_tiles < 1) a->row_tiles = 1;
     const int64_t items = (int64_t)a->c.B * a->c.Hkv * a->row_tiles;
     const int64_t slots = 512;                       // workgroups that run together
-    const int64_t least = a->wide ? 512 : 1024;      // slots per split at least
+    const int64_t least = a->wide ? 256 : 128;       // slots per split at least
     const int64_t most = (a->c.max_len + least - 1) / least;
+    const int64_t start = a->wide ? 256 : 192;       // a split's own cost, in slots
     int64_t best = 1;
     double best_t = 0;
     for (int64_t ns = 1; ns <= most && ns <= 256; ++ns) {
         const double rounds = (double)((items * ns + slots - 1) / slots);
-        const double t = rounds * ((double)a->c.max_len / ns + (a->wide ? 256 : 512)) + 8.0 * ns;
+        const double t = rounds * ((double)a->c.max_len / ns + start) + 4.0 * ns;
         if (ns == 1 || t < best_t) best = ns, best_t = t;
     }
     const int64_t ch = (a->c.max_len + best - 1) / best;
@@ -836,7 +840,7 @@ size_t attend_part_rows(const AttendArgs& a) {
 
 template <typename T>
 static void attend_go(const AttendArgs& a, hipStream_t st) {
-    const int64_t grid = (int64_t)a.c.B * a.c.Hkv * a.row_tiles * a.nsplit;
+    const int64_t grid = ((int64_t)a.c.B * a.c.Hkv * a.nsplit + 7) / 8 * 8 * a.row_tiles;
     if (a.wide)
         hipLaunchKernelGGL((k_cache_attend<T, true>), dim3(grid), dim3(256), 0, st, a);
     else

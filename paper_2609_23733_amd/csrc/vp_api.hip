@@ -891,7 +891,7 @@ vp_status attend_args(const vp_cache* cache, const vp_cache_batch* batch, int32_
     a->Hq = Hq;
     a->G = Hq / cache->Hkv;
     vp::attend_plan(a);
-    if ((int64_t)a->c.B * a->c.Hkv * a->row_tiles * a->nsplit > INT32_MAX) return VP_ERR_UNSUPPORTED;
+    if (((int64_t)a->c.B * a->c.Hkv * a->nsplit + 8) * a->row_tiles > INT32_MAX) return VP_ERR_UNSUPPORTED;
     return VP_OK;
 }
 
