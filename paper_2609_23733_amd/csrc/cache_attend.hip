@@ -21,24 +21,24 @@ __device__ __forceinline__ float maximum(float a, float b) {
 
 // ------------------------------------------------------------------------
 // Geometry of the two kernel variants.  Narrow: 32 rows per workgroup, its four waves split the
-// slots and each streams tiles of its own (no barrier until the end).  Wide: 64 rows per wave (bf16;
-// a tile's LDS reads serve two MFMA blocks) or 32 (fp32, whose MFMAs take 16 times the cycles: one
-// block keeps its registers within bounds), the waves share every tile.
+// slots and each streams tiles of its own (no barrier until the end).  Wide: 32 rows per wave, eight
+// waves (bf16) or four (fp32), which share every tile.
 // ------------------------------------------------------------------------
 template <typename T, bool WIDE>
 struct Geo {
     static constexpr bool kBf = sizeof(T) == 2;
-    static constexpr int NB = WIDE && kBf ? 2 : 1;              // 32-row blocks per wave
+    static constexpr int NB = 1;                                // 32-row blocks per wave
+    static constexpr int NW = WIDE && kBf ? 8 : 4;              // waves
     static constexpr int TK = WIDE && kBf ? 64 : 32;            // slots per tile
     static constexpr int KB = TK / 32;
-    static constexpr int RT = WIDE ? 128 * NB : 32;             // rows per workgroup
+    static constexpr int RT = WIDE ? 32 * NB * NW : 32;             // rows per workgroup
     static constexpr int ROWB = kD * sizeof(T);                 // bytes of a slot's K or V
     static constexpr int kTile = 2 * TK * ROWB;                 // K, then V
     static constexpr int NST = WIDE ? 3 : 2;                    // tiles in LDS
     static constexpr int kRing = NST * kTile;
     static constexpr int kLds = WIDE ? kRing : 4 * kRing;
     static constexpr int UC = 16 * ROWB / 1024;                 // 1 KB copies per 16 slots
-    static constexpr int PPW = (TK / 16) * 2 / (WIDE ? 4 : 1);  // (16 slots of K or V) per wave
+    static constexpr int PPW = (TK / 16) * 2 / (WIDE ? NW : 1);  // (16 slots of K or V) per wave
     static constexpr int CPT = PPW * UC;                        // copies per wave and tile
     // Slot within a 32-slot block that result register r of lane half hh belongs to.
     static __device__ __forceinline__ constexpr int key(int r, int hh) {
@@ -164,15 +164,19 @@ __device__ __forceinline__ void tile_mask(const WaveState<T, WIDE>& w, int k0, u
                                           f32x16 (&s)[Geo<T, WIDE>::NB][Geo<T, WIDE>::KB]) {
     typedef Geo<T, WIDE> G;
 #pragma unroll
-    for (int nb = 0; nb < G::NB; ++nb)
+    for (int nb = 0; nb < G::NB; ++nb) {
+        // (compared with constants: the slots' numbers, which the lane half shifts, would otherwise
+        // stay in registers through the loop over the tiles)
+        const int left = w.vis[nb] - k0 - G::key(0, 1) * (lane >> 5);
 #pragma unroll
         for (int kb = 0; kb < G::KB; ++kb)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const int k = 32 * kb + G::key(r, lane >> 5);
-                const bool ok = k0 + k < w.vis[nb] && ((units >> (k >> 4)) & 1);
+                const int k = 32 * kb + G::key(r, 0);
+                const bool ok = k < left && ((units >> (k >> 4)) & 1);
                 s[nb][kb][r] = ok ? s[nb][kb][r] : -INFINITY;
             }
+    }
 }
 
 // Logits to probabilities and their sum.
@@ -205,6 +209,8 @@ __device__ __forceinline__ void attend_tile(WaveState<T, WIDE>& w, lds_char* til
         far = far || !(sum[nb] < kMoveAt);
     }
     if (__builtin_amdgcn_ballot_w64(far)) {
+        // (read again: the first pass's operands and logits do not stay in registers for this)
+        asm volatile("" ::: "memory");
         tile_logits<T, WIDE>(w, tile, lane, s);
         if (partial) tile_mask<T, WIDE>(w, k0, units, lane, s);
 #pragma unroll
@@ -325,15 +331,24 @@ __device__ __forceinline__ void add_odd_values(const AttendArgs& a, WaveState<T,
         const T *kr = (const T*)a.c.K + at, *vr = (const T*)a.c.V + at;
 #pragma unroll
         for (int nb = 0; nb < G::NB; ++nb) {
+            // (few loads at a time: this must not set the kernel's register count)
             float x = 0.f;
             if constexpr (G::kBf) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                for (int i = 0; i < 4; ++i) {
+                    const bf16x8 kv = load_bf16x8((const bf16*)kr + 16 * i + 8 * hh);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) x = fmaf((float)kr[16 * i + 8 * hh + j], (float)w.qb[nb][i][j], x);
+                    for (int j = 0; j < 8; ++j) x = fmaf((float)kv[j], (float)w.qb[nb][i][j], x);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             } else {
 #pragma unroll
-                for (int i = 0; i < 32; ++i) x = fmaf(kr[8 * (i >> 2) + 4 * hh + (i & 3)], w.qf[nb][i], x);
+                for (int i = 0; i < 8; ++i) {
+                    const f32x4 kv = *(const f32x4*)(kr + 8 * i + 4 * hh);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x = fmaf(kv[e], w.qf[nb][4 * i + e], x);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             }
             x += __shfl_xor(x, 32);
             const float p = exp2f_fast(fmaf(x, a.c2, -w.m[nb]));
@@ -341,9 +356,13 @@ __device__ __forceinline__ void add_odd_values(const AttendArgs& a, WaveState<T,
 #pragma unroll
             for (int m = 0; m < 2; ++m)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const float v = (float)vr[32 * m + 8 * (r >> 2) + 4 * hh + (r & 3)];
-                    if (sees && !(fabsf(v) <= 3.4028235e38f)) w.o[nb][m][r] += p * v;
+                for (int g = 0; g < 4; ++g) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float v = (float)vr[32 * m + 8 * g + 4 * hh + e];
+                        if (sees && !(fabsf(v) <= 3.4028235e38f)) w.o[nb][m][4 * g + e] += p * v;
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
                 }
         }
     }
@@ -358,7 +377,7 @@ __device__ __forceinline__ void row_result(float m, float l, float* inv, float* 
 }
 
 template <typename T, bool WIDE>
-__global__ __launch_bounds__(256, 2) void k_cache_attend(AttendArgs a) {
+__global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), (Geo<T, WIDE>::NW / 2)) void k_cache_attend(AttendArgs a) {
     typedef Geo<T, WIDE> G;
     __shared__ __attribute__((aligned(1024))) char smem[G::kLds];
     const int tid = threadIdx.x, lane = tid & 63, l31 = lane & 31, hh = lane >> 5;
@@ -482,13 +501,12 @@ __global__ __launch_bounds__(256, 2) void k_cache_attend(AttendArgs a) {
                     }
                 }
                 // this wave's own copies have arrived: no barrier in between
-                if constexpr (G::kBf && WIDE)
-                    odd |= clean_values<T>(tile + (G::TK + 16 * wave) * G::ROWB, 16, k0 + 16 * wave, c1,
-                                           units >> wave, lane);
-                else if constexpr (WIDE) {
+                if constexpr (WIDE) {
+                    static_assert(G::PPW == 1, "a wave copies 16 slots of K or of V");
+                    const int u = 16 * (wave >> 1);
                     if (wave & 1)
-                        odd |= clean_values<T>(tile + (G::TK + 8 * (wave - 1)) * G::ROWB, 16, k0 + 8 * (wave - 1),
-                                               c1, units >> (wave >> 1), lane);
+                        odd |= clean_values<T>(tile + (G::TK + u) * G::ROWB, 16, k0 + u, c1, units >> (wave >> 1),
+                                               lane);
                 } else
                     odd |= clean_values<T>(tile + G::TK * G::ROWB, G::TK, k0, c1, units, lane);
             }
@@ -499,10 +517,10 @@ __global__ __launch_bounds__(256, 2) void k_cache_attend(AttendArgs a) {
             if (k0 < wlim) attend_tile<T, WIDE>(w, tile, a.c2, k0, partial, units, lane);
         }
         if constexpr (WIDE) {   // what one wave took out, all see to
-            __shared__ int s_odd[4];
+            __shared__ int s_odd[G::NW];
             if (lane == 0) s_odd[wave] = odd;
             __syncthreads();
-            odd = s_odd[0] | s_odd[1] | s_odd[2] | s_odd[3];
+            for (int v = 0; v < G::NW; ++v) odd |= s_odd[v] != 0;
         }
         if (odd && alive)
             for (int t = 0; t < nt; ++t) {
@@ -842,7 +860,7 @@ template <typename T>
 static void attend_go(const AttendArgs& a, hipStream_t st) {
     const int64_t grid = ((int64_t)a.c.B * a.c.Hkv * a.nsplit + 7) / 8 * 8 * a.row_tiles;
     if (a.wide)
-        hipLaunchKernelGGL((k_cache_attend<T, true>), dim3(grid), dim3(256), 0, st, a);
+        hipLaunchKernelGGL((k_cache_attend<T, true>), dim3(grid), dim3(64 * Geo<T, true>::NW), 0, st, a);
     else
         hipLaunchKernelGGL((k_cache_attend<T, false>), dim3(grid), dim3(256), 0, st, a);
     if (a.nsplit > 1)
