@@ -20,27 +20,31 @@ __device__ __forceinline__ float maximum(float a, float b) {
 }
 
 // ------------------------------------------------------------------------
-// Geometry of the two kernel variants.  Narrow: 32 rows per workgroup, its four waves split the
-// slots and each streams tiles of its own (no barrier until the end).  Wide: 32 rows per wave, eight
-// waves (bf16) or four (fp32), which share every tile.
+// Geometry of the two kernel variants.  A wave owns 32 rows and multiplies them with 32 slots (a
+// block) at a time.  Narrow: 32 rows per workgroup, its four waves split the slots and each
+// streams tiles of its own (no barrier until the end).  Wide: four waves of 32 rows each, which
+// share every tile.
 // ------------------------------------------------------------------------
 template <typename T, bool WIDE>
 struct Geo {
     static constexpr bool kBf = sizeof(T) == 2;
-    static constexpr int NB = 1;                                // 32-row blocks per wave
-    static constexpr int NW = WIDE && kBf ? 8 : 4;              // waves
+    static constexpr int NW = 4;                                // waves
     static constexpr int TK = WIDE && kBf ? 64 : 32;            // slots per tile
-    static constexpr int KB = TK / 32;
-    static constexpr int RT = WIDE ? 32 * NB * NW : 32;             // rows per workgroup
+    static constexpr int RT = WIDE ? 32 * NW : 32;              // rows per workgroup
     static constexpr int ROWB = kD * sizeof(T);                 // bytes of a slot's K or V
-    static constexpr int kTile = 2 * TK * ROWB;                 // K, then V
-    static constexpr int NST = WIDE ? 3 : 2;                    // tiles in LDS
+    static constexpr int kBlock = 32 * ROWB;                    // bytes of a block's K or V
+    static constexpr int kTileV = TK * ROWB;                    // a tile's V comes after its K
+    static constexpr int kTile = 2 * TK * ROWB;
+    // Tiles in LDS, and how many tiles ahead of the arriving one copies are issued: into the
+    // place of the tile before it, or (wide bf16, where that one is still in use) of the one before.
+    static constexpr int NST = WIDE ? 3 : 2;
+    static constexpr int AHEAD = WIDE && kBf ? NST - 2 : NST - 1;
     static constexpr int kRing = NST * kTile;
     static constexpr int kLds = WIDE ? kRing : 4 * kRing;
     static constexpr int UC = 16 * ROWB / 1024;                 // 1 KB copies per 16 slots
-    static constexpr int PPW = (TK / 16) * 2 / (WIDE ? NW : 1);  // (16 slots of K or V) per wave
+    static constexpr int PPW = (TK / 16) * 2 / (WIDE ? NW : 1); // (16 slots of K or V) per wave
     static constexpr int CPT = PPW * UC;                        // copies per wave and tile
-    // Slot within a 32-slot block that result register r of lane half hh belongs to.
+    // Slot within a block that result register r of lane half hh belongs to.
     static __device__ __forceinline__ constexpr int key(int r, int hh) {
         return kBf ? 16 * (r >> 3) + 8 * hh + (r & 7) : 8 * (r >> 2) + 4 * hh + (r & 3);
     }
@@ -97,7 +101,7 @@ __device__ __forceinline__ void wait_tiles(int behind) {
 }
 
 // ------------------------------------------------------------------------
-// The attention of one tile by one wave.  S^T = K Q^T, so that a lane owns one query row (lane %
+// The attention of one block by one wave.  S^T = K Q^T, so that a lane owns one query row (lane %
 // 32) and its registers run over slots: the softmax's sum is per lane, and the
 // probabilities are already the B operand of O^T += V^T P^T.  For that K's rows enter the MFMA
 // with index bits 2 and 3 swapped (bf16), which puts eight consecutive slots into each lane half.
@@ -105,181 +109,160 @@ __device__ __forceinline__ void wait_tiles(int behind) {
 // slot and 32 features per 32x32x2 MFMA and half).
 //
 // Probabilities are 2^(x - m) with a reference m (in log2 units) that is the row's maximum over its
-// first tile and moves only when a tile's sum passes 2^16: fp32 sums and bf16 probabilities
+// first block and moves only when a block's sum passes 2^16: fp32 sums and bf16 probabilities
 // (rounded to 8 bits, as their values are; the sum l takes them unrounded) keep their relative
-// precision at any scale, so ordinary tiles need no maximum.  When a tile passes the bound (and at
-// a row's first slots, where m = -inf makes the sum inf or NaN) its logits are formed again, m becomes
-// the maximum so far and O and l are scaled to it.
+// precision at any scale, so ordinary blocks need no maximum.  When a block passes the bound (and
+// at a row's first slots, where m = -inf makes the sum inf or NaN) its logits are formed again, m
+// becomes the maximum so far and O and l are scaled to it.
 // ------------------------------------------------------------------------
-template <typename T, bool WIDE>
-struct WaveState {
-    typedef Geo<T, WIDE> G;
-    bf16x8 qb[G::kBf ? G::NB : 1][4];
-    float qf[G::kBf ? 1 : G::NB][32];
-    f32x16 o[G::NB][2];
-    float m[G::NB], l[G::NB];
-    int vis[G::NB];
+template <typename T>
+struct Rows {
+    static constexpr bool kBf = sizeof(T) == 2;
+    bf16x8 qb[kBf ? 4 : 1];
+    float qf[kBf ? 1 : 32];
+    f32x16 o[2];
+    float m, l;
+    int vis;
+};
+// A block's probabilities as operands of the value product.
+template <typename T>
+struct Probs;
+template <>
+struct Probs<bf16> {
+    bf16x8 v[2];
+    __device__ __forceinline__ void set(const f32x16& s) {
+#pragma unroll
+        for (int st = 0; st < 2; ++st)
+            v[st] = pack_bf16x8(s[8 * st], s[8 * st + 1], s[8 * st + 2], s[8 * st + 3], s[8 * st + 4],
+                                s[8 * st + 5], s[8 * st + 6], s[8 * st + 7]);
+    }
+};
+template <>
+struct Probs<float> {
+    f32x16 v;
+    __device__ __forceinline__ void set(const f32x16& s) { v = s; }
 };
 constexpr float kMoveAt = 65536.f;
 
-template <typename T, bool WIDE>
-__device__ __forceinline__ void tile_logits(const WaveState<T, WIDE>& w, lds_char* tile, int lane,
-                                            f32x16 (&s)[Geo<T, WIDE>::NB][Geo<T, WIDE>::KB]) {
-    typedef Geo<T, WIDE> G;
+// Logits (without the scale) of the block whose K lies at `k`.
+template <typename T>
+__device__ __forceinline__ f32x16 block_logits(const Rows<T>& w, lds_char* k, int lane) {
     const int l31 = lane & 31, hh = lane >> 5;
-#pragma unroll
-    for (int nb = 0; nb < G::NB; ++nb)
-#pragma unroll
-        for (int kb = 0; kb < G::KB; ++kb) s[nb][kb] = zero_f32x16();
-    if constexpr (G::kBf) {
+    f32x16 s = zero_f32x16();
+    if constexpr (Rows<T>::kBf) {
         typedef __attribute__((address_space(3))) const bf16x8 lds_frag;
         const int row = swap23(l31);
         const int a0 = row * 128 + ((hh ^ ((row & 3) | ((row >> 3) & 1) << 2)) << 4);
 #pragma unroll
-        for (int kb = 0; kb < G::KB; ++kb)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const bf16x8 k = *(lds_frag*)(tile + kb * 4096 + (a0 ^ (i << 5)));
-#pragma unroll
-                for (int nb = 0; nb < G::NB; ++nb) s[nb][kb] = mfma_bf16(k, w.qb[nb][i], s[nb][kb]);
-            }
+        for (int i = 0; i < 4; ++i) s = mfma_bf16(*(lds_frag*)(k + (a0 ^ (i << 5))), w.qb[i], s);
     } else {
         typedef __attribute__((address_space(3))) const f32x4 lds_frag;
         const int a0 = l31 * 256 + ((hh ^ (l31 & 15)) << 4);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const f32x4 k = *(lds_frag*)(tile + (a0 ^ (i << 5)));
+            const f32x4 f = *(lds_frag*)(k + (a0 ^ (i << 5)));
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-#pragma unroll
-                for (int nb = 0; nb < G::NB; ++nb)
-                    s[nb][0] = mfma_f32(k[e], w.qf[nb][4 * i + e], s[nb][0]);
+            for (int e = 0; e < 4; ++e) s = mfma_f32(f[e], w.qf[4 * i + e], s);
         }
     }
+    return s;
 }
 
-// Slots that a row does not see: logits of -inf.  `units`: which groups of 16 slots exist.
-template <typename T, bool WIDE>
-__device__ __forceinline__ void tile_mask(const WaveState<T, WIDE>& w, int k0, uint32_t units, int lane,
-                                          f32x16 (&s)[Geo<T, WIDE>::NB][Geo<T, WIDE>::KB]) {
-    typedef Geo<T, WIDE> G;
+// Slots that a row does not see: logits of -inf.  `units`: which of the two groups of 16 slots exist.
+template <typename T>
+__device__ __forceinline__ void block_mask(const Rows<T>& w, int k0, uint32_t units, int lane, f32x16& s) {
+    typedef Geo<T, true> G;
+    // (compared with constants: the slots' numbers, which the lane half shifts, would otherwise
+    // stay in registers through the loop over the tiles)
+    const int left = w.vis - k0 - G::key(0, 1) * (lane >> 5);
 #pragma unroll
-    for (int nb = 0; nb < G::NB; ++nb) {
-        // (compared with constants: the slots' numbers, which the lane half shifts, would otherwise
-        // stay in registers through the loop over the tiles)
-        const int left = w.vis[nb] - k0 - G::key(0, 1) * (lane >> 5);
-#pragma unroll
-        for (int kb = 0; kb < G::KB; ++kb)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int k = 32 * kb + G::key(r, 0);
-                const bool ok = k < left && ((units >> (k >> 4)) & 1);
-                s[nb][kb][r] = ok ? s[nb][kb][r] : -INFINITY;
-            }
+    for (int r = 0; r < 16; ++r) {
+        const int k = G::key(r, 0);
+        s[r] = k < left && ((units >> (k >> 4)) & 1) ? s[r] : -INFINITY;
     }
 }
 
 // Logits to probabilities and their sum.
-template <int KB>
-__device__ __forceinline__ float tile_exp(f32x16 (&s)[KB], float c2, float ref) {
+__device__ __forceinline__ float block_exp(f32x16& s, float c2, float ref) {
     float ls[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            s[kb][r] = exp2f_fast(fmaf(s[kb][r], c2, -ref));
-            ls[r & 3] += s[kb][r];
-        }
+    for (int r = 0; r < 16; ++r) {
+        s[r] = exp2f_fast(fmaf(s[r], c2, -ref));
+        ls[r & 3] += s[r];
+    }
     return (ls[0] + ls[1]) + (ls[2] + ls[3]);
 }
 
-template <typename T, bool WIDE>
-__device__ __forceinline__ void attend_tile(WaveState<T, WIDE>& w, lds_char* tile, float c2, int k0,
-                                            bool partial, uint32_t units, int lane) {
-    typedef Geo<T, WIDE> G;
+// The block again, with the reference moved to the maximum so far.
+template <typename T>
+__device__ __forceinline__ float block_move(Rows<T>& w, lds_char* k, float c2, int k0, bool partial,
+                                            uint32_t units, int lane, Probs<T>& p) {
+    // (read again: the first pass's operands and logits do not stay in registers for this)
+    asm volatile("" ::: "memory");
+    f32x16 s = block_logits<T>(w, k, lane);
+    if (partial) block_mask<T>(w, k0, units, lane, s);
+    float top = s[0];
+#pragma unroll
+    for (int r = 0; r < 16; r += 2) top = maximum(maximum(top, s[r]), s[r + 1]);
+    const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+    top = maximum(__uint_as_float(x[0]), __uint_as_float(x[1])) * c2;
+    const float mn = top > w.m ? top : w.m;
+    const float f = w.m == mn ? 1.f : exp2f_fast(w.m - mn);   // 0 from -inf
+    w.l *= f;
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) w.o[m][r] *= f;
+    w.m = mn;
+    const float sum = block_exp(s, c2, mn == -INFINITY ? 0.f : mn);
+    p.set(s);
+    return sum;
+}
+
+// O^T += V^T P^T of the block whose V lies at `v`.
+template <typename T>
+__device__ __forceinline__ void block_values(Rows<T>& w, lds_char* v, const Probs<T>& p, int lane) {
     const int l31 = lane & 31, hh = lane >> 5;
-    f32x16 s[G::NB][G::KB];
-    float sum[G::NB];
-    tile_logits<T, WIDE>(w, tile, lane, s);
-    if (partial) tile_mask<T, WIDE>(w, k0, units, lane, s);
-    bool far = false;
-#pragma unroll
-    for (int nb = 0; nb < G::NB; ++nb) {
-        sum[nb] = tile_exp<G::KB>(s[nb], c2, w.m[nb]);   // inf or NaN while m is -inf
-        far = far || !(sum[nb] < kMoveAt);
-    }
-    if (__builtin_amdgcn_ballot_w64(far)) {
-        // (read again: the first pass's operands and logits do not stay in registers for this)
-        asm volatile("" ::: "memory");
-        tile_logits<T, WIDE>(w, tile, lane, s);
-        if (partial) tile_mask<T, WIDE>(w, k0, units, lane, s);
-#pragma unroll
-        for (int nb = 0; nb < G::NB; ++nb) {
-            float top = s[nb][0][0];
-#pragma unroll
-            for (int kb = 0; kb < G::KB; ++kb)
-#pragma unroll
-                for (int r = 0; r < 16; r += 2)
-                    top = maximum(maximum(top, s[nb][kb][r]), s[nb][kb][r + 1]);
-            const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
-            top = maximum(__uint_as_float(x[0]), __uint_as_float(x[1])) * c2;
-            const float mn = top > w.m[nb] ? top : w.m[nb];
-            const float f = w.m[nb] == mn ? 1.f : exp2f_fast(w.m[nb] - mn);   // 0 from -inf
-            w.l[nb] *= f;
-#pragma unroll
-            for (int m = 0; m < 2; ++m)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) w.o[nb][m][r] *= f;
-            w.m[nb] = mn;
-            sum[nb] = tile_exp<G::KB>(s[nb], c2, mn == -INFINITY ? 0.f : mn);
-        }
-    }
-#pragma unroll
-    for (int nb = 0; nb < G::NB; ++nb) w.l[nb] += sum[nb];
-    if constexpr (G::kBf) {
-        bf16x8 p[G::NB][G::KB][2];
-#pragma unroll
-        for (int nb = 0; nb < G::NB; ++nb)
-#pragma unroll
-            for (int kb = 0; kb < G::KB; ++kb)
-#pragma unroll
-                for (int st = 0; st < 2; ++st)
-                    p[nb][kb][st] = pack_bf16x8(
-                        s[nb][kb][8 * st], s[nb][kb][8 * st + 1], s[nb][kb][8 * st + 2],
-                        s[nb][kb][8 * st + 3], s[nb][kb][8 * st + 4], s[nb][kb][8 * st + 5],
-                        s[nb][kb][8 * st + 6], s[nb][kb][8 * st + 7]);
+    if constexpr (Rows<T>::kBf) {
         const int i16 = lane & 15, dq = (lane >> 4) & 1;
         const int v0 = (8 * hh + (i16 >> 2)) * 128 +
                        (((2 * dq + ((i16 & 3) >> 1)) ^ (2 * (i16 >> 2))) << 4) + (i16 & 1) * 8;
         typedef __attribute__((address_space(3))) s16x4 lds_tr;
-        lds_char* vt = tile + G::TK * G::ROWB;
+        typedef uint32_t u32x2 __attribute__((__vector_size__(8)));
 #pragma unroll
-        for (int kb = 0; kb < G::KB; ++kb)
+        for (int st = 0; st < 2; ++st)
 #pragma unroll
-            for (int st = 0; st < 2; ++st)
-#pragma unroll
-                for (int m = 0; m < 2; ++m) {
-                    lds_char* a = vt + (v0 ^ (m << 6)) + kb * 4096 + st * 2048;
-                    typedef uint32_t u32x2 __attribute__((__vector_size__(8)));
-                    const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr*)a));
-                    const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr*)(a + 512)));
-                    const u32x4 f = {x[0], x[1], y[0], y[1]};
-#pragma unroll
-                    for (int nb = 0; nb < G::NB; ++nb)
-                        w.o[nb][m] = mfma_bf16(__builtin_bit_cast(bf16x8, f), p[nb][kb][st], w.o[nb][m]);
-                }
+            for (int m = 0; m < 2; ++m) {
+                lds_char* a = v + (v0 ^ (m << 6)) + st * 2048;
+                const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr*)a));
+                const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr*)(a + 512)));
+                const u32x4 f = {x[0], x[1], y[0], y[1]};
+                w.o[m] = mfma_bf16(__builtin_bit_cast(bf16x8, f), p.v[st], w.o[m]);
+            }
     } else {
         typedef __attribute__((address_space(3))) const float lds_f32;
-        lds_char* vt = tile + G::TK * G::ROWB + hh * 1024 + l31 * 4;
+        lds_char* vt = v + hh * 1024 + l31 * 4;
 #pragma unroll
         for (int r = 0; r < 16; ++r)
 #pragma unroll
-            for (int m = 0; m < 2; ++m) {
-                const float v = *(lds_f32*)(vt + G::key(r, 0) * 256 + m * 128);
-#pragma unroll
-                for (int nb = 0; nb < G::NB; ++nb) w.o[nb][m] = mfma_f32(v, s[nb][0][r], w.o[nb][m]);
-            }
+            for (int m = 0; m < 2; ++m)
+                w.o[m] = mfma_f32(*(lds_f32*)(vt + Geo<T, true>::key(r, 0) * 256 + m * 128), p.v[r], w.o[m]);
     }
+}
+
+// One block after the other: logits, probabilities, values.
+template <typename T>
+__device__ __forceinline__ void block_attend(Rows<T>& w, lds_char* k, lds_char* v, float c2, int k0,
+                                             bool partial, uint32_t units, int lane) {
+    f32x16 s = block_logits<T>(w, k, lane);
+    if (partial) block_mask<T>(w, k0, units, lane, s);
+    float sum = block_exp(s, c2, w.m);   // inf or NaN while m is -inf
+    Probs<T> p;
+    p.set(s);
+    if (__builtin_amdgcn_ballot_w64(!(sum < kMoveAt)))
+        sum = block_move<T>(w, k, c2, k0, partial, units, lane, p);
+    w.l += sum;
+    block_values<T>(w, v, p, lane);
 }
 
 // Values of a tile that is seen in part, `rows` slots from slot k of the cache at `v` in LDS, before any
@@ -316,11 +299,11 @@ __device__ __forceinline__ bool clean_values(lds_char* v, int rows, int k, int e
 }
 
 // Values that are not finite in slots [k0, k1) of a tile seen in part, which clean_values() took
-// out, for the rows that see them.  Rare: slot by slot from memory, logits by plain sums.
-template <typename T, bool WIDE>
-__device__ __forceinline__ void add_odd_values(const AttendArgs& a, WaveState<T, WIDE>& w, int b, int hk,
-                                               int k0, int k1, int lane) {
-    typedef Geo<T, WIDE> G;
+// out, for the rows that see them.  Rare: slot by slot from memory, logits by plain sums, few loads
+// at a time (this must not set the kernel's register count).
+template <typename T>
+__device__ __forceinline__ void add_odd_values(const AttendArgs& a, Rows<T>& w, int b, int hk, int k0, int k1,
+                                               int lane) {
     const int hh = lane >> 5;
 #pragma unroll 1
     for (int k = k0; k < k1; ++k) {
@@ -329,42 +312,38 @@ __device__ __forceinline__ void add_odd_values(const AttendArgs& a, WaveState<T,
         const int64_t at = ((((int64_t)page * a.c.Hkv + hk) << a.c.page_log2) +
                             (k & ((1 << a.c.page_log2) - 1))) * kD;
         const T *kr = (const T*)a.c.K + at, *vr = (const T*)a.c.V + at;
+        float x = 0.f;
+        if constexpr (Rows<T>::kBf) {
 #pragma unroll
-        for (int nb = 0; nb < G::NB; ++nb) {
-            // (few loads at a time: this must not set the kernel's register count)
-            float x = 0.f;
-            if constexpr (G::kBf) {
+            for (int i = 0; i < 4; ++i) {
+                const bf16x8 kv = load_bf16x8((const bf16*)kr + 16 * i + 8 * hh);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const bf16x8 kv = load_bf16x8((const bf16*)kr + 16 * i + 8 * hh);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) x = fmaf((float)kv[j], (float)w.qb[nb][i][j], x);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const f32x4 kv = *(const f32x4*)(kr + 8 * i + 4 * hh);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) x = fmaf(kv[e], w.qf[nb][4 * i + e], x);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
+                for (int j = 0; j < 8; ++j) x = fmaf((float)kv[j], (float)w.qb[i][j], x);
+                __builtin_amdgcn_sched_barrier(0);
             }
-            x += __shfl_xor(x, 32);
-            const float p = exp2f_fast(fmaf(x, a.c2, -w.m[nb]));
-            const bool sees = k < w.vis[nb];
+        } else {
 #pragma unroll
-            for (int m = 0; m < 2; ++m)
+            for (int i = 0; i < 8; ++i) {
+                const f32x4 kv = *(const f32x4*)(kr + 8 * i + 4 * hh);
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float v = (float)vr[32 * m + 8 * g + 4 * hh + e];
-                        if (sees && !(fabsf(v) <= 3.4028235e38f)) w.o[nb][m][4 * g + e] += p * v;
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
-                }
+                for (int e = 0; e < 4; ++e) x = fmaf(kv[e], w.qf[4 * i + e], x);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
+        x += __shfl_xor(x, 32);
+        const float p = exp2f_fast(fmaf(x, a.c2, -w.m));
+        const bool sees = k < w.vis;
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float v = (float)vr[32 * m + 8 * g + 4 * hh + e];
+                    if (sees && !(fabsf(v) <= 3.4028235e38f)) w.o[m][4 * g + e] += p * v;
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
     }
 }
 
@@ -377,7 +356,7 @@ __device__ __forceinline__ void row_result(float m, float l, float* inv, float* 
 }
 
 template <typename T, bool WIDE>
-__global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), (Geo<T, WIDE>::NW / 2)) void k_cache_attend(AttendArgs a) {
+__global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), (WIDE && sizeof(T) == 2 ? 3 : 2)) void k_cache_attend(AttendArgs a) {
     typedef Geo<T, WIDE> G;
     __shared__ __attribute__((aligned(1024))) char smem[G::kLds];
     const int tid = threadIdx.x, lane = tid & 63, l31 = lane & 31, hh = lane >> 5;
@@ -393,7 +372,7 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), (Geo<T, WIDE>::NW / 2)) vo
     if (b >= a.c.B) return;
 
     const CacheSeq sq = cache_seq(a.c, b);
-    const int nrows = sq.nq * a.G, row0 = rt * G::RT + (WIDE ? wave * 32 * G::NB : 0);
+    const int nrows = sq.nq * a.G, row0 = rt * G::RT + (WIDE ? wave * 32 : 0);
     if (rt * G::RT >= nrows) return;
     const int tile_last = rt * G::RT + G::RT - 1 < nrows ? rt * G::RT + G::RT - 1 : nrows - 1;
     const int klim = cache_visible(sq, a.causal, tile_last / a.G);
@@ -401,33 +380,32 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), (Geo<T, WIDE>::NW / 2)) vo
     if (split > 0 && c0 >= klim) return;
 
     // ---- this wave's rows
-    WaveState<T, WIDE> w;
+    Rows<T> w;
     const bool alive = row0 < nrows;
-    int64_t orow[G::NB];   // row of O
-#pragma unroll
-    for (int nb = 0; nb < G::NB; ++nb) {
-        int r = row0 + 32 * nb + l31;
+    int64_t orow;   // row of O
+    {
+        int r = row0 + l31;
         r = r < nrows ? r : nrows - 1;
         const int i = r / a.G, head = hk * a.G + r - i * a.G;
-        w.vis[nb] = cache_visible(sq, a.causal, i);
-        w.m[nb] = -INFINITY;
-        w.l[nb] = 0.f;
-        w.o[nb][0] = w.o[nb][1] = zero_f32x16();
-        orow[nb] = (int64_t)(sq.q0 + i) * a.Hq + head;
+        w.vis = cache_visible(sq, a.causal, i);
+        w.m = -INFINITY;
+        w.l = 0.f;
+        w.o[0] = w.o[1] = zero_f32x16();
+        orow = (int64_t)(sq.q0 + i) * a.Hq + head;
         const T* q = (const T*)a.Q + (int64_t)(sq.q0 + i) * a.q_stride + head * kD;
         if constexpr (G::kBf) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) w.qb[nb][k] = load_bf16x8(q + 16 * k + 8 * hh);
+            for (int k = 0; k < 4; ++k) w.qb[k] = load_bf16x8(q + 16 * k + 8 * hh);
         } else {
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 const f32x4 v = *(const f32x4*)(q + 8 * k + 4 * hh);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) w.qf[nb][4 * k + e] = v[e];
+                for (int e = 0; e < 4; ++e) w.qf[4 * k + e] = v[e];
             }
         }
     }
-    const int wave_last = row0 + 32 * G::NB - 1 < nrows ? row0 + 32 * G::NB - 1 : nrows - 1;
+    const int wave_last = row0 + 31 < nrows ? row0 + 31 : nrows - 1;
     const int wlim = alive ? cache_visible(sq, a.causal, wave_last / a.G) : 0;
     // slots of this range that every row of the workgroup sees
     const int all = cache_visible(sq, a.causal, rt * G::RT / a.G), seen_by_all = all < c1 ? all : c1;
@@ -475,46 +453,146 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), (Geo<T, WIDE>::NW / 2)) vo
             }
         };
 #pragma unroll
-        for (int t = 0; t < G::NST - 1; ++t)
+        for (int t = 0; t < G::AHEAD; ++t)
             if (t < nt) issue(t);
+        // Groups of 16 slots of the tile at k0 that exist (all, unless the table is wrong).
+        auto groups = [&](int k0) {
+            uint32_t units = ~0u;
+            if (!pw.sane) {
+                units = 0;
+#pragma unroll
+                for (int u = 0; u < G::TK / 16; ++u) {
+                    const int at = (k0 + 16 * u) >> a.c.page_log2;
+                    if (at <= pw.last && pw.valid(pw.row[at])) units |= 1u << u;
+                }
+            }
+            return units;
+        };
         bool odd = false;
-        for (int t = 0; t < nt; ++t) {
-            const int more = nt - 1 - t;
-            const int k0 = c0 + (tfirst + t * tstep) * G::TK;
+        // Tile t has come: its copies, and where it is seen in part its values are cleaned by the wave
+        // that copied them.  Then (wide) all waves are past the tile whose place the next copies take.
+        auto arrive = [&](int t) {
+            const int more = nt - 1 - t, k0 = c0 + (tfirst + t * tstep) * G::TK;
             lds_char* tile = ring + (t % G::NST) * G::kTile;
             if constexpr (WIDE) {
-                wait_tiles<G::CPT>(more < G::NST - 2 ? more : G::NST - 2);
+                wait_tiles<G::CPT>(more < G::AHEAD - 1 ? more : G::AHEAD - 1);
             } else {
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the tile before is read
-                if (t + G::NST - 1 < nt) issue(t + G::NST - 1);
-                wait_tiles<G::CPT>(more < G::NST - 1 ? more : G::NST - 1);
+                if (t + G::AHEAD < nt) issue(t + G::AHEAD);
+                wait_tiles<G::CPT>(more < G::AHEAD ? more : G::AHEAD);
             }
-            const bool partial = !pw.sane || k0 + G::TK > seen_by_all;
-            uint32_t units = ~0u;
-            if (partial) {
-                if (!pw.sane) {
-                    units = 0;
-#pragma unroll
-                    for (int u = 0; u < G::TK / 16; ++u) {
-                        const int at = (k0 + 16 * u) >> a.c.page_log2;
-                        if (at <= pw.last && pw.valid(pw.row[at])) units |= 1u << u;
-                    }
-                }
-                // this wave's own copies have arrived: no barrier in between
+            if (!pw.sane || k0 + G::TK > seen_by_all) {
+                const uint32_t units = groups(k0);
                 if constexpr (WIDE) {
-                    static_assert(G::PPW == 1, "a wave copies 16 slots of K or of V");
-                    const int u = 16 * (wave >> 1);
-                    if (wave & 1)
-                        odd |= clean_values<T>(tile + (G::TK + u) * G::ROWB, 16, k0 + u, c1, units >> (wave >> 1),
-                                               lane);
+                    // (a wave copies 16 slots, or K or V of them)
+                    const int u = 16 * (wave * G::PPW >> 1);
+                    if (G::PPW == 2 || (wave & 1))
+                        odd |= clean_values<T>(tile + G::kTileV + u * G::ROWB, 16, k0 + u, c1, units >> (u >> 4), lane);
                 } else
-                    odd |= clean_values<T>(tile + G::TK * G::ROWB, G::TK, k0, c1, units, lane);
+                    odd |= clean_values<T>(tile + G::kTileV, G::TK, k0, c1, units, lane);
             }
             if constexpr (WIDE) {
                 __builtin_amdgcn_s_barrier();
-                if (t + G::NST - 1 < nt) issue(t + G::NST - 1);
+                if (t + G::AHEAD < nt) issue(t + G::AHEAD);
             }
-            if (k0 < wlim) attend_tile<T, WIDE>(w, tile, a.c2, k0, partial, units, lane);
+        };
+        auto tile_at = [&](int t) { return ring + (t % G::NST) * G::kTile; };
+        // Every block with its bound on the reference checked.
+        auto careful = [&]() {
+            for (int t = 0; t < nt; ++t) {
+                const int k0 = c0 + (tfirst + t * tstep) * G::TK;
+                lds_char* tile = tile_at(t);
+                arrive(t);
+                const bool partial = !pw.sane || k0 + G::TK > seen_by_all;
+                const uint32_t units = partial ? groups(k0) : 0;
+                if (k0 < wlim)
+#pragma unroll 1
+                    for (int j = 0; j < G::TK / 32; ++j)
+                        block_attend<T>(w, tile + j * G::kBlock, tile + G::kTileV + j * G::kBlock, a.c2, k0 + 32 * j,
+                                        partial, units >> (2 * j), lane);
+            }
+        };
+        if constexpr (WIDE && G::kBf) {
+            // The reference stays that of the first block.  While block j's probabilities are formed, block
+            // j + 1's logits and block j - 1's values are multiplied: matrix and vector
+            // instructions without a dependence or a branch between them.  Should a row's sum or
+            // result leave fp32's range with it (its logits grew by more than 41 over the first block's, its
+            // first block had none, or values are huge), the workgroup does its range again carefully.
+            __shared__ int s_redo[G::NW];
+            const int tfull = pw.sane ? (seen_by_all - c0) / G::TK : 0;   // tiles all rows see
+            f32x16 s0, s1;
+            Probs<T> p0, p1;
+            float ref = 0.f, sum[4] = {0.f, 0.f, 0.f, 0.f};
+            auto probs = [&](auto mask, f32x16& s, int k0, Probs<T>& p) {
+                if constexpr (decltype(mask)::value) block_mask<T>(w, k0, ~0u, lane, s);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    s[r] = exp2f_fast(fmaf(s[r], a.c2, -ref));
+                    sum[r & 3] += s[r];
+                }
+                p.set(s);
+            };
+            auto body = [&](auto mask, int t) {   // second block of tile t, first of tile t + 1
+                lds_char *cur = tile_at(t), *next = tile_at(t + 1);
+                const int k0 = c0 + t * G::TK;
+                s0 = block_logits<T>(w, next, lane);
+                block_values<T>(w, cur + G::kTileV, p0, lane);
+                probs(mask, s1, k0 + 32, p1);
+                s1 = block_logits<T>(w, next + G::kBlock, lane);
+                block_values<T>(w, cur + G::kTileV + G::kBlock, p1, lane);
+                probs(mask, s0, k0 + 64, p0);
+            };
+            arrive(0);
+            if (alive && pw.sane) {
+                s0 = block_logits<T>(w, tile_at(0), lane);
+                block_mask<T>(w, c0, ~0u, lane, s0);
+                float top = s0[0];
+#pragma unroll
+                for (int r = 0; r < 16; r += 2) top = maximum(maximum(top, s0[r]), s0[r + 1]);
+                const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+                w.m = maximum(__uint_as_float(x[0]), __uint_as_float(x[1])) * a.c2;
+                ref = w.m == -INFINITY ? 0.f : w.m;
+                s1 = block_logits<T>(w, tile_at(0) + G::kBlock, lane);
+                probs(std::true_type(), s0, c0, p0);
+                int t = 0;
+                for (; t + 1 < nt && t + 1 < tfull; ++t) {
+                    arrive(t + 1);
+                    body(std::false_type(), t);
+                }
+                for (; t + 1 < nt; ++t) {
+                    arrive(t + 1);
+                    body(std::true_type(), t);
+                }
+                probs(std::true_type(), s1, c0 + t * G::TK + 32, p1);
+                block_values<T>(w, tile_at(t) + G::kTileV, p0, lane);
+                block_values<T>(w, tile_at(t) + G::kTileV + G::kBlock, p1, lane);
+                w.l = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            } else {
+                for (int t = 1; t < nt; ++t) arrive(t);
+            }
+            bool redo = !pw.sane;
+            if (alive) {
+                bool far = !(w.l < 1152921504606846976.f) || (w.m == -INFINITY && w.vis > c0);   // 2^60
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) far = far || !(fabsf(w.o[m][r]) <= 3.4028235e38f);
+                redo = redo || __builtin_amdgcn_ballot_w64(far);
+            }
+            if (lane == 0) s_redo[wave] = redo;
+            __syncthreads();
+            if (s_redo[0] | s_redo[1] | s_redo[2] | s_redo[3]) {
+                w.o[0] = w.o[1] = zero_f32x16();
+                w.m = -INFINITY;
+                w.l = 0.f;
+                pw.start(a.c, b, c0, c1 - 1, lane);
+#pragma unroll
+                for (int t = 0; t < G::AHEAD; ++t)
+                    if (t < nt) issue(t);
+                careful();
+            }
+        } else {
+            careful();
         }
         if constexpr (WIDE) {   // what one wave took out, all see to
             __shared__ int s_odd[G::NW];
@@ -526,66 +604,62 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), (Geo<T, WIDE>::NW / 2)) vo
             for (int t = 0; t < nt; ++t) {
                 const int k0 = c0 + (tfirst + t * tstep) * G::TK;
                 if (!pw.sane || k0 + G::TK > seen_by_all)
-                    add_odd_values<T, WIDE>(a, w, b, hk, k0, k0 + G::TK < c1 ? k0 + G::TK : c1, lane);
+                    add_odd_values<T>(a, w, b, hk, k0, k0 + G::TK < c1 ? k0 + G::TK : c1, lane);
             }
     }
-#pragma unroll
-    for (int nb = 0; nb < G::NB; ++nb) w.l[nb] += __shfl_xor(w.l[nb], 32);
+    w.l += __shfl_xor(w.l, 32);
 
     const int64_t all_rows = (int64_t)a.c.T * a.Hq;
     if constexpr (WIDE) {
+        if (row0 + l31 >= nrows) return;
+        if (a.nsplit > 1) {
+            float* po = a.part + (split * all_rows + orow) * kD;
+            if (hh == 0) {
+                f32x2 ml = {w.m, w.l};
+                *(f32x2*)(a.part_ml + (split * all_rows + orow) * 2) = ml;
+            }
 #pragma unroll
-        for (int nb = 0; nb < G::NB; ++nb) {
-            if (row0 + 32 * nb + l31 >= nrows) continue;
-            if (a.nsplit > 1) {
-                float* po = a.part + (split * all_rows + orow[nb]) * kD;
-                if (hh == 0) {
-                    f32x2 ml = {w.m[nb], w.l[nb]};
-                    *(f32x2*)(a.part_ml + (split * all_rows + orow[nb]) * 2) = ml;
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    f32x4 v;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = w.o[m][4 * g + e];
+                    *(f32x4*)(po + 32 * m + 8 * g + 4 * hh) = v;
                 }
+            return;
+        }
+        float inv, lse;
+        row_result(w.m, w.l, &inv, &lse);
+        if (hh == 0) a.lse[orow] = lse;
+        T* out = (T*)a.O + orow * kD;
+        if constexpr (G::kBf) {
 #pragma unroll
-                for (int m = 0; m < 2; ++m)
+            for (int m = 0; m < 2; ++m)
 #pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        f32x4 v;
+                for (int g = 0; g < 2; ++g) {
+                    uint32_t d[4];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) v[e] = w.o[nb][m][4 * g + e];
-                        *(f32x4*)(po + 32 * m + 8 * g + 4 * hh) = v;
+                    for (int e = 0; e < 4; ++e) {
+                        bf16x2 pr = {(bf16)(w.o[m][8 * g + 2 * e] * inv),
+                                     (bf16)(w.o[m][8 * g + 2 * e + 1] * inv)};
+                        d[e] = __builtin_bit_cast(uint32_t, pr);
                     }
-                continue;
-            }
-            float inv, lse;
-            row_result(w.m[nb], w.l[nb], &inv, &lse);
-            if (hh == 0) a.lse[orow[nb]] = lse;
-            T* out = (T*)a.O + orow[nb] * kD;
-            if constexpr (G::kBf) {
+                    swap_halves(d[0], d[2]);
+                    swap_halves(d[1], d[3]);
+                    u32x4 v = {d[0], d[1], d[2], d[3]};
+                    *(u32x4*)(out + 32 * m + 16 * g + 8 * hh) = v;
+                }
+        } else {
 #pragma unroll
-                for (int m = 0; m < 2; ++m)
+            for (int m = 0; m < 2; ++m)
 #pragma unroll
-                    for (int g = 0; g < 2; ++g) {
-                        uint32_t d[4];
+                for (int g = 0; g < 4; ++g) {
+                    f32x4 v;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            bf16x2 pr = {(bf16)(w.o[nb][m][8 * g + 2 * e] * inv),
-                                         (bf16)(w.o[nb][m][8 * g + 2 * e + 1] * inv)};
-                            d[e] = __builtin_bit_cast(uint32_t, pr);
-                        }
-                        swap_halves(d[0], d[2]);
-                        swap_halves(d[1], d[3]);
-                        u32x4 v = {d[0], d[1], d[2], d[3]};
-                        *(u32x4*)(out + 32 * m + 16 * g + 8 * hh) = v;
-                    }
-            } else {
-#pragma unroll
-                for (int m = 0; m < 2; ++m)
-#pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        f32x4 v;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) v[e] = w.o[nb][m][4 * g + e] * inv;
-                        *(f32x4*)(out + 32 * m + 8 * g + 4 * hh) = v;
-                    }
-            }
+                    for (int e = 0; e < 4; ++e) v[e] = w.o[m][4 * g + e] * inv;
+                    *(f32x4*)(out + 32 * m + 8 * g + 4 * hh) = v;
+                }
         }
     } else {
         // The four waves' partial results meet in LDS (the ring is free then).
@@ -595,14 +669,14 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), (Geo<T, WIDE>::NW / 2)) vo
         static_assert((256 + 4 * 32 * kRow) * 4 <= G::kLds, "partial results fit the ring");
         __syncthreads();
         if (hh == 0) {
-            sml[(wave * 32 + l31) * 2] = w.m[0];
-            sml[(wave * 32 + l31) * 2 + 1] = w.l[0];
+            sml[(wave * 32 + l31) * 2] = w.m;
+            sml[(wave * 32 + l31) * 2 + 1] = w.l;
         }
         __syncthreads();
         float M = -INFINITY;
 #pragma unroll
         for (int v = 0; v < 4; ++v) M = maximum(M, sml[(v * 32 + l31) * 2]);
-        const float f = w.m[0] == -INFINITY ? 0.f : w.m[0] == M ? 1.f : exp2f_fast(w.m[0] - M);
+        const float f = w.m == -INFINITY ? 0.f : w.m == M ? 1.f : exp2f_fast(w.m - M);
         if (row0 + l31 < nrows) {
 #pragma unroll
             for (int m = 0; m < 2; ++m)
@@ -610,7 +684,7 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), (Geo<T, WIDE>::NW / 2)) vo
                 for (int g = 0; g < 4; ++g) {
                     f32x4 v;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = w.o[0][m][4 * g + e] * f;
+                    for (int e = 0; e < 4; ++e) v[e] = w.o[m][4 * g + e] * f;
                     *(f32x4*)(so + (wave * 32 + l31) * kRow + 32 * m + 8 * g + 4 * hh) = v;
                 }
         }
@@ -830,7 +904,7 @@ __global__ __launch_bounds__(256, 2) void k_cache_weight(AttendArgs a) {
 void attend_plan(AttendArgs* a) {
     const int64_t rows = (int64_t)a->c.max_q * a->G;
     a->wide = rows > 64;
-    const int rt = !a->wide ? 32 : a->c.dtype == DT_BF16 ? 256 : 128;
+    const int rt = a->wide ? 128 : 32;
     a->row_tiles = (int)((rows + rt - 1) / rt);
     if (a->row_tiles < 1) a->row_tiles = 1;
     const int64_t items = (int64_t)a->c.B * a->c.Hkv * a->row_tiles;
