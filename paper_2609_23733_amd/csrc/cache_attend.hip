@@ -20,24 +20,26 @@ __device__ __forceinline__ float maximum(float a, float b) {
 }
 
 // ------------------------------------------------------------------------
-// Geometry of the two kernel variants.  A wave owns 32 rows and multiplies them with 32 slots (a
-// block) at a time.  Narrow: 32 rows per workgroup, its four waves split the slots and each
-// streams tiles of its own (no barrier until the end).  Wide: four waves of 32 rows each, which
-// share every tile.
+// Geometry of the two kernel variants.  A wave multiplies groups of 32 rows with 32 slots (a block)
+// at a time.  Narrow: 32 rows per workgroup, its four waves split the slots and each
+// streams tiles of its own (no barrier until the end).  Wide: the four waves share every tile, with
+// 64 rows each (bf16: an operand read from LDS serves two MFMAs; with 32 rows the LDS reads
+// alone take as long as the MFMAs) or 32 (fp32, whose MFMAs take eight times as long).
 // ------------------------------------------------------------------------
 template <typename T, bool WIDE>
 struct Geo {
     static constexpr bool kBf = sizeof(T) == 2;
     static constexpr int NW = 4;                                // waves
+    static constexpr int NB = WIDE && kBf ? 2 : 1;              // groups of 32 rows per wave
     static constexpr int TK = WIDE && kBf ? 64 : 32;            // slots per tile
-    static constexpr int RT = WIDE ? 32 * NW : 32;              // rows per workgroup
+    static constexpr int RT = WIDE ? 32 * NB * NW : 32;         // rows per workgroup
     static constexpr int ROWB = kD * sizeof(T);                 // bytes of a slot's K or V
     static constexpr int kBlock = 32 * ROWB;                    // bytes of a block's K or V
     static constexpr int kTileV = TK * ROWB;                    // a tile's V comes after its K
     static constexpr int kTile = 2 * TK * ROWB;
     // Tiles in LDS, and how many tiles ahead of the arriving one copies are issued: into the
     // place of the tile before it, or (wide bf16, where that one is still in use) of the one before.
-    static constexpr int NST = WIDE ? 3 : 2;
+    static constexpr int NST = WIDE ? (kBf ? 4 : 3) : 2;
     static constexpr int AHEAD = WIDE && kBf ? NST - 2 : NST - 1;
     static constexpr int kRing = NST * kTile;
     static constexpr int kLds = WIDE ? kRing : 4 * kRing;
@@ -152,7 +154,7 @@ __device__ __forceinline__ f32x16 block_logits(const Rows<T>& w, lds_char* k, in
     if constexpr (Rows<T>::kBf) {
         typedef __attribute__((address_space(3))) const bf16x8 lds_frag;
         const int row = swap23(l31);
-        const int a0 = row * 128 + ((hh ^ ((row & 3) | ((row >> 3) & 1) << 2)) << 4);
+        const int a0 = row * 128 + ((hh ^ ((row >> 1) & 7)) << 4);
 #pragma unroll
         for (int i = 0; i < 4; ++i) s = mfma_bf16(*(lds_frag*)(k + (a0 ^ (i << 5))), w.qb[i], s);
     } else {
@@ -219,6 +221,17 @@ __device__ __forceinline__ float block_move(Rows<T>& w, lds_char* k, float c2, i
     return sum;
 }
 
+// Transposing read: of 16 lanes, lane i gets column i of the 4 x 16 values whose rows its quads
+// address; two of them, four rows (512 bytes) apart, make eight slots of a feature.
+__device__ __forceinline__ bf16x8 tr_read(lds_char* a) {
+    typedef __attribute__((address_space(3))) s16x4 lds_tr;
+    typedef uint32_t u32x2 __attribute__((__vector_size__(8)));
+    const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr*)a));
+    const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr*)(a + 512)));
+    const u32x4 f = {x[0], x[1], y[0], y[1]};
+    return __builtin_bit_cast(bf16x8, f);
+}
+
 // O^T += V^T P^T of the block whose V lies at `v`.
 template <typename T>
 __device__ __forceinline__ void block_values(Rows<T>& w, lds_char* v, const Probs<T>& p, int lane) {
@@ -227,17 +240,11 @@ __device__ __forceinline__ void block_values(Rows<T>& w, lds_char* v, const Prob
         const int i16 = lane & 15, dq = (lane >> 4) & 1;
         const int v0 = (8 * hh + (i16 >> 2)) * 128 +
                        (((2 * dq + ((i16 & 3) >> 1)) ^ (2 * (i16 >> 2))) << 4) + (i16 & 1) * 8;
-        typedef __attribute__((address_space(3))) s16x4 lds_tr;
-        typedef uint32_t u32x2 __attribute__((__vector_size__(8)));
 #pragma unroll
         for (int st = 0; st < 2; ++st)
 #pragma unroll
             for (int m = 0; m < 2; ++m) {
-                lds_char* a = v + (v0 ^ (m << 6)) + st * 2048;
-                const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr*)a));
-                const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr*)(a + 512)));
-                const u32x4 f = {x[0], x[1], y[0], y[1]};
-                w.o[m] = mfma_bf16(__builtin_bit_cast(bf16x8, f), p.v[st], w.o[m]);
+                w.o[m] = mfma_bf16(tr_read(v + (v0 ^ (m << 6)) + st * 2048), p.v[st], w.o[m]);
             }
     } else {
         typedef __attribute__((address_space(3))) const float lds_f32;
@@ -356,7 +363,7 @@ __device__ __forceinline__ void row_result(float m, float l, float* inv, float* 
 }
 
 template <typename T, bool WIDE>
-__global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), (WIDE && sizeof(T) == 2 ? 3 : 2)) void k_cache_attend(AttendArgs a) {
+__global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(AttendArgs a) {
     typedef Geo<T, WIDE> G;
     __shared__ __attribute__((aligned(1024))) char smem[G::kLds];
     const int tid = threadIdx.x, lane = tid & 63, l31 = lane & 31, hh = lane >> 5;
@@ -372,7 +379,7 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), (WIDE && sizeof(T) == 2 ? 
     if (b >= a.c.B) return;
 
     const CacheSeq sq = cache_seq(a.c, b);
-    const int nrows = sq.nq * a.G, row0 = rt * G::RT + (WIDE ? wave * 32 : 0);
+    const int nrows = sq.nq * a.G, row0 = rt * G::RT + (WIDE ? wave * 32 * G::NB : 0);
     if (rt * G::RT >= nrows) return;
     const int tile_last = rt * G::RT + G::RT - 1 < nrows ? rt * G::RT + G::RT - 1 : nrows - 1;
     const int klim = cache_visible(sq, a.causal, tile_last / a.G);
@@ -380,32 +387,33 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), (WIDE && sizeof(T) == 2 ? 
     if (split > 0 && c0 >= klim) return;
 
     // ---- this wave's rows
-    Rows<T> w;
+    Rows<T> w[G::NB];
     const bool alive = row0 < nrows;
-    int64_t orow;   // row of O
-    {
-        int r = row0 + l31;
+    int64_t orow[G::NB];   // row of O
+#pragma unroll
+    for (int nb = 0; nb < G::NB; ++nb) {
+        int r = row0 + 32 * nb + l31;
         r = r < nrows ? r : nrows - 1;
         const int i = r / a.G, head = hk * a.G + r - i * a.G;
-        w.vis = cache_visible(sq, a.causal, i);
-        w.m = -INFINITY;
-        w.l = 0.f;
-        w.o[0] = w.o[1] = zero_f32x16();
-        orow = (int64_t)(sq.q0 + i) * a.Hq + head;
+        w[nb].vis = cache_visible(sq, a.causal, i);
+        w[nb].m = -INFINITY;
+        w[nb].l = 0.f;
+        w[nb].o[0] = w[nb].o[1] = zero_f32x16();
+        orow[nb] = (int64_t)(sq.q0 + i) * a.Hq + head;
         const T* q = (const T*)a.Q + (int64_t)(sq.q0 + i) * a.q_stride + head * kD;
         if constexpr (G::kBf) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) w.qb[k] = load_bf16x8(q + 16 * k + 8 * hh);
+            for (int k = 0; k < 4; ++k) w[nb].qb[k] = load_bf16x8(q + 16 * k + 8 * hh);
         } else {
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 const f32x4 v = *(const f32x4*)(q + 8 * k + 4 * hh);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) w.qf[4 * k + e] = v[e];
+                for (int e = 0; e < 4; ++e) w[nb].qf[4 * k + e] = v[e];
             }
         }
     }
-    const int wave_last = row0 + 31 < nrows ? row0 + 31 : nrows - 1;
+    const int wave_last = row0 + 32 * G::NB - 1 < nrows ? row0 + 32 * G::NB - 1 : nrows - 1;
     const int wlim = alive ? cache_visible(sq, a.causal, wave_last / a.G) : 0;
     // slots of this range that every row of the workgroup sees
     const int all = cache_visible(sq, a.causal, rt * G::RT / a.G), seen_by_all = all < c1 ? all : c1;
@@ -422,12 +430,12 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), (WIDE && sizeof(T) == 2 ? 
         const int page_mask = (1 << a.c.page_log2) - 1;
         const int last_unit = (c1 - 1) & ~15;
         // Per lane: byte within a 1 KB copy.  K's and V's 16-byte pieces are exchanged within
-        // their row so that the tile's readers meet no bank twice: K's piece p of slot s lies at p ^
-        // (s & 3 | s bit 3 << 2) (bf16) or p ^ (s & 15) (fp32), V's at p ^ 2 (s & 3) (bf16).
+        // their row so that the tile's readers meet no bank twice (64 banks: two bf16 rows): K's piece p of
+        // slot s lies at p ^ (s / 2 & 7) (bf16) or p ^ (s & 15) (fp32), V's at p ^ 2 (s & 3) (bf16).
         uint32_t kv, vv;
         if constexpr (G::kBf) {
             const int r = lane >> 3, pc = lane & 7;
-            kv = r * 128 + ((pc ^ (r & 3)) << 4);
+            kv = r * 128 + ((pc ^ (r >> 1)) << 4);
             vv = r * 128 + ((pc ^ (2 * (r & 3))) << 4);
         } else {
             const int r = lane >> 4, pc = lane & 15;
@@ -508,8 +516,10 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), (WIDE && sizeof(T) == 2 ? 
                 if (k0 < wlim)
 #pragma unroll 1
                     for (int j = 0; j < G::TK / 32; ++j)
-                        block_attend<T>(w, tile + j * G::kBlock, tile + G::kTileV + j * G::kBlock, a.c2, k0 + 32 * j,
-                                        partial, units >> (2 * j), lane);
+#pragma unroll
+                        for (int nb = 0; nb < G::NB; ++nb)
+                            block_attend<T>(w[nb], tile + j * G::kBlock, tile + G::kTileV + j * G::kBlock, a.c2,
+                                            k0 + 32 * j, partial, units >> (2 * j), lane);
             }
         };
         if constexpr (WIDE && G::kBf) {
@@ -520,40 +530,92 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), (WIDE && sizeof(T) == 2 ? 
             // first block had none, or values are huge), the workgroup does its range again carefully.
             __shared__ int s_redo[G::NW];
             const int tfull = pw.sane ? (seen_by_all - c0) / G::TK : 0;   // tiles all rows see
-            f32x16 s0, s1;
-            Probs<T> p0, p1;
-            float ref = 0.f, sum[4] = {0.f, 0.f, 0.f, 0.f};
-            auto probs = [&](auto mask, f32x16& s, int k0, Probs<T>& p) {
-                if constexpr (decltype(mask)::value) block_mask<T>(w, k0, ~0u, lane, s);
+            f32x16 s0[G::NB], s1[G::NB];
+            Probs<T> p0[G::NB], p1[G::NB];
+            float ref[G::NB], sum[G::NB][4] = {};
+            // Half a tile: eight operands from LDS, each for the MFMAs of the row groups and followed by the
+            // vector instructions of two of a group's 16 logits; they are read three ahead.  The first three are values, of a tile
+            // that has been there for long: they are read before the barrier that K waits for.
+            bf16x8 ahead[3];
+            auto value_at = [&](lds_char* v, int i) {
+                const int i16 = lane & 15, dq = (lane >> 4) & 1;
+                const int v0 = (8 * hh + (i16 >> 2)) * 128 +
+                               (((2 * dq + ((i16 & 3) >> 1)) ^ (2 * (i16 >> 2))) << 4) + (i16 & 1) * 8;
+                return tr_read(v + (v0 ^ ((i & 1) << 6)) + (i >> 1) * 2048);
+            };
+            auto key_at = [&](lds_char* k, int i) {
+                typedef __attribute__((address_space(3))) const bf16x8 lds_frag;
+                const int row = swap23(l31);
+                const int a0 = row * 128 + ((hh ^ ((row >> 1) & 7)) << 4);
+                return *(lds_frag*)(k + (a0 ^ (i << 5)));
+            };
+            typedef f32x16 Logits[G::NB];
+            typedef Probs<T> BlockP[G::NB];
+            auto half = [&](auto mask, Logits& s, int k0, Logits& sn, lds_char* k, lds_char* v, lds_char* v_next,
+                            const BlockP& pv, BlockP& pn) {
+                if constexpr (decltype(mask)::value)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    s[r] = exp2f_fast(fmaf(s[r], a.c2, -ref));
-                    sum[r & 3] += s[r];
+                    for (int nb = 0; nb < G::NB; ++nb) block_mask<T>(w[nb], k0, ~0u, lane, s[nb]);
+                constexpr int kOf[8] = {4, 5, 6, 0, 7, 1, 2, 3};   // 0-3: logits, 4-7: values
+                bf16x8 f[8] = {ahead[0], ahead[1], ahead[2]};
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    if (i < 5) f[i + 3] = kOf[i + 3] < 4 ? key_at(k, kOf[i + 3]) : value_at(v, kOf[i + 3] - 4);
+                    else ahead[i - 5] = value_at(v_next, i - 5);
+                    const int n = kOf[i];
+#pragma unroll
+                    for (int nb = 0; nb < G::NB; ++nb) {
+                        Rows<T>& x = w[nb];
+                        if (n < 4) sn[nb] = mfma_bf16(f[i], x.qb[n], n ? sn[nb] : zero_f32x16());
+                        else x.o[n & 1] = mfma_bf16(f[i], pv[nb].v[(n - 4) >> 1], x.o[n & 1]);
+#pragma unroll
+                        for (int r = 2 * i; r < 2 * i + 2; ++r) {
+                            s[nb][r] = exp2f_fast(fmaf(s[nb][r], a.c2, -ref[nb]));
+                            sum[nb][r & 3] += s[nb][r];
+                        }
+                        pn[nb].v[i >> 2][(2 * i) & 7] = (bf16)s[nb][2 * i];
+                        pn[nb].v[i >> 2][(2 * i + 1) & 7] = (bf16)s[nb][2 * i + 1];
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
                 }
-                p.set(s);
+            };
+            auto probs = [&](Logits& s, int k0, BlockP& p) {
+#pragma unroll
+                for (int nb = 0; nb < G::NB; ++nb) {
+                    block_mask<T>(w[nb], k0, ~0u, lane, s[nb]);
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        s[nb][r] = exp2f_fast(fmaf(s[nb][r], a.c2, -ref[nb]));
+                        sum[nb][r & 3] += s[nb][r];
+                    }
+                    p[nb].set(s[nb]);
+                }
             };
             auto body = [&](auto mask, int t) {   // second block of tile t, first of tile t + 1
                 lds_char *cur = tile_at(t), *next = tile_at(t + 1);
                 const int k0 = c0 + t * G::TK;
-                s0 = block_logits<T>(w, next, lane);
-                block_values<T>(w, cur + G::kTileV, p0, lane);
-                probs(mask, s1, k0 + 32, p1);
-                s1 = block_logits<T>(w, next + G::kBlock, lane);
-                block_values<T>(w, cur + G::kTileV + G::kBlock, p1, lane);
-                probs(mask, s0, k0 + 64, p0);
+                half(mask, s1, k0 + 32, s0, next, cur + G::kTileV, cur + G::kTileV + G::kBlock, p0, p1);
+                half(mask, s0, k0 + 64, s1, next + G::kBlock, cur + G::kTileV + G::kBlock, next + G::kTileV, p1, p0);
             };
             arrive(0);
             if (alive && pw.sane) {
-                s0 = block_logits<T>(w, tile_at(0), lane);
-                block_mask<T>(w, c0, ~0u, lane, s0);
-                float top = s0[0];
 #pragma unroll
-                for (int r = 0; r < 16; r += 2) top = maximum(maximum(top, s0[r]), s0[r + 1]);
-                const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
-                w.m = maximum(__uint_as_float(x[0]), __uint_as_float(x[1])) * a.c2;
-                ref = w.m == -INFINITY ? 0.f : w.m;
-                s1 = block_logits<T>(w, tile_at(0) + G::kBlock, lane);
-                probs(std::true_type(), s0, c0, p0);
+                for (int nb = 0; nb < G::NB; ++nb) {
+                    f32x16& s = s0[nb];
+                    s = block_logits<T>(w[nb], tile_at(0), lane);
+                    block_mask<T>(w[nb], c0, ~0u, lane, s);
+                    float top = s[0];
+#pragma unroll
+                    for (int r = 0; r < 16; r += 2) top = maximum(maximum(top, s[r]), s[r + 1]);
+                    const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false,
+                                                                    false);
+                    w[nb].m = maximum(__uint_as_float(x[0]), __uint_as_float(x[1])) * a.c2;
+                    ref[nb] = w[nb].m == -INFINITY ? 0.f : w[nb].m;
+                    s1[nb] = block_logits<T>(w[nb], tile_at(0) + G::kBlock, lane);
+                }
+                probs(s0, c0, p0);
+#pragma unroll
+                for (int i = 0; i < 3; ++i) ahead[i] = value_at(tile_at(0) + G::kTileV, i);
                 int t = 0;
                 for (; t + 1 < nt && t + 1 < tfull; ++t) {
                     arrive(t + 1);
@@ -563,28 +625,39 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), (WIDE && sizeof(T) == 2 ? 
                     arrive(t + 1);
                     body(std::true_type(), t);
                 }
-                probs(std::true_type(), s1, c0 + t * G::TK + 32, p1);
-                block_values<T>(w, tile_at(t) + G::kTileV, p0, lane);
-                block_values<T>(w, tile_at(t) + G::kTileV + G::kBlock, p1, lane);
-                w.l = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                probs(s1, c0 + t * G::TK + 32, p1);
+#pragma unroll
+                for (int nb = 0; nb < G::NB; ++nb) {
+                    block_values<T>(w[nb], tile_at(t) + G::kTileV, p0[nb], lane);
+                    block_values<T>(w[nb], tile_at(t) + G::kTileV + G::kBlock, p1[nb], lane);
+                    w[nb].l = (sum[nb][0] + sum[nb][1]) + (sum[nb][2] + sum[nb][3]);
+                }
             } else {
                 for (int t = 1; t < nt; ++t) arrive(t);
             }
             bool redo = !pw.sane;
             if (alive) {
-                bool far = !(w.l < 1152921504606846976.f) || (w.m == -INFINITY && w.vis > c0);   // 2^60
+                bool far = false;
 #pragma unroll
-                for (int m = 0; m < 2; ++m)
+                for (int nb = 0; nb < G::NB; ++nb) {
+                    const Rows<T>& x = w[nb];
+                    far = far || !(x.l < 1152921504606846976.f) || (x.m == -INFINITY && x.vis > c0);   // 2^60
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) far = far || !(fabsf(w.o[m][r]) <= 3.4028235e38f);
+                    for (int m = 0; m < 2; ++m)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) far = far || !(fabsf(x.o[m][r]) <= 3.4028235e38f);
+                }
                 redo = redo || __builtin_amdgcn_ballot_w64(far);
             }
             if (lane == 0) s_redo[wave] = redo;
             __syncthreads();
             if (s_redo[0] | s_redo[1] | s_redo[2] | s_redo[3]) {
-                w.o[0] = w.o[1] = zero_f32x16();
-                w.m = -INFINITY;
-                w.l = 0.f;
+#pragma unroll
+                for (int nb = 0; nb < G::NB; ++nb) {
+                    w[nb].o[0] = w[nb].o[1] = zero_f32x16();
+                    w[nb].m = -INFINITY;
+                    w[nb].l = 0.f;
+                }
                 pw.start(a.c, b, c0, c1 - 1, lane);
 #pragma unroll
                 for (int t = 0; t < G::AHEAD; ++t)
@@ -604,62 +677,68 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), (WIDE && sizeof(T) == 2 ? 
             for (int t = 0; t < nt; ++t) {
                 const int k0 = c0 + (tfirst + t * tstep) * G::TK;
                 if (!pw.sane || k0 + G::TK > seen_by_all)
-                    add_odd_values<T>(a, w, b, hk, k0, k0 + G::TK < c1 ? k0 + G::TK : c1, lane);
+#pragma unroll
+                    for (int nb = 0; nb < G::NB; ++nb)
+                        add_odd_values<T>(a, w[nb], b, hk, k0, k0 + G::TK < c1 ? k0 + G::TK : c1, lane);
             }
     }
-    w.l += __shfl_xor(w.l, 32);
+#pragma unroll
+    for (int nb = 0; nb < G::NB; ++nb) w[nb].l += __shfl_xor(w[nb].l, 32);
 
     const int64_t all_rows = (int64_t)a.c.T * a.Hq;
     if constexpr (WIDE) {
-        if (row0 + l31 >= nrows) return;
-        if (a.nsplit > 1) {
-            float* po = a.part + (split * all_rows + orow) * kD;
-            if (hh == 0) {
-                f32x2 ml = {w.m, w.l};
-                *(f32x2*)(a.part_ml + (split * all_rows + orow) * 2) = ml;
-            }
 #pragma unroll
-            for (int m = 0; m < 2; ++m)
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    f32x4 v;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = w.o[m][4 * g + e];
-                    *(f32x4*)(po + 32 * m + 8 * g + 4 * hh) = v;
+        for (int nb = 0; nb < G::NB; ++nb) {
+            if (row0 + 32 * nb + l31 >= nrows) return;
+            if (a.nsplit > 1) {
+                float* po = a.part + (split * all_rows + orow[nb]) * kD;
+                if (hh == 0) {
+                    f32x2 ml = {w[nb].m, w[nb].l};
+                    *(f32x2*)(a.part_ml + (split * all_rows + orow[nb]) * 2) = ml;
                 }
-            return;
-        }
-        float inv, lse;
-        row_result(w.m, w.l, &inv, &lse);
-        if (hh == 0) a.lse[orow] = lse;
-        T* out = (T*)a.O + orow * kD;
-        if constexpr (G::kBf) {
 #pragma unroll
-            for (int m = 0; m < 2; ++m)
+                for (int m = 0; m < 2; ++m)
 #pragma unroll
-                for (int g = 0; g < 2; ++g) {
-                    uint32_t d[4];
+                    for (int g = 0; g < 4; ++g) {
+                        f32x4 v;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        bf16x2 pr = {(bf16)(w.o[m][8 * g + 2 * e] * inv),
-                                     (bf16)(w.o[m][8 * g + 2 * e + 1] * inv)};
-                        d[e] = __builtin_bit_cast(uint32_t, pr);
+                        for (int e = 0; e < 4; ++e) v[e] = w[nb].o[m][4 * g + e];
+                        *(f32x4*)(po + 32 * m + 8 * g + 4 * hh) = v;
                     }
-                    swap_halves(d[0], d[2]);
-                    swap_halves(d[1], d[3]);
-                    u32x4 v = {d[0], d[1], d[2], d[3]};
-                    *(u32x4*)(out + 32 * m + 16 * g + 8 * hh) = v;
-                }
-        } else {
+                continue;
+            }
+            float inv, lse;
+            row_result(w[nb].m, w[nb].l, &inv, &lse);
+            if (hh == 0) a.lse[orow[nb]] = lse;
+            T* out = (T*)a.O + orow[nb] * kD;
+            if constexpr (G::kBf) {
 #pragma unroll
-            for (int m = 0; m < 2; ++m)
+                for (int m = 0; m < 2; ++m)
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    f32x4 v;
+                    for (int g = 0; g < 2; ++g) {
+                        uint32_t d[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = w.o[m][4 * g + e] * inv;
-                    *(f32x4*)(out + 32 * m + 8 * g + 4 * hh) = v;
-                }
+                        for (int e = 0; e < 4; ++e) {
+                            bf16x2 pr = {(bf16)(w[nb].o[m][8 * g + 2 * e] * inv),
+                                         (bf16)(w[nb].o[m][8 * g + 2 * e + 1] * inv)};
+                            d[e] = __builtin_bit_cast(uint32_t, pr);
+                        }
+                        swap_halves(d[0], d[2]);
+                        swap_halves(d[1], d[3]);
+                        u32x4 v = {d[0], d[1], d[2], d[3]};
+                        *(u32x4*)(out + 32 * m + 16 * g + 8 * hh) = v;
+                    }
+            } else {
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        f32x4 v;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v[e] = w[nb].o[m][4 * g + e] * inv;
+                        *(f32x4*)(out + 32 * m + 8 * g + 4 * hh) = v;
+                    }
+            }
         }
     } else {
         // The four waves' partial results meet in LDS (the ring is free then).
@@ -669,14 +748,14 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), (WIDE && sizeof(T) == 2 ? 
         static_assert((256 + 4 * 32 * kRow) * 4 <= G::kLds, "partial results fit the ring");
         __syncthreads();
         if (hh == 0) {
-            sml[(wave * 32 + l31) * 2] = w.m;
-            sml[(wave * 32 + l31) * 2 + 1] = w.l;
+            sml[(wave * 32 + l31) * 2] = w[0].m;
+            sml[(wave * 32 + l31) * 2 + 1] = w[0].l;
         }
         __syncthreads();
         float M = -INFINITY;
 #pragma unroll
         for (int v = 0; v < 4; ++v) M = maximum(M, sml[(v * 32 + l31) * 2]);
-        const float f = w.m == -INFINITY ? 0.f : w.m == M ? 1.f : exp2f_fast(w.m - M);
+        const float f = w[0].m == -INFINITY ? 0.f : w[0].m == M ? 1.f : exp2f_fast(w[0].m - M);
         if (row0 + l31 < nrows) {
 #pragma unroll
             for (int m = 0; m < 2; ++m)
@@ -684,7 +763,7 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), (WIDE && sizeof(T) == 2 ? 
                 for (int g = 0; g < 4; ++g) {
                     f32x4 v;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = w.o[m][4 * g + e] * f;
+                    for (int e = 0; e < 4; ++e) v[e] = w[0].o[m][4 * g + e] * f;
                     *(f32x4*)(so + (wave * 32 + l31) * kRow + 32 * m + 8 * g + 4 * hh) = v;
                 }
         }
@@ -904,14 +983,14 @@ __global__ __launch_bounds__(256, 2) void k_cache_weight(AttendArgs a) {
 void attend_plan(AttendArgs* a) {
     const int64_t rows = (int64_t)a->c.max_q * a->G;
     a->wide = rows > 64;
-    const int rt = a->wide ? 128 : 32;
+    const int rt = !a->wide ? 32 : a->c.dtype == DT_BF16 ? Geo<bf16, true>::RT : Geo<float, true>::RT;
     a->row_tiles = (int)((rows + rt - 1) / rt);
     if (a->row_tiles < 1) a->row_tiles = 1;
     const int64_t items = (int64_t)a->c.B * a->c.Hkv * a->row_tiles;
     const int64_t slots = 512;                       // workgroups that run together
     const int64_t least = a->wide ? 256 : 128;       // slots per split at least
     const int64_t most = (a->c.max_len + least - 1) / least;
-    const int64_t start = a->wide ? 256 : 192;       // a split's own cost, in slots
+    const int64_t start = a->wide ? 512 : 192;       // a split's own cost, in slots
     int64_t best = 1;
     double best_t = 0;
     for (int64_t ns = 1; ns <= most && ns <= 256; ++ns) {
