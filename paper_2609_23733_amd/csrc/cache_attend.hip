@@ -556,28 +556,40 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(Att
                 if constexpr (decltype(mask)::value)
 #pragma unroll
                     for (int nb = 0; nb < G::NB; ++nb) block_mask<T>(w[nb], k0, ~0u, lane, s[nb]);
-                constexpr int kOf[8] = {4, 5, 6, 0, 7, 1, 2, 3};   // 0-3: logits, 4-7: values
+                constexpr int kOf[8] = {4, 5, 6, 0, 1, 2, 3, 7};   // 0-3: logits, 4-7: values
                 bf16x8 f[8] = {ahead[0], ahead[1], ahead[2]};
+                // Two logits at a time, in three steps an MFMA apart so that none waits for the last:
+                // the exponent, its power, the sum and the rounding.
+                auto exponent = [&](int u) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    if (i < 5) f[i + 3] = kOf[i + 3] < 4 ? key_at(k, kOf[i + 3]) : value_at(v, kOf[i + 3] - 4);
-                    else ahead[i - 5] = value_at(v_next, i - 5);
-                    const int n = kOf[i];
+                    for (int r = 2 * (u / G::NB); r < 2 * (u / G::NB) + 2; ++r)
+                        s[u % G::NB][r] = fmaf(s[u % G::NB][r], a.c2, -ref[u % G::NB]);
+                };
+                auto add = [&](int u) {
+                    const int nb = u % G::NB, i = u / G::NB;
+                    sum[nb][(2 * i) & 3] += s[nb][2 * i];
+                    sum[nb][(2 * i + 1) & 3] += s[nb][2 * i + 1];
+                    pn[nb].v[i >> 2][(2 * i) & 7] = (bf16)s[nb][2 * i];
+                    pn[nb].v[i >> 2][(2 * i + 1) & 7] = (bf16)s[nb][2 * i + 1];
+                };
+                exponent(0);
 #pragma unroll
-                    for (int nb = 0; nb < G::NB; ++nb) {
-                        Rows<T>& x = w[nb];
-                        if (n < 4) sn[nb] = mfma_bf16(f[i], x.qb[n], n ? sn[nb] : zero_f32x16());
-                        else x.o[n & 1] = mfma_bf16(f[i], pv[nb].v[(n - 4) >> 1], x.o[n & 1]);
-#pragma unroll
-                        for (int r = 2 * i; r < 2 * i + 2; ++r) {
-                            s[nb][r] = exp2f_fast(fmaf(s[nb][r], a.c2, -ref[nb]));
-                            sum[nb][r & 3] += s[nb][r];
-                        }
-                        pn[nb].v[i >> 2][(2 * i) & 7] = (bf16)s[nb][2 * i];
-                        pn[nb].v[i >> 2][(2 * i + 1) & 7] = (bf16)s[nb][2 * i + 1];
-                        __builtin_amdgcn_sched_barrier(0);
+                for (int u = 0; u < 8 * G::NB; ++u) {
+                    const int i = u / G::NB, nb = u % G::NB, n = kOf[i];
+                    if (nb == 0) {
+                        if (i < 5) f[i + 3] = kOf[i + 3] < 4 ? key_at(k, kOf[i + 3]) : value_at(v, kOf[i + 3] - 4);
+                        else ahead[i - 5] = value_at(v_next, i - 5);
                     }
+                    Rows<T>& x = w[nb];
+                    if (n < 4) sn[nb] = mfma_bf16(f[i], x.qb[n], n ? sn[nb] : zero_f32x16());
+                    else x.o[n & 1] = mfma_bf16(f[i], pv[nb].v[(n - 4) >> 1], x.o[n & 1]);
+                    if (u + 1 < 8 * G::NB) exponent(u + 1);
+                    s[nb][2 * i] = exp2f_fast(s[nb][2 * i]);
+                    s[nb][2 * i + 1] = exp2f_fast(s[nb][2 * i + 1]);
+                    if (u > 0) add(u - 1);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
+                add(8 * G::NB - 1);
             };
             auto probs = [&](Logits& s, int k0, BlockP& p) {
 #pragma unroll
