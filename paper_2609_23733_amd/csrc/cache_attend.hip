@@ -258,11 +258,17 @@ __device__ __forceinline__ void block_values(Rows<T>& w, lds_char* v, const Prob
 }
 
 // One block after the other: logits, probabilities, values.
+// `logits`: null, or where the row's logits (of slots from 0 on) are kept.
 template <typename T>
 __device__ __forceinline__ void block_attend(Rows<T>& w, lds_char* k, lds_char* v, float c2, int k0,
-                                             bool partial, uint32_t units, int lane) {
+                                             bool partial, uint32_t units, int lane, float* logits) {
     f32x16 s = block_logits<T>(w, k, lane);
     if (partial) block_mask<T>(w, k0, units, lane, s);
+    if (logits)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+            *(f32x4*)(logits + k0 + Geo<T, true>::key(4 * g, lane >> 5)) =
+                f32x4{s[4 * g], s[4 * g + 1], s[4 * g + 2], s[4 * g + 3]};
     float sum = block_exp(s, c2, w.m);   // inf or NaN while m is -inf
     Probs<T> p;
     p.set(s);
@@ -505,6 +511,8 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(Att
             }
         };
         auto tile_at = [&](int t) { return ring + (t % G::NST) * G::kTile; };
+        float* logits = nullptr;
+        if (!WIDE && a.logits && row0 + l31 < nrows) logits = a.logits + orow[0] * a.logit_stride;
         // Every block with its bound on the reference checked.
         auto careful = [&]() {
             for (int t = 0; t < nt; ++t) {
@@ -519,7 +527,7 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(Att
 #pragma unroll
                         for (int nb = 0; nb < G::NB; ++nb)
                             block_attend<T>(w[nb], tile + j * G::kBlock, tile + G::kTileV + j * G::kBlock, a.c2,
-                                            k0 + 32 * j, partial, units >> (2 * j), lane);
+                                            k0 + 32 * j, partial, units >> (2 * j), lane, logits);
             }
         };
         if constexpr (WIDE && G::kBf) {
@@ -861,13 +869,50 @@ __global__ __launch_bounds__(256) void k_cache_join(AttendArgs a) {
 
 // ------------------------------------------------------------------------
 // Attention weights that fall on every slot, weight_out = weight + sum over the group's rows of
-// e^{x_j - lse}.  Keys stay in registers as the MFMA's B operand (a lane owns one slot of the
-// wave's 32), the rows stream through LDS as A with -lse in the accumulator's input, so that
-// a result is the exponent itself.  Every slot is written by one wave: no atomics, one order.
+// e^{x_j - lse}.  Every slot is written by one wave: no atomics, one order.
+//
+// Few rows (single tokens): the attention kept its logits; four slots a thread, rows one after the other.
 // ------------------------------------------------------------------------
-constexpr int kWRows = 64;    // rows per step
+__global__ __launch_bounds__(256) void k_cache_weight_rows(AttendArgs a) {
+    const int hk = blockIdx.y % a.c.Hkv, b = blockIdx.y / a.c.Hkv;
+    const CacheSeq sq = cache_seq(a.c, b);
+    const int k0 = (blockIdx.x * 256 + threadIdx.x) * 4;
+    if (k0 >= sq.len || sq.nq == 0) return;
+    const int page = a.c.table[(int64_t)b * a.c.max_pages + (k0 >> a.c.page_log2)];
+    if (page < 0 || page >= a.c.npages) return;
+    const int64_t at = (((int64_t)page * a.c.Hkv + hk) << a.c.page_log2) + (k0 & ((1 << a.c.page_log2) - 1));
+    const int left = sq.len - k0;
+    float w[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = e < left ? a.c.weight[at + e] : 0.f;
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < sq.nq; ++i) {
+        const int seen = cache_visible(sq, a.causal, i) - k0;
+        for (int g = 0; g < a.G; ++g) {
+            const int64_t row = (int64_t)(sq.q0 + i) * a.Hq + hk * a.G + g;
+            const float lse = a.lse[row];
+            const f32x4 x = *(const f32x4*)(a.logits + row * a.logit_stride + k0);
+            const float off = lse * kLog2e;
+            if (lse == -INFINITY) continue;   // a row without weights adds none
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                sum[e] += e < seen ? exp2f_fast(fmaf(x[e], a.c2, -off)) : 0.f;
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (e < left) a.weight_out[at + e] = w[e] + sum[e];
+}
 
-template <typename T>
+// ------------------------------------------------------------------------
+// Chunks: logits formed again.  Keys stay in registers as the MFMA's B operand (a lane owns one slot
+// of each of the wave's KN blocks of 32), the rows stream through LDS as A with -lse in the
+// accumulator's input, so that a result is the exponent itself.  A step's products are formed
+// while the last one's exponentials are summed.
+// ------------------------------------------------------------------------
+constexpr int kWRows = 64;    // rows per LDS buffer
+
+template <typename T, int KN>
 __global__ __launch_bounds__(256, 2) void k_cache_weight(AttendArgs a) {
     constexpr bool kBf = sizeof(T) == 2;
     constexpr int ROW = kBf ? 144 : 272;   // LDS bytes per row: 16 beyond a multiple of 128
@@ -876,29 +921,35 @@ __global__ __launch_bounds__(256, 2) void k_cache_weight(AttendArgs a) {
     const int tid = threadIdx.x, lane = tid & 63, l31 = lane & 31, hh = lane >> 5, wave = tid >> 6;
     const int hk = blockIdx.y % a.c.Hkv, b = blockIdx.y / a.c.Hkv;
     const CacheSeq sq = cache_seq(a.c, b);
-    const int k0 = blockIdx.x * 128;
+    const int k0 = blockIdx.x * 128 * KN;
     if (k0 >= sq.len || sq.nq == 0) return;
-    const int slot = k0 + 32 * wave + l31;
-    int page = -1;
-    if (slot < sq.len) page = a.c.table[(int64_t)b * a.c.max_pages + (slot >> a.c.page_log2)];
-    const bool live = page >= 0 && page < a.c.npages;
-    const int64_t at = (((int64_t)(live ? page : 0) * a.c.Hkv + hk) << a.c.page_log2) +
-                       (slot & ((1 << a.c.page_log2) - 1));
-    bf16x8 kb[4];
-    float kf[kBf ? 1 : 32];
-    if constexpr (kBf) {
+    int slot[KN];
+    bool live[KN];
+    int64_t at[KN];
+    bf16x8 kb[KN][4];
+    float kf[KN][kBf ? 1 : 32];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            kb[i] = zero_bf16x8();
-            if (live) kb[i] = load_bf16x8((const T*)a.c.K + at * kD + 16 * i + 8 * hh);
-        }
-    } else {
+    for (int n = 0; n < KN; ++n) {
+        slot[n] = k0 + 32 * (KN * wave + n) + l31;
+        int page = -1;
+        if (slot[n] < sq.len) page = a.c.table[(int64_t)b * a.c.max_pages + (slot[n] >> a.c.page_log2)];
+        live[n] = page >= 0 && page < a.c.npages;
+        at[n] = (((int64_t)(live[n] ? page : 0) * a.c.Hkv + hk) << a.c.page_log2) +
+                (slot[n] & ((1 << a.c.page_log2) - 1));
+        if constexpr (kBf) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            f32x4 v = {0.f, 0.f, 0.f, 0.f};
-            if (live) v = *(const f32x4*)((const T*)a.c.K + at * kD + 8 * i + 4 * hh);
+            for (int i = 0; i < 4; ++i) {
+                kb[n][i] = zero_bf16x8();
+                if (live[n]) kb[n][i] = load_bf16x8((const T*)a.c.K + at[n] * kD + 16 * i + 8 * hh);
+            }
+        } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) kf[4 * i + e] = v[e];
+            for (int i = 0; i < 8; ++i) {
+                f32x4 v = {0.f, 0.f, 0.f, 0.f};
+                if (live[n]) v = *(const f32x4*)((const T*)a.c.K + at[n] * kD + 8 * i + 4 * hh);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) kf[n][4 * i + e] = v[e];
+            }
         }
     }
     // Rows that see the workgroup's first slot: causal rows before them add nothing.
@@ -938,7 +989,16 @@ __global__ __launch_bounds__(256, 2) void k_cache_weight(AttendArgs a) {
         }
         if (tid < kWRows) so[buf][tid] = off;
     };
-    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    float sum[KN][4] = {};
+    f32x16 s[2][KN];   // exponents over c2 of the last 32 rows and of these
+#pragma unroll
+    for (int n = 0; n < KN; ++n)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[1][n][r] = -INFINITY;
+    auto add = [&](const f32x16& x, int n) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sum[n][r & 3] += exp2f_fast(x[r] * a.c2);
+    };
     if (first < nrows) {
         fetch(first);
         put(0);
@@ -948,44 +1008,57 @@ __global__ __launch_bounds__(256, 2) void k_cache_weight(AttendArgs a) {
         __syncthreads();
         if (r0 + kWRows < nrows) fetch(r0 + kWRows);
         // slots that row r0 sees all rows of the step see
-        const bool mask = a.causal && k0 + 128 > cache_visible(sq, 1, r0 / a.G);
+        const bool mask = a.causal && k0 + 128 * KN > cache_visible(sq, 1, r0 / a.G);
 #pragma unroll
-        for (int rb = 0; rb < kWRows / 32; ++rb) {
-            f32x16 s;
+        for (int rb = 0; rb < 2; ++rb) {
+            f32x16 init;
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const f32x4 v = *(const f32x4*)(so[buf] + 32 * rb + 8 * g + 4 * hh);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[4 * g + e] = v[e];
+                for (int e = 0; e < 4; ++e) init[4 * g + e] = v[e];
             }
             const char* qr = sq_[buf] + (32 * rb + l31) * ROW;
             if constexpr (kBf) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) s = mfma_bf16(*(const bf16x8*)(qr + 32 * i + 16 * hh), kb[i], s);
+                for (int i = 0; i < 4; ++i) {
+                    const bf16x8 q = *(const bf16x8*)(qr + 32 * i + 16 * hh);
+#pragma unroll
+                    for (int n = 0; n < KN; ++n) s[rb][n] = mfma_bf16(q, kb[n][i], i ? s[rb][n] : init);
+                }
             } else {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const f32x4 q = *(const f32x4*)(qr + 32 * i + 16 * hh);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) s = mfma_f32(q[e], kf[4 * i + e], s);
+                    for (int e = 0; e < 4; ++e)
+#pragma unroll
+                        for (int n = 0; n < KN; ++n)
+                            s[rb][n] = mfma_f32(q[e], kf[n][4 * i + e], i + e ? s[rb][n] : init);
                 }
             }
+#pragma unroll
+            for (int n = 0; n < KN; ++n) add(s[rb ^ 1][n], n);
             if (mask) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int row = r0 + 32 * rb + 8 * (r >> 2) + 4 * hh + (r & 3);
-                    const int i = row / a.G;
-                    if (slot >= cache_visible(sq, 1, i)) s[r] = -INFINITY;
+                    const int seen = cache_visible(sq, 1, row / a.G);
+#pragma unroll
+                    for (int n = 0; n < KN; ++n)
+                        if (slot[n] >= seen) s[rb][n][r] = -INFINITY;
                 }
             }
-#pragma unroll
-            for (int r = 0; r < 16; ++r) sum[r & 3] += exp2f_fast(s[r] * a.c2);
         }
         if (r0 + kWRows < nrows) put(buf ^ 1);
     }
-    float t = (sum[0] + sum[1]) + (sum[2] + sum[3]);
-    t += __shfl_xor(t, 32);
-    if (live && hh == 0) a.weight_out[at] = a.c.weight[at] + t;
+#pragma unroll
+    for (int n = 0; n < KN; ++n) {
+        add(s[1][n], n);
+        float t = (sum[n][0] + sum[n][1]) + (sum[n][2] + sum[n][3]);
+        t += __shfl_xor(t, 32);
+        if (live[n] && hh == 0) a.weight_out[at[n]] = a.c.weight[at[n]] + t;
+    }
 }
 
 // ------------------------------------------------------------------ launchers
@@ -1013,12 +1086,21 @@ void attend_plan(AttendArgs* a) {
     const int64_t ch = (a->c.max_len + best - 1) / best;
     a->chunk = (int)((ch + 63) / 64 * 64);
     if (a->chunk < 64) a->chunk = 64;
+    a->logit_stride = (a->c.max_len + 63) / 64 * 64;
     a->nsplit = (int)((a->c.max_len + a->chunk - 1) / a->chunk);
     if (a->nsplit < 1) a->nsplit = 1;
 }
 
 size_t attend_part_rows(const AttendArgs& a) {
     return a.nsplit > 1 ? (size_t)a.nsplit * a.c.T * a.Hq : 0;
+}
+
+// Keeping a logit costs 8 bytes (written and read) per row and slot, forming it again a key's
+// 128 or 256 per slot: up to eight rows of a key head they are kept (two tokens over 137,400 slots:
+// 106 us to form them again).
+size_t attend_logits(const AttendArgs& a) {
+    if (!a.c.weight || a.wide || (int64_t)a.c.max_q * a.G > 8) return 0;
+    return (size_t)a.c.T * a.Hq * a.logit_stride;
 }
 
 template <typename T>
@@ -1031,9 +1113,16 @@ static void attend_go(const AttendArgs& a, hipStream_t st) {
     if (a.nsplit > 1)
         hipLaunchKernelGGL(k_cache_join<T>, dim3(((int64_t)a.c.max_q * a.Hq + 3) / 4, a.c.B), dim3(256), 0,
                            st, a);
-    if (a.weight_out && a.c.max_len > 0)
-        hipLaunchKernelGGL(k_cache_weight<T>, dim3((a.c.max_len + 127) / 128, a.c.B * a.c.Hkv), dim3(256), 0,
-                           st, a);
+    if (!a.weight_out || a.c.max_len == 0) return;
+    const unsigned bh = a.c.B * a.c.Hkv;
+    if (a.logits) {
+        hipLaunchKernelGGL(k_cache_weight_rows, dim3((a.c.max_len + 1023) / 1024, bh), dim3(256), 0, st, a);
+    } else if (((int64_t)a.c.max_len + 255) / 256 * bh >= 512) {
+        // (two blocks a wave where that still leaves two workgroups for every compute unit)
+        hipLaunchKernelGGL((k_cache_weight<T, 2>), dim3((a.c.max_len + 255) / 256, bh), dim3(256), 0, st, a);
+    } else {
+        hipLaunchKernelGGL((k_cache_weight<T, 1>), dim3((a.c.max_len + 127) / 128, bh), dim3(256), 0, st, a);
+    }
 }
 
 void launch_cache_attend(const AttendArgs& a, hipStream_t st) {

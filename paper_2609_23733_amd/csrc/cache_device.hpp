@@ -39,6 +39,8 @@ struct AttendArgs {
     int wide;                // kernel variant
     int row_tiles, nsplit, chunk;
     float *part, *part_ml;   // split results [nsplit, T * Hq, 64] and [nsplit, T * Hq, 2]
+    float* logits;           // null, or [T * Hq, logit_stride]: kept for the weights
+    int64_t logit_stride;
 };
 
 struct AppendArgs {
@@ -96,6 +98,7 @@ void launch_rotary(int dtype, const void* x, int64_t x_stride, void* y, int64_t 
 void launch_cache_append(const AppendArgs& a, const RotArgs& r, hipStream_t st);
 void attend_plan(AttendArgs* a);
 size_t attend_part_rows(const AttendArgs& a);
+size_t attend_logits(const AttendArgs& a);
 void launch_cache_attend(const AttendArgs& a, hipStream_t st);
 size_t evict_ws_bytes(int B, int Hkv, int max_len);
 void launch_cache_evict(const EvictArgs& a, hipStream_t st);

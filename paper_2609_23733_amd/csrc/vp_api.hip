@@ -897,7 +897,8 @@ vp_status attend_args(const vp_cache* cache, const vp_cache_batch* batch, int32_
 
 size_t attend_ws(const vp::AttendArgs& a) {
     const size_t rows = vp::attend_part_rows(a);
-    return kAlign + align_up(rows * VP_HEAD_DIM * sizeof(float)) + align_up(rows * 2 * sizeof(float));
+    return kAlign + align_up(rows * VP_HEAD_DIM * sizeof(float)) + align_up(rows * 2 * sizeof(float)) +
+           align_up(vp::attend_logits(a) * sizeof(float));
 }
 
 }  // namespace
@@ -1006,6 +1007,8 @@ vp_status vp_cache_attend(const vp_cache* cache, const vp_cache_batch* batch, in
     const size_t rows = vp::attend_part_rows(a);
     a.part = (float*)((char*)ws + kAlign);
     a.part_ml = (float*)((char*)ws + kAlign + align_up(rows * VP_HEAD_DIM * sizeof(float)));
+    if (weight_out && vp::attend_logits(a))
+        a.logits = (float*)((char*)a.part_ml + align_up(rows * 2 * sizeof(float)));
     (void)hipGetLastError();
     vp::launch_cache_attend(a, (hipStream_t)stream);
     return hip_status("vp_cache_attend");
