@@ -368,6 +368,13 @@ __device__ __forceinline__ void row_result(float m, float l, float* inv, float* 
     *lse = l == 0.f ? -INFINITY : (m + __log2f(l)) * kLn2;
 }
 
+// lse, and the accumulator input that the weights' products start from (see k_cache_weight): a row
+// without weights adds none.
+__device__ __forceinline__ void put_lse(const AttendArgs& a, int64_t row, float lse) {
+    a.lse[row] = lse;
+    if (a.off) a.off[row] = lse == -INFINITY ? -INFINITY : lse * (-kLog2e / a.c2);
+}
+
 template <typename T, bool WIDE>
 __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(AttendArgs a) {
     typedef Geo<T, WIDE> G;
@@ -729,7 +736,7 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(Att
             }
             float inv, lse;
             row_result(w[nb].m, w[nb].l, &inv, &lse);
-            if (hh == 0) a.lse[orow[nb]] = lse;
+            if (hh == 0) put_lse(a, orow[nb], lse);
             T* out = (T*)a.O + orow[nb] * kD;
             if constexpr (G::kBf) {
 #pragma unroll
@@ -814,7 +821,7 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(Att
             } else {
                 float inv, lse;
                 row_result(MM, L, &inv, &lse);
-                if (d0 == 0) a.lse[at] = lse;
+                if (d0 == 0) put_lse(a, at, lse);
                 T* out = (T*)a.O + at * kD + d0;
                 if constexpr (G::kBf) {
                     *(bf16x8*)out = pack_bf16x8(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv,
@@ -863,7 +870,7 @@ __global__ __launch_bounds__(256) void k_cache_join(AttendArgs a) {
     L = wave_sum(L);
     float inv, lse;
     row_result(M, L, &inv, &lse);
-    if (lane == 0) a.lse[at] = lse;
+    if (lane == 0) put_lse(a, at, lse);
     ((T*)a.O)[at * kD + lane] = (T)(acc * inv);
 }
 
@@ -905,160 +912,184 @@ __global__ __launch_bounds__(256) void k_cache_weight_rows(AttendArgs a) {
 }
 
 // ------------------------------------------------------------------------
-// Chunks: logits formed again.  Keys stay in registers as the MFMA's B operand (a lane owns one slot
-// of each of the wave's KN blocks of 32), the rows stream through LDS as A with -lse in the
-// accumulator's input, so that a result is the exponent itself.  A step's products are formed
-// while the last one's exponentials are summed.
+// Chunks: logits formed again.  64 slots per workgroup: keys stay in registers as the MFMA's B
+// operand (a lane owns one slot), two waves for each 32 slots that take half a tile's rows each.
+// The rows stream through LDS as A with -lse in the accumulator's input (`off`, written with lse), so
+// that a result is the exponent itself.  The products of 32 rows are formed while the exponentials
+// of the 32 before are summed.
 // ------------------------------------------------------------------------
-constexpr int kWRows = 64;    // rows per LDS buffer
-
-template <typename T, int KN>
-__global__ __launch_bounds__(256, 2) void k_cache_weight(AttendArgs a) {
+template <typename T>
+__global__ __launch_bounds__(256, 3) void k_cache_weight(AttendArgs a) {
     constexpr bool kBf = sizeof(T) == 2;
-    constexpr int ROW = kBf ? 144 : 272;   // LDS bytes per row: 16 beyond a multiple of 128
-    __shared__ __attribute__((aligned(16))) char sq_[2][kWRows * ROW];
-    __shared__ __attribute__((aligned(16))) float so[2][kWRows];
-    const int tid = threadIdx.x, lane = tid & 63, l31 = lane & 31, hh = lane >> 5, wave = tid >> 6;
+    constexpr int kStep = kBf ? 128 : 64, RB = kStep / 64;    // rows per tile, 32-row blocks of a wave
+    constexpr int ROWB = kD * sizeof(T), RPC = 1024 / ROWB;   // bytes per row, rows per copy
+    constexpr int kTile = kStep * ROWB + kStep * 4;           // rows, then their offsets
+    constexpr int NST = 3, AHEAD = NST - 1, NC = kStep / RPC / 4, CPT = NC + 1;
+    __shared__ __attribute__((aligned(1024))) char smem[NST * kTile];
+    const int tid = threadIdx.x, lane = tid & 63, l31 = lane & 31, hh = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int hk = blockIdx.y % a.c.Hkv, b = blockIdx.y / a.c.Hkv;
     const CacheSeq sq = cache_seq(a.c, b);
-    const int k0 = blockIdx.x * 128 * KN;
+    const int k0 = blockIdx.x * 64;
     if (k0 >= sq.len || sq.nq == 0) return;
-    int slot[KN];
-    bool live[KN];
-    int64_t at[KN];
-    bf16x8 kb[KN][4];
-    float kf[KN][kBf ? 1 : 32];
-#pragma unroll
-    for (int n = 0; n < KN; ++n) {
-        slot[n] = k0 + 32 * (KN * wave + n) + l31;
-        int page = -1;
-        if (slot[n] < sq.len) page = a.c.table[(int64_t)b * a.c.max_pages + (slot[n] >> a.c.page_log2)];
-        live[n] = page >= 0 && page < a.c.npages;
-        at[n] = (((int64_t)(live[n] ? page : 0) * a.c.Hkv + hk) << a.c.page_log2) +
-                (slot[n] & ((1 << a.c.page_log2) - 1));
-        if constexpr (kBf) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                kb[n][i] = zero_bf16x8();
-                if (live[n]) kb[n][i] = load_bf16x8((const T*)a.c.K + at[n] * kD + 16 * i + 8 * hh);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                f32x4 v = {0.f, 0.f, 0.f, 0.f};
-                if (live[n]) v = *(const f32x4*)((const T*)a.c.K + at[n] * kD + 8 * i + 4 * hh);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) kf[n][4 * i + e] = v[e];
-            }
-        }
-    }
     // Rows that see the workgroup's first slot: causal rows before them add nothing.
     const int nrows = sq.nq * a.G;
     int first = 0;
     if (a.causal) first = clampi(k0 - (sq.len - sq.n), 0, sq.nq) * a.G;
-    first &= ~(kWRows - 1);
-    const float noff = -kLog2e / a.c2;
-    constexpr int EPT = kBf ? 8 : 4;                   // elements per 16 bytes
-    constexpr int LPR = kD / EPT;                      // 16-byte pieces per row
-    constexpr int NP = kWRows * LPR / 256;             // pieces per thread
-    u32x4 piece[NP];
-    float off = 0.f;
-    auto fetch = [&](int r0) {
-#pragma unroll
-        for (int j = 0; j < NP; ++j) {
-            const int p = tid + 256 * j, rr = p / LPR, r = r0 + rr < nrows ? r0 + rr : nrows - 1;
-            const int i = r / a.G;
-            piece[j] = *(const u32x4*)((const T*)a.Q + (int64_t)(sq.q0 + i) * a.q_stride +
-                                       (hk * a.G + r - i * a.G) * kD + (p % LPR) * EPT);
-        }
-        if (tid < kWRows) {
-            off = -INFINITY;
-            const int r = r0 + tid;
-            if (r < nrows) {
-                const int i = r / a.G;
-                const float lse = a.lse[(int64_t)(sq.q0 + i) * a.Hq + hk * a.G + r - i * a.G];
-                off = lse == -INFINITY ? -INFINITY : lse * noff;   // a row without weights adds none
-            }
+    first &= ~(kStep - 1);
+    const int nt = (nrows - first + kStep - 1) / kStep;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)smem;
+    // Rows r = i G + g that this lane copies, stepped along with the tiles (a division each costs
+    // more than the rest of a copy).
+    struct Row {
+        int i, g;
+        __device__ __forceinline__ void next(int di, int dg, int G) {
+            i += di;
+            g += dg;
+            if (g >= G) g -= G, ++i;
         }
     };
-    auto put = [&](int buf) {
+    const int di = kStep / a.G, dg = kStep - di * a.G;
+    Row base, last, row[NC + 1];
+    auto row_of = [&](int r) {
+        Row x;
+        x.i = r / a.G;
+        x.g = r - x.i * a.G;
+        return x;
+    };
+    base = row_of(first);
+    last = row_of(nrows - 1);
+    const int off_row = (wave * 64) % kStep;   // (the offsets' copies: one a wave)
 #pragma unroll
-        for (int j = 0; j < NP; ++j) {
-            const int p = tid + 256 * j;
-            *(u32x4*)(sq_[buf] + (p / LPR) * ROW + (p % LPR) * 16) = piece[j];
+    for (int j = 0; j < NC; ++j) row[j] = row_of(first + (wave * NC + j) * RPC + lane / (64 / RPC));
+    row[NC] = row_of(first + off_row + lane);
+    auto issue = [&](int t) {
+        const uint32_t stage = lds0 + (t % NST) * kTile;
+        const char* q0 = (const char*)((const T*)a.Q + (int64_t)(sq.q0 + base.i) * a.q_stride + hk * a.G * kD);
+        const uint32_t qs = (uint32_t)a.q_stride;
+        const uint32_t lim = ((uint32_t)(last.i - base.i) * qs + last.g * kD) * sizeof(T);
+        const bool tail = last.i - base.i <= di + 1;   // rows past the last one: the last again
+#pragma unroll
+        for (int j = 0; j < NC; ++j) {
+            // pieces of 16 bytes exchanged within their row so that reads meet no bank twice
+            const int c = wave * NC + j, rr = c * RPC + lane / (64 / RPC), pc = lane % (64 / RPC);
+            const int f = kBf ? (rr >> 1) & 7 : rr & 15;
+            uint32_t at = ((uint32_t)(row[j].i - base.i) * qs + row[j].g * kD) * sizeof(T);
+            if (tail) at = at < lim ? at : lim;
+            copy_to_lds(stage + c * 1024, q0, at + ((pc ^ f) << 4));
+            row[j].next(di, dg, a.G);
         }
-        if (tid < kWRows) so[buf][tid] = off;
+        uint32_t at = ((uint32_t)(row[NC].i - base.i) * a.Hq + row[NC].g) * 4;
+        const uint32_t olim = ((uint32_t)(last.i - base.i) * a.Hq + last.g) * 4;
+        if (tail) at = at < olim ? at : olim;
+        copy4_to_lds(stage + kStep * ROWB + off_row * 4,
+                     (const char*)(a.off + (int64_t)(sq.q0 + base.i) * a.Hq + hk * a.G), at);
+        row[NC].next(di, dg, a.G);
+        base.next(di, dg, a.G);
     };
-    float sum[KN][4] = {};
-    f32x16 s[2][KN];   // exponents over c2 of the last 32 rows and of these
 #pragma unroll
-    for (int n = 0; n < KN; ++n)
+    for (int t = 0; t < AHEAD; ++t)
+        if (t < nt) issue(t);
+    const int slot = k0 + 32 * (wave & 1) + l31;
+    int page = -1;
+    if (slot < sq.len) page = a.c.table[(int64_t)b * a.c.max_pages + (slot >> a.c.page_log2)];
+    const bool live = page >= 0 && page < a.c.npages;
+    const int64_t at = (((int64_t)(live ? page : 0) * a.c.Hkv + hk) << a.c.page_log2) +
+                       (slot & ((1 << a.c.page_log2) - 1));
+    bf16x8 kb[4];
+    float kf[kBf ? 1 : 32];
+    if constexpr (kBf) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[1][n][r] = -INFINITY;
-    auto add = [&](const f32x16& x, int n) {
+        for (int i = 0; i < 4; ++i) {
+            kb[i] = zero_bf16x8();
+            if (live) kb[i] = load_bf16x8((const T*)a.c.K + at * kD + 16 * i + 8 * hh);
+        }
+    } else {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) sum[n][r & 3] += exp2f_fast(x[r] * a.c2);
-    };
-    if (first < nrows) {
-        fetch(first);
-        put(0);
+        for (int i = 0; i < 8; ++i) {
+            f32x4 v = {0.f, 0.f, 0.f, 0.f};
+            if (live) v = *(const f32x4*)((const T*)a.c.K + at * kD + 8 * i + 4 * hh);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) kf[4 * i + e] = v[e];
+        }
     }
-    int buf = 0;
-    for (int r0 = first; r0 < nrows; r0 += kWRows, buf ^= 1) {
-        __syncthreads();
-        if (r0 + kWRows < nrows) fetch(r0 + kWRows);
-        // slots that row r0 sees all rows of the step see
-        const bool mask = a.causal && k0 + 128 * KN > cache_visible(sq, 1, r0 / a.G);
+    // first row that sees this lane's slot (token i sees slots up to len - n + i)
+    const int row_min = a.causal && slot > sq.len - sq.n ? (slot - (sq.len - sq.n)) * a.G : 0;
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    f32x16 s[2];   // exponents over c2 of the 32 rows before and of these
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[0][r] = s[1][r] = -INFINITY;
+    auto add = [&](const f32x16& x) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sum[r & 3] += exp2f_fast(x[r] * a.c2);
+    };
+    const int half = wave >> 1;
+    for (int t = 0; t < nt; ++t) {
+        const int more = nt - 1 - t, r0 = first + t * kStep;
+        wait_tiles<CPT>(more < AHEAD - 1 ? more : AHEAD - 1);
+        __builtin_amdgcn_s_barrier();
+        if (t + AHEAD < nt) issue(t + AHEAD);
+        lds_char* tile = (lds_char*)smem + (t % NST) * kTile;
+        // slots that row r0 sees all rows of the tile see
+        const bool mask = (a.causal && k0 + 64 > cache_visible(sq, 1, r0 / a.G)) || r0 + kStep > nrows;
 #pragma unroll
         for (int rb = 0; rb < 2; ++rb) {
-            f32x16 init;
+            if (rb >= RB) break;
+            typedef __attribute__((address_space(3))) const f32x4 lds_f32x4;
+            typedef __attribute__((address_space(3))) const bf16x8 lds_bf16x8;
+            const int br = 32 * (RB * half + rb);   // first row of the block
+            f32x16& x = s[rb];
+            f32x16 done;
+            if constexpr (RB == 1) done = s[0];
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const f32x4 v = *(const f32x4*)(so[buf] + 32 * rb + 8 * g + 4 * hh);
+                const f32x4 v = *(lds_f32x4*)(tile + kStep * ROWB + (br + 8 * g + 4 * hh) * 4);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) init[4 * g + e] = v[e];
+                for (int e = 0; e < 4; ++e) x[4 * g + e] = v[e];
             }
-            const char* qr = sq_[buf] + (32 * rb + l31) * ROW;
-            if constexpr (kBf) {
+            lds_char* qr = tile + (br + l31) * ROWB;
+            const int f = kBf ? (l31 >> 1) & 7 : l31 & 15;
+            // an MFMA's time holds the vector instructions of four (fp32: two) of the 16 exponentials
+            const f32x16& y = RB == 1 ? done : s[rb ^ 1];
+            constexpr int kParts = kBf ? 4 : 8, kEach = 16 / kParts;
+            bf16x8 qb[kBf ? 4 : 1];
+            if constexpr (kBf)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const bf16x8 q = *(const bf16x8*)(qr + 32 * i + 16 * hh);
+                for (int i = 0; i < 4; ++i) qb[i] = *(lds_bf16x8*)(qr + (((2 * i + hh) ^ f) << 4));
 #pragma unroll
-                    for (int n = 0; n < KN; ++n) s[rb][n] = mfma_bf16(q, kb[n][i], i ? s[rb][n] : init);
+            for (int i = 0; i < kParts; ++i) {
+                if constexpr (kBf) {
+                    x = mfma_bf16(qb[i], kb[i], x);
+                } else {
+                    const f32x4 q = *(lds_f32x4*)(qr + (((2 * i + hh) ^ f) << 4));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x = mfma_f32(q[e], kf[4 * i + e], x);
                 }
-            } else {
+                float z[kEach];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const f32x4 q = *(const f32x4*)(qr + 32 * i + 16 * hh);
+                for (int e = 0; e < kEach; ++e) z[e] = exp2f_fast(y[kEach * i + e] * a.c2);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-#pragma unroll
-                        for (int n = 0; n < KN; ++n)
-                            s[rb][n] = mfma_f32(q[e], kf[n][4 * i + e], i + e ? s[rb][n] : init);
-                }
+                for (int e = 0; e < kEach; ++e) sum[(kEach * i + e) & 3] += z[e];
+                if (kBf) __builtin_amdgcn_sched_barrier(0);
             }
-#pragma unroll
-            for (int n = 0; n < KN; ++n) add(s[rb ^ 1][n], n);
             if (mask) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    const int row = r0 + 32 * rb + 8 * (r >> 2) + 4 * hh + (r & 3);
-                    const int seen = cache_visible(sq, 1, row / a.G);
-#pragma unroll
-                    for (int n = 0; n < KN; ++n)
-                        if (slot[n] >= seen) s[rb][n][r] = -INFINITY;
+                    const int rr = r0 + br + 8 * (r >> 2) + 4 * hh + (r & 3);
+                    x[r] = rr >= row_min && rr < nrows ? x[r] : -INFINITY;
                 }
             }
         }
-        if (r0 + kWRows < nrows) put(buf ^ 1);
     }
-#pragma unroll
-    for (int n = 0; n < KN; ++n) {
-        add(s[1][n], n);
-        float t = (sum[n][0] + sum[n][1]) + (sum[n][2] + sum[n][3]);
-        t += __shfl_xor(t, 32);
-        if (live[n] && hh == 0) a.weight_out[at[n]] = a.c.weight[at[n]] + t;
-    }
+    add(s[RB - 1]);
+    float t = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    t += __shfl_xor(t, 32);
+    // the two halves of the rows
+    __syncthreads();
+    float* meet = (float*)smem;
+    if (half == 1 && hh == 0) meet[32 * (wave & 1) + l31] = t;
+    __syncthreads();
+    if (half == 0 && hh == 0 && live) a.weight_out[at] = a.c.weight[at] + (t + meet[32 * (wave & 1) + l31]);
 }
 
 // ------------------------------------------------------------------ launchers
@@ -1117,11 +1148,8 @@ static void attend_go(const AttendArgs& a, hipStream_t st) {
     const unsigned bh = a.c.B * a.c.Hkv;
     if (a.logits) {
         hipLaunchKernelGGL(k_cache_weight_rows, dim3((a.c.max_len + 1023) / 1024, bh), dim3(256), 0, st, a);
-    } else if (((int64_t)a.c.max_len + 255) / 256 * bh >= 512) {
-        // (two blocks a wave where that still leaves two workgroups for every compute unit)
-        hipLaunchKernelGGL((k_cache_weight<T, 2>), dim3((a.c.max_len + 255) / 256, bh), dim3(256), 0, st, a);
     } else {
-        hipLaunchKernelGGL((k_cache_weight<T, 1>), dim3((a.c.max_len + 127) / 128, bh), dim3(256), 0, st, a);
+        hipLaunchKernelGGL(k_cache_weight<T>, dim3((a.c.max_len + 63) / 64, bh), dim3(256), 0, st, a);
     }
 }
 

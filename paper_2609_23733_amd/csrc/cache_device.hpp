@@ -41,6 +41,7 @@ struct AttendArgs {
     float *part, *part_ml;   // split results [nsplit, T * Hq, 64] and [nsplit, T * Hq, 2]
     float* logits;           // null, or [T * Hq, logit_stride]: kept for the weights
     int64_t logit_stride;
+    float* off;              // null, or [T * Hq]: -lse log2 e / c2, for the weights
 };
 
 struct AppendArgs {

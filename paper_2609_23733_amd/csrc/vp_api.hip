@@ -821,9 +821,11 @@ int log2_of(int32_t x) {
     return ((int32_t)1 << n) == x ? n : -1;
 }
 
-// Elements between tokens: whole 16-byte units, rows that do not overlap.
+// Elements between tokens: whole 16-byte units, rows that do not overlap, 64 tokens within 32-bit
+// byte offsets.
 bool stride_ok(int64_t stride, int32_t heads, vp_dtype dt) {
-    return stride >= (int64_t)heads * VP_HEAD_DIM && stride % (dt == VP_BF16 ? 8 : 4) == 0;
+    return stride >= (int64_t)heads * VP_HEAD_DIM && stride % (dt == VP_BF16 ? 8 : 4) == 0 &&
+           stride <= (1 << 23);
 }
 
 vp_status check_cache(const vp_cache* c, const vp_cache_batch* b, bool chunk, vp::CacheArgs* a) {
@@ -897,8 +899,10 @@ vp_status attend_args(const vp_cache* cache, const vp_cache_batch* batch, int32_
 
 size_t attend_ws(const vp::AttendArgs& a) {
     const size_t rows = vp::attend_part_rows(a);
+    // (logits or, where the weights form them again, one offset per row)
+    const size_t keep = std::max(vp::attend_logits(a), a.c.weight ? (size_t)a.c.T * a.Hq : 0);
     return kAlign + align_up(rows * VP_HEAD_DIM * sizeof(float)) + align_up(rows * 2 * sizeof(float)) +
-           align_up(vp::attend_logits(a) * sizeof(float));
+           align_up(keep * sizeof(float));
 }
 
 }  // namespace
@@ -1007,8 +1011,11 @@ vp_status vp_cache_attend(const vp_cache* cache, const vp_cache_batch* batch, in
     const size_t rows = vp::attend_part_rows(a);
     a.part = (float*)((char*)ws + kAlign);
     a.part_ml = (float*)((char*)ws + kAlign + align_up(rows * VP_HEAD_DIM * sizeof(float)));
-    if (weight_out && vp::attend_logits(a))
-        a.logits = (float*)((char*)a.part_ml + align_up(rows * 2 * sizeof(float)));
+    if (weight_out) {
+        float* keep = (float*)((char*)a.part_ml + align_up(rows * 2 * sizeof(float)));
+        if (vp::attend_logits(a)) a.logits = keep;
+        else a.off = keep;
+    }
     (void)hipGetLastError();
     vp::launch_cache_attend(a, (hipStream_t)stream);
     return hip_status("vp_cache_attend");

@@ -154,6 +154,14 @@ __device__ __forceinline__ void copy_to_lds(uint32_t lds, const char* base, uint
                  : "memory", "m0");
 }
 
+// The same with 4 bytes per lane: 256 bytes of LDS.
+__device__ __forceinline__ void copy4_to_lds(uint32_t lds, const char* base, uint32_t voff) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
+                 :
+                 : "s"(lds), "v"(voff), "s"(base)
+                 : "memory", "m0");
+}
+
 // Remap a linear work index so that consecutive work items land on the same
 // XCD.  The dispatcher assigns workgroup i to XCD i % 8; item k of XCD x then
 // receives work index x * q + min(x, r) + k over `active` items (q = active / 8,
