@@ -26,6 +26,7 @@ struct EvictWs {
     int32_t *count;     // [B * Hkv, chunks, 2]: above, ties
     int32_t *hole, *mover;   // [B * Hkv, cap]
     int32_t *kbn, *left;     // [B * Hkv]: kept slots below n; n
+    uint32_t* bound;         // [B * Hkv, 2]: the n-th largest key, its ties that are kept
     int cap, chunks;
 };
 
@@ -50,6 +51,7 @@ static EvictWs evict_layout(int B, int Hkv, int max_len, void* ws, size_t* total
     w.mover = (int32_t*)take(bh * w.cap * 4);
     w.kbn = (int32_t*)take(bh * 4);
     w.left = (int32_t*)take(bh * 4);
+    w.bound = (uint32_t*)take(bh * 8);
     if (total) *total = off;
     return w;
 }
@@ -117,6 +119,34 @@ __device__ __forceinline__ void find_digit(const int32_t* hist, int bins, int ne
     __syncthreads();
 }
 
+// Keys of the chunk's slots, four in a row per thread and step (a page holds at least 16), all
+// loads of a thread issued before the first is used.
+constexpr int kEvSteps = kEvChunk / 1024;
+__device__ __forceinline__ void chunk_keys(const EvictArgs& a, int b, int hk, int s0, int s1, uint32_t (&k)[kEvSteps][4]) {
+    int64_t at[kEvSteps];
+    f32x4 w[kEvSteps];
+    typedef int32_t i32x4 __attribute__((__vector_size__(16), aligned(4)));
+    typedef float f32x4u __attribute__((__vector_size__(16), aligned(4)));
+    i32x4 st[kEvSteps];
+    const int64_t latest = (int64_t)a.c.seen[b] - a.recent;
+#pragma unroll
+    for (int j = 0; j < kEvSteps; ++j) {
+        const int s = s0 + j * 1024 + threadIdx.x * 4;
+        at[j] = s < s1 ? slot_at(a.c, b, hk, s) : -1;
+    }
+#pragma unroll
+    for (int j = 0; j < kEvSteps; ++j) {
+        const int64_t p = at[j] >= 0 ? at[j] : 0;   // (slot 0 of the pool for those without a page)
+        w[j] = *(const f32x4u*)(a.c.weight + p);
+        st[j] = *(const i32x4*)(a.c.stamp + p);
+    }
+#pragma unroll
+    for (int j = 0; j < kEvSteps; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            k[j][e] = at[j] >= 0 ? evict_key(w[j][e], st[j][e], a.sink, latest) : 0;
+}
+
 // Counting pass PASS (0: keys made, top 11 bits; 1: next 11; 2: last 10).
 template <int PASS>
 __global__ __launch_bounds__(256) void k_evict_digit(EvictArgs a, EvictWs w) {
@@ -127,6 +157,24 @@ __global__ __launch_bounds__(256) void k_evict_digit(EvictArgs a, EvictWs w) {
     __shared__ int bins[kEvBins];
     __shared__ int tmp[16];
     int32_t* hist = w.hist + (int64_t)bh * 3 * kEvBins;
+    uint32_t* key = w.key + (int64_t)bh * w.cap;
+    uint32_t k[kEvSteps][4];
+    if (PASS == 0) {
+        chunk_keys(a, b, hk, s0, s1, k);
+#pragma unroll
+        for (int j = 0; j < kEvSteps; ++j) {
+            const u32x4 v = {k[j][0], k[j][1], k[j][2], k[j][3]};
+            *(u32x4*)(key + s0 + j * 1024 + threadIdx.x * 4) = v;   // (cap is whole chunks)
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < kEvSteps; ++j) {
+            const u32x4 v = *(const u32x4*)(key + s0 + j * 1024 + threadIdx.x * 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) k[j][e] = v[e];
+        }
+    }
+    for (int i = threadIdx.x; i < kEvBins; i += 256) bins[i] = 0;
     uint32_t prefix = 0;
     int need = n, d;
     if (PASS >= 1) {
@@ -137,24 +185,17 @@ __global__ __launch_bounds__(256) void k_evict_digit(EvictArgs a, EvictWs w) {
         find_digit(hist + kEvBins, 2048, need, &d, &need, tmp);
         prefix = prefix << 11 | d;
     }
-    for (int i = threadIdx.x; i < kEvBins; i += 256) bins[i] = 0;
     __syncthreads();
-    uint32_t* key = w.key + (int64_t)bh * w.cap;
-    const int64_t latest = PASS == 0 ? (int64_t)a.c.seen[b] - a.recent : 0;
-#pragma unroll 4
-    for (int s = s0 + threadIdx.x; s < s1; s += 256) {
-        uint32_t k;
-        if (PASS == 0) {
-            const int64_t at = slot_at(a.c, b, hk, s);
-            k = at >= 0 ? evict_key(a.c.weight[at], a.c.stamp[at], a.sink, latest) : 0;
-            key[s] = k;
-            atomicAdd(&bins[k >> 21], 1);
-        } else {
-            k = key[s];
-            if (PASS == 1 && k >> 21 == prefix) atomicAdd(&bins[(k >> 10) & 2047], 1);
-            if (PASS == 2 && k >> 10 == prefix) atomicAdd(&bins[k & 1023], 1);
+#pragma unroll
+    for (int j = 0; j < kEvSteps; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t x = k[j][e];
+            if (s0 + j * 1024 + (int)threadIdx.x * 4 + e >= s1) continue;
+            if (PASS == 0) atomicAdd(&bins[x >> 21], 1);
+            if (PASS == 1 && x >> 21 == prefix) atomicAdd(&bins[(x >> 10) & 2047], 1);
+            if (PASS == 2 && x >> 10 == prefix) atomicAdd(&bins[x & 1023], 1);
         }
-    }
     __syncthreads();
     for (int i = threadIdx.x; i < kEvBins; i += 256)
         if (bins[i]) atomicAdd(hist + PASS * kEvBins + i, bins[i]);
@@ -204,6 +245,30 @@ __global__ __launch_bounds__(256) void k_evict_count(EvictArgs a, EvictWs w) {
         int32_t* c = w.count + ((int64_t)bh * w.chunks + blockIdx.x) * 2;
         c[0] = tmp[0] + tmp[1] + tmp[2] + tmp[3];
         c[1] = tmp[4] + tmp[5] + tmp[6] + tmp[7];
+        if (blockIdx.x == 0) w.bound[2 * bh] = bound, w.bound[2 * bh + 1] = ties;
+    }
+}
+
+// Weights and stamps of slots [s0, e1) as they are, for output arrays of their own.
+__device__ __forceinline__ void copy_kept(const EvictArgs& a, int b, int hk, int s0, int e1) {
+    typedef int32_t i32x4 __attribute__((__vector_size__(16), aligned(4)));
+    typedef float f32x4u __attribute__((__vector_size__(16), aligned(4)));
+    for (int s = s0 + threadIdx.x * 4; s < e1; s += blockDim.x * 4) {
+        const int64_t at = slot_at(a.c, b, hk, s);
+        if (at < 0) continue;
+        const f32x4u w = *(const f32x4u*)(a.c.weight + at);
+        const i32x4 t = *(const i32x4*)(a.c.stamp + at);
+        if (s + 4 <= e1) {
+            *(f32x4u*)(a.weight_out + at) = w;
+            *(i32x4*)(a.stamp_out + at) = t;
+            continue;
+        }
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+            if (s + e < e1) {
+                a.weight_out[at + e] = w[e];
+                a.stamp_out[at + e] = t[e];
+            }
     }
 }
 
@@ -221,8 +286,8 @@ __global__ __launch_bounds__(256) void k_evict_lists(EvictArgs a, EvictWs w) {
     if (n < len) {
         __shared__ int tmp[16];
         const int t = threadIdx.x, lane = t & 63, wv = t >> 6;
-        int ties;
-        const uint32_t bound = evict_bound(w.hist + (int64_t)bh * 3 * kEvBins, n, &ties, tmp);
+        const uint32_t bound = w.bound[2 * bh];
+        const int ties = (int)w.bound[2 * bh + 1];
         const uint32_t* key = w.key + (int64_t)bh * w.cap;
         // counts of the chunks before
         int above = 0, tie = 0;
@@ -282,13 +347,118 @@ __global__ __launch_bounds__(256) void k_evict_lists(EvictArgs a, EvictWs w) {
         }
     }
     if (same) return;
-    const int e1 = s1 < n ? s1 : n;
-    for (int s = s0 + threadIdx.x; s < e1; s += 256) {
-        const int64_t at = slot_at(a.c, b, hk, s);
-        if (at < 0) continue;
-        a.weight_out[at] = a.c.weight[at];
-        a.stamp_out[at] = a.c.stamp[at];
+    copy_kept(a, b, hk, s0, s1 < n ? s1 : n);
+}
+
+// ------------------------------------------------------------------------
+// Short sequences (up to kEvSmall slots): one workgroup per sequence and head does the counting and the
+// lists with its keys in LDS; one launch in place of six.
+// ------------------------------------------------------------------------
+constexpr int kEvSmall = 16384, kEvThreads = 1024;
+
+__global__ __launch_bounds__(kEvThreads) void k_evict_small(EvictArgs a, EvictWs w) {
+    const int bh = blockIdx.x, hk = bh % a.c.Hkv, b = bh / a.c.Hkv;
+    const int len = cache_length(a.c, b), n = len < a.keep ? len : a.keep;
+    const int t = threadIdx.x, lane = t & 63, wv = t >> 6;
+    if (t == 0) {
+        w.left[bh] = n;
+        if (n == len) w.kbn[bh] = n;   // nothing moves
     }
+    const bool same = a.weight_out == a.c.weight && a.stamp_out == a.c.stamp;
+    if (n < len) {
+        __shared__ __attribute__((aligned(16))) uint32_t key[kEvSmall];
+        __shared__ int bins[kEvBins];
+        __shared__ int tmp[40];
+        const int64_t latest = (int64_t)a.c.seen[b] - a.recent;
+        typedef int32_t i32x4 __attribute__((__vector_size__(16), aligned(4)));
+        typedef float f32x4u __attribute__((__vector_size__(16), aligned(4)));
+        // ---- keys, four slots per thread and step
+        constexpr int kSteps = kEvSmall / (4 * kEvThreads);
+        int64_t at[kSteps];
+#pragma unroll
+        for (int j = 0; j < kSteps; ++j) {
+            const int s = (j * kEvThreads + t) * 4;
+            at[j] = s < len ? slot_at(a.c, b, hk, s) : -1;
+        }
+#pragma unroll
+        for (int j = 0; j < kSteps; ++j) {
+            const int s = (j * kEvThreads + t) * 4;
+            if (s >= len) break;
+            u32x4 k = {0u, 0u, 0u, 0u};
+            if (at[j] >= 0) {
+                const f32x4u x = *(const f32x4u*)(a.c.weight + at[j]);
+                const i32x4 st = *(const i32x4*)(a.c.stamp + at[j]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) k[e] = evict_key(x[e], st[e], a.sink, latest);
+            }
+            *(u32x4*)(key + s) = k;
+        }
+        // ---- the n-th largest: digits of 11, 11 and 10 bits
+        uint32_t prefix = 0;
+        int need = n;
+#pragma unroll 1
+        for (int pass = 0; pass < 3; ++pass) {
+            const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, nb = pass == 2 ? 1024 : 2048;
+            for (int i = t; i < kEvBins; i += kEvThreads) bins[i] = 0;
+            __syncthreads();
+            for (int s = t; s < len; s += kEvThreads) {
+                const uint32_t k = key[s];
+                if (pass == 0 || k >> (pass == 1 ? 21 : 10) == prefix) atomicAdd(&bins[(k >> shift) & (nb - 1)], 1);
+            }
+            __syncthreads();
+            // the digit, two bins per thread, from the largest down
+            const int own0 = 2 * t < nb ? bins[nb - 1 - 2 * t] : 0, own1 = 2 * t + 1 < nb ? bins[nb - 2 - 2 * t] : 0;
+            int inc = own0 + own1;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const int v = __shfl_up(inc, o);
+                if (lane >= o) inc += v;
+            }
+            if (lane == 63) tmp[wv] = inc;
+            __syncthreads();
+            int before = inc - own0 - own1;
+            for (int v = 0; v < wv; ++v) before += tmp[v];
+            if (before < need && before + own0 + own1 >= need) {
+                const bool first = before + own0 >= need;
+                tmp[32] = first ? nb - 1 - 2 * t : nb - 2 - 2 * t;
+                tmp[33] = need - before - (first ? 0 : own0);
+            }
+            __syncthreads();
+            prefix = prefix << (pass == 2 ? 10 : 11) | (uint32_t)tmp[32];
+            need = tmp[33];
+            __syncthreads();
+        }
+        // ---- lists: a run of slots in a row per thread
+        const uint32_t bound = prefix;
+        const int ties = need, per = (len + kEvThreads - 1) / kEvThreads, p0 = t * per;
+        const int p1 = p0 + per < len ? p0 + per : len;
+        int above = 0, tie = 0;
+        for (int s = p0; s < p1; ++s) above += key[s] > bound, tie += key[s] == bound;
+        int ia = above, it = tie;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int va = __shfl_up(ia, o), vt = __shfl_up(it, o);
+            if (lane >= o) ia += va, it += vt;
+        }
+        if (lane == 63) tmp[wv] = ia, tmp[16 + wv] = it;
+        __syncthreads();
+        above = ia - above;
+        tie = it - tie;
+        for (int v = 0; v < wv; ++v) above += tmp[v], tie += tmp[16 + v];
+        int32_t* hole = w.hole + (int64_t)bh * w.cap;
+        int32_t* mover = w.mover + (int64_t)bh * w.cap;
+        for (int s = p0; s < p1; ++s) {
+            const uint32_t k = key[s];
+            const int kb = above + (tie < ties ? tie : ties);
+            const bool kept = k > bound || (k == bound && tie < ties);
+            above += k > bound;
+            tie += k == bound;
+            if (s == n) w.kbn[bh] = kb;
+            if (s < n && !kept) hole[s - kb] = s;
+            if (s >= n && kept) mover[kb] = s;
+        }
+    }
+    if (!same) copy_kept(a, b, hk, 0, n);
 }
 
 // The moves: eight threads per move and tensor row.
@@ -327,12 +497,16 @@ void launch_cache_evict(const EvictArgs& a, hipStream_t st) {
     const int bh = a.c.B * a.c.Hkv;
     const int64_t nh = (int64_t)bh * 3 * kEvBins;
     const dim3 grid(w.chunks, bh);
-    hipLaunchKernelGGL(k_evict_clear, dim3((nh + 255) / 256), dim3(256), 0, st, w.hist, nh);
-    hipLaunchKernelGGL(k_evict_digit<0>, grid, dim3(256), 0, st, a, w);
-    hipLaunchKernelGGL(k_evict_digit<1>, grid, dim3(256), 0, st, a, w);
-    hipLaunchKernelGGL(k_evict_digit<2>, grid, dim3(256), 0, st, a, w);
-    hipLaunchKernelGGL(k_evict_count, grid, dim3(256), 0, st, a, w);
-    hipLaunchKernelGGL(k_evict_lists, grid, dim3(256), 0, st, a, w);
+    if (a.c.max_len <= kEvSmall) {
+        hipLaunchKernelGGL(k_evict_small, dim3(bh), dim3(kEvThreads), 0, st, a, w);
+    } else {
+        hipLaunchKernelGGL(k_evict_clear, dim3((nh + 255) / 256), dim3(256), 0, st, w.hist, nh);
+        hipLaunchKernelGGL(k_evict_digit<0>, grid, dim3(256), 0, st, a, w);
+        hipLaunchKernelGGL(k_evict_digit<1>, grid, dim3(256), 0, st, a, w);
+        hipLaunchKernelGGL(k_evict_digit<2>, grid, dim3(256), 0, st, a, w);
+        hipLaunchKernelGGL(k_evict_count, grid, dim3(256), 0, st, a, w);
+        hipLaunchKernelGGL(k_evict_lists, grid, dim3(256), 0, st, a, w);
+    }
     // A move for every slot past the first `keep` at most.
     int64_t most = a.c.max_len - a.keep;
     most = most < 1 ? 1 : most < a.keep ? most : a.keep;
