@@ -836,42 +836,90 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(Att
 }
 
 // ------------------------------------------------------------------------
-// Join of the split results, one wave per row: the splits whose slot range the row sees.
+// Join of the split results whose slot range a row sees.  16 lanes hold a row's 64 features.  MANY:
+// a wave per row, four splits at a time; otherwise (up to kFew splits) four rows per wave.  All of a
+// lane's loads are issued before the first is used.
 // ------------------------------------------------------------------------
-template <typename T>
+constexpr int kFew = 8;
+
+template <typename T, bool MANY>
 __global__ __launch_bounds__(256) void k_cache_join(AttendArgs a) {
-    const int lane = threadIdx.x & 63;
+    const int lane = threadIdx.x & 63, grp = lane >> 4, d = (lane & 15) * 4;
     const int b = blockIdx.y;
     const CacheSeq sq = cache_seq(a.c, b);
-    const int r = blockIdx.x * 4 + (threadIdx.x >> 6);   // (token, head) of the sequence
+    const int wv = blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int r = MANY ? wv : 4 * wv + grp;   // (token, head) of the sequence
     const int i = r / a.Hq;
     if (i >= sq.nq) return;
     const int64_t at = (int64_t)sq.q0 * a.Hq + r, all_rows = (int64_t)a.c.T * a.Hq;
     const int vis = cache_visible(sq, a.causal, i);
     int ns = (vis + a.chunk - 1) / a.chunk;
     ns = ns < 1 ? 1 : ns < a.nsplit ? ns : a.nsplit;
+    constexpr int kLanes = MANY ? 64 : 16;        // lanes that share a row
+    const int own = lane & (kLanes - 1);
+    // The reference of all splits, their factors (a lane's splits: own, own + kLanes, ..), the sum.
+    constexpr int kMl = MANY ? 4 : 1;             // (at most 256 splits)
+    f32x2 ml[kMl];
     float M = -INFINITY;
-    for (int s = lane; s < ns; s += 64) M = maximum(M, a.part_ml[(s * all_rows + at) * 2]);
 #pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) M = maximum(M, __shfl_xor(M, o));
-    float L = 0.f, acc = 0.f;
-    for (int s0 = 0; s0 < ns; s0 += 64) {
-        float f = 0.f;
-        if (s0 + lane < ns) {
-            const f32x2 ml = *(const f32x2*)(a.part_ml + ((s0 + lane) * all_rows + at) * 2);
-            f = ml[0] == -INFINITY ? 0.f : ml[0] == M ? 1.f : exp2f_fast(ml[0] - M);
-            L += f * ml[1];
-        }
-        const int n = ns - s0 < 64 ? ns - s0 : 64;
-        const float* po = a.part + (s0 * all_rows + at) * kD + lane;
-#pragma unroll 8
-        for (int s = 0; s < n; ++s) acc += __shfl(f, s) * po[s * all_rows * kD];
+    for (int j = 0; j < kMl; ++j) {
+        ml[j] = f32x2{-INFINITY, 0.f};
+        const int s = own + j * kLanes;
+        if (s < ns) ml[j] = *(const f32x2*)(a.part_ml + (s * all_rows + at) * 2);
     }
-    L = wave_sum(L);
+    constexpr int kBatch = MANY ? 4 * kFew : kFew;   // splits per batch of loads
+    f32x4 v[kFew];
+    auto load = [&](int s0) {
+#pragma unroll
+        for (int k = 0; k < kFew; ++k) {
+            const int s = s0 + (MANY ? 4 * k + grp : k);
+            v[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (s < ns) v[k] = *(const f32x4*)(a.part + (s * all_rows + at) * kD + d);
+        }
+    };
+    load(0);
+#pragma unroll
+    for (int j = 0; j < kMl; ++j) M = maximum(M, ml[j][0]);
+#pragma unroll
+    for (int o = kLanes / 2; o >= 1; o >>= 1) M = maximum(M, __shfl_xor(M, o));
+    float f[kMl], L = 0.f;
+#pragma unroll
+    for (int j = 0; j < kMl; ++j) {
+        f[j] = ml[j][0] == -INFINITY ? 0.f : ml[j][0] == M ? 1.f : exp2f_fast(ml[j][0] - M);
+        L += f[j] * ml[j][1];
+    }
+#pragma unroll
+    for (int o = kLanes / 2; o >= 1; o >>= 1) L += __shfl_xor(L, o);
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int s0 = 0; s0 < ns; s0 += kBatch) {
+        if (s0 > 0) load(s0);
+        const float fj = MANY ? (s0 < 64 ? f[0] : s0 < 128 ? f[kMl > 1 ? 1 : 0] : s0 < 192 ? f[kMl > 2 ? 2 : 0] : f[kMl - 1]) : f[0];
+#pragma unroll
+        for (int k = 0; k < kFew; ++k) {
+            const int s = s0 + (MANY ? 4 * k + grp : k);
+            const float x = __shfl(fj, MANY ? s & 63 : (lane & 48) + k);
+            // (a split without weight may hold anything)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[e] += s < ns && x != 0.f ? x * v[k][e] : 0.f;
+        }
+    }
+    if constexpr (MANY) {
+#pragma unroll
+        for (int o = 16; o <= 32; o <<= 1)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], o);
+        if (grp) return;
+    }
     float inv, lse;
     row_result(M, L, &inv, &lse);
-    if (lane == 0) put_lse(a, at, lse);
-    ((T*)a.O)[at * kD + lane] = (T)(acc * inv);
+    if ((lane & 15) == 0) put_lse(a, at, lse);
+    T* out = (T*)a.O + at * kD + d;
+    if constexpr (sizeof(T) == 2) {
+        bf16x4 y = {(bf16)(acc[0] * inv), (bf16)(acc[1] * inv), (bf16)(acc[2] * inv), (bf16)(acc[3] * inv)};
+        *(bf16x4*)out = y;
+    } else {
+        *(f32x4*)out = f32x4{acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
+    }
 }
 
 // ------------------------------------------------------------------------
@@ -1141,9 +1189,11 @@ static void attend_go(const AttendArgs& a, hipStream_t st) {
         hipLaunchKernelGGL((k_cache_attend<T, true>), dim3(grid), dim3(64 * Geo<T, true>::NW), 0, st, a);
     else
         hipLaunchKernelGGL((k_cache_attend<T, false>), dim3(grid), dim3(256), 0, st, a);
-    if (a.nsplit > 1)
-        hipLaunchKernelGGL(k_cache_join<T>, dim3(((int64_t)a.c.max_q * a.Hq + 3) / 4, a.c.B), dim3(256), 0,
-                           st, a);
+    const int64_t rows = (int64_t)a.c.max_q * a.Hq;
+    if (a.nsplit > kFew)
+        hipLaunchKernelGGL((k_cache_join<T, true>), dim3((rows + 3) / 4, a.c.B), dim3(256), 0, st, a);
+    else if (a.nsplit > 1)
+        hipLaunchKernelGGL((k_cache_join<T, false>), dim3((rows + 15) / 16, a.c.B), dim3(256), 0, st, a);
     if (!a.weight_out || a.c.max_len == 0) return;
     const unsigned bh = a.c.B * a.c.Hkv;
     if (a.logits) {
