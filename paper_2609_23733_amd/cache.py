@@ -15,7 +15,7 @@ from typing import Optional, Sequence
 import torch
 
 from . import vp
-from .vp import HEAD_DIM, _check, _dt, _need, _ptr, _stream, load_library
+from .vp import HEAD_DIM, VPError, _check, _dt, _need, _ptr, load_library
 
 ROT_INTERLEAVED, ROT_HALF = 0, 1
 ROT_SCALE_NONE, ROT_SCALE_LINEAR, ROT_SCALE_PARTS = 0, 1, 2
@@ -23,19 +23,51 @@ _LAYOUTS = {"interleaved": ROT_INTERLEAVED, "half": ROT_HALF}
 _SCALINGS = {"none": ROT_SCALE_NONE, "linear": ROT_SCALE_LINEAR, "parts": ROT_SCALE_PARTS}
 
 
+# A single token's attention takes the GPU some 10 us, so the calls below keep the host's part short:
+# addresses go to the library as plain integers, a tensor's properties are compared in one
+# pass, and only a tensor that fails is looked at again for the message.
+
+def _stream() -> int:
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+
+
+def _done(code: int, where: str):
+    if code:
+        raise VPError(code, where)
+
+
 def _rows(t: torch.Tensor, name: str, T: int, H: int, dtype) -> int:
     """Checks a [T, H, 64] tensor whose tokens may lie apart; returns their distance."""
-    if not isinstance(t, torch.Tensor):
-        raise TypeError("%s must be a tensor" % name)
+    try:
+        st = t.stride()
+        if t.shape == (T, H, HEAD_DIM) and t.dtype is dtype and t.is_cuda and \
+                (T == 0 or (st[2] == 1 and (H == 1 or st[1] == HEAD_DIM))):
+            return st[0] if T > 1 else H * HEAD_DIM
+    except AttributeError:
+        raise TypeError("%s must be a tensor" % name) from None
     if not t.is_cuda:
         raise ValueError("%s must be a GPU tensor" % name)
     if t.dtype != dtype:
         raise ValueError("%s has dtype %s, expected %s" % (name, t.dtype, dtype))
     if tuple(t.shape) != (T, H, HEAD_DIM):
         raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), (T, H, HEAD_DIM)))
-    if (t.stride(2) != 1 or (H > 1 and t.stride(1) != HEAD_DIM)) and T > 0:
-        raise ValueError("%s must have contiguous [H, %d] rows" % (name, HEAD_DIM))
-    return t.stride(0) if T > 1 else H * HEAD_DIM
+    raise ValueError("%s must have contiguous [H, %d] rows" % (name, HEAD_DIM))
+
+
+def _whole(t: torch.Tensor, name: str, shape, dtype) -> int:
+    """Checks a contiguous tensor; returns its address."""
+    if isinstance(t, torch.Tensor) and t.shape == shape and t.dtype is dtype and t.is_cuda and \
+            t.is_contiguous():
+        return t.data_ptr()
+    _need(t, name, shape, dtype)
+    raise ValueError("%s is not as expected" % name)
+
+
+def _work(ws: torch.Tensor):
+    """Address and size in bytes of a workspace."""
+    if not (isinstance(ws, torch.Tensor) and ws.is_cuda and ws.is_contiguous()):
+        _need(ws, "ws")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
 
 
 class Rotary:
@@ -49,8 +81,7 @@ class Rotary:
             raise ValueError("freq must be [dim / 2]")
         self.freq, self.layout, self.axes, self.mag = freq, layout, int(axes), float(mag)
         self.dim = 2 * freq.numel()
-        self._c = vp.vp_rotary_spec(None, freq.data_ptr(), self.dim, self.axes, _LAYOUTS[layout],
-                                    self.mag)
+        self._fields = (freq.data_ptr(), self.dim, self.axes, _LAYOUTS[layout], self.mag)
 
     @staticmethod
     def make(dim: int = HEAD_DIM, base: float = 10000.0, axes: int = 1, layout: str = "half",
@@ -68,10 +99,8 @@ class Rotary:
 
     def at(self, pos: torch.Tensor, T: int):
         """The C argument for positions pos int32 [T, axes]."""
-        _need(pos, "pos", (T, self.axes), torch.int32)
-        c = self._c
-        c.pos = pos.data_ptr()
-        return ctypes.byref(c)
+        return ctypes.byref(vp.vp_rotary_spec(_whole(pos, "pos", (T, self.axes), torch.int32),
+                                              *self._fields))
 
 
 def rotary(x, pos, rot: Rotary, out: Optional[torch.Tensor] = None, transpose: bool = False):
@@ -82,8 +111,8 @@ def rotary(x, pos, rot: Rotary, out: Optional[torch.Tensor] = None, transpose: b
     if out is None:
         out = torch.empty(T, H, HEAD_DIM, dtype=x.dtype, device=x.device)
     ys = _rows(out, "out", T, H, x.dtype)
-    _check(load_library().vp_rotary(rot.at(pos, T), _dt(x), T, H, _ptr(x), xs, _ptr(out), ys,
-                                    int(transpose), _stream()), "vp_rotary")
+    _done(load_library().vp_rotary(rot.at(pos, T), _dt(x), T, H, x.data_ptr(), xs, out.data_ptr(), ys,
+                                   transpose, _stream()), "vp_rotary")
     return out
 
 
@@ -102,7 +131,7 @@ class PagedCache:
             _need(weight, "weight", K.shape[:3], torch.float32)
         if stamp is not None:
             _need(stamp, "stamp", K.shape[:3], torch.int32)
-        self.K, self.V, self.weight, self.stamp = K, V, weight, stamp
+        self.K, self.V, self.weight, self.stamp, self.dtype = K, V, weight, stamp, K.dtype
         ptr = lambda t: None if t is None else t.data_ptr()
         self._c = vp.vp_cache(K.data_ptr(), V.data_ptr(), ptr(weight), ptr(stamp), self.npages,
                               self.page, self.Hkv, HEAD_DIM, _dt(K))
@@ -133,34 +162,31 @@ class Batch:
             _need(seen, "seen", (self.B,), torch.int32)
         self.table, self.length, self.q_start, self.seen = table, length, q_start, seen
         self.max_q, self.max_len = int(max_q), int(max_len)
-        self._c = vp.vp_cache_batch(table.data_ptr(), length.data_ptr(),
-                                    None if seen is None else seen.data_ptr(), q_start.data_ptr(),
-                                    self.B, self.max_pages, 0, self.max_q, self.max_len)
+        self._first = (table.data_ptr(), length.data_ptr(), None if seen is None else seen.data_ptr(),
+                       q_start.data_ptr(), self.B, self.max_pages)
 
     def _for(self, T: int):
-        self._c.T = T
-        return ctypes.byref(self._c)
+        return ctypes.byref(vp.vp_cache_batch(*self._first, T, self.max_q, self.max_len))
 
 
 def append(pc: PagedCache, batch: Batch, Q, K, V, pos=None, rot: Optional[Rotary] = None,
            Q_out: Optional[torch.Tensor] = None):
     """New tokens into the cache: K [T, Hkv, 64] rotated, V as it is; returns the rotated Q [T, Hq,
     64] (None without Q)."""
-    T, Hkv, dt = K.shape[0], pc.Hkv, pc.K.dtype
+    T, Hkv, dt = K.shape[0], pc.Hkv, pc.dtype
     ks, vs = _rows(K, "K", T, Hkv, dt), _rows(V, "V", T, Hkv, dt)
-    Hq, qs = Hkv, 0
+    Hq = qs = q = qo = 0
     if Q is not None:
         Hq = Q.shape[1]
-        qs = _rows(Q, "Q", T, Hq, dt)
+        qs, q = _rows(Q, "Q", T, Hq, dt), Q.data_ptr()
         if Q_out is None:
             Q_out = torch.empty(T, Hq, HEAD_DIM, dtype=dt, device=Q.device)
-        _need(Q_out, "Q_out", (T, Hq, HEAD_DIM), dt)
+        qo = _whole(Q_out, "Q_out", (T, Hq, HEAD_DIM), dt)
     if rot is not None and pos is None:
         raise ValueError("a rotation needs positions")
-    _check(load_library().vp_cache_append(pc._ref, batch._for(T), Hq, _ptr(Q), qs, _ptr(K), ks,
-                                          _ptr(V), vs, None if rot is None else rot.at(pos, T),
-                                          _ptr(Q_out) if Q is not None else None, _stream()),
-           "vp_cache_append")
+    _done(load_library().vp_cache_append(pc._ref, batch._for(T), Hq, q, qs, K.data_ptr(), ks, V.data_ptr(), vs,
+                                         None if rot is None else rot.at(pos, T), qo, _stream()),
+          "vp_cache_append")
     return Q_out if Q is not None else None
 
 
@@ -177,25 +203,23 @@ def attend(pc: PagedCache, batch: Batch, Q, causal: bool = True, scale: float = 
     """Attention of the new tokens' queries Q [T, Hq, 64] over their sequences' slots: (O [T, Hq,
     64], lse [T, Hq] fp32).  With `weight_out` (it may be pc.weight) the attention weights of
     the call are added to the slots they fall on."""
-    T, Hq, dt = Q.shape[0], Q.shape[1], pc.K.dtype
+    T, Hq, _ = Q.shape
+    dt = pc.dtype
     qs = _rows(Q, "Q", T, Hq, dt)
     if O is None:
         O = torch.empty(T, Hq, HEAD_DIM, dtype=dt, device=Q.device)
     if lse is None:
         lse = torch.empty(T, Hq, dtype=torch.float32, device=Q.device)
-    _need(O, "O", (T, Hq, HEAD_DIM), dt)
-    _need(lse, "lse", (T, Hq), torch.float32)
+    o, ls, wo = _whole(O, "O", (T, Hq, HEAD_DIM), dt), _whole(lse, "lse", (T, Hq), torch.float32), None
     if weight_out is not None:
         if pc.weight is None:
             raise ValueError("the cache has no weights")
-        _need(weight_out, "weight_out", pc.weight.shape, torch.float32)
+        wo = _whole(weight_out, "weight_out", pc.weight.shape, torch.float32)
     if ws is None:
         ws = attend_workspace(pc, batch, Hq, T)
-    _need(ws, "ws")
-    _check(load_library().vp_cache_attend(pc._ref, batch._for(T), Hq, _ptr(Q), qs, int(causal),
-                                          float(scale), _ptr(O), _ptr(lse), _ptr(weight_out),
-                                          _ptr(ws), ws.numel() * ws.element_size(), _stream()),
-           "vp_cache_attend")
+    w, n = _work(ws)
+    _done(load_library().vp_cache_attend(pc._ref, batch._for(T), Hq, Q.data_ptr(), qs, causal, scale, o, ls, wo, w,
+                                         n, _stream()), "vp_cache_attend")
     return O, lse
 
 
@@ -221,18 +245,16 @@ def evict(pc: PagedCache, table, length, seen, keep: int, max_len: int, sink: in
     weight_out = pc.weight if weight_out is None else weight_out
     stamp_out = pc.stamp if stamp_out is None else stamp_out
     length_out = length if length_out is None else length_out
-    _need(weight_out, "weight_out", pc.weight.shape, torch.float32)
-    _need(stamp_out, "stamp_out", pc.stamp.shape, torch.int32)
-    _need(length_out, "length_out", (B,), torch.int32)
+    wo = _whole(weight_out, "weight_out", pc.weight.shape, torch.float32)
+    so = _whole(stamp_out, "stamp_out", pc.stamp.shape, torch.int32)
+    lo = _whole(length_out, "length_out", (B,), torch.int32)
     if ws is None:
         ws = evict_workspace(pc, B, max_len)
-    _need(ws, "ws")
+    w, n = _work(ws)
     c = vp.vp_cache_batch(table.data_ptr(), length.data_ptr(), seen.data_ptr(), None, B, pages, 0, 0,
                           int(max_len))
-    _check(load_library().vp_cache_evict(pc._ref, ctypes.byref(c), int(keep), int(sink), int(recent),
-                                         _ptr(weight_out), _ptr(stamp_out), _ptr(length_out),
-                                         _ptr(ws), ws.numel() * ws.element_size(), _stream()),
-           "vp_cache_evict")
+    _done(load_library().vp_cache_evict(pc._ref, ctypes.byref(c), int(keep), int(sink), int(recent), wo, so, lo, w, n,
+                                        _stream()), "vp_cache_evict")
     return length_out
 
 
