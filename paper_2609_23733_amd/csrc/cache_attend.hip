@@ -43,6 +43,9 @@ struct Geo {
     static constexpr int AHEAD = WIDE && kBf ? NST - 2 : NST - 1;
     static constexpr int kRing = NST * kTile;
     static constexpr int kLds = WIDE ? kRing : 4 * kRing;
+    // fp32, wide: a tile as three bf16 planes of K and three of V, two tiles
+    static constexpr int kPlane = 32 * 128, kPlanes = 6 * kPlane;
+    static_assert(kBf || !WIDE || 2 * kPlanes <= kLds, "the planes fit the ring");
     static constexpr int UC = 16 * ROWB / 1024;                 // 1 KB copies per 16 slots
     static constexpr int PPW = (TK / 16) * 2 / (WIDE ? NW : 1); // (16 slots of K or V) per wave
     static constexpr int CPT = PPW * UC;                        // copies per wave and tile
@@ -257,6 +260,40 @@ __device__ __forceinline__ void block_values(Rows<T>& w, lds_char* v, const Prob
     }
 }
 
+// fp32 values as sums of three bf16 values, x = h + m + l: each takes the next eight significant bits,
+// cut, not rounded, so that the sum is exact and h does not overflow.  Products of two such sums leave out
+// m l, l m and l l, at most 2^-21 of the product and 2^-23 on the average.
+struct Planes {
+    bf16x8 h, m, l;
+};
+__device__ __forceinline__ Planes split8(const float (&x)[8]) {
+    u32x4 h, m, l;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        uint32_t a[2], b[2], c[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const float v = x[2 * j + e];
+            a[e] = __float_as_uint(v) & 0xffff0000u;
+            const float r = v - __uint_as_float(a[e]);
+            b[e] = __float_as_uint(r) & 0xffff0000u;
+            c[e] = __float_as_uint(r - __uint_as_float(b[e]));
+        }
+        h[j] = __builtin_amdgcn_perm(a[1], a[0], 0x07060302u);   // the upper halves
+        m[j] = __builtin_amdgcn_perm(b[1], b[0], 0x07060302u);
+        l[j] = __builtin_amdgcn_perm(c[1], c[0], 0x07060302u);
+    }
+    return Planes{__builtin_bit_cast(bf16x8, h), __builtin_bit_cast(bf16x8, m), __builtin_bit_cast(bf16x8, l)};
+}
+__device__ __forceinline__ f32x16 mfma_planes(const Planes& a, const Planes& b, f32x16 c) {
+    c = mfma_bf16(a.m, b.m, c);
+    c = mfma_bf16(a.l, b.h, c);
+    c = mfma_bf16(a.h, b.l, c);
+    c = mfma_bf16(a.m, b.h, c);
+    c = mfma_bf16(a.h, b.m, c);
+    return mfma_bf16(a.h, b.h, c);
+}
+
 // One block after the other: logits, probabilities, values.
 // `logits`: null, or where the row's logits (of slots from 0 on) are kept.
 template <typename T>
@@ -403,6 +440,7 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(Att
     Rows<T> w[G::NB];
     const bool alive = row0 < nrows;
     int64_t orow[G::NB];   // row of O
+    const T* qrow[G::NB];
 #pragma unroll
     for (int nb = 0; nb < G::NB; ++nb) {
         int r = row0 + 32 * nb + l31;
@@ -413,19 +451,25 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(Att
         w[nb].l = 0.f;
         w[nb].o[0] = w[nb].o[1] = zero_f32x16();
         orow[nb] = (int64_t)(sq.q0 + i) * a.Hq + head;
-        const T* q = (const T*)a.Q + (int64_t)(sq.q0 + i) * a.q_stride + head * kD;
-        if constexpr (G::kBf) {
+        qrow[nb] = (const T*)a.Q + (int64_t)(sq.q0 + i) * a.q_stride + head * kD;
+    }
+    auto load_q = [&]() {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) w[nb].qb[k] = load_bf16x8(q + 16 * k + 8 * hh);
-        } else {
+        for (int nb = 0; nb < G::NB; ++nb) {
+            if constexpr (G::kBf) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const f32x4 v = *(const f32x4*)(q + 8 * k + 4 * hh);
+                for (int k = 0; k < 4; ++k) w[nb].qb[k] = load_bf16x8(qrow[nb] + 16 * k + 8 * hh);
+            } else {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) w[nb].qf[4 * k + e] = v[e];
+                for (int k = 0; k < 8; ++k) {
+                    const f32x4 v = *(const f32x4*)(qrow[nb] + 8 * k + 4 * hh);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[nb].qf[4 * k + e] = v[e];
+                }
             }
         }
-    }
+    };
+    if constexpr (!WIDE || G::kBf) load_q();
     const int wave_last = row0 + 32 * G::NB - 1 < nrows ? row0 + 32 * G::NB - 1 : nrows - 1;
     const int wlim = alive ? cache_visible(sq, a.causal, wave_last / a.G) : 0;
     // slots of this range that every row of the workgroup sees
@@ -473,9 +517,12 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(Att
                     copy_to_lds(dst + u * 1024, src + u * 1024, isv ? vv : kv ^ (64 * u));
             }
         };
+        auto issue_first = [&]() {
 #pragma unroll
-        for (int t = 0; t < G::AHEAD; ++t)
-            if (t < nt) issue(t);
+            for (int t = 0; t < G::AHEAD; ++t)
+                if (t < nt) issue(t);
+        };
+        if constexpr (!WIDE || G::kBf) issue_first();
         // Groups of 16 slots of the tile at k0 that exist (all, unless the table is wrong).
         auto groups = [&](int k0) {
             uint32_t units = ~0u;
@@ -537,13 +584,13 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(Att
                                             k0 + 32 * j, partial, units >> (2 * j), lane, logits);
             }
         };
+        bool redo = false;
         if constexpr (WIDE && G::kBf) {
             // The reference stays that of the first block.  While block j's probabilities are formed, block
             // j + 1's logits and block j - 1's values are multiplied: matrix and vector
             // instructions without a dependence or a branch between them.  Should a row's sum or
             // result leave fp32's range with it (its logits grew by more than 41 over the first block's, its
             // first block had none, or values are huge), the workgroup does its range again carefully.
-            __shared__ int s_redo[G::NW];
             const int tfull = pw.sane ? (seen_by_all - c0) / G::TK : 0;   // tiles all rows see
             f32x16 s0[G::NB], s1[G::NB];
             Probs<T> p0[G::NB], p1[G::NB];
@@ -662,7 +709,152 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(Att
             } else {
                 for (int t = 1; t < nt; ++t) arrive(t);
             }
-            bool redo = !pw.sane;
+        } else if constexpr (WIDE) {
+            // fp32: six bf16 MFMAs for every eight fp32 ones, of which each takes 16 times its share.  K and
+            // V are split once per workgroup on their way into LDS; reference and fallback (fp32
+            // MFMAs) as above.
+            const int slot8 = tid >> 3, pc = tid & 7;   // this thread's eight features of a slot
+            f32x4 kr[2], vr[2];
+            // The matrix units take bf16 values below 2^-126 as 0.  What keys and queries lose by it shows
+            // if any of them, 0 aside, lies below 2^-103; what probabilities and values lose is at
+            // most 2^-125 of the largest value per slot and of l, and may not reach 2^-24 of a
+            // result.  Otherwise the range is done again, too.
+            uint32_t kq_min = ~0u, v_max = 0;   // twice the bits (less one: 0 comes last)
+            auto fetch = [&](int t) {
+                const int k0 = c0 + t * 32;
+                int unit = k0 + 16 * (wave >> 1);   // (a wave's eight slots lie on one page)
+                unit = unit < last_unit ? unit : last_unit;
+                const int id = pw.page(unit >> a.c.page_log2, lane);
+                const int64_t at = ((((int64_t)id * a.c.Hkv + hk) << a.c.page_log2) + (unit & page_mask) +
+                                    (slot8 & 15)) * kD + pc * 8;
+                const float *kp = (const float*)a.c.K + at, *vp_ = (const float*)a.c.V + at;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    kr[e] = *(const f32x4*)(kp + 4 * e);
+                    vr[e] = *(const f32x4*)(vp_ + 4 * e);
+                }
+            };
+            auto put = [&](int t) {
+                char* buf = smem + (t & 1) * G::kPlanes;
+                const bool live = c0 + t * 32 + slot8 < c1;   // (others may hold anything)
+                float x[8];
+                uint32_t least = ~0u;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    x[e] = kr[e >> 2][e & 3];
+                    least = min(least, (__float_as_uint(x[e]) << 1) - 1u);
+                }
+                if (live) kq_min = min(kq_min, least);
+                Planes p = split8(x);
+                char* d = buf + slot8 * 128 + ((pc ^ ((slot8 >> 1) & 7)) << 4);
+                *(bf16x8*)d = p.h;
+                *(bf16x8*)(d + G::kPlane) = p.m;
+                *(bf16x8*)(d + 2 * G::kPlane) = p.l;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    x[e] = live ? vr[e >> 2][e & 3] : 0.f;
+                    v_max = max(v_max, __float_as_uint(x[e]) << 1);
+                }
+                p = split8(x);
+                d = buf + 3 * G::kPlane + slot8 * 128 + ((pc ^ (2 * (slot8 & 3))) << 4);
+                *(bf16x8*)d = p.h;
+                *(bf16x8*)(d + G::kPlane) = p.m;
+                *(bf16x8*)(d + 2 * G::kPlane) = p.l;
+            };
+            fetch(0);
+            Planes q[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                float x[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    x[e] = qrow[0][16 * k + 8 * hh + e];
+                    kq_min = min(kq_min, (__float_as_uint(x[e]) << 1) - 1u);
+                }
+                q[k] = split8(x);
+            }
+            put(0);
+            if (nt > 1) fetch(1);
+            Rows<T>& x = w[0];
+            float ref = 0.f, sum[4] = {0.f, 0.f, 0.f, 0.f};
+            const int row = swap23(l31), ka = row * 128 + ((hh ^ ((row >> 1) & 7)) << 4);
+            const int i16 = lane & 15, dq = (lane >> 4) & 1;
+            const int va = (8 * hh + (i16 >> 2)) * 128 +
+                           (((2 * dq + ((i16 & 3) >> 1)) ^ (2 * (i16 >> 2))) << 4) + (i16 & 1) * 8;
+            for (int t = 0; t < nt; ++t) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                __builtin_amdgcn_s_barrier();
+                const int k0 = c0 + t * 32;
+                if (k0 < wlim) {
+                    typedef __attribute__((address_space(3))) const bf16x8 lds_frag;
+                    lds_char* buf = (lds_char*)smem + (t & 1) * G::kPlanes;
+                    f32x16 s = zero_f32x16();
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        lds_char* k = buf + (ka ^ (i << 5));
+                        const Planes f = {*(lds_frag*)k, *(lds_frag*)(k + G::kPlane), *(lds_frag*)(k + 2 * G::kPlane)};
+                        s = mfma_planes(f, q[i], s);
+                    }
+                    if (k0 + 32 > seen_by_all) {   // (a lane's slots lie as in the bf16 blocks)
+                        const int left = x.vis - k0 - 8 * hh;
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) s[r] = Geo<bf16, true>::key(r, 0) < left ? s[r] : -INFINITY;
+                    }
+                    if (t == 0) {
+                        float top = s[0];
+#pragma unroll
+                        for (int r = 0; r < 16; r += 2) top = maximum(maximum(top, s[r]), s[r + 1]);
+                        const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false,
+                                                                        false);
+                        x.m = maximum(__uint_as_float(y[0]), __uint_as_float(y[1])) * a.c2;
+                        ref = x.m == -INFINITY ? 0.f : x.m;
+                    }
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        s[r] = exp2f_fast(fmaf(s[r], a.c2, -ref));
+                        sum[r & 3] += s[r];
+                    }
+#pragma unroll
+                    for (int st = 0; st < 2; ++st) {
+                        float z[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) z[e] = s[8 * st + e];
+                        const Planes p = split8(z);
+#pragma unroll
+                        for (int m = 0; m < 2; ++m) {
+                            lds_char* v = buf + 3 * G::kPlane + (va ^ (m << 6)) + st * 2048;
+                            const Planes f = {tr_read(v), tr_read(v + G::kPlane), tr_read(v + 2 * G::kPlane)};
+                            x.o[m] = mfma_planes(f, p, x.o[m]);
+                        }
+                    }
+                }
+                if (t + 1 < nt) {
+                    put(t + 1);
+                    if (t + 2 < nt) fetch(t + 2);
+                }
+            }
+            x.l = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            constexpr uint32_t kLeast = (24u << 24) - 1u;   // 2^-103
+            if (__builtin_amdgcn_ballot_w64(kq_min < kLeast)) redo = true;
+            __shared__ uint32_t s_vmax[G::NW];
+#pragma unroll
+            for (int o = 32; o >= 1; o >>= 1) v_max = max(v_max, (uint32_t)__shfl_xor((int)v_max, o));
+            if (lane == 0) s_vmax[wave] = v_max;
+            __syncthreads();
+            for (int v = 0; v < G::NW; ++v) v_max = max(v_max, s_vmax[v]);
+            const float lim = ((float)(c1 - c0) * __uint_as_float(v_max >> 1) + x.l) * 7.8886090522101181e-31f;   // 2^-100
+            bool lost = false;
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) lost = lost || (x.o[m][r] != 0.f && fabsf(x.o[m][r]) < lim);
+            if (alive && __builtin_amdgcn_ballot_w64(lost)) redo = true;
+        } else {
+            careful();
+        }
+        if constexpr (WIDE) {
+            __shared__ int s_redo[G::NW];
+            redo = redo || !pw.sane;
             if (alive) {
                 bool far = false;
 #pragma unroll
@@ -686,13 +878,10 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(Att
                     w[nb].l = 0.f;
                 }
                 pw.start(a.c, b, c0, c1 - 1, lane);
-#pragma unroll
-                for (int t = 0; t < G::AHEAD; ++t)
-                    if (t < nt) issue(t);
+                if constexpr (!G::kBf) load_q();
+                issue_first();
                 careful();
             }
-        } else {
-            careful();
         }
         if constexpr (WIDE) {   // what one wave took out, all see to
             __shared__ int s_odd[G::NW];

@@ -414,6 +414,41 @@ def test_attend_large_logits(cache, dtype):
     check_attend(cache, pool, normal(15, (1, 4, 64), dtype, 6.0), [1], True, scale=0.5)
 
 
+@pytest.mark.parametrize("ks,qs,vs", [(1, 1, 1e-30), (1, 1, 1e-36), (1, 1, 1e35), (1e30, 1e-30, 1), (1e-30, 1e30, 1e-33),
+                                      (1e35, 1e-35, 1), (1e-36, 1e36, 1), (3, 3, 1)])
+def test_attend_fp32_ranges(cache, ks, qs, vs):
+    """fp32 operands far from 1 and of unequal size keep their bits, in chunks (whose products are
+    made of bf16 parts where those hold them) as in single tokens."""
+    log("attend fp32 ranges k=%g q=%g v=%g" % (ks, qs, vs))
+    pool = Pool(cache, [333, 200], 1, 32, F32, seed=41, std=ks, vstd=vs)
+    check_attend(cache, pool, normal(42, (333, 1, 64), F32, qs), [200, 133], True)
+    check_attend(cache, pool, normal(43, (2, 1, 64), F32, qs), [1, 1], True)
+
+
+def test_attend_fp32_small_parts(cache):
+    """One feature whose key is far below the others and whose query makes up for it; values that are 0
+    but for slots of vanishing probability; large values at such slots."""
+    log("attend fp32 small parts")
+    pool = Pool(cache, [300], 1, 32, F32, seed=44)
+    k, v = pool.k[0].clone(), pool.v[0].clone()
+    k[:, 0, 7] *= 2.0 ** -112
+    pool.put(0, k, v)
+    Q = normal(45, (100, 1, 64), F32)
+    Q[:, 0, 7] *= 2.0 ** 113
+    check_attend(cache, pool, Q, [100], False)
+    k = normal(46, (300, 1, 64), F32)
+    k[100:200] *= 0.01
+    k[:, 0, 0] = 0
+    k[100:200, 0, 0] = -8 * 78.0        # logits 78 below the others for queries of 1
+    Q = normal(47, (100, 1, 64), F32)
+    Q[:, 0, 0] = 1
+    for big in (1.0, 1e30):
+        v = torch.zeros(300, 1, 64)
+        v[100:200] = normal(48, (100, 1, 64), F32) * big
+        pool.put(0, k, v)
+        check_attend(cache, pool, Q, [100], False)
+
+
 def test_attend_strided_queries_streams_and_bounds(cache):
     """Queries as a slice of a projection's output; a stream of its own; bounds above the sizes."""
     log("attend strides, streams, bounds")
