@@ -248,7 +248,7 @@ def check_attend(cache, pool, Q, qs, causal, scale=0.0, weights=True, slack=0, w
     t = 0
     for b, m in enumerate(qs):
         n = pool.lens[b]
-        p_, s_ = pool.at(b, n)
+        p_, s_ = (x.numpy() for x in pool.at(b, n))
         vis = np.clip(n - m + np.arange(m) + 1, 0, n) if causal else np.full(m, n)
         for h in range(Hq):
             if m == 0:
@@ -804,3 +804,36 @@ def test_stream_layer(cache, dtype, causal, Hq, Hkv):
                     w = float(Wn[p, h, s][j])
                     assert abs(w - old[x][0]) <= 1e-4 * abs(old[x][0]) + 1e-6
             lens[b] = left[b]
+
+
+def test_stream_example(cache):
+    """examples/stream_views.py: three small views through a block; the attention of every view
+    against 64 bits over all views' keys and values, formed by the block's own first stage."""
+    log("stream example")
+    import importlib.util
+    import os
+    from paper_2609_23733_amd import synth
+    at = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "stream_views.py")
+    spec = importlib.util.spec_from_file_location("stream_views", at)
+    ex = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(ex)
+    P = 150
+    outs = ex.main(3, 10 * P, P)
+    w = {k: v.cuda() for k, v in synth.make_block_weights((1, 0)).items()}
+    pos = torch.from_numpy(synth.token_positions(1, P)).cuda()
+    ws = torch.empty(vp.block_workspace_bytes(1, P), dtype=torch.uint8, device="cuda")
+    ks, vs = [], []
+    for v in range(3):
+        X = synth.make_block_input(1, P, (1, v), device="cuda")
+        Q, K, V = (t.cpu() for t in vp.block_qkv(X, pos, w, 1, P, ws))
+        ks.append(K), vs.append(V)
+        K, V = torch.cat(ks), torch.cat(vs)
+        Y = torch.empty(P, 16, 64, dtype=BF)
+        for h in range(16):
+            ro = attend64(Q[:, h], K[:, h], V[:, h], np.full(P, K.shape[0]))[0]
+            Y[:, h] = torch.from_numpy(ro).to(BF)
+        ref = vp.block_out(X, Y.cuda(), w, 1, P, ws).float()
+        err = (outs[v].float() - ref).abs().max().item()
+        # Y's two roundings (at most 2^-7 of its largest entry, most of it random) through W_O, LayerScale
+        # (at most 1.5), LN_2 and the FFN: a few 2^-7 of the output's largest entry, 2^-5 as the bar
+        assert err <= 2.0 ** -5 * ref.abs().max().item(), (v, err)
