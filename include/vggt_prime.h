@@ -466,7 +466,7 @@ vp_status vp_cache_append(const vp_cache *cache, const vp_cache_batch *batch, in
 
 /* Attend: row (t, h) sees the first `length` slots of its sequence, with `causal`
  * the first length - n + i + 1 (token i of n in the chunk).  With x_j = scale q . k_j
- * (1/8 when 0; positive), O = sum_j e^(x_j - lse) v_j [T, Hq, 64] in the cache's dtype and
+ * (1/8 when 0; 2^-100 to 2^100), O = sum_j e^(x_j - lse) v_j [T, Hq, 64] in the cache's dtype and
  * lse = log sum_j e^x_j [T, Hq] fp32.  A row that sees no slot, or only
  * logits of -inf, gives zeros and -inf; slots a row does not see never reach it,
  * whatever they hold.  With weight_out (fp32, laid out as cache->weight, which may be

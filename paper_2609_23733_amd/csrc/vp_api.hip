@@ -993,7 +993,8 @@ vp_status vp_cache_attend(const vp_cache* cache, const vp_cache_batch* batch, in
     vp::AttendArgs a;
     vp_status st = attend_args(cache, batch, Hq, &a);
     if (st != VP_OK) return st;
-    if (!isfinite(scale) || scale < 0.f) return VP_ERR_INVALID_ARG;
+    // (the weights' offsets are lse / scale, the logits' factor scale log2 e: both in fp32's range)
+    if (!(scale == 0.f || (scale >= 0x1p-100f && scale <= 0x1p100f))) return VP_ERR_INVALID_ARG;
     if (weight_out && (!cache->weight || !aligned4(weight_out))) return VP_ERR_INVALID_ARG;
     if (!ws || ((uintptr_t)ws & (kAlign - 1))) return VP_ERR_INVALID_ARG;
     if (ws_bytes < attend_ws(a)) return VP_ERR_WORKSPACE;

@@ -83,7 +83,8 @@ def test_bad_attend(lib):
     c, b = cache(), batch()
     for kw, code in [(dict(Hq=6), 1), (dict(Hq=0), 1), (dict(Hq=2), 1), (dict(Hq=132), 2), (dict(Q=None), 1),
                      (dict(Q=FAKE_ODD), 1), (dict(qs=504), 1), (dict(qs=516), 1), (dict(scale=-1.0), 1),
-                     (dict(scale=math.inf), 1), (dict(scale=math.nan), 1), (dict(O=None), 1), (dict(O=FAKE_ODD), 1),
+                     (dict(scale=math.inf), 1), (dict(scale=math.nan), 1),
+                     (dict(scale=2.0 ** -101), 1), (dict(scale=2.0 ** 101), 1), (dict(O=None), 1), (dict(O=FAKE_ODD), 1),
                      (dict(lse=None), 1), (dict(wo=FAKE_ODD), 1), (dict(ws=None), 1), (dict(ws=FAKE + 16), 1),
                      (dict(n=0), 3)]:
         assert attend(lib, c, b, **kw) == code, kw
