@@ -1154,16 +1154,18 @@ __global__ __launch_bounds__(256) void k_cache_weight_rows(AttendArgs a) {
 // Chunks: logits formed again.  64 slots per workgroup: keys stay in registers as the MFMA's B
 // operand (a lane owns one slot), two waves for each 32 slots that take half a tile's rows each.
 // The rows stream through LDS as A with -lse in the accumulator's input (`off`, written with lse), so
-// that a result is the exponent itself.  The products of 32 rows are formed while the exponentials
-// of the 32 before are summed.
+// that a result is the exponent itself.  Bound by the vector units (a product, a power and a sum
+// per logit: 1,374 tokens over 20,000 slots of 16 heads some 105 us).  Two tiles of 128 rows in LDS
+// let four workgroups share a compute unit; their waves fill each other's waits, and forming the products of
+// one block amid another's powers, or six workgroups with half the rows, gained nothing.
 // ------------------------------------------------------------------------
 template <typename T>
-__global__ __launch_bounds__(256, 3) void k_cache_weight(AttendArgs a) {
+__global__ __launch_bounds__(256, 4) void k_cache_weight(AttendArgs a) {
     constexpr bool kBf = sizeof(T) == 2;
     constexpr int kStep = kBf ? 128 : 64, RB = kStep / 64;    // rows per tile, 32-row blocks of a wave
     constexpr int ROWB = kD * sizeof(T), RPC = 1024 / ROWB;   // bytes per row, rows per copy
     constexpr int kTile = kStep * ROWB + kStep * 4;           // rows, then their offsets
-    constexpr int NST = 3, AHEAD = NST - 1, NC = kStep / RPC / 4, CPT = NC + 1;
+    constexpr int NST = 2, AHEAD = NST - 1, NC = kStep / RPC / 4, CPT = NC + 1;
     __shared__ __attribute__((aligned(1024))) char smem[NST * kTile];
     const int tid = threadIdx.x, lane = tid & 63, l31 = lane & 31, hh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -1178,53 +1180,62 @@ __global__ __launch_bounds__(256, 3) void k_cache_weight(AttendArgs a) {
     first &= ~(kStep - 1);
     const int nt = (nrows - first + kStep - 1) / kStep;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)smem;
-    // Rows r = i G + g that this lane copies, stepped along with the tiles (a division each costs
-    // more than the rest of a copy).
-    struct Row {
-        int i, g;
-        __device__ __forceinline__ void next(int di, int dg, int G) {
-            i += di;
-            g += dg;
-            if (g >= G) g -= G, ++i;
-        }
-    };
+    // Row r = i G + g lies at i (tokens' distance) + g (heads' distance).  Offsets count from the first
+    // row's token of their tile and are stepped along with the tiles, di tokens and dg heads at a time
+    // (nothing moves where G divides the tile; a division and a product per copy took as many
+    // vector instructions as the exponentials: 67 us -> 61 us for 1,031 tokens of two heads each over
+    // 10,992 slots).
     const int di = kStep / a.G, dg = kStep - di * a.G;
-    Row base, last, row[NC + 1];
-    auto row_of = [&](int r) {
-        Row x;
-        x.i = r / a.G;
-        x.g = r - x.i * a.G;
-        return x;
-    };
-    base = row_of(first);
-    last = row_of(nrows - 1);
+    const int last_i = (nrows - 1) / a.G, last_g = nrows - 1 - last_i * a.G;
+    int base_i = first / a.G, base_g = first - base_i * a.G;
+    const uint32_t qs = (uint32_t)a.q_stride * sizeof(T), hs = ROWB;   // bytes
+    const uint32_t os = (uint32_t)a.Hq * 4;
     const int off_row = (wave * 64) % kStep;   // (the offsets' copies: one a wave)
+    uint32_t off[NC + 1];   // per copy: row, and for Q the lane's 16 bytes of it
+    int g[NC + 1];
+    // pieces of 16 bytes exchanged within their row so that reads meet no bank twice
+    auto piece = [&](int j) {
+        const int rr = (wave * NC + j) * RPC + lane / (64 / RPC), pc = lane % (64 / RPC);
+        return (uint32_t)(pc ^ (kBf ? (rr >> 1) & 7 : rr & 15)) << 4;
+    };
 #pragma unroll
-    for (int j = 0; j < NC; ++j) row[j] = row_of(first + (wave * NC + j) * RPC + lane / (64 / RPC));
-    row[NC] = row_of(first + off_row + lane);
+    for (int j = 0; j <= NC; ++j) {
+        const int r = first + (j < NC ? (wave * NC + j) * RPC + lane / (64 / RPC) : off_row + lane), i = r / a.G;
+        g[j] = r - i * a.G;
+        off[j] = j < NC ? (uint32_t)(i - base_i) * qs + g[j] * hs + piece(j) : (uint32_t)(i - base_i) * os + g[j] * 4;
+    }
     auto issue = [&](int t) {
         const uint32_t stage = lds0 + (t % NST) * kTile;
-        const char* q0 = (const char*)((const T*)a.Q + (int64_t)(sq.q0 + base.i) * a.q_stride + hk * a.G * kD);
-        const uint32_t qs = (uint32_t)a.q_stride;
-        const uint32_t lim = ((uint32_t)(last.i - base.i) * qs + last.g * kD) * sizeof(T);
-        const bool tail = last.i - base.i <= di + 1;   // rows past the last one: the last again
+        const char* q0 = (const char*)((const T*)a.Q + (int64_t)(sq.q0 + base_i) * a.q_stride + hk * a.G * kD);
+        const char* o0 = (const char*)(a.off + (int64_t)(sq.q0 + base_i) * a.Hq + hk * a.G);
+        const int ahead = last_i - base_i;
+        uint32_t v[NC + 1];
 #pragma unroll
-        for (int j = 0; j < NC; ++j) {
-            // pieces of 16 bytes exchanged within their row so that reads meet no bank twice
-            const int c = wave * NC + j, rr = c * RPC + lane / (64 / RPC), pc = lane % (64 / RPC);
-            const int f = kBf ? (rr >> 1) & 7 : rr & 15;
-            uint32_t at = ((uint32_t)(row[j].i - base.i) * qs + row[j].g * kD) * sizeof(T);
-            if (tail) at = at < lim ? at : lim;
-            copy_to_lds(stage + c * 1024, q0, at + ((pc ^ f) << 4));
-            row[j].next(di, dg, a.G);
+        for (int j = 0; j <= NC; ++j) v[j] = off[j];
+        if (ahead <= di + 1) {   // rows past the last one: the last again
+            const uint32_t lim = (uint32_t)ahead * qs + last_g * hs, olim = (uint32_t)ahead * os + last_g * 4;
+#pragma unroll
+            for (int j = 0; j < NC; ++j) v[j] = min(v[j] - piece(j), lim) + piece(j);
+            v[NC] = min(v[NC], olim);
         }
-        uint32_t at = ((uint32_t)(row[NC].i - base.i) * a.Hq + row[NC].g) * 4;
-        const uint32_t olim = ((uint32_t)(last.i - base.i) * a.Hq + last.g) * 4;
-        if (tail) at = at < olim ? at : olim;
-        copy4_to_lds(stage + kStep * ROWB + off_row * 4,
-                     (const char*)(a.off + (int64_t)(sq.q0 + base.i) * a.Hq + hk * a.G), at);
-        row[NC].next(di, dg, a.G);
-        base.next(di, dg, a.G);
+#pragma unroll
+        for (int j = 0; j < NC; ++j) copy_to_lds(stage + (wave * NC + j) * 1024, q0, v[j]);
+        copy4_to_lds(stage + kStep * ROWB + off_row * 4, o0, v[NC]);
+        base_i += di;
+        if (dg == 0) return;
+        base_g += dg;
+        const bool over = base_g >= a.G;
+        if (over) base_g -= a.G, ++base_i;
+#pragma unroll
+        for (int j = 0; j <= NC; ++j) {
+            const uint32_t row = j < NC ? qs : os, head = j < NC ? hs : 4;
+            g[j] += dg;
+            off[j] += dg * head - (over ? row : 0);
+            if (g[j] >= a.G) {
+                g[j] -= a.G;
+                off[j] += row - a.G * head;
+            }
+        }
     };
 #pragma unroll
     for (int t = 0; t < AHEAD; ++t)
@@ -1255,13 +1266,6 @@ __global__ __launch_bounds__(256, 3) void k_cache_weight(AttendArgs a) {
     // first row that sees this lane's slot (token i sees slots up to len - n + i)
     const int row_min = a.causal && slot > sq.len - sq.n ? (slot - (sq.len - sq.n)) * a.G : 0;
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
-    f32x16 s[2];   // exponents over c2 of the 32 rows before and of these
-#pragma unroll
-    for (int r = 0; r < 16; ++r) s[0][r] = s[1][r] = -INFINITY;
-    auto add = [&](const f32x16& x) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) sum[r & 3] += exp2f_fast(x[r] * a.c2);
-    };
     const int half = wave >> 1;
     for (int t = 0; t < nt; ++t) {
         const int more = nt - 1 - t, r0 = first + t * kStep;
@@ -1272,14 +1276,11 @@ __global__ __launch_bounds__(256, 3) void k_cache_weight(AttendArgs a) {
         // slots that row r0 sees all rows of the tile see
         const bool mask = (a.causal && k0 + 64 > cache_visible(sq, 1, r0 / a.G)) || r0 + kStep > nrows;
 #pragma unroll
-        for (int rb = 0; rb < 2; ++rb) {
-            if (rb >= RB) break;
+        for (int rb = 0; rb < RB; ++rb) {
             typedef __attribute__((address_space(3))) const f32x4 lds_f32x4;
             typedef __attribute__((address_space(3))) const bf16x8 lds_bf16x8;
             const int br = 32 * (RB * half + rb);   // first row of the block
-            f32x16& x = s[rb];
-            f32x16 done;
-            if constexpr (RB == 1) done = s[0];
+            f32x16 x;
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const f32x4 v = *(lds_f32x4*)(tile + kStep * ROWB + (br + 8 * g + 4 * hh) * 4);
@@ -1288,28 +1289,15 @@ __global__ __launch_bounds__(256, 3) void k_cache_weight(AttendArgs a) {
             }
             lds_char* qr = tile + (br + l31) * ROWB;
             const int f = kBf ? (l31 >> 1) & 7 : l31 & 15;
-            // an MFMA's time holds the vector instructions of four (fp32: two) of the 16 exponentials
-            const f32x16& y = RB == 1 ? done : s[rb ^ 1];
-            constexpr int kParts = kBf ? 4 : 8, kEach = 16 / kParts;
-            bf16x8 qb[kBf ? 4 : 1];
-            if constexpr (kBf)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) qb[i] = *(lds_bf16x8*)(qr + (((2 * i + hh) ^ f) << 4));
-#pragma unroll
-            for (int i = 0; i < kParts; ++i) {
+            for (int i = 0; i < (kBf ? 4 : 8); ++i) {
                 if constexpr (kBf) {
-                    x = mfma_bf16(qb[i], kb[i], x);
+                    x = mfma_bf16(*(lds_bf16x8*)(qr + (((2 * i + hh) ^ f) << 4)), kb[i], x);
                 } else {
                     const f32x4 q = *(lds_f32x4*)(qr + (((2 * i + hh) ^ f) << 4));
 #pragma unroll
                     for (int e = 0; e < 4; ++e) x = mfma_f32(q[e], kf[4 * i + e], x);
                 }
-                float z[kEach];
-#pragma unroll
-                for (int e = 0; e < kEach; ++e) z[e] = exp2f_fast(y[kEach * i + e] * a.c2);
-#pragma unroll
-                for (int e = 0; e < kEach; ++e) sum[(kEach * i + e) & 3] += z[e];
-                if (kBf) __builtin_amdgcn_sched_barrier(0);
             }
             if (mask) {
 #pragma unroll
@@ -1318,9 +1306,10 @@ __global__ __launch_bounds__(256, 3) void k_cache_weight(AttendArgs a) {
                     x[r] = rr >= row_min && rr < nrows ? x[r] : -INFINITY;
                 }
             }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sum[r & 3] += exp2f_fast(x[r] * a.c2);
         }
     }
-    add(s[RB - 1]);
     float t = (sum[0] + sum[1]) + (sum[2] + sum[3]);
     t += __shfl_xor(t, 32);
     // the two halves of the rows
