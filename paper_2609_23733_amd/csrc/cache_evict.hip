@@ -26,7 +26,8 @@ struct EvictWs {
     int32_t *count;     // [B * Hkv, chunks, 2]: above, ties
     int32_t *hole, *mover;   // [B * Hkv, cap]
     int32_t *kbn, *left;     // [B * Hkv]: kept slots below n; n
-    uint32_t* bound;         // [B * Hkv, 2]: the n-th largest key, its ties that are kept
+    uint32_t* bound;         // [B * Hkv, 4]: after pass 1 the top digit and what is wanted of it; then (2, 3)
+                             // two digits; then (0, 1) the n-th largest key, its ties that are kept
     int cap, chunks;
 };
 
@@ -51,7 +52,7 @@ static EvictWs evict_layout(int B, int Hkv, int max_len, void* ws, size_t* total
     w.mover = (int32_t*)take(bh * w.cap * 4);
     w.kbn = (int32_t*)take(bh * 4);
     w.left = (int32_t*)take(bh * 4);
-    w.bound = (uint32_t*)take(bh * 8);
+    w.bound = (uint32_t*)take(bh * 16);
     if (total) *total = off;
     return w;
 }
@@ -176,14 +177,17 @@ __global__ __launch_bounds__(256) void k_evict_digit(EvictArgs a, EvictWs w) {
     }
     for (int i = threadIdx.x; i < kEvBins; i += 256) bins[i] = 0;
     uint32_t prefix = 0;
-    int need = n, d;
-    if (PASS >= 1) {
-        find_digit(hist, 2048, need, &d, &need, tmp);
+    int need, d;
+    uint32_t* bound = w.bound + 4 * (int64_t)bh;
+    if (PASS == 1) {
+        find_digit(hist, 2048, n, &d, &need, tmp);
         prefix = d;
+        if (blockIdx.x == 0 && threadIdx.x == 0) bound[0] = prefix, bound[1] = need;
     }
-    if (PASS >= 2) {
-        find_digit(hist + kEvBins, 2048, need, &d, &need, tmp);
-        prefix = prefix << 11 | d;
+    if (PASS == 2) {
+        find_digit(hist + kEvBins, 2048, (int)bound[1], &d, &need, tmp);
+        prefix = bound[0] << 11 | d;
+        if (blockIdx.x == 0 && threadIdx.x == 0) bound[2] = prefix, bound[3] = need;
     }
     __syncthreads();
 #pragma unroll
@@ -201,19 +205,6 @@ __global__ __launch_bounds__(256) void k_evict_digit(EvictArgs a, EvictWs w) {
         if (bins[i]) atomicAdd(hist + PASS * kEvBins + i, bins[i]);
 }
 
-// The n-th largest key and the number of its ties that are kept.
-__device__ __forceinline__ uint32_t evict_bound(const int32_t* hist, int n, int* ties, int* tmp) {
-    int d, need = n;
-    uint32_t k;
-    find_digit(hist, 2048, need, &d, &need, tmp);
-    k = d;
-    find_digit(hist + kEvBins, 2048, need, &d, &need, tmp);
-    k = k << 11 | d;
-    find_digit(hist + 2 * kEvBins, 1024, need, &d, &need, tmp);
-    *ties = need;
-    return k << 10 | d;
-}
-
 // Per chunk: slots above the bound, and ties.
 __global__ __launch_bounds__(256) void k_evict_count(EvictArgs a, EvictWs w) {
     const int bh = blockIdx.y, b = bh / a.c.Hkv;
@@ -221,8 +212,11 @@ __global__ __launch_bounds__(256) void k_evict_count(EvictArgs a, EvictWs w) {
     const int s0 = blockIdx.x * kEvChunk, s1 = s0 + kEvChunk < len ? s0 + kEvChunk : len;
     if (s0 >= len || n == len) return;
     __shared__ int tmp[16];
-    int ties;
-    const uint32_t bound = evict_bound(w.hist + (int64_t)bh * 3 * kEvBins, n, &ties, tmp);
+    // the n-th largest key and the number of its ties that are kept
+    int ties, d;
+    const uint32_t* two = w.bound + 4 * (int64_t)bh + 2;
+    find_digit(w.hist + ((int64_t)bh * 3 + 2) * kEvBins, 1024, (int)two[1], &d, &ties, tmp);
+    const uint32_t bound = two[0] << 10 | d;
     const uint32_t* key = w.key + (int64_t)bh * w.cap;
     int above = 0, tie = 0;
 #pragma unroll 4
@@ -245,7 +239,7 @@ __global__ __launch_bounds__(256) void k_evict_count(EvictArgs a, EvictWs w) {
         int32_t* c = w.count + ((int64_t)bh * w.chunks + blockIdx.x) * 2;
         c[0] = tmp[0] + tmp[1] + tmp[2] + tmp[3];
         c[1] = tmp[4] + tmp[5] + tmp[6] + tmp[7];
-        if (blockIdx.x == 0) w.bound[2 * bh] = bound, w.bound[2 * bh + 1] = ties;
+        if (blockIdx.x == 0) w.bound[4 * (int64_t)bh] = bound, w.bound[4 * (int64_t)bh + 1] = ties;
     }
 }
 
@@ -253,22 +247,36 @@ __global__ __launch_bounds__(256) void k_evict_count(EvictArgs a, EvictWs w) {
 __device__ __forceinline__ void copy_kept(const EvictArgs& a, int b, int hk, int s0, int e1) {
     typedef int32_t i32x4 __attribute__((__vector_size__(16), aligned(4)));
     typedef float f32x4u __attribute__((__vector_size__(16), aligned(4)));
-    for (int s = s0 + threadIdx.x * 4; s < e1; s += blockDim.x * 4) {
-        const int64_t at = slot_at(a.c, b, hk, s);
-        if (at < 0) continue;
-        const f32x4u w = *(const f32x4u*)(a.c.weight + at);
-        const i32x4 t = *(const i32x4*)(a.c.stamp + at);
-        if (s + 4 <= e1) {
-            *(f32x4u*)(a.weight_out + at) = w;
-            *(i32x4*)(a.stamp_out + at) = t;
-            continue;
+    constexpr int kAtOnce = 4;   // the loads of four steps are issued before the first is used
+    const int step = blockDim.x * 4;
+    for (int first = s0 + threadIdx.x * 4; first < e1; first += kAtOnce * step) {
+        int64_t at[kAtOnce];
+        f32x4u w[kAtOnce];
+        i32x4 t[kAtOnce];
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) at[j] = first + j * step < e1 ? slot_at(a.c, b, hk, first + j * step) : -1;
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) {
+            const int64_t p = at[j] >= 0 ? at[j] : 0;
+            w[j] = *(const f32x4u*)(a.c.weight + p);
+            t[j] = *(const i32x4*)(a.c.stamp + p);
         }
 #pragma unroll
-        for (int e = 0; e < 3; ++e)
-            if (s + e < e1) {
-                a.weight_out[at + e] = w[e];
-                a.stamp_out[at + e] = t[e];
+        for (int j = 0; j < kAtOnce; ++j) {
+            if (at[j] < 0) continue;
+            const int left = e1 - (first + j * step);
+            if (left >= 4) {
+                *(f32x4u*)(a.weight_out + at[j]) = w[j];
+                *(i32x4*)(a.stamp_out + at[j]) = t[j];
+                continue;
             }
+#pragma unroll
+            for (int e = 0; e < 3; ++e)
+                if (e < left) {
+                    a.weight_out[at[j] + e] = w[j][e];
+                    a.stamp_out[at[j] + e] = t[j][e];
+                }
+        }
     }
 }
 
@@ -286,8 +294,8 @@ __global__ __launch_bounds__(256) void k_evict_lists(EvictArgs a, EvictWs w) {
     if (n < len) {
         __shared__ int tmp[16];
         const int t = threadIdx.x, lane = t & 63, wv = t >> 6;
-        const uint32_t bound = w.bound[2 * bh];
-        const int ties = (int)w.bound[2 * bh + 1];
+        const uint32_t bound = w.bound[4 * (int64_t)bh];
+        const int ties = (int)w.bound[4 * (int64_t)bh + 1];
         const uint32_t* key = w.key + (int64_t)bh * w.cap;
         // counts of the chunks before
         int above = 0, tie = 0;
