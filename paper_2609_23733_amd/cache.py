@@ -301,15 +301,16 @@ class StreamLayer:
             start.append(start[-1] + c)
         q_start = torch.tensor(start, dtype=torch.int32).to(Q.device)
         new = q_start[1:] - q_start[:-1]
-        self.length += new
-        self.seen += new
-        self.lens = [n + c for n, c in zip(self.lens, counts)]
-        batch = Batch(self.table, self.length, q_start, max(counts), max(self.lens), self.seen)
+        # (the layer's own counts change once the chunk is in: a refused one leaves it as it was)
+        length, seen = self.length + new, self.seen + new
+        lens = [n + c for n, c in zip(self.lens, counts)]
+        batch = Batch(self.table, length, q_start, max(counts), max(lens), seen)
         Q = append(self.pc, batch, Q, K, V, pos, self.rot)
         n = load_library().vp_cache_attend_workspace_bytes(self.pc._ref, batch._for(T), self.Hq)
         if self.attend_ws is None or self.attend_ws.numel() < n:
             self.attend_ws = torch.empty(n, dtype=torch.uint8, device=Q.device)
         O, _ = attend(self.pc, batch, Q, self.causal, weight_out=self.pc.weight, ws=self.attend_ws)
+        self.length, self.seen, self.lens = length, seen, lens
         if max(self.lens) > self.keep:
             evict(self.pc, self.table, self.length, self.seen, self.keep, max(self.lens), self.sink,
                   self.recent, ws=self.ws)

@@ -837,3 +837,40 @@ def test_stream_example(cache):
         # Y's two roundings (at most 2^-7 of its largest entry, most of it random) through W_O, LayerScale
         # (at most 1.5), LN_2 and the FFN: a few 2^-7 of the output's largest entry, 2^-5 as the bar
         assert err <= 2.0 ** -5 * ref.abs().max().item(), (v, err)
+
+
+def test_stream_layer_refused_chunk(cache):
+    """A chunk that is refused leaves the layer as it was: the steps after it equal those of a
+    layer that never saw it."""
+    log("stream layer refused chunk")
+    rot = cache.Rotary.make(64, 10000.0)
+    a, b = (cache.StreamLayer(1, keep=60, max_chunk=40, Hq=4, Hkv=2, page=16, rot=rot) for _ in range(2))
+    pos = torch.arange(40, dtype=torch.int32, device="cuda")[:, None]
+    for step in range(3):
+        Q, K, V = (normal(950 + 3 * step + i, (40, h, 64)).cuda() for i, h in enumerate((4, 2, 2)))
+        for bad in (dict(K=K[:, :1]), dict(V=V.float()), dict(pos=None), dict(pos=pos[:39]), dict(Q=Q[:, :3]), dict(counts=[41])):
+            kw = dict(dict(Q=Q, K=K, V=V, pos=pos, counts=[40]), **bad)
+            with pytest.raises((ValueError, vp.VPError)):
+                a.step(**kw)
+        assert torch.equal(a.step(Q, K, V, pos), b.step(Q, K, V, pos))
+        assert a.lens == b.lens and a.length.tolist() == b.length.tolist() == a.lens
+        assert a.seen.tolist() == [40 * (step + 1)]
+
+
+@pytest.mark.parametrize("G,q,dtype", [(3, 70, BF), (5, 41, BF), (7, 19, F32), (48, 5, BF), (65, 3, F32), (128, 2, BF), (2, 300, F32), (3, 5, BF)])
+def test_attend_weights_any_group(cache, G, q, dtype):
+    """Weights of chunks whose groups do not divide the tiles of rows: heads and tokens step together."""
+    log("attend weights G=%d q=%d %s" % (G, q, dtype))
+    lens, qs = [q + 130, q + 3], [q, max(1, q // 2)]
+    pool = Pool(cache, lens, 1, 16, dtype, seed=G)
+    check_attend(cache, pool, normal(G + 1, (sum(qs), G, 64), dtype), qs, True)
+
+
+@pytest.mark.parametrize("B,q", [(9, 1), (17, 3), (5, 90)])
+def test_attend_ragged_batches(cache, B, q):
+    """Many sequences, one long, most short, some idle: ranges past a sequence's end."""
+    log("attend ragged B=%d q=%d" % (B, q))
+    lens = [2000] + [q + 37 * b for b in range(1, B)]
+    qs = [q] + [(0 if b % 4 == 3 else max(1, q - b)) for b in range(1, B)]
+    pool = Pool(cache, lens, 2, 16, BF, seed=B)
+    check_attend(cache, pool, normal(B + 1, (sum(qs), 6, 64), BF), qs, True)
