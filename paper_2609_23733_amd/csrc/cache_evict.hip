@@ -243,28 +243,55 @@ __global__ __launch_bounds__(256) void k_evict_count(EvictArgs a, EvictWs w) {
     }
 }
 
-// Weights and stamps of slots [s0, e1) as they are, for output arrays of their own.
-__device__ __forceinline__ void copy_kept(const EvictArgs& a, int b, int hk, int s0, int e1) {
+// Lists of holes and movers, 64 slots at a time, one per lane of a wave: the entries of a step lie side
+// by side (a thread with a run of slots of its own scatters them).
+__device__ __forceinline__ int lanes_before(uint64_t mask) {
+    return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+}
+__device__ __forceinline__ void count_step(uint32_t k, bool in, uint32_t bound, int* above, int* tie) {
+    *above += __popcll(__builtin_amdgcn_ballot_w64(in && k > bound));
+    *tie += __popcll(__builtin_amdgcn_ballot_w64(in && k == bound));
+}
+// `above`, `tie`: slots above the bound and ties before the step's.
+__device__ __forceinline__ void list_step(uint32_t k, int s, bool in, int n, uint32_t bound, int ties, int* above, int* tie,
+                                          int32_t* hole, int32_t* mover, int32_t* kbn) {
+    const bool up = in && k > bound, eq = in && k == bound;
+    const uint64_t mu = __builtin_amdgcn_ballot_w64(up), me = __builtin_amdgcn_ballot_w64(eq);
+    const int before = *tie + lanes_before(me), kb = *above + lanes_before(mu) + (before < ties ? before : ties);
+    const bool kept = up || (eq && before < ties);
+    if (in) {
+        if (s == n) *kbn = kb;
+        if (s < n && !kept) hole[s - kb] = s;
+        if (s >= n && kept) mover[kb] = s;
+    }
+    *above += __popcll(mu);
+    *tie += __popcll(me);
+}
+
+// Weights and stamps of slots s0 + 4 t, s0 + 4 (t + step), .. below e1 of thread t, four loads at once, as
+// they are, for output arrays of their own.
+struct KeptCopy {
     typedef int32_t i32x4 __attribute__((__vector_size__(16), aligned(4)));
     typedef float f32x4u __attribute__((__vector_size__(16), aligned(4)));
-    constexpr int kAtOnce = 4;   // the loads of four steps are issued before the first is used
-    const int step = blockDim.x * 4;
-    for (int first = s0 + threadIdx.x * 4; first < e1; first += kAtOnce * step) {
-        int64_t at[kAtOnce];
-        f32x4u w[kAtOnce];
-        i32x4 t[kAtOnce];
+    static constexpr int kAtOnce = 4;
+    int64_t at[kAtOnce];
+    f32x4u w[kAtOnce];
+    i32x4 t[kAtOnce];
+    __device__ __forceinline__ void load(const EvictArgs& a, int b, int hk, int s, int step, int e1) {
 #pragma unroll
-        for (int j = 0; j < kAtOnce; ++j) at[j] = first + j * step < e1 ? slot_at(a.c, b, hk, first + j * step) : -1;
+        for (int j = 0; j < kAtOnce; ++j) at[j] = s + j * step < e1 ? slot_at(a.c, b, hk, s + j * step) : -1;
 #pragma unroll
         for (int j = 0; j < kAtOnce; ++j) {
             const int64_t p = at[j] >= 0 ? at[j] : 0;
             w[j] = *(const f32x4u*)(a.c.weight + p);
             t[j] = *(const i32x4*)(a.c.stamp + p);
         }
+    }
+    __device__ __forceinline__ void store(const EvictArgs& a, int s, int step, int e1) const {
 #pragma unroll
         for (int j = 0; j < kAtOnce; ++j) {
             if (at[j] < 0) continue;
-            const int left = e1 - (first + j * step);
+            const int left = e1 - (s + j * step);
             if (left >= 4) {
                 *(f32x4u*)(a.weight_out + at[j]) = w[j];
                 *(i32x4*)(a.stamp_out + at[j]) = t[j];
@@ -278,84 +305,57 @@ __device__ __forceinline__ void copy_kept(const EvictArgs& a, int b, int hk, int
                 }
         }
     }
-}
+};
 
-// The lists of holes and movers, and the weights and stamps of the slots that stay.
+// The lists, and the weights and stamps of the slots that stay.  Everything that does not depend on the
+// counts is loaded first.
 __global__ __launch_bounds__(256) void k_evict_lists(EvictArgs a, EvictWs w) {
     const int bh = blockIdx.y, hk = bh % a.c.Hkv, b = bh / a.c.Hkv;
+    const int t = threadIdx.x, lane = t & 63, wv = __builtin_amdgcn_readfirstlane(t >> 6);
+    constexpr int kRun = kEvChunk / 4, kSteps = kRun / 64;   // slots per wave
+    static_assert(kEvChunk == KeptCopy::kAtOnce * 1024, "a chunk's copies at once");
+    const int s0 = blockIdx.x * kEvChunk, p0 = s0 + wv * kRun;
+    const uint32_t* key = w.key + (int64_t)bh * w.cap;
+    const int32_t* cnt = w.count + (int64_t)bh * w.chunks * 2;
+    uint32_t k[kSteps];   // (cap is whole chunks)
+#pragma unroll
+    for (int j = 0; j < kSteps; ++j) k[j] = key[p0 + 64 * j + lane];
+    const uint32_t bound = w.bound[4 * (int64_t)bh];
+    const int ties = (int)w.bound[4 * (int64_t)bh + 1];
+    int above = 0, tie = 0;   // counts of the chunks before
+    for (int c = lane; c < (int)blockIdx.x; c += 64) above += cnt[2 * c], tie += cnt[2 * c + 1];
     const int len = cache_length(a.c, b), n = len < a.keep ? len : a.keep;
-    const int s0 = blockIdx.x * kEvChunk, s1 = s0 + kEvChunk < len ? s0 + kEvChunk : len;
-    if (blockIdx.x == 0 && threadIdx.x == 0) {
+    const int s1 = s0 + kEvChunk < len ? s0 + kEvChunk : len;
+    if (blockIdx.x == 0 && t == 0) {
         w.left[bh] = n;
         if (n == len) w.kbn[bh] = n;   // nothing moves
     }
     if (s0 >= len) return;
     const bool same = a.weight_out == a.c.weight && a.stamp_out == a.c.stamp;
+    const int e1 = s1 < n ? s1 : n;
+    KeptCopy copy;
+    if (!same && s0 < e1) copy.load(a, b, hk, s0 + t * 4, 1024, e1);
     if (n < len) {
-        __shared__ int tmp[16];
-        const int t = threadIdx.x, lane = t & 63, wv = t >> 6;
-        const uint32_t bound = w.bound[4 * (int64_t)bh];
-        const int ties = (int)w.bound[4 * (int64_t)bh + 1];
-        const uint32_t* key = w.key + (int64_t)bh * w.cap;
-        // counts of the chunks before
-        int above = 0, tie = 0;
-        const int32_t* cnt = w.count + (int64_t)bh * w.chunks * 2;
-        for (int c = t; c < (int)blockIdx.x; c += 256) above += cnt[2 * c], tie += cnt[2 * c + 1];
+        __shared__ int tmp[8];
 #pragma unroll
         for (int o = 32; o >= 1; o >>= 1) {
             above += __shfl_xor(above, o);
             tie += __shfl_xor(tie, o);
         }
-        if (lane == 0) tmp[wv] = above, tmp[4 + wv] = tie;
-        __syncthreads();
-        above = tmp[0] + tmp[1] + tmp[2] + tmp[3];
-        tie = tmp[4] + tmp[5] + tmp[6] + tmp[7];
-        __syncthreads();
-        // sixteen slots in a row per thread
-        constexpr int kPer = kEvChunk / 256;
-        const int p0 = s0 + t * kPer;
-        uint32_t k[kPer];
         int ma = 0, mt = 0;
 #pragma unroll
-        for (int j = 0; j < kPer; j += 4) {
-            u32x4 v = *(const u32x4*)(key + p0 + j);    // (cap is whole chunks)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const bool in = p0 + j + e < s1;
-                k[j + e] = v[e];
-                ma += in && v[e] > bound;
-                mt += in && v[e] == bound;
-            }
-        }
-        int ia = ma, it = mt;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int va = __shfl_up(ia, o), vt = __shfl_up(it, o);
-            if (lane >= o) ia += va, it += vt;
-        }
-        if (lane == 63) tmp[wv] = ia, tmp[4 + wv] = it;
+        for (int j = 0; j < kSteps; ++j) count_step(k[j], p0 + 64 * j + lane < s1, bound, &ma, &mt);
+        if (lane == 0) tmp[wv] = ma, tmp[4 + wv] = mt;
         __syncthreads();
-        above += ia - ma;
-        tie += it - mt;
         for (int v = 0; v < wv; ++v) above += tmp[v], tie += tmp[4 + v];
-        int32_t* hole = w.hole + (int64_t)bh * w.cap;
-        int32_t* mover = w.mover + (int64_t)bh * w.cap;
+        int32_t *hole = w.hole + (int64_t)bh * w.cap, *mover = w.mover + (int64_t)bh * w.cap;
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-            const int s = p0 + j;
-            if (s >= s1) break;
-            const int kb = above + (tie < ties ? tie : ties);
-            const bool up = k[j] > bound, eq = k[j] == bound;
-            const bool kept = up || (eq && tie < ties);
-            above += up;
-            tie += eq;
-            if (s == n) w.kbn[bh] = kb;
-            if (s < n && !kept) hole[s - kb] = s;
-            if (s >= n && kept) mover[kb] = s;
+        for (int j = 0; j < kSteps; ++j) {
+            const int s = p0 + 64 * j + lane;
+            list_step(k[j], s, s < s1, n, bound, ties, &above, &tie, hole, mover, w.kbn + bh);
         }
     }
-    if (same) return;
-    copy_kept(a, b, hk, s0, s1 < n ? s1 : n);
+    if (!same && s0 < e1) copy.store(a, s0 + t * 4, 1024, e1);
 }
 
 // ------------------------------------------------------------------------
@@ -425,7 +425,8 @@ __global__ __launch_bounds__(kEvThreads) void k_evict_small(EvictArgs a, EvictWs
             if (lane == 63) tmp[wv] = inc;
             __syncthreads();
             int before = inc - own0 - own1;
-            for (int v = 0; v < wv; ++v) before += tmp[v];
+#pragma unroll
+            for (int v = 0; v < kEvThreads / 64; ++v) before += v < wv ? tmp[v] : 0;
             if (before < need && before + own0 + own1 >= need) {
                 const bool first = before + own0 >= need;
                 tmp[32] = first ? nb - 1 - 2 * t : nb - 2 - 2 * t;
@@ -436,37 +437,29 @@ __global__ __launch_bounds__(kEvThreads) void k_evict_small(EvictArgs a, EvictWs
             need = tmp[33];
             __syncthreads();
         }
-        // ---- lists: a run of slots in a row per thread
+        // ---- lists: a run of slots per wave
         const uint32_t bound = prefix;
-        const int ties = need, per = (len + kEvThreads - 1) / kEvThreads, p0 = t * per;
-        const int p1 = p0 + per < len ? p0 + per : len;
-        int above = 0, tie = 0;
-        for (int s = p0; s < p1; ++s) above += key[s] > bound, tie += key[s] == bound;
-        int ia = above, it = tie;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int va = __shfl_up(ia, o), vt = __shfl_up(it, o);
-            if (lane >= o) ia += va, it += vt;
-        }
-        if (lane == 63) tmp[wv] = ia, tmp[16 + wv] = it;
+        const int ties = need, per = (len + kEvThreads - 1) / kEvThreads * 64;
+        const int p0 = __builtin_amdgcn_readfirstlane(wv) * per, p1 = p0 + per < len ? p0 + per : len;
+        int ma = 0, mt = 0, above = 0, tie = 0;
+        for (int q = p0; q < p1; q += 64) count_step(key[q + lane], q + lane < p1, bound, &ma, &mt);
+        if (lane == 0) tmp[wv] = ma, tmp[16 + wv] = mt;
         __syncthreads();
-        above = ia - above;
-        tie = it - tie;
-        for (int v = 0; v < wv; ++v) above += tmp[v], tie += tmp[16 + v];
-        int32_t* hole = w.hole + (int64_t)bh * w.cap;
-        int32_t* mover = w.mover + (int64_t)bh * w.cap;
-        for (int s = p0; s < p1; ++s) {
-            const uint32_t k = key[s];
-            const int kb = above + (tie < ties ? tie : ties);
-            const bool kept = k > bound || (k == bound && tie < ties);
-            above += k > bound;
-            tie += k == bound;
-            if (s == n) w.kbn[bh] = kb;
-            if (s < n && !kept) hole[s - kb] = s;
-            if (s >= n && kept) mover[kb] = s;
+#pragma unroll
+        for (int v = 0; v < kEvThreads / 64; ++v) {
+            above += v < wv ? tmp[v] : 0;
+            tie += v < wv ? tmp[16 + v] : 0;
         }
+        int32_t *hole = w.hole + (int64_t)bh * w.cap, *mover = w.mover + (int64_t)bh * w.cap;
+        for (int q = p0; q < p1; q += 64)
+            list_step(key[q + lane], q + lane, q + lane < p1, n, bound, ties, &above, &tie, hole, mover, w.kbn + bh);
     }
-    if (!same) copy_kept(a, b, hk, 0, n);
+    if (!same)
+        for (int s = 0; s < n; s += 4 * KeptCopy::kAtOnce * kEvThreads) {
+            KeptCopy copy;
+            copy.load(a, b, hk, s + t * 4, 4 * kEvThreads, n);
+            copy.store(a, s + t * 4, 4 * kEvThreads, n);
+        }
 }
 
 // The moves: eight threads per move and tensor row.
