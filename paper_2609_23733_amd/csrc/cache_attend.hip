@@ -40,7 +40,8 @@ struct Geo {
     static constexpr int kTile = 2 * TK * ROWB;
     // Tiles in LDS, and how many tiles ahead of the arriving one copies are issued: into the
     // place of the tile before it, or (wide bf16, where that one is still in use) of the one before.
-    static constexpr int NST = WIDE ? (kBf ? 4 : 3) : 2;
+    // Narrow fp32: one tile, whose K and V are replaced in turn.
+    static constexpr int NST = WIDE ? (kBf ? 4 : 3) : kBf ? 2 : 1;
     static constexpr int AHEAD = WIDE && kBf ? NST - 2 : NST - 1;
     static constexpr int kRing = NST * kTile;
     static constexpr int kLds = WIDE ? kRing : 4 * kRing;
@@ -295,11 +296,11 @@ __device__ __forceinline__ f32x16 mfma_planes(const Planes& a, const Planes& b, 
     return mfma_bf16(a.h, b.h, c);
 }
 
-// One block after the other: logits, probabilities, values.
+// A block's logits and probabilities.
 // `logits`: null, or where the row's logits (of slots from 0 on) are kept.
 template <typename T>
-__device__ __forceinline__ void block_attend(Rows<T>& w, lds_char* k, lds_char* v, float c2, int k0,
-                                             bool partial, uint32_t units, int lane, float* logits) {
+__device__ __forceinline__ void block_probs(Rows<T>& w, lds_char* k, float c2, int k0, bool partial, uint32_t units,
+                                            int lane, float* logits, Probs<T>& p) {
     f32x16 s = block_logits<T>(w, k, lane);
     if (partial) block_mask<T>(w, k0, units, lane, s);
     if (logits)
@@ -308,12 +309,10 @@ __device__ __forceinline__ void block_attend(Rows<T>& w, lds_char* k, lds_char* 
             *(f32x4*)(logits + k0 + Geo<T, true>::key(4 * g, lane >> 5)) =
                 f32x4{s[4 * g], s[4 * g + 1], s[4 * g + 2], s[4 * g + 3]};
     float sum = block_exp(s, c2, w.m);   // inf or NaN while m is -inf
-    Probs<T> p;
     p.set(s);
     if (__builtin_amdgcn_ballot_w64(!(sum < kMoveAt)))
         sum = block_move<T>(w, k, c2, k0, partial, units, lane, p);
     w.l += sum;
-    block_values<T>(w, v, p, lane);
 }
 
 // Values of a tile that is seen in part, `rows` slots from slot k of the cache at `v` in LDS, before any
@@ -501,22 +500,25 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(Att
             kv = r * 256 + ((pc ^ r) << 4);
             vv = lane * 16;
         }
+        // 16 slots of a tile: their first one, its page, and the copies of their K or V.
+        auto unit_slot = [&](int t, int unit) {
+            const int slot = c0 + (tfirst + t * tstep) * G::TK + 16 * unit;
+            return slot < last_unit ? slot : last_unit;
+        };
+        auto unit_page = [&](int t, int unit) { return pw.page(unit_slot(t, unit) >> a.c.page_log2, lane); };
+        auto issue_unit = [&](int t, int unit, bool isv, int id) {
+            const int64_t at = ((((int64_t)id * a.c.Hkv + hk) << a.c.page_log2) + (unit_slot(t, unit) & page_mask)) * G::ROWB;
+            const char* src = (const char*)(isv ? a.c.V : a.c.K) + at;
+            const uint32_t dst = lds0 + (t % G::NST) * G::kTile + (isv ? G::TK * G::ROWB : 0) + unit * 16 * G::ROWB;
+#pragma unroll
+            for (int u = 0; u < G::UC; ++u)
+                copy_to_lds(dst + u * 1024, src + u * 1024, isv ? vv : kv ^ (64 * u));
+        };
         auto issue = [&](int t) {
-            const int k0 = c0 + (tfirst + t * tstep) * G::TK;
-            const uint32_t stage = lds0 + (t % G::NST) * G::kTile;
 #pragma unroll
             for (int j = 0; j < G::PPW; ++j) {
                 const int part = WIDE ? wave * G::PPW + j : j, unit = part >> 1;
-                const bool isv = part & 1;
-                int slot = k0 + 16 * unit;
-                slot = slot < last_unit ? slot : last_unit;
-                const int id = pw.page(slot >> a.c.page_log2, lane);
-                const int64_t at = ((((int64_t)id * a.c.Hkv + hk) << a.c.page_log2) + (slot & page_mask)) * G::ROWB;
-                const char* src = (const char*)(isv ? a.c.V : a.c.K) + at;
-                const uint32_t dst = stage + (isv ? G::TK * G::ROWB : 0) + unit * 16 * G::ROWB;
-#pragma unroll
-                for (int u = 0; u < G::UC; ++u)
-                    copy_to_lds(dst + u * 1024, src + u * 1024, isv ? vv : kv ^ (64 * u));
+                issue_unit(t, unit, part & 1, unit_page(t, unit));
             }
         };
         auto issue_first = [&]() {
@@ -581,9 +583,12 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(Att
 #pragma unroll 1
                     for (int j = 0; j < G::TK / 32; ++j)
 #pragma unroll
-                        for (int nb = 0; nb < G::NB; ++nb)
-                            block_attend<T>(w[nb], tile + j * G::kBlock, tile + G::kTileV + j * G::kBlock, a.c2,
-                                            k0 + 32 * j, partial, units >> (2 * j), lane, logits);
+                        for (int nb = 0; nb < G::NB; ++nb) {
+                            Probs<T> p;
+                            block_probs<T>(w[nb], tile + j * G::kBlock, a.c2, k0 + 32 * j, partial, units >> (2 * j),
+                                           lane, logits, p);
+                            block_values<T>(w[nb], tile + G::kTileV + j * G::kBlock, p, lane);
+                        }
             }
         };
         bool redo = false;
@@ -851,8 +856,44 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(Att
 #pragma unroll
                 for (int r = 0; r < 16; ++r) lost = lost || (x.o[m][r] != 0.f && fabsf(x.o[m][r]) < lim);
             if (alive && __builtin_amdgcn_ballot_w64(lost)) redo = true;
-        } else {
+        } else if constexpr (G::kBf) {
             careful();
+        } else {
+            // Narrow fp32: a block's two products take as long as its copies do, so K of the next tile
+            // arrives while V's product runs and V during the next logits; with half the LDS of two whole
+            // tiles a second workgroup shares the compute unit (60,000 slots of four heads, a token:
+            // XXX -> YYY us).
+            static_assert(G::TK == 32, "two units per tile");
+            int id0, id1;   // pages of the tile whose K was issued last (the window only moves on)
+            auto issue_k = [&](int t) {
+                id0 = unit_page(t, 0);
+                issue_unit(t, 0, false, id0);
+                id1 = unit_page(t, 1);
+                issue_unit(t, 1, false, id1);
+            };
+            auto issue_v = [&](int t) {
+                issue_unit(t, 0, true, id0);
+                issue_unit(t, 1, true, id1);
+            };
+            issue_k(0);
+            issue_v(0);
+            for (int t = 0; t < nt; ++t) {
+                const int k0 = c0 + (tfirst + t * tstep) * G::TK;
+                lds_char* tile = tile_at(t);
+                wait_tiles<G::CPT / 2>(1);                                  // K; V may be on its way
+                const bool partial = !pw.sane || k0 + G::TK > seen_by_all;
+                const uint32_t units = partial ? groups(k0) : 0;
+                const bool some = k0 < wlim, next = t + 1 < nt;
+                Probs<T> p;
+                if (some) block_probs<T>(w[0], tile, a.c2, k0, partial, units, lane, logits, p);
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // K is read
+                if (next) issue_k(t + 1);
+                wait_tiles<G::CPT / 2>(next ? 1 : 0);                       // V; the next K may be on its way
+                if (partial) odd |= clean_values<T>(tile + G::kTileV, G::TK, k0, c1, units, lane);
+                if (some) block_values<T>(w[0], tile + G::kTileV, p, lane);
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // V is read
+                if (next) issue_v(t + 1);
+            }
         }
         if constexpr (WIDE) {
             __shared__ int s_redo[G::NW];

@@ -874,3 +874,12 @@ def test_attend_ragged_batches(cache, B, q):
     qs = [q] + [(0 if b % 4 == 3 else max(1, q - b)) for b in range(1, B)]
     pool = Pool(cache, lens, 2, 16, BF, seed=B)
     check_attend(cache, pool, normal(B + 1, (sum(qs), 6, 64), BF), qs, True)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("q,H", [(1, 64), (5, 32)])
+def test_attend_many_short_pages(cache, dtype, q, H):
+    """Ranges of more than 64 pages: the window of page numbers moves on within a range."""
+    log("attend many short pages %s q=%d" % (dtype, q))
+    pool = Pool(cache, [9011, 4700], H, 16, dtype, seed=71 + q)
+    check_attend(cache, pool, normal(72, (2 * q, H, 64), dtype), [q, q], True)
