@@ -6,6 +6,7 @@
 //   x_j = scale q . k_j,  lse = log sum_{j < vis_i} e^{x_j},  O = sum_{j < vis_i} e^{x_j - lse} v_j.
 // The G heads that share a key head are rows of one matrix product (row r = i G + g), so their
 // keys and values are read once.
+#include <algorithm>
 #include <cmath>
 #include <type_traits>
 
@@ -862,7 +863,7 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(Att
             // Narrow fp32: a block's two products take as long as its copies do, so K of the next tile
             // arrives while V's product runs and V during the next logits; with half the LDS of two whole
             // tiles a second workgroup shares the compute unit (60,000 slots of four heads, a token:
-            // XXX -> YYY us).
+            // 43 us with two whole tiles, so 35).
             static_assert(G::TK == 32, "two units per tile");
             int id0, id1;   // pages of the tile whose K was issued last (the window only moves on)
             auto issue_k = [&](int t) {
@@ -1371,26 +1372,33 @@ void attend_plan(AttendArgs* a) {
     const int rt = !a->wide ? 32 : a->c.dtype == DT_BF16 ? Geo<bf16, true>::RT : Geo<float, true>::RT;
     a->row_tiles = (int)((rows + rt - 1) / rt);
     if (a->row_tiles < 1) a->row_tiles = 1;
-    // Work in units of the largest sequence's: as many sequences as the tokens make, the others'
-    // lengths taken as 0.65 of the bound on the average, unless all have chunks of the same size, more
-    // than a token.  (32 ragged sequences: 31 us, with every one counted as the largest 34; if all
-    // are equal after all, 49 against 45.  Three ragged prompts in fp32: 68 and 80.)
-    const double live = a->c.max_q > 0 ? (double)a->c.T / a->c.max_q : 1;
-    const double other = a->c.max_q > 1 && a->c.T == (int64_t)a->c.B * a->c.max_q ? 1 : 0.65;
-    const double items = (double)a->c.Hkv * a->row_tiles * (live > 1 ? 1 + (live - 1) * other : 1);
-    const double slots = 512;                        // workgroups that run together
-    const int64_t least = a->wide ? 256 : 128;       // slots per split at least
-    const int64_t most = (a->c.max_len + least - 1) / least;
-    const int64_t start = a->wide ? 512 : 192;       // a split's own cost, in slots
+    // Row tiles of the sequences beside the largest, of which only the sum of the tokens is known, in
+    // units of its tiles: their lengths are taken as 0.65 of the bound on the average, unless all have
+    // chunks of the same size, more than a token.  (32 ragged sequences: 31 us, with every one counted as
+    // the largest 34; if all are equal after all, 49 against 45.  Three ragged prompts in fp32: 68 and 80.)
+    const int64_t rest = a->c.T > a->c.max_q ? a->c.T - a->c.max_q : 0;
+    const int64_t others = a->c.B - 1 < rest ? a->c.B - 1 : rest;
+    const bool equal = a->c.max_q > 1 && a->c.T == (int64_t)a->c.B * a->c.max_q;
+    double tiles = (double)others * a->row_tiles;
+    if (!equal) tiles = 0.65 * (a->row_tiles == 1 ? tiles : std::min(tiles, (double)(rest * a->G) / rt + 0.5 * others));
+    const double items = a->c.Hkv * (a->row_tiles + tiles);
+    // Time of a division into ns ranges, in us: rounds of workgroups that run together, each its slots
+    // and a start in units of slots; the join, a launch, and what it reads per range.  (300 slots, a token,
+    // bf16: 8.3 us in one range, 11.1 in three; 1,000 slots, 200 tokens: 25 in one, 17 in eight.)
+    const bool bf = a->c.dtype == DT_BF16;
+    const double slot = a->wide ? (bf ? 0.016 : 0.038) : (bf ? 0.006 : 0.019);
+    const double start = a->wide ? 512 : 192;
+    const double together = 512, range = a->wide ? 0.15 : 0.05;
+    const int64_t most = (a->c.max_len + 127) / 128;
     int64_t best = 1;
     double best_t = 0;
     for (int64_t ns = 1; ns <= most && ns <= 256; ++ns) {
-        const double rounds = ceil(items * ns / slots);
-        const double t = rounds * ((double)a->c.max_len / ns + start) + 4.0 * ns;
+        const int64_t ch = ((a->c.max_len + ns - 1) / ns + 63) / 64 * 64;
+        const double rounds = ceil(items * ns / together);
+        const double t = rounds * (ch + start) * slot + range * ns + (ns == 1 ? 0. : ns <= kFew ? 3. : 4.5);
         if (ns == 1 || t < best_t) best = ns, best_t = t;
     }
-    const int64_t ch = (a->c.max_len + best - 1) / best;
-    a->chunk = (int)((ch + 63) / 64 * 64);
+    a->chunk = (int)(((a->c.max_len + best - 1) / best + 63) / 64 * 64);
     if (a->chunk < 64) a->chunk = 64;
     a->logit_stride = (a->c.max_len + 63) / 64 * 64;
     a->nsplit = (int)((a->c.max_len + a->chunk - 1) / a->chunk);
