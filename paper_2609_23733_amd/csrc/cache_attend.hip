@@ -1373,29 +1373,36 @@ void attend_plan(AttendArgs* a) {
     a->row_tiles = (int)((rows + rt - 1) / rt);
     if (a->row_tiles < 1) a->row_tiles = 1;
     // Row tiles of the sequences beside the largest, of which only the sum of the tokens is known, in
-    // units of its tiles: their lengths are taken as 0.65 of the bound on the average, unless all have
-    // chunks of the same size, more than a token.  (32 ragged sequences: 31 us, with every one counted as
-    // the largest 34; if all are equal after all, 49 against 45.  Three ragged prompts in fp32: 68 and 80.)
+    // units of its tiles: their lengths are taken as about half of the bound on the average (single tokens, whose
+    // ranges all wait for HBM, as 0.65), unless all have chunks of the same size, more than a token.  (32
+    // ragged sequences: 31 us, with every one counted as the largest 34; if all are equal after all, 49
+    // against 45.  Three ragged prompts in fp32: 68 and 80.)
     const int64_t rest = a->c.T > a->c.max_q ? a->c.T - a->c.max_q : 0;
     const int64_t others = a->c.B - 1 < rest ? a->c.B - 1 : rest;
-    const bool equal = a->c.max_q > 1 && a->c.T == (int64_t)a->c.B * a->c.max_q;
+    const bool equal = a->c.B == 1 || (a->c.max_q > 1 && a->c.T == (int64_t)a->c.B * a->c.max_q);
     double tiles = (double)others * a->row_tiles;
-    if (!equal) tiles = 0.65 * (a->row_tiles == 1 ? tiles : std::min(tiles, (double)(rest * a->G) / rt + 0.5 * others));
+    if (!equal) {
+        if (a->row_tiles > 1) tiles = std::min(tiles, (double)(rest * a->G) / rt + 0.5 * others);
+        tiles *= a->wide ? 0.5 : 0.65;
+    }
     const double items = a->c.Hkv * (a->row_tiles + tiles);
-    // Time of a division into ns ranges, in us: rounds of workgroups that run together, each its slots
-    // and a start in units of slots; the join, a launch, and what it reads per range.  (300 slots, a token,
-    // bf16: 8.3 us in one range, 11.1 in three; 1,000 slots, 200 tokens: 25 in one, 17 in eight.)
+    // Time of a division into ns ranges, in us: the slots of a workgroup and its start, in units of
+    // slots, times the rounds of workgroups that run together, or, ragged and more than a round, all the work and
+    // a last workgroup; the join, a launch, and what it reads per range.  (300 slots, a token, bf16: 8.3 us
+    // in one range, 11.1 in three; 1,000 slots, 200 tokens: 25 in one, 17 in eight; 30 sequences of up to
+    // 102 tokens and 8,333 slots: 140 in one, 115 in eight, 131 in sixteen.)
     const bool bf = a->c.dtype == DT_BF16;
     const double slot = a->wide ? (bf ? 0.016 : 0.038) : (bf ? 0.006 : 0.019);
-    const double start = a->wide ? 512 : 192;
-    const double together = 512, range = a->wide ? 0.15 : 0.05;
+    const double start = a->wide ? 512 : 192, together = 512, range = a->wide ? 0.15 : 0.05;
     const int64_t most = (a->c.max_len + 127) / 128;
     int64_t best = 1;
     double best_t = 0;
     for (int64_t ns = 1; ns <= most && ns <= 256; ++ns) {
         const int64_t ch = ((a->c.max_len + ns - 1) / ns + 63) / 64 * 64;
-        const double rounds = ceil(items * ns / together);
-        const double t = rounds * (ch + start) * slot + range * ns + (ns == 1 ? 0. : ns <= kFew ? 3. : 4.5);
+        const double rounds = items * ns / together;
+        const double slots = equal || rounds <= 1 ? ceil(rounds) * (ch + start)
+                                                  : items * (a->c.max_len + start * ns) / together + ch + start;
+        const double t = slots * slot + range * ns + (ns == 1 ? 0. : ns <= kFew ? 3. : 4.5);
         if (ns == 1 || t < best_t) best = ns, best_t = t;
     }
     a->chunk = (int)(((a->c.max_len + best - 1) / best + 63) / 64 * 64);
