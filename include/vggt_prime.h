@@ -474,7 +474,8 @@ vp_status vp_cache_append(const vp_cache *cache, const vp_cache_batch *batch, in
  * heads of e^(x_j - lse), for every slot in use of the sequences with new tokens.
  * Logits, sums and results in fp32; bf16 caches round the probabilities of the
  * value product to bf16.  Deterministic (no atomics; the work's division follows from
- * the host's sizes). */
+ * the host's sizes).  The workspace is that of the batch's own bounds (B, T, max_q, max_len): a
+ * smaller batch can need more, as its slots are divided further; one that is too small is refused. */
 size_t vp_cache_attend_workspace_bytes(const vp_cache *cache, const vp_cache_batch *batch,
                                        int32_t Hq);
 vp_status vp_cache_attend(const vp_cache *cache, const vp_cache_batch *batch, int32_t Hq,
