@@ -1181,17 +1181,28 @@ __global__ __launch_bounds__(256) void k_cache_weight_rows(AttendArgs a) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) w[e] = e < left ? a.c.weight[at + e] : 0.f;
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int i = 0; i < sq.nq; ++i) {
-        const int seen = cache_visible(sq, a.causal, i) - k0;
-        for (int g = 0; g < a.G; ++g) {
+    constexpr int kAtOnce = 4;   // rows whose loads are issued together
+    const int rows = sq.nq * a.G;
+    int i = 0, g = 0;            // the next row's token and head
+    for (int r0 = 0; r0 < rows; r0 += kAtOnce) {
+        f32x4 x[kAtOnce];
+        float lse[kAtOnce];
+        int seen[kAtOnce];
+#pragma unroll
+        for (int n = 0; n < kAtOnce; ++n) {
             const int64_t row = (int64_t)(sq.q0 + i) * a.Hq + hk * a.G + g;
-            const float lse = a.lse[row];
-            const f32x4 x = *(const f32x4*)(a.logits + row * a.logit_stride + k0);
-            const float off = lse * kLog2e;
-            if (lse == -INFINITY) continue;   // a row without weights adds none
+            x[n] = *(const f32x4*)(a.logits + row * a.logit_stride + k0);
+            lse[n] = a.lse[row];
+            seen[n] = r0 + n < rows ? cache_visible(sq, a.causal, i) - k0 : 0;   // (past the last row: it again)
+            if (r0 + n + 1 < rows && ++g == a.G) g = 0, ++i;
+        }
+#pragma unroll
+        for (int n = 0; n < kAtOnce; ++n) {
+            if (lse[n] == -INFINITY) seen[n] = 0;   // a row without weights adds none
+            const float off = lse[n] * kLog2e;
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                sum[e] += e < seen ? exp2f_fast(fmaf(x[e], a.c2, -off)) : 0.f;
+                sum[e] += e < seen[n] ? exp2f_fast(fmaf(x[n][e], a.c2, -off)) : 0.f;
         }
     }
 #pragma unroll
@@ -1375,30 +1386,37 @@ __global__ __launch_bounds__(256, 4) void k_cache_weight(AttendArgs a) {
 // the lengths' values on the device).
 void attend_plan(AttendArgs* a) {
     const int64_t rows = (int64_t)a->c.max_q * a->G;
-    a->wide = rows > 64;
-    const int rt = !a->wide ? 32 : a->c.dtype == DT_BF16 ? Geo<bf16, true>::RT : Geo<float, true>::RT;
-    a->row_tiles = (int)((rows + rt - 1) / rt);
-    if (a->row_tiles < 1) a->row_tiles = 1;
-    // Row tiles of the sequences beside the largest, of which only the sum of the tokens is known, in
-    // units of its tiles: their lengths are taken as about half of the bound on the average (single tokens, whose
-    // ranges all wait for HBM, as 0.65), unless all have chunks of the same size, more than a token.  (32
-    // ragged sequences: 31 us, with every one counted as the largest 34; if all are equal after all, 49
-    // against 45.  Three ragged prompts in fp32: 68 and 80.)
+    const bool bf = a->c.dtype == DT_BF16;
+    // Row tiles of rt rows: the largest sequence's, and the others', of which only the sum of the tokens
+    // is known, in units of its tiles: their lengths are taken as about half of the bound on the average (single
+    // tokens, whose ranges all wait for HBM, as 0.65), unless all have chunks of the same size, more than a
+    // token.  (32 ragged sequences: 31 us, with every one counted as the largest 34; if all are equal
+    // after all, 49 against 45.  Three ragged prompts in fp32: 68 and 80.)
     const int64_t rest = a->c.T > a->c.max_q ? a->c.T - a->c.max_q : 0;
     const int64_t others = a->c.B - 1 < rest ? a->c.B - 1 : rest;
     const bool equal = a->c.B == 1 || (a->c.max_q > 1 && a->c.T == (int64_t)a->c.B * a->c.max_q);
-    double tiles = (double)others * a->row_tiles;
-    if (!equal) {
-        if (a->row_tiles > 1) tiles = std::min(tiles, (double)(rest * a->G) / rt + 0.5 * others);
-        tiles *= a->wide ? 0.5 : 0.65;
-    }
-    const double items = a->c.Hkv * (a->row_tiles + tiles);
+    auto work_items = [&](int rt, bool wide) {
+        a->row_tiles = (int)std::max<int64_t>(1, (rows + rt - 1) / rt);
+        double tiles = (double)others * a->row_tiles;
+        if (!equal) {
+            if (a->row_tiles > 1) tiles = std::min(tiles, (double)(rest * a->G) / rt + 0.5 * others);
+            tiles *= wide ? 0.5 : 0.65;
+        }
+        return a->c.Hkv * (a->row_tiles + tiles);
+    };
+    // Narrow workgroups start and end sooner, wide ones read less from L2 and LDS per row: narrow up to 64
+    // rows, or where each of 512 workgroups has few slots, fewer if that takes more than a round.  (bf16, 16
+    // heads: 1,000 tokens over 1,000 slots, 1,000 slots each, 13.5 us narrow, 23.3 wide; 400 over 5,000, 2,000 each,
+    // 29.5 and 34; 200 over 20,000, 4,400 each, 49 and 41; 1,374 over themselves, 1,850 each in 1.3 rounds,
+    // 37 and 29.  fp32: 90 over 300, 28 each, 13.3 and 15.8; 200 over 600, 130 each, 22 and 18.)
+    double items = work_items(32, false);
+    a->wide = rows > 64 && items * a->c.max_len > 512. * (!bf ? 50 : items > 512 ? 1500 : 2500);
+    if (a->wide) items = work_items(bf ? Geo<bf16, true>::RT : Geo<float, true>::RT, true);
     // Time of a division into ns ranges, in us: the slots of a workgroup and its start, in units of
     // slots, times the rounds of workgroups that run together, or, ragged and more than a round, all the work and
     // a last workgroup; the join, a launch, and what it reads per range.  (300 slots, a token, bf16: 8.3 us
     // in one range, 11.1 in three; 1,000 slots, 200 tokens: 25 in one, 17 in eight; 30 sequences of up to
     // 102 tokens and 8,333 slots: 140 in one, 115 in eight, 131 in sixteen.)
-    const bool bf = a->c.dtype == DT_BF16;
     const double slot = a->wide ? (bf ? 0.016 : 0.038) : (bf ? 0.006 : 0.019);
     const double start = a->wide ? 512 : 192, together = 512, range = a->wide ? 0.15 : 0.05;
     const int64_t most = (a->c.max_len + 127) / 128;
@@ -1424,11 +1442,15 @@ size_t attend_part_rows(const AttendArgs& a) {
 }
 
 // Keeping a logit costs 8 bytes (written and read) per row and slot, forming it again a key's
-// 128 or 256 per slot: up to eight rows of a key head they are kept (two tokens over 137,400 slots:
-// 106 us to form them again).
+// 128 or 256 per slot and a tile of 128 or 64 rows however few there are.  60,000 slots of 16 heads, bf16: 8
+// rows of a key head 56 us kept, 111 formed again, 32 rows 104 and 112; fp32, 16 rows 135 and 220, 64 rows
+// 237 and 268.  More than eight rows of a short cache are formed again, as a thread takes them one after the other
+// (16 rows, 2,000 slots: 17.6 kept, 16.0 again), and so is what would take more than 2 GiB.
 size_t attend_logits(const AttendArgs& a) {
-    if (!a.c.weight || a.wide || (int64_t)a.c.max_q * a.G > 8) return 0;
-    return (size_t)a.c.T * a.Hq * a.logit_stride;
+    const int64_t rows = (int64_t)a.c.max_q * a.G;
+    if (!a.c.weight || a.wide || rows > (a.c.dtype == DT_BF16 ? 32 : 64) || (rows > 8 && a.c.max_len < 4096)) return 0;
+    const int64_t n = (int64_t)a.c.T * a.Hq * a.logit_stride;
+    return n <= (int64_t)1 << 29 ? n : 0;
 }
 
 template <typename T>

@@ -883,3 +883,22 @@ def test_attend_many_short_pages(cache, dtype, q, H):
     log("attend many short pages %s q=%d" % (dtype, q))
     pool = Pool(cache, [9011, 4700], H, 16, dtype, seed=71 + q)
     check_attend(cache, pool, normal(72, (2 * q, H, 64), dtype), [q, q], True)
+
+
+@pytest.mark.parametrize("lens,qs,Hq,Hkv,page,dtype,causal", [
+    # many rows over few slots: both kernels' divisions of rows, ragged and equal
+    ([200], [200], 2, 2, 16, BF, True), ([700, 700], [300, 300], 4, 2, 32, BF, False), ([90, 1, 300], [90, 1, 70], 3, 1, 16, F32, True),
+    ([1374, 1374], [1374, 1374], 8, 8, 64, BF, False), ([3000, 2000, 100], [400, 17, 100], 8, 4, 64, BF, True),
+    ([9000], [150], 16, 16, 64, BF, True), ([600], [200], 2, 2, 16, F32, True)])
+def test_attend_many_rows(cache, lens, qs, Hq, Hkv, page, dtype, causal):
+    log("attend many rows %s %s %s" % (lens, qs, dtype))
+    pool = Pool(cache, lens, Hkv, page, dtype, seed=300 + sum(lens))
+    check_attend(cache, pool, normal(8, (sum(qs), Hq, 64), dtype), qs, causal)
+
+
+@pytest.mark.parametrize("q,H,dtype", [(9, 2, BF), (32, 1, BF), (33, 1, BF), (17, 2, F32), (64, 1, F32)])
+def test_attend_weights_of_kept_logits(cache, q, H, dtype):
+    """Long caches: up to 32 (fp32: 64) rows of a key head keep their logits for the weights."""
+    log("attend weights of kept logits q=%d %s" % (q, dtype))
+    pool = Pool(cache, [4500, 4097], H, 64, dtype, seed=400 + q)
+    check_attend(cache, pool, normal(9, (q + 3, H, 64), dtype), [q, 3], True)
