@@ -1190,11 +1190,16 @@ __global__ __launch_bounds__(256) void k_cache_weight_rows(AttendArgs a) {
         int seen[kAtOnce];
 #pragma unroll
         for (int n = 0; n < kAtOnce; ++n) {
-            const int64_t row = (int64_t)(sq.q0 + i) * a.Hq + hk * a.G + g;
-            x[n] = *(const f32x4*)(a.logits + row * a.logit_stride + k0);
-            lse[n] = a.lse[row];
-            seen[n] = r0 + n < rows ? cache_visible(sq, a.causal, i) - k0 : 0;   // (past the last row: it again)
-            if (r0 + n + 1 < rows && ++g == a.G) g = 0, ++i;
+            x[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+            lse[n] = -INFINITY;
+            seen[n] = 0;
+            if (r0 + n < rows) {
+                const int64_t row = (int64_t)(sq.q0 + i) * a.Hq + hk * a.G + g;
+                x[n] = *(const f32x4*)(a.logits + row * a.logit_stride + k0);
+                lse[n] = a.lse[row];
+                seen[n] = cache_visible(sq, a.causal, i) - k0;
+                if (++g == a.G) g = 0, ++i;
+            }
         }
 #pragma unroll
         for (int n = 0; n < kAtOnce; ++n) {
@@ -1405,12 +1410,13 @@ void attend_plan(AttendArgs* a) {
         return a->c.Hkv * (a->row_tiles + tiles);
     };
     // Narrow workgroups start and end sooner, wide ones read less from L2 and LDS per row: narrow up to 64
-    // rows, or where each of 512 workgroups has few slots, fewer if that takes more than a round.  (bf16, 16
+    // rows and, in bf16, where each of 512 workgroups has few slots, fewer if that takes more than a round.  (16
     // heads: 1,000 tokens over 1,000 slots, 1,000 slots each, 13.5 us narrow, 23.3 wide; 400 over 5,000, 2,000 each,
-    // 29.5 and 34; 200 over 20,000, 4,400 each, 49 and 41; 1,374 over themselves, 1,850 each in 1.3 rounds,
-    // 37 and 29.  fp32: 90 over 300, 28 each, 13.3 and 15.8; 200 over 600, 130 each, 22 and 18.)
+    // 29.5 and 34; 200 over 20,000, 4,400 each, 49 and 41; 1,374 over themselves, 1,850 each in 1.3 rounds, 37 and
+    // 29.  fp32, whose wide kernel has the faster products: 64 over 20,000 56 and 57, 90 over 20,000 80 and
+    // 61, 200 over 600 22 and 18; 90 over 300 13.3 and 15.8.)
     double items = work_items(32, false);
-    a->wide = rows > 64 && items * a->c.max_len > 512. * (!bf ? 50 : items > 512 ? 1500 : 2500);
+    a->wide = rows > 64 && (!bf || items * a->c.max_len > 512. * (items > 512 ? 1500 : 2500));
     if (a->wide) items = work_items(bf ? Geo<bf16, true>::RT : Geo<float, true>::RT, true);
     // Time of a division into ns ranges, in us: the slots of a workgroup and its start, in units of
     // slots, times the rounds of workgroups that run together, or, ragged and more than a round, all the work and
@@ -1444,7 +1450,7 @@ size_t attend_part_rows(const AttendArgs& a) {
 // Keeping a logit costs 8 bytes (written and read) per row and slot, forming it again a key's
 // 128 or 256 per slot and a tile of 128 or 64 rows however few there are.  60,000 slots of 16 heads, bf16: 8
 // rows of a key head 56 us kept, 111 formed again, 32 rows 104 and 112; fp32, 16 rows 135 and 220, 64 rows
-// 237 and 268.  More than eight rows of a short cache are formed again, as a thread takes them one after the other
+// 228 and 268.  More than eight rows of a short cache are formed again, as a thread takes them one after the other
 // (16 rows, 2,000 slots: 17.6 kept, 16.0 again), and so is what would take more than 2 GiB.
 size_t attend_logits(const AttendArgs& a) {
     const int64_t rows = (int64_t)a.c.max_q * a.G;
