@@ -893,7 +893,10 @@ vp_status attend_args(const vp_cache* cache, const vp_cache_batch* batch, int32_
     a->Hq = Hq;
     a->G = Hq / cache->Hkv;
     vp::attend_plan(a);
-    if (((int64_t)a->c.B * a->c.Hkv * a->nsplit + 8) * a->row_tiles > INT32_MAX) return VP_ERR_UNSUPPORTED;
+    // a launch has fewer than 2^32 threads, 2^24 workgroups: of the attention, the join and the weights
+    if (((int64_t)a->c.B * a->c.Hkv * a->nsplit + 8) * a->row_tiles >= 1 << 24 ||
+        (a->nsplit > 1 && (int64_t)a->c.max_q * Hq >= 1 << 26) || a->c.max_len > (1 << 30) - 64)
+        return VP_ERR_UNSUPPORTED;
     return VP_OK;
 }
 

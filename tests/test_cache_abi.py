@@ -190,3 +190,13 @@ def test_python_checks():
         c._rows(None, "x", 2, 4, torch.bfloat16)
     with pytest.raises(vp.VPError):
         c.Rotary.make(65, device="cpu")
+
+
+def test_attend_launches_fit(lib):
+    """Bounds that would take 2^24 workgroups or more, 2^32 threads, are refused."""
+    f = lambda **kw: lib.vp_cache_attend_workspace_bytes(R(cache(npages=1 << 30, Hkv=4)), R(batch(**kw)), 8)
+    big = 1 << 23
+    assert f(B=1, T=big, max_q=big, max_pages=1 << 20, max_len=1 << 25) > 0
+    assert f(B=16000, T=big, max_q=big, max_pages=1 << 20, max_len=1 << 25) == 0
+    assert f(B=1, T=8, max_q=8, max_pages=1 << 24, max_len=1 << 30) == 0
+    assert f(B=1, T=8, max_q=8, max_pages=1 << 24, max_len=(1 << 30) - 64) > 0
