@@ -596,6 +596,28 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(Att
                         }
             }
         };
+        // Values so large that their sums left fp32's range: once more, with a reference that is known now, a row's
+        // log-sum-exp and one: its probabilities sum to 1/2, so no sum passes the largest value.
+        auto overflown = [&]() {
+            float top = 0.f;
+#pragma unroll
+            for (int nb = 0; nb < G::NB; ++nb)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) top = maximum(maximum(top, fabsf(w[nb].o[0][r])), fabsf(w[nb].o[1][r]));
+            return alive && __builtin_amdgcn_ballot_w64(!(top <= 3.4028235e38f)) != 0;
+        };
+        auto restart = [&](bool known) {
+#pragma unroll
+            for (int nb = 0; nb < G::NB; ++nb) {
+                Rows<T>& x = w[nb];
+                const float l = x.l + __shfl_xor(x.l, 32), m = x.m + __log2f(l) + 1.f;
+                x.m = known && fabsf(m) <= 3.4028235e38f ? m : -INFINITY;   // (no logits, or not finite: as ever)
+                x.l = 0.f;
+                x.o[0] = x.o[1] = zero_f32x16();
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            pw.start(a.c, b, c0, c1 - 1, lane);
+        };
         bool redo = false;
         if constexpr (WIDE && G::kBf) {
             // The reference stays that of the first block.  While block j's probabilities are formed, block
@@ -862,7 +884,15 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(Att
                 for (int r = 0; r < 16; ++r) lost = lost || (x.o[m][r] != 0.f && fabsf(x.o[m][r]) < lim);
             if (alive && __builtin_amdgcn_ballot_w64(lost)) redo = true;
         } else if constexpr (G::kBf) {
-            careful();
+#pragma unroll 1
+            for (int pass = 0; pass < 2; ++pass) {
+                if (pass) {
+                    restart(true);
+                    issue_first();
+                }
+                careful();
+                if (!overflown()) break;
+            }
         } else {
             // Narrow fp32: a block's two products take as long as its copies do, so K of the next tile
             // arrives while V's product runs and V during the next logits; with half the LDS of two whole
@@ -880,55 +910,56 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(Att
                 issue_unit(t, 0, true, id0);
                 issue_unit(t, 1, true, id1);
             };
-            issue_k(0);
-            issue_v(0);
-            for (int t = 0; t < nt; ++t) {
-                const int k0 = c0 + (tfirst + t * tstep) * G::TK;
-                lds_char* tile = tile_at(t);
-                wait_tiles<G::CPT / 2>(1);                                  // K; V may be on its way
-                const bool partial = !pw.sane || k0 + G::TK > seen_by_all;
-                const uint32_t units = partial ? groups(k0) : 0;
-                const bool some = k0 < wlim, next = t + 1 < nt;
-                Probs<T> p;
-                if (some) block_probs<T>(w[0], tile, a.c2, k0, partial, units, lane, logits, p);
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // K is read
-                if (next) issue_k(t + 1);
-                wait_tiles<G::CPT / 2>(next ? 1 : 0);                       // V; the next K may be on its way
-                if (partial) odd |= clean_values<T>(tile + G::kTileV, G::TK, k0, c1, units, lane);
-                if (some) block_values<T>(w[0], tile + G::kTileV, p, lane);
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // V is read
-                if (next) issue_v(t + 1);
+#pragma unroll 1
+            for (int pass = 0; pass < 2; ++pass) {
+                if (pass) restart(true);
+                issue_k(0);
+                issue_v(0);
+                for (int t = 0; t < nt; ++t) {
+                    const int k0 = c0 + (tfirst + t * tstep) * G::TK;
+                    lds_char* tile = tile_at(t);
+                    wait_tiles<G::CPT / 2>(1);                                  // K; V may be on its way
+                    const bool partial = !pw.sane || k0 + G::TK > seen_by_all;
+                    const uint32_t units = partial ? groups(k0) : 0;
+                    const bool some = k0 < wlim, next = t + 1 < nt;
+                    Probs<T> p;
+                    if (some) block_probs<T>(w[0], tile, a.c2, k0, partial, units, lane, logits, p);
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // K is read
+                    if (next) issue_k(t + 1);
+                    wait_tiles<G::CPT / 2>(next ? 1 : 0);                       // V; the next K may be on its way
+                    if (partial) odd |= clean_values<T>(tile + G::kTileV, G::TK, k0, c1, units, lane);
+                    if (some) block_values<T>(w[0], tile + G::kTileV, p, lane);
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // V is read
+                    if (next) issue_v(t + 1);
+                }
+                if (!overflown()) break;
             }
         }
         if constexpr (WIDE) {
             __shared__ int s_redo[G::NW];
-            redo = redo || !pw.sane;
+            redo = redo || !pw.sane || overflown();
             if (alive) {
                 bool far = false;
 #pragma unroll
-                for (int nb = 0; nb < G::NB; ++nb) {
-                    const Rows<T>& x = w[nb];
-                    far = far || !(x.l < 1152921504606846976.f) || (x.m == -INFINITY && x.vis > c0);   // 2^60
-#pragma unroll
-                    for (int m = 0; m < 2; ++m)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) far = far || !(fabsf(x.o[m][r]) <= 3.4028235e38f);
-                }
+                for (int nb = 0; nb < G::NB; ++nb)
+                    far = far || !(w[nb].l < 1152921504606846976.f) || (w[nb].m == -INFINITY && w[nb].vis > c0);   // 2^60
                 redo = redo || __builtin_amdgcn_ballot_w64(far);
             }
             if (lane == 0) s_redo[wave] = redo;
             __syncthreads();
             if (s_redo[0] | s_redo[1] | s_redo[2] | s_redo[3]) {
-#pragma unroll
-                for (int nb = 0; nb < G::NB; ++nb) {
-                    w[nb].o[0] = w[nb].o[1] = zero_f32x16();
-                    w[nb].m = -INFINITY;
-                    w[nb].l = 0.f;
-                }
-                pw.start(a.c, b, c0, c1 - 1, lane);
                 if constexpr (!G::kBf) load_q();
-                issue_first();
-                careful();
+#pragma unroll 1
+                for (int pass = 0; pass < 2; ++pass) {
+                    restart(pass > 0);
+                    issue_first();
+                    careful();
+                    const bool far = overflown();
+                    __syncthreads();
+                    if (lane == 0) s_redo[wave] = far;
+                    __syncthreads();
+                    if (!(s_redo[0] | s_redo[1] | s_redo[2] | s_redo[3])) break;
+                }
             }
         }
         if constexpr (WIDE) {   // what one wave took out, all see to
@@ -950,10 +981,13 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(Att
     for (int nb = 0; nb < G::NB; ++nb) w[nb].l += __shfl_xor(w[nb].l, 32);
 
     const int64_t all_rows = (int64_t)a.c.T * a.Hq;
+    // (Parts of a row are divided by their own l, so that no sum of them passes the largest value.)
     if constexpr (WIDE) {
 #pragma unroll
         for (int nb = 0; nb < G::NB; ++nb) {
             if (row0 + 32 * nb + l31 >= nrows) return;
+            float inv, lse;
+            row_result(w[nb].m, w[nb].l, &inv, &lse);
             if (a.nsplit > 1) {
                 float* po = a.part + (split * all_rows + orow[nb]) * kD;
                 if (hh == 0) {
@@ -966,13 +1000,11 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(Att
                     for (int g = 0; g < 4; ++g) {
                         f32x4 v;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) v[e] = w[nb].o[m][4 * g + e];
+                        for (int e = 0; e < 4; ++e) v[e] = w[nb].o[m][4 * g + e] * inv;
                         *(f32x4*)(po + 32 * m + 8 * g + 4 * hh) = v;
                     }
                 continue;
             }
-            float inv, lse;
-            row_result(w[nb].m, w[nb].l, &inv, &lse);
             if (hh == 0) put_lse(a, orow[nb], lse);
             T* out = (T*)a.O + orow[nb] * kD;
             if constexpr (G::kBf) {
@@ -1008,18 +1040,28 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(Att
         // The four waves' partial results meet in LDS (the ring is free then).
         constexpr int kRow = 68;
         float* sml = (float*)smem;                 // [4][32][2]
-        float* so = (float*)smem + 256;            // [4][32][68]
-        static_assert((256 + 4 * 32 * kRow) * 4 <= G::kLds, "partial results fit the ring");
+        float* smeet = (float*)smem + 256;         // [32][2]
+        float* so = (float*)smem + 320;            // [4][32][68]
+        static_assert((320 + 4 * 32 * kRow) * 4 <= G::kLds, "partial results fit the ring");
         __syncthreads();
         if (hh == 0) {
             sml[(wave * 32 + l31) * 2] = w[0].m;
             sml[(wave * 32 + l31) * 2 + 1] = w[0].l;
         }
         __syncthreads();
-        float M = -INFINITY;
+        float M = -INFINITY, L = 0.f, inv, lse;
+        float mv[4];
 #pragma unroll
-        for (int v = 0; v < 4; ++v) M = maximum(M, sml[(v * 32 + l31) * 2]);
-        const float f = w[0].m == -INFINITY ? 0.f : w[0].m == M ? 1.f : exp2f_fast(w[0].m - M);
+        for (int v = 0; v < 4; ++v) M = maximum(M, mv[v] = sml[(v * 32 + l31) * 2]);
+        const float ref = M == -INFINITY ? 0.f : M;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) L += exp2f_fast(mv[v] - ref) * sml[(v * 32 + l31) * 2 + 1];
+        row_result(M, L, &inv, &lse);
+        const float f = exp2f_fast(w[0].m - ref) * inv;
+        if (wave == 0 && hh == 0) {
+            smeet[l31 * 2] = M;
+            smeet[l31 * 2 + 1] = L;
+        }
         if (row0 + l31 < nrows) {
 #pragma unroll
             for (int m = 0; m < 2; ++m)
@@ -1036,36 +1078,26 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(Att
         if (r < nrows) {
             const int i = r / a.G;
             const int64_t at = (int64_t)(sq.q0 + i) * a.Hq + hk * a.G + r - i * a.G;
-            float mm[4], MM = -INFINITY, L = 0.f;
-#pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                mm[v] = sml[(v * 32 + rr) * 2];
-                MM = maximum(MM, mm[v]);
-            }
+            M = smeet[rr * 2], L = smeet[rr * 2 + 1];
             float acc[8] = {};
 #pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                const float g = mm[v] == -INFINITY ? 0.f : mm[v] == MM ? 1.f : exp2f_fast(mm[v] - MM);
-                L += g * sml[(v * 32 + rr) * 2 + 1];
+            for (int v = 0; v < 4; ++v)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) acc[e] += so[(v * 32 + rr) * kRow + d0 + e];
-            }
             if (a.nsplit > 1) {
                 float* po = a.part + (split * all_rows + at) * kD + d0;
                 *(f32x4*)po = f32x4{acc[0], acc[1], acc[2], acc[3]};
                 *(f32x4*)(po + 4) = f32x4{acc[4], acc[5], acc[6], acc[7]};
-                if (d0 == 0) *(f32x2*)(a.part_ml + (split * all_rows + at) * 2) = f32x2{MM, L};
+                if (d0 == 0) *(f32x2*)(a.part_ml + (split * all_rows + at) * 2) = f32x2{M, L};
             } else {
-                float inv, lse;
-                row_result(MM, L, &inv, &lse);
+                row_result(M, L, &inv, &lse);
                 if (d0 == 0) put_lse(a, at, lse);
                 T* out = (T*)a.O + at * kD + d0;
                 if constexpr (G::kBf) {
-                    *(bf16x8*)out = pack_bf16x8(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv,
-                                                acc[4] * inv, acc[5] * inv, acc[6] * inv, acc[7] * inv);
+                    *(bf16x8*)out = pack_bf16x8(acc[0], acc[1], acc[2], acc[3], acc[4], acc[5], acc[6], acc[7]);
                 } else {
-                    *(f32x4*)out = f32x4{acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
-                    *(f32x4*)(out + 4) = f32x4{acc[4] * inv, acc[5] * inv, acc[6] * inv, acc[7] * inv};
+                    *(f32x4*)out = f32x4{acc[0], acc[1], acc[2], acc[3]};
+                    *(f32x4*)(out + 4) = f32x4{acc[4], acc[5], acc[6], acc[7]};
                 }
             }
         }
@@ -1129,6 +1161,10 @@ __global__ __launch_bounds__(256) void k_cache_join(AttendArgs a) {
     }
 #pragma unroll
     for (int o = kLanes / 2; o >= 1; o >>= 1) L += __shfl_xor(L, o);
+    float inv, lse;
+    row_result(M, L, &inv, &lse);
+#pragma unroll
+    for (int j = 0; j < kMl; ++j) f[j] *= ml[j][1] * inv;   // the part's share (its sums are divided by its own l)
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     for (int s0 = 0; s0 < ns; s0 += kBatch) {
         if (s0 > 0) load(s0);
@@ -1149,15 +1185,13 @@ __global__ __launch_bounds__(256) void k_cache_join(AttendArgs a) {
             for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], o);
         if (grp) return;
     }
-    float inv, lse;
-    row_result(M, L, &inv, &lse);
     if ((lane & 15) == 0) put_lse(a, at, lse);
     T* out = (T*)a.O + at * kD + d;
     if constexpr (sizeof(T) == 2) {
-        bf16x4 y = {(bf16)(acc[0] * inv), (bf16)(acc[1] * inv), (bf16)(acc[2] * inv), (bf16)(acc[3] * inv)};
+        bf16x4 y = {(bf16)acc[0], (bf16)acc[1], (bf16)acc[2], (bf16)acc[3]};
         *(bf16x4*)out = y;
     } else {
-        *(f32x4*)out = f32x4{acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
+        *(f32x4*)out = acc;
     }
 }
 

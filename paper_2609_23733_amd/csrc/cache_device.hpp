@@ -38,7 +38,7 @@ struct AttendArgs {
     float* weight_out;       // null: weights are not gathered
     int wide;                // kernel variant
     int row_tiles, nsplit, chunk;
-    float *part, *part_ml;   // split results [nsplit, T * Hq, 64] and [nsplit, T * Hq, 2]
+    float *part, *part_ml;   // ranges' results [nsplit, T * Hq, 64], references and sums [nsplit, T * Hq, 2]
     float* logits;           // null, or [T * Hq, logit_stride]: kept for the weights
     int64_t logit_stride;
     float* off;              // null, or [T * Hq]: -lse log2 e / c2, for the weights
