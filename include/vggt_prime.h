@@ -472,9 +472,11 @@ vp_status vp_cache_append(const vp_cache *cache, const vp_cache_batch *batch, in
  * whatever they hold.  With weight_out (fp32, laid out as cache->weight, which may be
  * the same array), weight_out = weight + the sum over the chunk's tokens and the key head's query
  * heads of e^(x_j - lse), for every slot in use of the sequences with new tokens.
- * Logits, sums and results in fp32; bf16 caches round the probabilities of the
- * value product to bf16.  Deterministic (no atomics; the work's division follows from
- * the host's sizes).  The workspace is that of the batch's own bounds (B, T, max_q, max_len): a
+ * Logits, sums and results in fp32.  bf16 caches: the value product takes the probabilities as sums
+ * of two bf16 values (2^-16 of each); rounded to bf16 in calls of many rows over many slots, and for
+ * rows computed along with rows whose values are infinite or whose sums overflow.
+ * Deterministic (no atomics; the work's division follows from the host's sizes).  The workspace is
+ * that of the batch's own bounds (B, T, max_q, max_len): a
  * smaller batch can need more, as its slots are divided further; one that is too small is refused. */
 size_t vp_cache_attend_workspace_bytes(const vp_cache *cache, const vp_cache_batch *batch,
                                        int32_t Hq);

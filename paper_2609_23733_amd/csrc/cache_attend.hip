@@ -31,6 +31,7 @@ __device__ __forceinline__ float maximum(float a, float b) {
 template <typename T, bool WIDE>
 struct Geo {
     static constexpr bool kBf = sizeof(T) == 2;
+    static constexpr bool kSplit = kBf && !WIDE;                // probabilities as two bf16 values
     static constexpr int NW = 4;                                // waves
     static constexpr int NB = WIDE && kBf ? 2 : 1;              // groups of 32 rows per wave
     static constexpr int TK = WIDE && kBf ? 64 : 32;            // slots per tile
@@ -118,7 +119,7 @@ __device__ __forceinline__ void wait_tiles(int behind) {
 //
 // Probabilities are 2^(x - m) with a reference m (in log2 units) that is the row's maximum over its
 // first block and moves only when a block's sum passes 2^16: fp32 sums and bf16 probabilities
-// (rounded to 8 bits, as their values are; the sum l takes them unrounded) keep their relative
+// (see Probs; the sum l takes them unrounded) keep their relative
 // precision at any scale, so ordinary blocks need no maximum.  When a block passes the bound (and
 // at a row's first slots, where m = -inf makes the sum inf or NaN) its logits are formed again, m
 // becomes the maximum so far and O and l are scaled to it.
@@ -132,21 +133,35 @@ struct Rows {
     float m, l;
     int vis;
 };
-// A block's probabilities as operands of the value product.
-template <typename T>
+// A block's probabilities as operands of the value product.  bf16, SPLIT: each as the sum of two bf16
+// values, within 2^-16 of it, so that an output's own rounding is all that shows; two MFMAs for one.  Without it
+// the rounding of the probabilities adds as much again (errors of 2.35e-3 of the result, with it 1.66e-3).
+// Narrow workgroups split, as HBM hides most of it (tokens over 137,400 and 62,724 slots 182.8 us and 183.2, 32
+// sequences ragged to 10,992 36.5 and 37.3, a token over 600 slots 8.9 and 9.8; 400 tokens over 5,000
+// slots 29.6 and 34.0).  Wide ones, bound by their instructions and their registers, do not (a view over
+// 43,968 slots 264 us, split 445).
+template <typename T, bool SPLIT>
 struct Probs;
-template <>
-struct Probs<bf16> {
-    bf16x8 v[2];
+template <bool SPLIT>
+struct Probs<bf16, SPLIT> {
+    bf16x8 v[2], rest[SPLIT ? 2 : 1];
     __device__ __forceinline__ void set(const f32x16& s) {
 #pragma unroll
         for (int st = 0; st < 2; ++st)
             v[st] = pack_bf16x8(s[8 * st], s[8 * st + 1], s[8 * st + 2], s[8 * st + 3], s[8 * st + 4],
                                 s[8 * st + 5], s[8 * st + 6], s[8 * st + 7]);
+        if constexpr (SPLIT)
+#pragma unroll
+            for (int st = 0; st < 2; ++st) {
+                float r[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) r[e] = s[8 * st + e] - (float)v[st][e];
+                rest[st] = pack_bf16x8(r[0], r[1], r[2], r[3], r[4], r[5], r[6], r[7]);
+            }
     }
 };
-template <>
-struct Probs<float> {
+template <bool SPLIT>
+struct Probs<float, SPLIT> {
     f32x16 v;
     __device__ __forceinline__ void set(const f32x16& s) { v = s; }
 };
@@ -202,9 +217,9 @@ __device__ __forceinline__ float block_exp(f32x16& s, float c2, float ref) {
 }
 
 // The block again, with the reference moved to the maximum so far.
-template <typename T>
+template <typename T, bool SPLIT>
 __device__ __forceinline__ float block_move(Rows<T>& w, lds_char* k, float c2, int k0, bool partial,
-                                            uint32_t units, int lane, Probs<T>& p) {
+                                            uint32_t units, int lane, Probs<T, SPLIT>& p) {
     // (read again: the first pass's operands and logits do not stay in registers for this)
     asm volatile("" ::: "memory");
     f32x16 s = block_logits<T>(w, k, lane);
@@ -238,9 +253,10 @@ __device__ __forceinline__ bf16x8 tr_read(lds_char* a) {
     return __builtin_bit_cast(bf16x8, f);
 }
 
-// O^T += V^T P^T of the block whose V lies at `v`.
-template <typename T>
-__device__ __forceinline__ void block_values(Rows<T>& w, lds_char* v, const Probs<T>& p, int lane) {
+// O^T += V^T P^T of the block whose V lies at `v`.  `rest`: with the second parts of split probabilities
+// (which an infinite value would turn into NaN).
+template <typename T, bool SPLIT>
+__device__ __forceinline__ void block_values(Rows<T>& w, lds_char* v, const Probs<T, SPLIT>& p, bool rest, int lane) {
     const int l31 = lane & 31, hh = lane >> 5;
     if constexpr (Rows<T>::kBf) {
         const int i16 = lane & 15, dq = (lane >> 4) & 1;
@@ -250,7 +266,9 @@ __device__ __forceinline__ void block_values(Rows<T>& w, lds_char* v, const Prob
         for (int st = 0; st < 2; ++st)
 #pragma unroll
             for (int m = 0; m < 2; ++m) {
-                w.o[m] = mfma_bf16(tr_read(v + (v0 ^ (m << 6)) + st * 2048), p.v[st], w.o[m]);
+                const bf16x8 f = tr_read(v + (v0 ^ (m << 6)) + st * 2048);
+                w.o[m] = mfma_bf16(f, p.v[st], w.o[m]);
+                if (SPLIT && rest) w.o[m] = mfma_bf16(f, p.rest[SPLIT ? st : 0], w.o[m]);
             }
     } else {
         typedef __attribute__((address_space(3))) const float lds_f32;
@@ -299,9 +317,9 @@ __device__ __forceinline__ f32x16 mfma_planes(const Planes& a, const Planes& b, 
 
 // A block's logits and probabilities.
 // `logits`: null, or where the row's logits (of slots from 0 on) are kept.
-template <typename T>
+template <typename T, bool SPLIT>
 __device__ __forceinline__ void block_probs(Rows<T>& w, lds_char* k, float c2, int k0, bool partial, uint32_t units,
-                                            int lane, float* logits, Probs<T>& p) {
+                                            int lane, float* logits, Probs<T, SPLIT>& p) {
     f32x16 s = block_logits<T>(w, k, lane);
     if (partial) block_mask<T>(w, k0, units, lane, s);
     if (logits)
@@ -312,7 +330,7 @@ __device__ __forceinline__ void block_probs(Rows<T>& w, lds_char* k, float c2, i
     float sum = block_exp(s, c2, w.m);   // inf or NaN while m is -inf
     p.set(s);
     if (__builtin_amdgcn_ballot_w64(!(sum < kMoveAt)))
-        sum = block_move<T>(w, k, c2, k0, partial, units, lane, p);
+        sum = block_move<T, SPLIT>(w, k, c2, k0, partial, units, lane, p);
     w.l += sum;
 }
 
@@ -577,7 +595,7 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(Att
         float* logits = nullptr;
         if (!WIDE && a.logits && row0 + l31 < nrows) logits = a.logits + orow[0] * a.logit_stride;
         // Every block with its bound on the reference checked.
-        auto careful = [&]() {
+        auto careful = [&](bool rest) {
             for (int t = 0; t < nt; ++t) {
                 const int k0 = c0 + (tfirst + t * tstep) * G::TK;
                 lds_char* tile = tile_at(t);
@@ -589,15 +607,15 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(Att
                     for (int j = 0; j < G::TK / 32; ++j)
 #pragma unroll
                         for (int nb = 0; nb < G::NB; ++nb) {
-                            Probs<T> p;
-                            block_probs<T>(w[nb], tile + j * G::kBlock, a.c2, k0 + 32 * j, partial, units >> (2 * j),
+                            Probs<T, G::kSplit> p;
+                            block_probs<T, G::kSplit>(w[nb], tile + j * G::kBlock, a.c2, k0 + 32 * j, partial, units >> (2 * j),
                                            lane, logits, p);
-                            block_values<T>(w[nb], tile + G::kTileV + j * G::kBlock, p, lane);
+                            block_values<T, G::kSplit>(w[nb], tile + G::kTileV + j * G::kBlock, p, rest, lane);
                         }
             }
         };
-        // Values so large that their sums left fp32's range: once more, with a reference that is known now, a row's
-        // log-sum-exp and one: its probabilities sum to 1/2, so no sum passes the largest value.
+        // Values so large that their sums left fp32's range, or infinite: once more, with a reference that is known
+        // now, a row's log-sum-exp and one: its probabilities sum to 1/2, so no sum passes the largest value.
         auto overflown = [&]() {
             float top = 0.f;
 #pragma unroll
@@ -627,7 +645,7 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(Att
             // first block had none, or values are huge), the workgroup does its range again carefully.
             const int tfull = pw.sane ? (seen_by_all - c0) / G::TK : 0;   // tiles all rows see
             f32x16 s0[G::NB], s1[G::NB];
-            Probs<T> p0[G::NB], p1[G::NB];
+            Probs<T, G::kSplit> p0[G::NB], p1[G::NB];
             float ref[G::NB], sum[G::NB][4] = {};
             // Half a tile: eight operands from LDS, each for the MFMAs of the row groups and followed by the
             // vector instructions of two of a group's 16 logits; they are read three ahead.  The first three are values, of a tile
@@ -646,7 +664,7 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(Att
                 return *(lds_frag*)(k + (a0 ^ (i << 5)));
             };
             typedef f32x16 Logits[G::NB];
-            typedef Probs<T> BlockP[G::NB];
+            typedef Probs<T, G::kSplit> BlockP[G::NB];
             auto half = [&](auto mask, Logits& s, int k0, Logits& sn, lds_char* k, lds_char* v, lds_char* v_next,
                             const BlockP& pv, BlockP& pn) {
                 if constexpr (decltype(mask)::value)
@@ -736,8 +754,8 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(Att
                 probs(s1, c0 + t * G::TK + 32, p1);
 #pragma unroll
                 for (int nb = 0; nb < G::NB; ++nb) {
-                    block_values<T>(w[nb], tile_at(t) + G::kTileV, p0[nb], lane);
-                    block_values<T>(w[nb], tile_at(t) + G::kTileV + G::kBlock, p1[nb], lane);
+                    block_values<T, G::kSplit>(w[nb], tile_at(t) + G::kTileV, p0[nb], false, lane);
+                    block_values<T, G::kSplit>(w[nb], tile_at(t) + G::kTileV + G::kBlock, p1[nb], false, lane);
                     w[nb].l = (sum[nb][0] + sum[nb][1]) + (sum[nb][2] + sum[nb][3]);
                 }
             } else {
@@ -890,7 +908,7 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(Att
                     restart(true);
                     issue_first();
                 }
-                careful();
+                careful(pass == 0);
                 if (!overflown()) break;
             }
         } else {
@@ -922,13 +940,13 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(Att
                     const bool partial = !pw.sane || k0 + G::TK > seen_by_all;
                     const uint32_t units = partial ? groups(k0) : 0;
                     const bool some = k0 < wlim, next = t + 1 < nt;
-                    Probs<T> p;
-                    if (some) block_probs<T>(w[0], tile, a.c2, k0, partial, units, lane, logits, p);
+                    Probs<T, G::kSplit> p;
+                    if (some) block_probs<T, G::kSplit>(w[0], tile, a.c2, k0, partial, units, lane, logits, p);
                     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // K is read
                     if (next) issue_k(t + 1);
                     wait_tiles<G::CPT / 2>(next ? 1 : 0);                       // V; the next K may be on its way
                     if (partial) odd |= clean_values<T>(tile + G::kTileV, G::TK, k0, c1, units, lane);
-                    if (some) block_values<T>(w[0], tile + G::kTileV, p, lane);
+                    if (some) block_values<T, G::kSplit>(w[0], tile + G::kTileV, p, false, lane);
                     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // V is read
                     if (next) issue_v(t + 1);
                 }
@@ -953,7 +971,7 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(Att
                 for (int pass = 0; pass < 2; ++pass) {
                     restart(pass > 0);
                     issue_first();
-                    careful();
+                    careful(false);
                     const bool far = overflown();
                     __syncthreads();
                     if (lane == 0) s_redo[wave] = far;
@@ -1445,8 +1463,8 @@ void attend_plan(AttendArgs* a) {
     };
     // Narrow workgroups start and end sooner, wide ones read less from L2 and LDS per row: narrow up to 64
     // rows and, in bf16, where each of 512 workgroups has few slots, fewer if that takes more than a round.  (16
-    // heads: 1,000 tokens over 1,000 slots, 1,000 slots each, 13.5 us narrow, 23.3 wide; 400 over 5,000, 2,000 each,
-    // 29.5 and 34; 200 over 20,000, 4,400 each, 49 and 41; 1,374 over themselves, 1,850 each in 1.3 rounds, 37 and
+    // heads: 1,000 tokens over 1,000 slots, 1,000 slots each, 15.9 us narrow, 23.3 wide; 400 over 5,000, 2,000 each,
+    // both 34; 200 over 20,000, 4,400 each, 49 and 41; 1,374 over themselves, 1,850 each in 1.3 rounds, 37 and
     // 29.  fp32, whose wide kernel has the faster products: 64 over 20,000 56 and 57, 90 over 20,000 80 and
     // 61, 200 over 600 22 and 18; 90 over 300 13.3 and 15.8.)
     double items = work_items(32, false);

@@ -1,9 +1,10 @@
 """More of the paged key-value cache on the GPU against the 64-bit computations of test_gpu_cache.py, with
 its tolerances: u = 2^-24, a row's E, one bf16 rounding up to 2^-8 of a value."""
+import numpy as np
 import pytest
 import torch
 
-from test_gpu_cache import BF, F32, Pool, _gpu, cache, check_attend, gen, log, normal  # noqa: F401
+from test_gpu_cache import BF, BFU, F32, U, Pool, _gpu, attend64, cache, check_attend, gen, log, normal  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -21,3 +22,26 @@ def test_attend_values_near_the_largest(cache, lens, qs, Hq, Hkv, page, dtype, c
         v[:, :, :4] = normal(821 + b, (n, Hkv, 4), F32).clamp(-3, 3) * 1e38     # of either sign in the first features
         pool.put(b, pool.k[b], v.to(dtype))
     check_attend(cache, pool, normal(822, (sum(qs), Hq, 64), dtype), qs, causal)
+
+
+@pytest.mark.parametrize("lens,qs,Hq,Hkv,page,causal", [
+    ([3], [1], 16, 16, 16, True), ([40, 31, 64], [1, 1, 1], 16, 4, 16, True), ([300], [1], 16, 16, 64, True),
+    ([90, 5, 200, 0], [1, 1, 0, 0], 16, 8, 32, False), ([120], [20], 3, 1, 64, True), ([64, 257], [33, 1], 2, 2, 16, False)])
+def test_attend_bf16_rows_to_the_outputs_rounding(cache, lens, qs, Hq, Hkv, page, causal):  # noqa: F811
+    """Up to 64 rows of a key head: the probabilities of the value product as sums of two bf16 values, each within
+    2^-16, so that beside fp32's errors only the output's rounding is left."""
+    log("attend bf16 two parts %s %s" % (lens, qs))
+    pool = Pool(cache, lens, Hkv, page, BF, seed=800 + sum(lens))
+    Q = normal(801, (sum(qs), Hq, 64), BF)
+    O, _ = cache.attend(pool.cuda(), pool.batch(qs), Q.cuda(), causal)
+    O, t = O.cpu().double().numpy(), 0
+    for b, m in enumerate(qs):
+        n = pool.lens[b]
+        vis = np.clip(n - m + np.arange(m) + 1, 0, n) if causal else np.full(m, n)
+        for h in range(Hq if m else 0):
+            ro, rl, _, A, X = attend64(Q[t:t + m, h], pool.k[b][:, h * Hkv // Hq], pool.v[b][:, h * Hkv // Hq], vis)
+            E = (64 * X + n / 16 + 16 + np.abs(rl)) * U
+            tol = (2 * E[:, None] + 2.0 ** -16) * A
+            tol += BFU * (np.abs(ro) + tol)
+            assert (np.abs(O[t:t + m, h] - ro) <= tol).all(), (b, h)
+        t += m
