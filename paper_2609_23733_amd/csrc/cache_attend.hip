@@ -1006,6 +1006,7 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(Att
             if (row0 + 32 * nb + l31 >= nrows) return;
             float inv, lse;
             row_result(w[nb].m, w[nb].l, &inv, &lse);
+            if (inv == 0.f) w[nb].o[0] = w[nb].o[1] = zero_f32x16();   // no weight on any values
             if (a.nsplit > 1) {
                 float* po = a.part + (split * all_rows + orow[nb]) * kD;
                 if (hh == 0) {
@@ -1087,7 +1088,7 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(Att
                 for (int g = 0; g < 4; ++g) {
                     f32x4 v;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = w[0].o[m][4 * g + e] * f;
+                    for (int e = 0; e < 4; ++e) v[e] = f == 0.f ? 0.f : w[0].o[m][4 * g + e] * f;   // (any values)
                     *(f32x4*)(so + (wave * 32 + l31) * kRow + 32 * m + 8 * g + 4 * hh) = v;
                 }
         }

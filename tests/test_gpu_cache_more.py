@@ -45,3 +45,23 @@ def test_attend_bf16_rows_to_the_outputs_rounding(cache, lens, qs, Hq, Hkv, page
             tol += BFU * (np.abs(ro) + tol)
             assert (np.abs(O[t:t + m, h] - ro) <= tol).all(), (b, h)
         t += m
+
+
+@pytest.mark.parametrize("lens,qs,H,page,dtype", [
+    ([70], [2], 2, 16, BF), ([5000, 3], [1, 1], 2, 64, BF), ([5000, 3], [1, 1], 2, 64, F32), ([700], [130], 2, 32, F32),
+    ([1374, 1374], [1374, 1374], 8, 64, BF)])
+def test_attend_only_logits_of_minus_infinity_over_any_values(cache, lens, qs, H, page, dtype):  # noqa: F811
+    """A row whose logits are all -inf gives zeros, also where the values are not finite; the other heads' rows
+    are not touched."""
+    log("attend -inf logits over NaN values %s %s %s" % (lens, qs, dtype))
+    pool = Pool(cache, lens, H, page, dtype, seed=840 + sum(lens))
+    Q = normal(841, (sum(qs), H, 64), dtype)
+    Q[:, 0, 2] = 1.0
+    for b, n in enumerate(lens):
+        k, v = pool.k[b].clone(), pool.v[b].clone()
+        k[:, 0, 2] = float("-inf")
+        v[::3, 0], v[1::3, 0] = float("nan"), float("inf")
+        pool.put(b, k, v)
+    O, lse = cache.attend(pool.cuda(), pool.batch(qs), Q.cuda(), True)
+    assert (O[:, 0] == 0).all() and torch.isneginf(lse[:, 0]).all()
+    assert torch.isfinite(O[:, 1:]).all() and torch.isfinite(lse[:, 1:]).all()
