@@ -182,8 +182,8 @@ def append(pc: PagedCache, batch: Batch, Q, K, V, pos=None, rot: Optional[Rotary
         if Q_out is None:
             Q_out = torch.empty(T, Hq, HEAD_DIM, dtype=dt, device=Q.device)
         qo = _whole(Q_out, "Q_out", (T, Hq, HEAD_DIM), dt)
-    if rot is not None and pos is None:
-        raise ValueError("a rotation needs positions")
+    if (rot is None) != (pos is None):
+        raise ValueError("a rotation needs positions" if pos is None else "positions need a rotation (rot)")
     _done(load_library().vp_cache_append(pc._ref, batch._for(T), Hq, q, qs, K.data_ptr(), ks, V.data_ptr(), vs,
                                          None if rot is None else rot.at(pos, T), qo, _stream()),
           "vp_cache_append")
@@ -273,6 +273,10 @@ class StreamLayer:
                  recent: int = 0, causal: bool = False, rot: Optional[Rotary] = None,
                  device="cuda"):
         Hkv = Hq if Hkv is None else Hkv
+        if Hkv < 1 or Hq < Hkv or Hq % Hkv:
+            raise ValueError("%d query heads for %d key heads" % (Hq, Hkv))
+        if min(B, keep, max_chunk) < 1 or min(sink, recent) < 0:
+            raise ValueError("B, keep and max_chunk must be at least 1, sink and recent at least 0")
         pages = -(-(keep + max_chunk) // page)
         self.B, self.Hq, self.keep, self.max_chunk = B, Hq, keep, max_chunk
         self.sink, self.recent, self.causal, self.rot = sink, recent, causal, rot
@@ -288,6 +292,8 @@ class StreamLayer:
         """Q [T, Hq, 64], K, V [T, Hkv, 64]: the chunks of the sequences, one after the other,
         counts[b] tokens each (equal parts when not given).  Returns O [T, Hq, 64]."""
         T = Q.shape[0]
+        if Q.dim() != 3 or Q.shape[1] != self.Hq:
+            raise ValueError("Q has shape %s, the layer %d heads" % (tuple(Q.shape), self.Hq))
         if counts is None:
             if T % self.B:
                 raise ValueError("%d tokens for %d sequences: give counts" % (T, self.B))

@@ -65,3 +65,35 @@ def test_attend_only_logits_of_minus_infinity_over_any_values(cache, lens, qs, H
     O, lse = cache.attend(pool.cuda(), pool.batch(qs), Q.cuda(), True)
     assert (O[:, 0] == 0).all() and torch.isneginf(lse[:, 0]).all()
     assert torch.isfinite(O[:, 1:]).all() and torch.isfinite(lse[:, 1:]).all()
+
+
+# ------------------------------------------------------------------ the stream layer
+
+def test_stream_layer_refuses_other_heads_and_idle_positions(cache):  # noqa: F811
+    """Queries of another number of heads, also one that the key heads divide, and positions that nothing would
+    turn; the layer stays as it was.  Numbers that no step could work with are refused when the layer is made."""
+    log("stream layer refusals")
+    layer = cache.StreamLayer(1, keep=60, max_chunk=40, Hq=4, Hkv=2, page=16)
+    Q, K, V = (normal(860 + i, (20, h, 64)).cuda() for i, h in enumerate((8, 2, 2)))
+    pos = torch.arange(20, dtype=torch.int32, device="cuda")[:, None]
+    layer.step(Q[:, :4], K, V)
+    state = lambda: [t.view(torch.uint8).clone() for t in (layer.pc.K, layer.pc.V, layer.pc.weight, layer.pc.stamp)]
+    held = state()     # (as bytes: slots not in use may hold NaN)
+    for bad in (Q[:, :2], Q, Q[:, :6]):
+        with pytest.raises(ValueError, match="heads"):
+            layer.step(bad, K, V)
+    with pytest.raises(ValueError, match="rot"):
+        layer.step(Q[:, :4], K, V, pos)
+    assert layer.lens == [20] and layer.length.tolist() == [20] and layer.seen.tolist() == [20]
+    assert all(torch.equal(a, b) for a, b in zip(held, state()))
+    for bad in (dict(keep=0), dict(max_chunk=0), dict(sink=-1), dict(recent=-1), dict(Hq=6, Hkv=4), dict(Hq=2, Hkv=4), dict(B=0)):
+        with pytest.raises(ValueError):
+            cache.StreamLayer(**dict(dict(B=1, keep=60, max_chunk=40, Hq=4, Hkv=2, page=16), **bad))
+
+
+def test_append_refuses_positions_without_rotation(cache):  # noqa: F811
+    log("append positions without rotation")
+    pool = Pool(cache, [40], 2, 16, BF, seed=870)
+    pc, x = pool.cuda(), normal(871, (5, 2, 64)).cuda()
+    with pytest.raises(ValueError, match="rot"):
+        cache.append(pc, pool.batch([5], [40]), x, x, x, pos=torch.zeros(5, 1, dtype=torch.int32, device="cuda"))
