@@ -1,7 +1,7 @@
 """Paged key-value cache: exact attention of views that arrive one after another.
 
 Binding of the vp_rotary* and vp_cache_* calls of include/vggt_prime.h, in the manner of vp.py
-(argument checks and marshalling; every step runs in the library's kernels, on the current torch
+(argument checks and marshalling; the operators run in the library's kernels, on the current torch
 stream, without synchronising), and StreamLayer, which runs them together.
 
 Handles: a PagedCache names the pool, a Batch the sequences of a call.  Both hold
@@ -266,7 +266,10 @@ class StreamLayer:
     B sequences of chunks up to `max_chunk` tokens.  `sink` first tokens (the first view, which the
     scene's frame of reference hangs on) and the `recent` latest ones are kept whatever
     weight they have.  `causal`: a token sees its own chunk up to itself, not all of
-    it.  `rot`: positions given to step() are applied to Q and K."""
+    it.  `rot`: positions given to step() are applied to Q and K.
+
+    A step is enqueued on the current stream without waiting for it.  Its chunks' starts and bounds
+    are the host's, so a captured step would repeat those of the capture."""
 
     def __init__(self, B: int, keep: int, max_chunk: int, Hq: int = vp.MAX_HEADS,
                  Hkv: Optional[int] = None, page: int = 64, dtype=torch.bfloat16, sink: int = 0,
@@ -305,7 +308,8 @@ class StreamLayer:
         start = [0]
         for c in counts:
             start.append(start[-1] + c)
-        q_start = torch.tensor(start, dtype=torch.int32).to(Q.device)
+        # (from pinned memory, which torch holds until the copy is done: the host does not wait)
+        q_start = torch.tensor(start, dtype=torch.int32, pin_memory=True).to(Q.device, non_blocking=True)
         new = q_start[1:] - q_start[:-1]
         # (the layer's own counts change once the chunk is in: a refused one leaves it as it was)
         length, seen = self.length + new, self.seen + new

@@ -97,3 +97,31 @@ def test_append_refuses_positions_without_rotation(cache):  # noqa: F811
     pc, x = pool.cuda(), normal(871, (5, 2, 64)).cuda()
     with pytest.raises(ValueError, match="rot"):
         cache.append(pc, pool.batch([5], [40]), x, x, x, pos=torch.zeros(5, 1, dtype=torch.int32, device="cuda"))
+
+
+def test_stream_layer_does_not_wait(cache):  # noqa: F811
+    """A step is enqueued without waiting for the stream, with equal chunks and others, with and without an
+    eviction, and its results do not depend on how far ahead the host is."""
+    log("stream layer does not wait")
+    rot = cache.Rotary.make(64, 10000.0)
+    steps = []
+    for i, counts in enumerate([[30, 10], [20, 20], [7, 33], [40, 1], None, [1, 1]]):
+        T = 40 if counts is None else sum(counts)
+        x = [normal(880 + 3 * i + j, (T, 4, 64)).cuda() for j in range(3)]
+        steps.append((x, torch.arange(T, dtype=torch.int32, device="cuda")[:, None], counts))
+    ahead, waiting = (cache.StreamLayer(2, keep=60, max_chunk=40, Hq=4, page=16, rot=rot) for _ in range(2))
+    for x, pos, counts in steps[:2]:      # (workspaces grow in the first steps)
+        assert torch.equal(ahead.step(*x, pos, counts), waiting.step(*x, pos, counts))
+    busy = normal(879, (4096, 4096)).cuda()
+    torch.cuda.synchronize()
+    for _ in range(8):
+        busy = busy @ busy
+    torch.cuda.set_sync_debug_mode("error")
+    try:
+        got = [ahead.step(*x, pos, counts) for x, pos, counts in steps[2:]]
+    finally:
+        torch.cuda.set_sync_debug_mode("default")
+    for (x, pos, counts), O in zip(steps[2:], got):
+        want = waiting.step(*x, pos, counts)
+        torch.cuda.synchronize()
+        assert torch.equal(O, want)
