@@ -105,7 +105,12 @@ class Rotary:
 
 def rotary(x, pos, rot: Rotary, out: Optional[torch.Tensor] = None, transpose: bool = False):
     """x [T, H, 64] with the features turned by their positions; with `transpose` the gradient's
-    map.  `out` may be x."""
+    map.  `out` may be x.  An x that requires gradients gets them (no `out` then); the cache's
+    operators below have none."""
+    if torch.is_grad_enabled() and (x.requires_grad or (out is not None and out.requires_grad)):
+        if out is not None:
+            raise ValueError("out would not be part of the gradient's graph")
+        return _Rotation.apply(x, pos, rot, transpose)
     T, H = x.shape[0], x.shape[1]
     xs = _rows(x, "x", T, H, x.dtype)
     if out is None:
@@ -114,6 +119,21 @@ def rotary(x, pos, rot: Rotary, out: Optional[torch.Tensor] = None, transpose: b
     _done(load_library().vp_rotary(rot.at(pos, T), _dt(x), T, H, x.data_ptr(), xs, out.data_ptr(), ys,
                                    transpose, _stream()), "vp_rotary")
     return out
+
+
+class _Rotation(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, pos, rot, transpose):
+        ctx.save_for_backward(pos)
+        ctx.rot, ctx.transpose = rot, bool(transpose)
+        return rotary(x, pos, rot, None, transpose)
+
+    @staticmethod
+    def backward(ctx, g):
+        pos, = ctx.saved_tensors
+        if not g.is_contiguous() or g.data_ptr() % 16:     # (broadcast, or a part of something)
+            g = g.clone(memory_format=torch.contiguous_format)
+        return rotary(g, pos, ctx.rot, None, not ctx.transpose), None, None, None
 
 
 class PagedCache:

@@ -125,3 +125,38 @@ def test_stream_layer_does_not_wait(cache):  # noqa: F811
         want = waiting.step(*x, pos, counts)
         torch.cuda.synchronize()
         assert torch.equal(O, want)
+
+
+# ------------------------------------------------------------------ rotary
+
+@pytest.mark.parametrize("dtype,layout,axes", [(F32, "half", 2), (BF, "interleaved", 1)])
+@pytest.mark.parametrize("transpose", [False, True])
+def test_rotary_in_a_graph(cache, dtype, layout, axes, transpose):  # noqa: F811
+    """An input that requires gradients gets the transposed map of the output's, also of one that is
+    broadcast or lies apart, and the gradient's gradient; `out` would leave the graph and is refused."""
+    log("rotary in a graph %s %s" % (dtype, layout))
+    rot = cache.Rotary.make(32, 100.0, axes, layout, "parts", 4.0, 64.0)
+    pos = torch.randint(0, 500, (9, axes), generator=gen(890)).to(torch.int32).cuda()
+    fused = normal(891, (9, 6, 64), dtype).cuda().requires_grad_()
+    x = fused[:, 1:4]
+    g = normal(892, (9, 6, 64), dtype).cuda()[:, 2:5]
+    y = cache.rotary(x, pos, rot, transpose=transpose)
+    with torch.no_grad():
+        assert torch.equal(y, cache.rotary(x, pos, rot, transpose=transpose)) and y.requires_grad
+        want = cache.rotary(g, pos, rot, transpose=not transpose)
+        ones = cache.rotary(torch.ones_like(y), pos, rot, transpose=not transpose)
+    dx, = torch.autograd.grad(y, fused, g, retain_graph=True)
+    assert torch.equal(dx[:, 1:4], want) and (dx[:, :1] == 0).all() and (dx[:, 4:] == 0).all()
+    odd = torch.empty(g.numel() + 1, dtype=dtype, device="cuda")[1:].view_as(g).copy_(g)
+    dx, = torch.autograd.grad(y, fused, odd, retain_graph=True)
+    assert torch.equal(dx[:, 1:4], want)
+    dx, = torch.autograd.grad(y.float().sum(), fused, retain_graph=True)
+    assert torch.equal(dx[:, 1:4], ones)
+    h = g.detach().clone().requires_grad_()
+    dx, = torch.autograd.grad(y, fused, h, create_graph=True)
+    dh, = torch.autograd.grad(dx[:, 1:4], h, g)
+    with torch.no_grad():
+        assert torch.equal(dh, cache.rotary(g, pos, rot, transpose=transpose))
+    for kw in (dict(x=x, out=torch.empty_like(y).detach()), dict(x=x.detach(), out=h)):
+        with pytest.raises(ValueError, match="gradient"):
+            cache.rotary(pos=pos, rot=rot, **kw)
