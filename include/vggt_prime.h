@@ -480,6 +480,16 @@ vp_status vp_cache_append(const vp_cache *cache, const vp_cache_batch *batch, in
  * smaller batch can need more, as its slots are divided further; one that is too small is refused. */
 size_t vp_cache_attend_workspace_bytes(const vp_cache *cache, const vp_cache_batch *batch,
                                        int32_t Hq);
+
+/* How a call with these bounds is computed (host only): workgroups of `rows` rows of a key head, 32 of
+ * which the four waves split the slots, or more that share them (`shared`); their number for the
+ * largest chunk; the ranges that the slots are divided into, and the slots of one; whether
+ * the weights are gathered from logits that the attention keeps, or formed again. */
+typedef struct {
+    int32_t shared, rows, row_tiles, ranges, range_slots, logits_kept;
+} vp_cache_plan;
+vp_status vp_cache_attend_plan(const vp_cache *cache, const vp_cache_batch *batch, int32_t Hq,
+                               vp_cache_plan *plan);
 vp_status vp_cache_attend(const vp_cache *cache, const vp_cache_batch *batch, int32_t Hq,
                           const void *Q, int64_t q_stride, int32_t causal, float scale, void *O,
                           float *lse, float *weight_out, void *ws, size_t ws_bytes,

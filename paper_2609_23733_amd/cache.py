@@ -217,6 +217,14 @@ def attend_workspace(pc: PagedCache, batch: Batch, Hq: int, T: int) -> torch.Ten
     return torch.empty(n, dtype=torch.uint8, device=pc.K.device)
 
 
+def attend_plan(pc: PagedCache, batch: Batch, Hq: int, T: int) -> vp.vp_cache_plan:
+    """How a call with these bounds is computed (see vp_cache_plan)."""
+    plan = vp.vp_cache_plan()
+    _done(load_library().vp_cache_attend_plan(pc._ref, batch._for(T), int(Hq), ctypes.byref(plan)),
+          "vp_cache_attend_plan")
+    return plan
+
+
 def attend(pc: PagedCache, batch: Batch, Q, causal: bool = True, scale: float = 0.0,
            O: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
            weight_out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):

@@ -1470,7 +1470,7 @@ void attend_plan(AttendArgs* a) {
     // 61, 200 over 600 22 and 18; 90 over 300 13.3 and 15.8.)
     double items = work_items(32, false);
     a->wide = rows > 64 && (!bf || items * a->c.max_len > 512. * (items > 512 ? 1500 : 2500));
-    if (a->wide) items = work_items(bf ? Geo<bf16, true>::RT : Geo<float, true>::RT, true);
+    if (a->wide) items = work_items(attend_rows(*a), true);
     // Time of a division into ns ranges, in us: the slots of a workgroup and its start, in units of
     // slots, times the rounds of workgroups that run together, or, ragged and more than a round, all the work and
     // a last workgroup; the join, a launch, and what it reads per range.  (300 slots, a token, bf16: 8.3 us
@@ -1494,6 +1494,12 @@ void attend_plan(AttendArgs* a) {
     a->logit_stride = (a->c.max_len + 63) / 64 * 64;
     a->nsplit = (int)((a->c.max_len + a->chunk - 1) / a->chunk);
     if (a->nsplit < 1) a->nsplit = 1;
+}
+
+// Rows per workgroup.
+int attend_rows(const AttendArgs& a) {
+    if (a.c.dtype == DT_BF16) return a.wide ? Geo<bf16, true>::RT : Geo<bf16, false>::RT;
+    return a.wide ? Geo<float, true>::RT : Geo<float, false>::RT;
 }
 
 size_t attend_part_rows(const AttendArgs& a) {

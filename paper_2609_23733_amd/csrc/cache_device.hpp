@@ -98,6 +98,7 @@ void launch_rotary(int dtype, const void* x, int64_t x_stride, void* y, int64_t 
                    int H, const RotArgs& r, hipStream_t st);
 void launch_cache_append(const AppendArgs& a, const RotArgs& r, hipStream_t st);
 void attend_plan(AttendArgs* a);
+int attend_rows(const AttendArgs& a);
 size_t attend_part_rows(const AttendArgs& a);
 size_t attend_logits(const AttendArgs& a);
 void launch_cache_attend(const AttendArgs& a, hipStream_t st);

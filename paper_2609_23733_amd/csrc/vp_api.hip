@@ -990,6 +990,16 @@ size_t vp_cache_attend_workspace_bytes(const vp_cache* cache, const vp_cache_bat
     return attend_args(cache, batch, Hq, &a) == VP_OK ? attend_ws(a) : 0;
 }
 
+vp_status vp_cache_attend_plan(const vp_cache* cache, const vp_cache_batch* batch, int32_t Hq,
+                               vp_cache_plan* plan) {
+    vp::AttendArgs a;
+    vp_status st = attend_args(cache, batch, Hq, &a);
+    if (st != VP_OK) return st;
+    if (!plan) return VP_ERR_INVALID_ARG;
+    *plan = {a.wide, vp::attend_rows(a), a.row_tiles, a.nsplit, a.chunk, vp::attend_logits(a) ? 1 : 0};
+    return VP_OK;
+}
+
 vp_status vp_cache_attend(const vp_cache* cache, const vp_cache_batch* batch, int32_t Hq,
                           const void* Q, int64_t q_stride, int32_t causal, float scale, void* O,
                           float* lse, float* weight_out, void* ws, size_t ws_bytes, void* stream) {

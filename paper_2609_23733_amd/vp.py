@@ -36,7 +36,7 @@ EXPORTS = ("vp_workspace_bytes", "vp_router_score", "vp_router_score_noalloc",
            "vp_teacher_targets", "vp_router_loss", "vp_latent_loss", "vp_tome_split",
            "vp_tome_workspace_bytes", "vp_tome_plan", "vp_tome_merge", "vp_tome_merge_qkv",
            "vp_tome_unmerge", "vp_rotary_frequencies", "vp_rotary", "vp_cache_append",
-           "vp_cache_attend_workspace_bytes", "vp_cache_attend",
+           "vp_cache_attend_workspace_bytes", "vp_cache_attend_plan", "vp_cache_attend",
            "vp_cache_evict_workspace_bytes", "vp_cache_evict")
 TOME_SPECIAL = 5   # special tokens per view (camera + registers), never merged
 MODEL_DIM = MAX_HEADS * HEAD_DIM
@@ -86,6 +86,10 @@ class vp_cache_batch(ctypes.Structure):
     _fields_ = [("table", ctypes.c_void_p), ("length", ctypes.c_void_p), ("seen", ctypes.c_void_p),
                 ("q_start", ctypes.c_void_p), ("B", ctypes.c_int32), ("max_pages", ctypes.c_int32),
                 ("T", ctypes.c_int32), ("max_q", ctypes.c_int32), ("max_len", ctypes.c_int32)]
+
+
+class vp_cache_plan(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_int32) for f in ("shared", "rows", "row_tiles", "ranges", "range_slots", "logits_kept")]
 
 
 class vp_rotary_spec(ctypes.Structure):
@@ -162,12 +166,13 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.vp_cache_append.argtypes = [cch, cba, i32, P, i64, P, i64, P, i64, rsp, P, P]
     lib.vp_cache_attend_workspace_bytes.argtypes = [cch, cba, i32]
     lib.vp_cache_attend_workspace_bytes.restype = ctypes.c_size_t
+    lib.vp_cache_attend_plan.argtypes = [cch, cba, i32, ctypes.POINTER(vp_cache_plan)]
     lib.vp_cache_attend.argtypes = [cch, cba, i32, P, i64, i32, f32, P, P, P, P, ctypes.c_size_t, P]
     lib.vp_cache_evict_workspace_bytes.argtypes = [i32, i32, i32]
     lib.vp_cache_evict_workspace_bytes.restype = ctypes.c_size_t
     lib.vp_cache_evict.argtypes = [cch, cba, i32, i32, i32, P, P, P, P, ctypes.c_size_t, P]
-    for f in ("vp_rotary_frequencies", "vp_rotary", "vp_cache_append", "vp_cache_attend",
-              "vp_cache_evict"):
+    for f in ("vp_rotary_frequencies", "vp_rotary", "vp_cache_append", "vp_cache_attend_plan",
+              "vp_cache_attend", "vp_cache_evict"):
         getattr(lib, f).restype = ctypes.c_int
     for f in ("vp_router_score", "vp_router_score_noalloc", "vp_router_logits", "vp_assign_heads",
               "vp_routed_global_attention", "vp_gather_full_heads", "vp_full_head_attention",
