@@ -262,3 +262,143 @@ def test_attend_wide_graph_replays(cache, dtype):  # noqa: F811
         for a, b in zip(want, (O, lse, W2)):
             assert torch.equal(a, b), r
         ws.random_(0, 255)     # the workspace holds nothing from call to call
+
+
+# ------------------------------------------------------------------ eviction in six launches
+
+def keep64(w, safe, keep):
+    """Indices that stay: the protected ones, then NaN, then by weight; lower ones among equals."""
+    n, nan = len(w), np.isnan(w)
+    group = np.where(safe, 0, np.where(nan, 1, 2))
+    order = np.lexsort((np.arange(n), np.where(group < 2, 0.0, -w.astype(np.float64)), group))
+    return np.sort(order[:min(n, keep)])
+
+
+def evict64(pool, seen, keep, sink, recent):
+    """The pool after the eviction (CPU): (K, V, W, S, lengths)."""
+    K, V, W, S = pool.K.clone(), pool.V.clone(), pool.W.clone(), pool.S.clone()
+    left = [min(n, keep) for n in pool.lens]
+    for b, n in enumerate(pool.lens):
+        p, s = pool.at(b, n)
+        for h in range(pool.Hkv):
+            st = pool.S[p, h, s].numpy().astype(np.int64)
+            kept = keep64(pool.W[p, h, s].numpy(), (st < sink) | (st >= seen[b] - recent), keep)
+            src = torch.from_numpy(kept[kept >= left[b]])
+            dst = torch.from_numpy(np.setdiff1d(np.arange(left[b]), kept))
+            assert len(src) == len(dst)
+            for x, y in ((K, pool.K), (V, pool.V), (W, pool.W), (S, pool.S)):
+                x[p[dst], h, s[dst]] = y[p[src], h, s[src]]
+    return K, V, W, S, left
+
+
+# Past 40,960 slots: their keys do not fit the LDS of a workgroup.
+LONG = [
+    # lens, keep, sink, recent, Hkv, page, dtype, kind of weights
+    ([45000, 700, 20481], 9001, 5, 257, 2, 64, BF, "ties"), ([45000, 700, 20481], 9001, 0, 0, 2, 16, F32, "odd"),
+    ([43001], 43000, 0, 0, 3, 32, BF, "plain"), ([49152, 49152], 24576, 1374, 1374, 1, 128, BF, "equal"),
+    ([50003, 0, 50003], 1, 0, 0, 1, 256, F32, "ties"), ([61440, 4096], 4096, 6000, 0, 1, 64, BF, "odd"),
+    ([41001, 41001, 12000], 30005, 0, 35000, 2, 64, F32, "equal"), ([43000, 5], 43000, 2, 2, 1, 64, BF, "ties"),
+]
+
+
+def long_pool(c, lens, Hkv, page, dtype, kind, sink):
+    from test_gpu_cache import weights_of
+    pool = Pool(c, lens, Hkv, page, dtype, seed=70, junk=0.5)
+    pool.W = weights_of(kind, pool.W.shape, 71)
+    for b, n in enumerate(lens):
+        p, s = pool.at(b, n)
+        for h in range(Hkv):
+            o = torch.randperm(n, generator=gen(72 + b + 10 * h))
+            pool.S[p, h, s] = torch.where(o < sink, o, o + n // 2).to(torch.int32)
+    return pool
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("lens,keep,sink,recent,Hkv,page,dtype,kind", LONG)
+def test_evict_long(cache, lens, keep, sink, recent, Hkv, page, dtype, kind, in_place):  # noqa: F811
+    log("evict long %s keep=%d sink=%d recent=%d %s" % (lens, keep, sink, recent, kind))
+    pool = long_pool(cache, lens, Hkv, page, dtype, kind, sink)
+    seen = [n + n // 2 for n in lens]
+    pc, length = pool.cuda(), i32(lens)
+    K, V, W, S, left = evict64(pool, seen, keep, sink, recent)
+    ws = cache.evict_workspace(pc, len(lens), max(lens))
+    ws.random_(0, 255)
+    if in_place:
+        wo, so, lo = pool.gW, pool.gS, length
+        cache.evict(pc, pool.gtable, length, i32(seen), keep, max(lens), sink, recent, ws=ws)
+    else:
+        wo, so, lo = torch.full_like(pool.gW, 3.0), torch.full_like(pool.gS, -9), torch.zeros_like(length)
+        cache.evict(pc, pool.gtable, length, i32(seen), keep, max(lens), sink, recent, wo, so, lo, ws)
+        assert torch.equal(pool.gW.cpu().view(torch.int32), pool.W.view(torch.int32))
+    assert lo.tolist() == left
+    assert torch.equal(pool.gK.cpu(), K) and torch.equal(pool.gV.cpu(), V)
+    wo, so, rest = wo.cpu(), so.cpu(), torch.ones(W.shape, dtype=torch.bool)
+    for b, n in enumerate(left):
+        p, s = pool.at(b, n)
+        assert torch.equal(wo[p, :, s].view(torch.int32), W[p, :, s].view(torch.int32)), b
+        assert torch.equal(so[p, :, s], S[p, :, s]), b
+        rest[p, :, s] = False
+    if not in_place:       # nothing but the slots that stay is written
+        assert (wo[rest] == 3.0).all() and (so[rest] == -9).all()
+
+
+def test_evict_long_graph_replays(cache):  # noqa: F811
+    """Captured, with a workspace that holds something else before every replay."""
+    log("evict long graph")
+    lens, keep = [45000, 9000], 12000
+    pool = long_pool(cache, lens, 2, 64, BF, "ties", 3)
+    pc = pool.cuda()
+    length, seen, lo = i32(lens), i32([n + n // 2 for n in lens]), i32([0, 0])
+    wo, so, ws = pool.gW.clone(), pool.gS.clone(), cache.evict_workspace(pc, 2, 45000)
+    go = lambda: cache.evict(pc, pool.gtable, length, seen, keep, 45000, 3, 64, wo, so, lo, ws)
+    K, V, W, S, left = evict64(pool, seen.tolist(), keep, 3, 64)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        go()
+    torch.cuda.current_stream().wait_stream(side)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        go()
+    for k in range(4):
+        pool.gK.copy_(pool.K)
+        pool.gV.copy_(pool.V)
+        wo.fill_(3.0), so.fill_(-9), lo.zero_()
+        ws.random_(0, 255)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(pool.gK.cpu(), K) and torch.equal(pool.gV.cpu(), V) and lo.tolist() == left, k
+        for b, n in enumerate(left):
+            p, s = pool.at(b, n)
+            assert torch.equal(wo.cpu()[p, :, s], W[p, :, s]) and torch.equal(so.cpu()[p, :, s], S[p, :, s]), k
+
+
+# ------------------------------------------------------------------ rotary positions past the caches
+
+@pytest.mark.parametrize("T,H,dtype,dim,axes,layout", [
+    (33001, 16, BF, 64, 2, "half"), (33001, 16, BF, 48, 1, "interleaved"), (17003, 16, F32, 64, 1, "interleaved"),
+    (17003, 16, F32, 40, 1, "half"), (44001, 3, F32, 12, 1, "half"), (44001, 3, F32, 20, 2, "interleaved")])
+def test_rotary_large(cache, T, H, dtype, dim, axes, layout):  # noqa: F811
+    """Outputs of more than 64 MiB (bf16), 33 MiB: stored past the caches; the transpose in place, rows that
+    lie apart and (fp32) start 16, not 32 bytes into one another's multiples."""
+    from test_gpu_cache import radians, rot_tol, rotate64
+    log("rotary large T=%d H=%d %s dim=%d %s" % (T, H, dtype, dim, layout))
+    assert T * H * 64 * (2 if dtype == BF else 4) > 32 << 20
+    rot = cache.Rotary.make(dim, 10000.0, axes, layout, "linear", 8.0)
+    step = 16 // (2 if dtype == BF else 4)
+    room = torch.zeros(T * (H * 64 + step) + step, dtype=dtype, device="cuda")
+    x = room[step:].view(T, H * 64 + step)[:, :H * 64].unflatten(1, (H, 64))
+    x.copy_(normal(T, (T, H, 64), dtype))
+    pos = torch.randint(-(1 << 20), 1 << 20, (T, axes), generator=gen(T)).to(torch.int32).cuda()
+    before = x.clone()
+    f = radians(rot)
+    ref = rotate64(before, pos, f, axes, layout, rot.mag)
+    y = cache.rotary(x, pos, rot)
+    assert ((y.double() - ref).abs() <= rot_tol(before, ref, rot.mag, dtype)).all()
+    assert torch.equal(y[:, :, dim:], before[:, :, dim:]) and torch.equal(x, before)
+    ref = rotate64(before, pos, f, axes, layout, rot.mag, -1.0)
+    assert cache.rotary(x, pos, rot, out=x, transpose=True) is x
+    assert ((x.double() - ref).abs() <= rot_tol(before, ref, rot.mag, dtype)).all()
+    assert torch.equal(x[:, :, dim:], before[:, :, dim:])
+    assert (room[:step] == 0).all() and (room[step:].view(T, -1)[:, H * 64:] == 0).all()
