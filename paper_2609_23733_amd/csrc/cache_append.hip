@@ -28,6 +28,18 @@ __device__ __forceinline__ void put(V* p, V v) {
     else *p = v;
 }
 
+// Eight features in a row, at a 16-byte boundary: 16 bytes at a time.
+template <bool NT, typename T>
+__device__ __forceinline__ void put8(T* p, typename Vec4<T>::type a, typename Vec4<T>::type b) {
+    if constexpr (sizeof(T) == 2) {
+        typedef T V8 __attribute__((__vector_size__(16)));
+        put<NT>((V8*)p, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+    } else {
+        put<NT>((typename Vec4<T>::type*)p, a);
+        put<NT>((typename Vec4<T>::type*)(p + 4), b);
+    }
+}
+
 // Sine and cosine of a fraction of a revolution, 32 bits: the nearest quarter turn from the top bits,
 // the rest, |x| <= pi / 4, by the Taylor series to x^9 and x^10 (errors 2e-9 and 2e-9 there).
 __device__ __forceinline__ void sincos_turn(uint32_t t, float* sn, float* cs) {
@@ -92,8 +104,7 @@ __device__ __forceinline__ void rotate8(const T* x, T* y, const Turn4& w, int lo
 #pragma unroll
     for (int e = 0; e < 4; ++e) ya[e] = (T)g[e], yb[e] = (T)g[4 + e];
     if (inter) {
-        typedef T V8 __attribute__((__vector_size__(8 * sizeof(T)), aligned(16)));
-        put<NT>((V8*)(y + lo), __builtin_bit_cast(V8, Pair{ya, yb}));
+        put8<NT>(y + lo, ya, yb);
     } else {
         put<NT>((V*)(y + lo), ya);
         put<NT>((V*)(y + hi), yb);
@@ -102,8 +113,11 @@ __device__ __forceinline__ void rotate8(const T* x, T* y, const Turn4& w, int lo
 
 template <typename T, bool NT>
 __device__ __forceinline__ void copy8(const T* x, T* y) {
-    typedef T V8 __attribute__((__vector_size__(8 * sizeof(T)), aligned(16)));
-    put<NT>((V8*)y, *(const V8*)x);
+    struct __attribute__((aligned(16))) Eight {
+        typename Vec4<T>::type a, b;
+    };
+    const Eight v = *(const Eight*)x;
+    put8<NT>(y, v.a, v.b);
 }
 
 // What a thread (chunk c of eight, token t) does to a head's row.
