@@ -192,7 +192,8 @@ __global__ __launch_bounds__(256) void k_rotary(const T* x, int64_t x_stride, T*
 }
 
 // Rows of a token: Q's heads (to Q_out), K's (to the page), V's (to the page, as they are).
-// 1,374 tokens of 16 + 16 + 16 heads, bf16: 7.2 us, 17 MB, its table entry and rows one after the other.
+// 1,374 tokens of 16 + 16 + 16 heads, bf16: 7.4 us, 17 MB.  Bound by the latency of a thread's rows one after the other:
+// Q_out may be Q, so no row is loaded before the last one's store.
 template <typename T, bool INTER>
 __global__ __launch_bounds__(256) void k_cache_append(AppendArgs a, RotArgs r, int hs) {
     const int b = blockIdx.y;

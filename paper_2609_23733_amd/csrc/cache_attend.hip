@@ -432,9 +432,11 @@ __device__ __forceinline__ void put_lse(const AttendArgs& a, int64_t row, float 
 }
 
 // A workgroup: RT rows of one key head and sequence over one range of its slots.  Narrow: bound by HBM
-// (tokens over 137,400 and 62,724 slots of 16 heads, bf16: 166 us, 4.9 TB/s).  Wide: by the vector units, a fused
-// product, a power, a sum and half a rounding per logit (1,374 tokens over 43,968 slots of 16 heads,
-// bf16: 262 us, 940 TFLOP/s; fp32, three prompts of 8.6 GFLOP: 66 us).
+// (tokens over 137,400 and 62,724 slots of 16 heads, bf16: 167 us, 4.9 TB/s).  Wide: by the issue of matrix and vector
+// instructions together, a fused product, a power, a sum and half a rounding per logit (1,374 tokens over 43,968 slots of
+// 16 heads, bf16: 260 us, 950 TFLOP/s, the SIMDs' cycles 58 % in vector instructions and 43 % in MFMAs;
+// kernel alone, after some 40 passes: the first ones run at lower clocks, 280-350.  fp32, three prompts of
+// 8.6 GFLOP: 63 us).
 template <typename T, bool WIDE>
 __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(AttendArgs a) {
     typedef Geo<T, WIDE> G;
@@ -1273,7 +1275,8 @@ __global__ __launch_bounds__(256) void k_cache_weight_rows(AttendArgs a) {
 // operand (a lane owns one slot), two waves for each 32 slots that take half a tile's rows each.
 // The rows stream through LDS as A with -lse in the accumulator's input (`off`, written with lse), so
 // that a result is the exponent itself.  Bound by the vector units (a product, a power and a sum
-// per logit: 1,374 tokens over 20,000 slots of 16 heads some 105 us).  Two tiles of 128 rows in LDS
+// per logit: 1,374 tokens over 43,968 slots of 16 heads 210 us; fp32, whose products are fp32 MFMAs,
+// 500 tokens of two heads each over 8,000 slots of eight 75 us).  Two tiles of 128 rows in LDS
 // let four workgroups share a compute unit; their waves fill each other's waits, and forming the products of
 // one block amid another's powers, or six workgroups with half the rows, gained nothing.
 // ------------------------------------------------------------------------
@@ -1471,9 +1474,11 @@ void attend_plan(AttendArgs* a) {
     double items = work_items(32, false);
     a->wide = rows > 64 && (!bf || items * a->c.max_len > 512. * (items > 512 ? 1500 : 2500));
     if (a->wide) items = work_items(attend_rows(*a), true);
-    // Time of a division into ns ranges, in us: the slots of a workgroup and its start, in units of
-    // slots, times the rounds of workgroups that run together, or, ragged and more than a round, all the work and
-    // a last workgroup; the join, a launch, and what it reads per range.  (300 slots, a token, bf16: 8.3 us
+    // An estimate that ranks divisions into ns ranges, in us where the card is lightly loaded (large calls, which HBM or
+    // all SIMDs at once bound, take up to three times as long: 50 for 167 us of tokens over 137,400 slots, 153
+    // for 260 of a view over 43,968): the slots of a workgroup and its start, in units of slots, times the rounds of
+    // workgroups that run together, or, ragged and more than a round, all the work and a last workgroup; the join, a
+    // launch, and what it reads per range.  (300 slots, a token, bf16: 8.3 us
     // in one range, 11.1 in three; 1,000 slots, 200 tokens: 25 in one, 17 in eight; 30 sequences of up to
     // 102 tokens and 8,333 slots: 140 in one, 115 in eight, 131 in sixteen.)
     const double slot = a->wide ? (bf ? 0.016 : 0.038) : (bf ? 0.006 : 0.019);
