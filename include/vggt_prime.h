@@ -471,7 +471,8 @@ vp_status vp_cache_append(const vp_cache *cache, const vp_cache_batch *batch, in
  * logits of -inf, gives zeros and -inf; slots a row does not see never reach it,
  * whatever they hold.  With weight_out (fp32, laid out as cache->weight, which may be
  * the same array), weight_out = weight + the sum over the chunk's tokens and the key head's query
- * heads of e^(x_j - lse), for every slot in use of the sequences with new tokens.
+ * heads of e^(x_j - lse), for every slot in use of the sequences with new tokens.  O may be Q, but not
+ * with weight_out, for which the logits may be formed again.
  * Logits, sums and results in fp32.  bf16 caches: the value product takes the probabilities as sums
  * of two bf16 values (2^-16 of each); rounded to bf16 in calls of many rows over many slots, and for
  * rows computed along with rows whose values are infinite or whose sums overflow.  fp32 caches: beyond

@@ -1013,7 +1013,7 @@ vp_status vp_cache_attend(const vp_cache* cache, const vp_cache_batch* batch, in
     if (ws_bytes < attend_ws(a)) return VP_ERR_WORKSPACE;
     if (batch->T == 0 || batch->max_q == 0) return VP_OK;
     if (!Q || !O || !lse || !aligned16(Q) || !aligned16(O) || !aligned4(lse) ||
-        !stride_ok(q_stride, Hq, cache->dtype))
+        !stride_ok(q_stride, Hq, cache->dtype) || (weight_out && Q == O))
         return VP_ERR_INVALID_ARG;
     a.Q = Q;
     a.q_stride = q_stride;

@@ -64,3 +64,9 @@ def test_plan_refusals(lib):
     assert lib.vp_cache_attend_plan(R(cache()), R(batch()), 6, R(p)) == 1
     assert lib.vp_cache_attend_plan(R(cache(page=48)), R(batch()), 8, R(p)) == 2
     assert lib.vp_cache_attend_plan(R(cache()), R(batch(max_len=641)), 8, ctypes.byref(p)) == 1
+
+
+def test_weights_need_the_queries_kept(lib):
+    """The weights' kernel reads Q after O is written: the same tensor for both is refused with them."""
+    from test_cache_abi import FAKE, attend
+    assert attend(lib, cache(), batch(), Q=FAKE, O=FAKE, wo=FAKE) == 1

@@ -4,6 +4,7 @@ import numpy as np
 import pytest
 import torch
 
+from paper_2609_23733_amd import vp
 from test_gpu_cache import BF, BFU, F32, U, Pool, _gpu, attend64, cache, check_attend, gen, log, normal  # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -160,3 +161,18 @@ def test_rotary_in_a_graph(cache, dtype, layout, axes, transpose):  # noqa: F811
     for kw in (dict(x=x, out=torch.empty_like(y).detach()), dict(x=x.detach(), out=h)):
         with pytest.raises(ValueError, match="gradient"):
             cache.rotary(pos=pos, rot=rot, **kw)
+
+
+@pytest.mark.parametrize("lens,qs,Hq,Hkv,page,dtype", [
+    ([300, 40], [1, 20], 4, 2, 16, BF), ([300, 40], [1, 20], 4, 2, 16, F32), ([9000], [1], 4, 2, 64, BF),
+    ([2500], [2000], 64, 16, 16, BF), ([700], [130], 2, 2, 32, F32)])
+def test_attend_into_its_queries(cache, lens, qs, Hq, Hkv, page, dtype):  # noqa: F811
+    """O may be Q; with weights, whose logits may be formed again, it is refused."""
+    log("attend O is Q %s %s %s" % (lens, qs, dtype))
+    pool = Pool(cache, lens, Hkv, page, dtype, seed=900 + sum(lens))
+    pc, batch, Q = pool.cuda(), pool.batch(qs), normal(901, (sum(qs), Hq, 64), dtype).cuda()
+    want, lse = cache.attend(pc, batch, Q)
+    with pytest.raises(vp.VPError):
+        cache.attend(pc, batch, Q, O=Q, weight_out=pc.weight)
+    got, l2 = cache.attend(pc, batch, Q, O=Q)
+    assert got is Q and torch.equal(got, want) and torch.equal(lse, l2)
