@@ -476,7 +476,7 @@ vp_status vp_cache_append(const vp_cache *cache, const vp_cache_batch *batch, in
  * Logits, sums and results in fp32.  bf16 caches: the value product takes the probabilities as sums
  * of two bf16 values (2^-16 of each); rounded to bf16 in calls of many rows over many slots, and for
  * rows computed along with rows whose values are infinite or whose sums overflow.  fp32 caches: beyond
- * 64 rows per key head, products of sums of three bf16 values (2^-21 of each at most, like one fp32 sum of 64).
+ * 64 rows per key head, products of sums of three bf16 values (2^-21 of each at most).
  * Deterministic (no atomics; the work's division follows from the host's sizes).  The workspace is
  * that of the batch's own bounds (B, T, max_q, max_len): a
  * smaller batch can need more, as its slots are divided further; one that is too small is refused. */
