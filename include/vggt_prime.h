@@ -51,7 +51,8 @@ typedef enum {
     VP_ERR_HIP = 4           /* a HIP runtime error while enqueueing */
 } vp_status;
 
-typedef enum { VP_F32 = 0, VP_BF16 = 1 } vp_dtype;
+/* VP_E4M3 and VP_INT8: the codes of a vp_cache8, for no other tensor. */
+typedef enum { VP_F32 = 0, VP_BF16 = 1, VP_E4M3 = 2, VP_INT8 = 3 } vp_dtype;
 
 /* Computation modes, ordered by cost (Eq.4). */
 enum { VP_MODE_MEAN = 0, VP_MODE_SURR = 1, VP_MODE_FULL = 2, VP_NUM_MODES = 3 };
@@ -509,6 +510,90 @@ size_t vp_cache_evict_workspace_bytes(int32_t B, int32_t Hkv, int32_t max_len);
 vp_status vp_cache_evict(const vp_cache *cache, const vp_cache_batch *batch, int32_t keep,
                          int32_t sink, int32_t recent, float *weight_out, int32_t *stamp_out,
                          int32_t *length_out, void *ws, size_t ws_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------
+ * Norms of queries and keys per head, with the rotation in the same pass.  A head's
+ * row x of 64 features, in fp32:
+ *   LAYER  n = (x - mean) / sqrt(mean (x - mean)^2 + eps)
+ *   RMS    n = x / sqrt(mean x^2 + eps)
+ *   y = R (n gain + bias),  R the rotation by the token's positions (rot may be NULL: none).
+ * gain and bias: device fp32, 16-byte aligned, [64] for all heads or with per_head [H, 64]; either may be
+ * NULL (1, 0).  eps >= 0; 1e-6 when 0.  A row whose mean square leaves fp32's range gives its limit (gain times
+ * zero, plus the bias). */
+typedef enum { VP_NORM_LAYER = 0, VP_NORM_RMS = 1 } vp_norm_kind;
+typedef struct {
+    vp_norm_kind kind;
+    const float *gain, *bias;
+    int32_t per_head;        /* 0 or 1 */
+    float eps;
+} vp_head_norm;
+
+/* y [T, H, 64] in `dtype`, one rounding; y may be x.  Tokens *_stride elements apart, as for vp_rotary. */
+vp_status vp_norm_rotary(const vp_head_norm *norm, const vp_rotary_spec *rot, vp_dtype dtype,
+                         int32_t T, int32_t H, const void *x, int64_t x_stride, void *y,
+                         int64_t y_stride, void *stream);
+
+/* Gradients of x (dx [T, H, 64] contiguous, in `dtype`), gain and bias (fp32, of their shapes) from x and that of
+ * y, g: with h = R^T g and z = h gain,
+ *   dx = (z - [mean z] - n mean(n z)) / sqrt(..)   ([..]: LAYER),  dgain = sum h n,  dbias = sum h,
+ * sums over tokens, and over heads with one gain for all.  dx, dgain and dbias may each be NULL: not
+ * computed; dx is neither x nor g.  Sums in fp32 per thread and in fp64 over workgroups, in an order that T and
+ * H fix.  The workspace (256-byte aligned) is needed for dgain or dbias. */
+size_t vp_norm_rotary_grad_workspace_bytes(int32_t T, int32_t H, int32_t per_head);
+vp_status vp_norm_rotary_grad(const vp_head_norm *norm, const vp_rotary_spec *rot, vp_dtype dtype,
+                              int32_t T, int32_t H, const void *x, int64_t x_stride, const void *g,
+                              int64_t g_stride, void *dx, float *dgain, float *dbias, void *ws,
+                              size_t ws_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------
+ * The paged cache in 8 bits.  cache.dtype VP_E4M3 (fp8, 4 exponent and 3 fraction bits, largest value 448) or
+ * VP_INT8: K and V are codes, one byte each, laid out as in vp_cache, and scale [npages, Hkv, page, 2] (bf16, 16-byte
+ * aligned) holds each slot's two scales, K's and V's.  A feature is code times scale.  `rows` is the type of the call's
+ * Q, K, V and O.  A plain cache (cache.dtype VP_F32 or VP_BF16, which `rows` repeats, scale NULL) is taken, too,
+ * for norms in its append, and to be read.
+ *
+ * Append writes the smallest power of two, from 2^-100 on, for which the row's largest magnitude is at most 127 or 448
+ * of it, and codes rounded to nearest, ties to even: an error of at most half a step, scale / 2 (INT8) or
+ * 2^-4 of the value and scale 2^-10 (E4M3).  A row with a NaN or an infinity gets scale NaN and codes 0.  Codes and
+ * scales of other origin are taken as they are: scales other than powers of two cost calls of many rows another rounding, of
+ * code times scale to bf16. */
+typedef struct {
+    vp_cache cache;
+    void *scale;
+    vp_dtype rows;
+} vp_cache8;
+
+/* Append as vp_cache_append, with norms of Q's and K's heads before the rotation (q_norm and k_norm may be NULL: none), and
+ * K and V quantised on their way, from fp32. */
+vp_status vp_cache8_append(const vp_cache8 *cache, const vp_cache_batch *batch, int32_t Hq,
+                           const void *Q, int64_t q_stride, const void *K, int64_t k_stride,
+                           const void *V, int64_t v_stride, const vp_head_norm *q_norm,
+                           const vp_head_norm *k_norm, const vp_rotary_spec *rot, void *Q_out,
+                           void *stream);
+
+/* Attend as vp_cache_attend (arguments, workspace, plan, weights, rows that see nothing) over code times scale; O and Q in
+ * `rows`.  A NaN in a slot's value (its scale, or an E4M3 code) makes results of rows that see the slot NaN, at
+ * least in its feature, and reaches no other row.  bf16 rows: probabilities as sums of two bf16 values, rounded to
+ * bf16 in calls of many rows over many slots (vp_cache_plan's `shared`).  fp32 rows: exact products, fp32 sums; a
+ * row of Q with an infinity gives NaN. */
+size_t vp_cache8_attend_workspace_bytes(const vp_cache8 *cache, const vp_cache_batch *batch,
+                                        int32_t Hq);
+vp_status vp_cache8_attend_plan(const vp_cache8 *cache, const vp_cache_batch *batch, int32_t Hq,
+                                vp_cache_plan *plan);
+vp_status vp_cache8_attend(const vp_cache8 *cache, const vp_cache_batch *batch, int32_t Hq,
+                           const void *Q, int64_t q_stride, int32_t causal, float scale, void *O,
+                           float *lse, float *weight_out, void *ws, size_t ws_bytes, void *stream);
+
+/* Evict as vp_cache_evict (the same workspace); codes and scales move together. */
+vp_status vp_cache8_evict(const vp_cache8 *cache, const vp_cache_batch *batch, int32_t keep,
+                          int32_t sink, int32_t recent, float *weight_out, int32_t *stamp_out,
+                          int32_t *length_out, void *ws, size_t ws_bytes, void *stream);
+
+/* Read: the inverse of append.  Row q_start[b] + i of K_out, V_out [T, Hkv, 64] (`dtype`: VP_F32 or VP_BF16) is slot
+ * length[b] - n + i of sequence b, n = q_start[b + 1] - q_start[b] rows; zeros where there is no such slot or page. Rows
+ * that belong to no sequence are left alone. */
+vp_status vp_cache8_read(const vp_cache8 *cache, const vp_cache_batch *batch, vp_dtype dtype,
+                         void *K_out, void *V_out, void *stream);
 
 /* Static description of a status code. */
 const char *vp_status_string(vp_status s);

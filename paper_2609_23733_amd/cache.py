@@ -1,6 +1,6 @@
 """Paged key-value cache: exact attention of views that arrive one after another.
 
-Binding of the vp_rotary* and vp_cache_* calls of include/vggt_prime.h, in the manner of vp.py
+Binding of the vp_rotary*, vp_norm_rotary*, vp_cache_* and vp_cache8_* calls of include/vggt_prime.h, in the manner of vp.py
 (argument checks and marshalling; the operators run in the library's kernels, on the current torch
 stream, without synchronising), and StreamLayer, which runs them together.
 
@@ -20,6 +20,8 @@ from .vp import HEAD_DIM, VPError, _check, _dt, _need, _ptr, load_library
 ROT_INTERLEAVED, ROT_HALF = 0, 1
 ROT_SCALE_NONE, ROT_SCALE_LINEAR, ROT_SCALE_PARTS = 0, 1, 2
 _LAYOUTS = {"interleaved": ROT_INTERLEAVED, "half": ROT_HALF}
+_NORMS = {"layer": vp.NORM_LAYER, "rms": vp.NORM_RMS}
+_CODES = {torch.float8_e4m3fn: vp.VP_E4M3, torch.int8: vp.VP_INT8}
 _SCALINGS = {"none": ROT_SCALE_NONE, "linear": ROT_SCALE_LINEAR, "parts": ROT_SCALE_PARTS}
 
 
@@ -136,12 +138,97 @@ class _Rotation(torch.autograd.Function):
         return rotary(g, pos, ctx.rot, None, not ctx.transpose), None, None, None
 
 
+class HeadNorm:
+    """The norm of a head's row over its 64 features: kind "layer" (mean and variance) or "rms" (mean
+    square), with gain and bias fp32 [64], or [H, 64] for a norm per head, or None (see vp_head_norm)."""
+
+    def __init__(self, kind: str = "layer", gain: Optional[torch.Tensor] = None,
+                 bias: Optional[torch.Tensor] = None, eps: float = 1e-6):
+        shape = None
+        for t, name in ((gain, "gain"), (bias, "bias")):
+            if t is None:
+                continue
+            _need(t, name, shape, torch.float32)
+            shape = tuple(t.shape)
+            if shape[-1:] != (HEAD_DIM,) or t.dim() > 2:
+                raise ValueError("%s must be [%d] or [heads, %d]" % (name, HEAD_DIM, HEAD_DIM))
+            if t.data_ptr() % 16:
+                raise ValueError("%s must start at a multiple of 16 bytes" % name)
+        if not 0 < eps < float("inf"):
+            raise ValueError("eps must be positive")
+        self.kind, self.gain, self.bias, self.eps = kind, gain, bias, float(eps)
+        self.heads = shape[0] if shape is not None and len(shape) == 2 else None
+        ptr = lambda t: None if t is None else t.data_ptr()
+        self._c = vp.vp_head_norm(_NORMS[kind], ptr(gain), ptr(bias), self.heads is not None, self.eps)
+        self._ref = ctypes.byref(self._c)
+
+    def at(self, H: int):
+        """The C argument for rows of H heads."""
+        if self.heads is not None and self.heads != H:
+            raise ValueError("a norm of %d heads for %d" % (self.heads, H))
+        return self._ref
+
+
+def norm_rotary(x, norm: HeadNorm, pos=None, rot: Optional[Rotary] = None, out: Optional[torch.Tensor] = None):
+    """x [T, H, 64], every head's row normalised and turned by its token's position, in one pass (without
+    `rot` only normalised).  `out` may be x.  Where x, gain or bias require gradients they get them (no `out`
+    then)."""
+    if (rot is None) != (pos is None):
+        raise ValueError("a rotation needs positions" if pos is None else "positions need a rotation (rot)")
+    if torch.is_grad_enabled() and (x.requires_grad or (norm.gain is not None and norm.gain.requires_grad) or
+                                    (norm.bias is not None and norm.bias.requires_grad) or
+                                    (out is not None and out.requires_grad)):
+        if out is not None:
+            raise ValueError("out would not be part of the gradient's graph")
+        return _NormRotation.apply(x, norm.gain, norm.bias, pos, norm, rot)
+    T, H = x.shape[0], x.shape[1]
+    xs = _rows(x, "x", T, H, x.dtype)
+    if out is None:
+        out = torch.empty(T, H, HEAD_DIM, dtype=x.dtype, device=x.device)
+    ys = _rows(out, "out", T, H, x.dtype)
+    _done(load_library().vp_norm_rotary(norm.at(H), None if rot is None else rot.at(pos, T), _dt(x), T, H, x.data_ptr(), xs,
+                                        out.data_ptr(), ys, _stream()), "vp_norm_rotary")
+    return out
+
+
+class _NormRotation(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, gain, bias, pos, norm, rot):
+        ctx.save_for_backward(x, gain, bias, pos)
+        ctx.norm, ctx.rot = norm, rot
+        return norm_rotary(x, norm, pos, rot)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, g):
+        x, gain, bias, pos = ctx.saved_tensors     # (refuses values that were changed in place)
+        norm, rot = ctx.norm, ctx.rot
+        T, H = x.shape[0], x.shape[1]
+        if not g.is_contiguous() or g.data_ptr() % 16:     # (broadcast, or a part of something)
+            g = g.clone(memory_format=torch.contiguous_format)
+        dx, dgain, dbias = (torch.empty(t.shape, dtype=t.dtype, device=t.device) if need else None
+                            for t, need in zip((x, gain, bias), ctx.needs_input_grad))
+        ptr = lambda t: None if t is None else t.data_ptr()
+        lib, ws, n = load_library(), None, 0
+        if dgain is not None or dbias is not None:
+            n = lib.vp_norm_rotary_grad_workspace_bytes(T, H, norm.heads is not None)
+            ws = torch.empty(n, dtype=torch.uint8, device=x.device)
+        _done(lib.vp_norm_rotary_grad(norm.at(H), None if rot is None else rot.at(pos, T), _dt(x), T, H, x.data_ptr(),
+                                      _rows(x, "x", T, H, x.dtype), g.data_ptr(), _rows(g, "the gradient", T, H, x.dtype),
+                                      ptr(dx), ptr(dgain), ptr(dbias), ptr(ws), n, _stream()), "vp_norm_rotary_grad")
+        return dx, dgain, dbias, None, None, None
+
+
 class PagedCache:
     """The pool: K, V [npages, Hkv, page, 64], and per slot weight fp32 and stamp int32 [npages,
-    Hkv, page] (needed by the eviction, optional otherwise)."""
+    Hkv, page] (needed by the eviction, optional otherwise).
+
+    K and V may be 8-bit codes (torch.float8_e4m3fn or torch.int8) with `scale` bf16 [npages, Hkv, page, 2],
+    a key's and a value's (see vp_cache8); `rows` is then the type of the calls' Q, K, V and O."""
 
     def __init__(self, K, V, weight: Optional[torch.Tensor] = None,
-                 stamp: Optional[torch.Tensor] = None):
+                 stamp: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
+                 rows: Optional[torch.dtype] = None):
         _need(K, "K")
         if K.dim() != 4 or K.shape[3] != HEAD_DIM:
             raise ValueError("K must be [pages, heads, page, %d]" % HEAD_DIM)
@@ -151,18 +238,39 @@ class PagedCache:
             _need(weight, "weight", K.shape[:3], torch.float32)
         if stamp is not None:
             _need(stamp, "stamp", K.shape[:3], torch.int32)
-        self.K, self.V, self.weight, self.stamp, self.dtype = K, V, weight, stamp, K.dtype
+        self.codes = K.dtype in _CODES
+        if self.codes:
+            if scale is None:
+                raise ValueError("a cache of codes needs scales")
+            _need(scale, "scale", tuple(K.shape[:3]) + (2,), torch.bfloat16)
+            rows = torch.bfloat16 if rows is None else rows
+            if rows not in (torch.bfloat16, torch.float32):
+                raise ValueError("rows are bf16 or fp32")
+        elif scale is not None or rows not in (None, K.dtype):
+            raise ValueError("scales, and rows of another type, are for codes")
+        self.K, self.V, self.weight, self.stamp, self.scale = K, V, weight, stamp, scale
+        self.dtype = rows if self.codes else K.dtype       # of the calls' rows
         ptr = lambda t: None if t is None else t.data_ptr()
         self._c = vp.vp_cache(K.data_ptr(), V.data_ptr(), ptr(weight), ptr(stamp), self.npages,
-                              self.page, self.Hkv, HEAD_DIM, _dt(K))
-        self._ref = ctypes.byref(self._c)
+                              self.page, self.Hkv, HEAD_DIM, _CODES[K.dtype] if self.codes else _dt(K))
+        self._c8 = vp.vp_cache8(self._c, ptr(scale), vp.VP_BF16 if self.dtype is torch.bfloat16 else vp.VP_F32)
+        self._ref8 = ctypes.byref(self._c8)
+        self._ref = self._ref8 if self.codes else ctypes.byref(self._c)
+
+    def _call(self, name: str):
+        """The library's call for this cache."""
+        return getattr(load_library(), ("vp_cache8_" if self.codes else "vp_cache_") + name)
 
     @staticmethod
-    def empty(npages: int, Hkv: int, page: int = 64, dtype=torch.bfloat16, device="cuda") -> "PagedCache":
+    def empty(npages: int, Hkv: int, page: int = 64, dtype=torch.bfloat16, device="cuda",
+              rows: Optional[torch.dtype] = None) -> "PagedCache":
         kv = lambda: torch.empty(npages, Hkv, page, HEAD_DIM, dtype=dtype, device=device)
+        scale = None
+        if dtype in _CODES:
+            scale = torch.empty(npages, Hkv, page, 2, dtype=torch.bfloat16, device=device)
         return PagedCache(kv(), kv(),
                           torch.zeros(npages, Hkv, page, dtype=torch.float32, device=device),
-                          torch.zeros(npages, Hkv, page, dtype=torch.int32, device=device))
+                          torch.zeros(npages, Hkv, page, dtype=torch.int32, device=device), scale, rows)
 
 
 class Batch:
@@ -190,9 +298,11 @@ class Batch:
 
 
 def append(pc: PagedCache, batch: Batch, Q, K, V, pos=None, rot: Optional[Rotary] = None,
-           Q_out: Optional[torch.Tensor] = None):
+           Q_out: Optional[torch.Tensor] = None, q_norm: Optional[HeadNorm] = None,
+           k_norm: Optional[HeadNorm] = None):
     """New tokens into the cache: K [T, Hkv, 64] rotated, V as it is; returns the rotated Q [T, Hq,
-    64] (None without Q)."""
+    64] (None without Q).  With q_norm or k_norm Q's or K's heads are normalised before the rotation.  A cache
+    of codes gets them quantised."""
     T, Hkv, dt = K.shape[0], pc.Hkv, pc.dtype
     ks, vs = _rows(K, "K", T, Hkv, dt), _rows(V, "V", T, Hkv, dt)
     Hq = qs = q = qo = 0
@@ -204,14 +314,38 @@ def append(pc: PagedCache, batch: Batch, Q, K, V, pos=None, rot: Optional[Rotary
         qo = _whole(Q_out, "Q_out", (T, Hq, HEAD_DIM), dt)
     if (rot is None) != (pos is None):
         raise ValueError("a rotation needs positions" if pos is None else "positions need a rotation (rot)")
-    _done(load_library().vp_cache_append(pc._ref, batch._for(T), Hq, q, qs, K.data_ptr(), ks, V.data_ptr(), vs,
-                                         None if rot is None else rot.at(pos, T), qo, _stream()),
-          "vp_cache_append")
+    turn = None if rot is None else rot.at(pos, T)
+    if pc.codes or q_norm is not None or k_norm is not None:
+        _done(load_library().vp_cache8_append(pc._ref8, batch._for(T), Hq, q, qs, K.data_ptr(), ks, V.data_ptr(), vs,
+                                              None if q_norm is None or Q is None else q_norm.at(Hq),
+                                              None if k_norm is None else k_norm.at(Hkv), turn, qo, _stream()),
+              "vp_cache8_append")
+    else:
+        _done(load_library().vp_cache_append(pc._ref, batch._for(T), Hq, q, qs, K.data_ptr(), ks, V.data_ptr(), vs,
+                                             turn, qo, _stream()), "vp_cache_append")
     return Q_out if Q is not None else None
 
 
+def read(pc: PagedCache, batch: Batch, T: int, dtype: Optional[torch.dtype] = None,
+         K_out: Optional[torch.Tensor] = None, V_out: Optional[torch.Tensor] = None):
+    """The last slots of every sequence, as many as the batch gives it rows, as (K, V) [T, Hkv, 64]: what an
+    append of those rows left in the cache.  `dtype`: bf16 or fp32 (that of K_out, or of the cache's rows)."""
+    if dtype is None:
+        dtype = pc.dtype if K_out is None else K_out.dtype
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("rows are read in bf16 or fp32")
+    # (zeros: rows past the last sequence's are left as they are)
+    new = lambda: torch.zeros(T, pc.Hkv, HEAD_DIM, dtype=dtype, device=pc.K.device)
+    K_out, V_out = new() if K_out is None else K_out, new() if V_out is None else V_out
+    shape = (T, pc.Hkv, HEAD_DIM)
+    _done(load_library().vp_cache8_read(pc._ref8, batch._for(T), vp.VP_BF16 if dtype is torch.bfloat16 else vp.VP_F32,
+                                        _whole(K_out, "K_out", shape, dtype), _whole(V_out, "V_out", shape, dtype),
+                                        _stream()), "vp_cache8_read")
+    return K_out, V_out
+
+
 def attend_workspace(pc: PagedCache, batch: Batch, Hq: int, T: int) -> torch.Tensor:
-    n = load_library().vp_cache_attend_workspace_bytes(pc._ref, batch._for(T), int(Hq))
+    n = pc._call("attend_workspace_bytes")(pc._ref, batch._for(T), int(Hq))
     if n == 0:
         raise ValueError("invalid cache or batch")
     return torch.empty(n, dtype=torch.uint8, device=pc.K.device)
@@ -220,8 +354,7 @@ def attend_workspace(pc: PagedCache, batch: Batch, Hq: int, T: int) -> torch.Ten
 def attend_plan(pc: PagedCache, batch: Batch, Hq: int, T: int) -> vp.vp_cache_plan:
     """How a call with these bounds is computed (see vp_cache_plan)."""
     plan = vp.vp_cache_plan()
-    _done(load_library().vp_cache_attend_plan(pc._ref, batch._for(T), int(Hq), ctypes.byref(plan)),
-          "vp_cache_attend_plan")
+    _done(pc._call("attend_plan")(pc._ref, batch._for(T), int(Hq), ctypes.byref(plan)), "vp_cache_attend_plan")
     return plan
 
 
@@ -246,8 +379,8 @@ def attend(pc: PagedCache, batch: Batch, Q, causal: bool = True, scale: float = 
     if ws is None:
         ws = attend_workspace(pc, batch, Hq, T)
     w, n = _work(ws)
-    _done(load_library().vp_cache_attend(pc._ref, batch._for(T), Hq, Q.data_ptr(), qs, causal, scale, o, ls, wo, w,
-                                         n, _stream()), "vp_cache_attend")
+    _done(pc._call("attend")(pc._ref, batch._for(T), Hq, Q.data_ptr(), qs, causal, scale, o, ls, wo, w, n, _stream()),
+          "vp_cache_attend")
     return O, lse
 
 
@@ -281,8 +414,8 @@ def evict(pc: PagedCache, table, length, seen, keep: int, max_len: int, sink: in
     w, n = _work(ws)
     c = vp.vp_cache_batch(table.data_ptr(), length.data_ptr(), seen.data_ptr(), None, B, pages, 0, 0,
                           int(max_len))
-    _done(load_library().vp_cache_evict(pc._ref, ctypes.byref(c), int(keep), int(sink), int(recent), wo, so, lo, w, n,
-                                        _stream()), "vp_cache_evict")
+    _done(pc._call("evict")(pc._ref, ctypes.byref(c), int(keep), int(sink), int(recent), wo, so, lo, w, n, _stream()),
+          "vp_cache_evict")
     return length_out
 
 
@@ -294,7 +427,9 @@ class StreamLayer:
     B sequences of chunks up to `max_chunk` tokens.  `sink` first tokens (the first view, which the
     scene's frame of reference hangs on) and the `recent` latest ones are kept whatever
     weight they have.  `causal`: a token sees its own chunk up to itself, not all of
-    it.  `rot`: positions given to step() are applied to Q and K.
+    it.  `rot`: positions given to step() are applied to Q and K; `q_norm`, `k_norm`: norms of their heads
+    before.  `dtype`: of the cache; torch.float8_e4m3fn or torch.int8 for 8-bit codes, `rows` (bf16 when not
+    given) then of Q, K, V and O.
 
     A step is enqueued on the current stream without waiting for it.  Its chunks' starts and bounds
     are the host's, so a captured step would repeat those of the capture."""
@@ -302,7 +437,8 @@ class StreamLayer:
     def __init__(self, B: int, keep: int, max_chunk: int, Hq: int = vp.MAX_HEADS,
                  Hkv: Optional[int] = None, page: int = 64, dtype=torch.bfloat16, sink: int = 0,
                  recent: int = 0, causal: bool = False, rot: Optional[Rotary] = None,
-                 device="cuda"):
+                 device="cuda", q_norm: Optional[HeadNorm] = None, k_norm: Optional[HeadNorm] = None,
+                 rows: Optional[torch.dtype] = None):
         Hkv = Hq if Hkv is None else Hkv
         if Hkv < 1 or Hq < Hkv or Hq % Hkv:
             raise ValueError("%d query heads for %d key heads" % (Hq, Hkv))
@@ -311,7 +447,8 @@ class StreamLayer:
         pages = -(-(keep + max_chunk) // page)
         self.B, self.Hq, self.keep, self.max_chunk = B, Hq, keep, max_chunk
         self.sink, self.recent, self.causal, self.rot = sink, recent, causal, rot
-        self.pc = PagedCache.empty(B * pages, Hkv, page, dtype, device)
+        self.q_norm, self.k_norm = q_norm, k_norm
+        self.pc = PagedCache.empty(B * pages, Hkv, page, dtype, device, rows)
         self.table = torch.arange(B * pages, dtype=torch.int32, device=device).view(B, pages)
         self.length = torch.zeros(B, dtype=torch.int32, device=device)
         self.seen = torch.zeros(B, dtype=torch.int32, device=device)
@@ -343,8 +480,8 @@ class StreamLayer:
         length, seen = self.length + new, self.seen + new
         lens = [n + c for n, c in zip(self.lens, counts)]
         batch = Batch(self.table, length, q_start, max(counts), max(lens), seen)
-        Q = append(self.pc, batch, Q, K, V, pos, self.rot)
-        n = load_library().vp_cache_attend_workspace_bytes(self.pc._ref, batch._for(T), self.Hq)
+        Q = append(self.pc, batch, Q, K, V, pos, self.rot, None, self.q_norm, self.k_norm)
+        n = self.pc._call("attend_workspace_bytes")(self.pc._ref, batch._for(T), self.Hq)
         if self.attend_ws is None or self.attend_ws.numel() < n:
             self.attend_ws = torch.empty(n, dtype=torch.uint8, device=Q.device)
         O, _ = attend(self.pc, batch, Q, self.causal, weight_out=self.pc.weight, ws=self.attend_ws)

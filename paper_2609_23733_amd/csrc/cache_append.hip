@@ -11,53 +11,9 @@
 //
 // Bound by memory (each value read and written once).  A thread owns four pairs of a token, whose
 // sines and cosines it computes once and uses for several heads; eight threads cover a head's row.
-#include "cache_device.hpp"
+#include "rotary_device.hpp"
 
 namespace vp {
-
-template <typename T>
-struct Vec4 {
-    typedef T type __attribute__((__vector_size__(4 * sizeof(T))));
-};
-
-// Stores that pass the caches by (NT), for outputs larger than these: 43,968 tokens of 16 heads
-// 50 -> 44 us.
-template <bool NT, typename V>
-__device__ __forceinline__ void put(V* p, V v) {
-    if constexpr (NT) __builtin_nontemporal_store(v, p);
-    else *p = v;
-}
-
-// Eight features in a row, at a 16-byte boundary: 16 bytes at a time.
-template <bool NT, typename T>
-__device__ __forceinline__ void put8(T* p, typename Vec4<T>::type a, typename Vec4<T>::type b) {
-    if constexpr (sizeof(T) == 2) {
-        typedef T V8 __attribute__((__vector_size__(16)));
-        put<NT>((V8*)p, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
-    } else {
-        put<NT>((typename Vec4<T>::type*)p, a);
-        put<NT>((typename Vec4<T>::type*)(p + 4), b);
-    }
-}
-
-// Sine and cosine of a fraction of a revolution, 32 bits: the nearest quarter turn from the top bits,
-// the rest, |x| <= pi / 4, by the Taylor series to x^9 and x^10 (errors 2e-9 and 2e-9 there).
-__device__ __forceinline__ void sincos_turn(uint32_t t, float* sn, float* cs) {
-    const uint32_t q = (t + 0x20000000u) >> 30;
-    const float x = (float)(int32_t)(t - (q << 30)) * (1.57079632679489662f / 1073741824.f), x2 = x * x;
-    float s = fmaf(x2, 1.f / 362880.f, -1.f / 5040.f);
-    s = fmaf(x2, s, 1.f / 120.f);
-    s = fmaf(x2, s, -1.f / 6.f);
-    s = fmaf(x2 * s, x, x);
-    float c = fmaf(x2, -1.f / 3628800.f, 1.f / 40320.f);
-    c = fmaf(x2, c, -1.f / 720.f);
-    c = fmaf(x2, c, 1.f / 24.f);
-    c = fmaf(x2, c, -0.5f);
-    c = fmaf(x2, c, 1.f);
-    const float a = q & 1 ? c : s, b = q & 1 ? s : c;
-    *sn = __uint_as_float(__float_as_uint(a) ^ ((q & 2) << 30));
-    *cs = __uint_as_float(__float_as_uint(b) ^ (((q + 1) & 2) << 30));
-}
 
 // Four pairs' sines and cosines: pair indices 4 c .. 4 c + 3 of token t.
 struct Turn4 {
@@ -231,15 +187,6 @@ __global__ __launch_bounds__(256) void k_cache_append(AppendArgs a, RotArgs r, i
     }
 }
 
-// Threads (of eight) per token: one per head while that leaves compute units idle, fewer, each
-// reusing its sines over more heads, when tokens alone make `threads` of them.  A view of 1,374
-// tokens appended takes 7.9 us with three rows per thread, 9.1 with one and a half.
-static int head_split(int64_t tokens, int heads, int64_t threads) {
-    int hs = 1;
-    while (hs < heads && tokens * 8 * hs < threads) hs *= 2;
-    return hs < heads ? hs : heads;
-}
-
 template <typename T, bool NT>
 static void rotary_go(const void* x, int64_t x_stride, void* y, int64_t y_stride, int Tn, int H,
                       const RotArgs& r, hipStream_t st) {
@@ -266,6 +213,7 @@ void launch_rotary(int dtype, const void* x, int64_t x_stride, void* y, int64_t 
     }
 }
 
+// A view of 1,374 tokens appended takes 7.9 us with three rows per thread, 9.1 with one and a half.
 void launch_cache_append(const AppendArgs& a, const RotArgs& r, hipStream_t st) {
     const int hs = head_split((int64_t)a.c.B * a.c.max_q, (a.Q ? a.Hq : 0) + 2 * a.c.Hkv, 128 * 1024);
     const dim3 grid((unsigned)(((int64_t)a.c.max_q * hs * 8 + 255) / 256), a.c.B);

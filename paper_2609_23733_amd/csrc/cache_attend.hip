@@ -10,16 +10,13 @@
 #include <cmath>
 #include <type_traits>
 
-#include "cache_device.hpp"
+#include "attend_device.hpp"
+#include "cache_codes.hpp"
 
 namespace vp {
 
 typedef __attribute__((address_space(3))) char lds_char;
 typedef short s16x4 __attribute__((__vector_size__(8)));
-
-__device__ __forceinline__ float maximum(float a, float b) {
-    return __builtin_elementwise_maximum(a, b);   // IEEE maximum: a NaN stays one
-}
 
 // ------------------------------------------------------------------------
 // Geometry of the two kernel variants.  A wave multiplies groups of 32 rows with 32 slots (a block)
@@ -56,47 +53,6 @@ struct Geo {
     // Slot within a block that result register r of lane half hh belongs to.
     static __device__ __forceinline__ constexpr int key(int r, int hh) {
         return kBf ? 16 * (r >> 3) + 8 * hh + (r & 7) : 8 * (r >> 2) + 4 * hh + (r & 3);
-    }
-};
-
-// Page numbers of a run of slots: lane i holds the page of the table's entry first + i.  Numbers
-// outside the pool count as page 0 here and clear `sane`; the slots on such pages are masked.
-struct PageWindow {
-    const int32_t* row;   // the sequence's table row
-    int last;             // last entry that may be read
-    int64_t npages;
-    int first, cur, next;
-    bool sane;
-
-    __device__ __forceinline__ int load(int at, int lane) const {
-        const int i = at + lane;
-        return row[i < last ? i : last];
-    }
-    __device__ __forceinline__ bool valid(int id) const { return id >= 0 && id < npages; }
-    __device__ __forceinline__ int settle(int id) {
-        if (__builtin_amdgcn_ballot_w64(!valid(id))) sane = false;
-        return valid(id) ? id : 0;
-    }
-    __device__ __forceinline__ void start(const CacheArgs& a, int b, int lo, int last_slot, int lane) {
-        row = a.table + (int64_t)b * a.max_pages;
-        last = last_slot >> a.page_log2;
-        npages = a.npages;
-        sane = true;
-        first = lo >> a.page_log2;
-        const int id = load(first, lane);
-        next = load(first + 64, lane);
-        cur = settle(id);
-    }
-    // Page of table entry `at` (uniform, never falling from call to call).
-    __device__ __forceinline__ int page(int at, int lane) {
-        if (at - first >= 64) {
-            const int hop = (at - first) >> 6;
-            first += hop * 64;
-            if (hop > 1) next = load(first, lane);
-            cur = settle(next);
-            next = load(first + 64, lane);
-        }
-        return __builtin_amdgcn_readlane(cur, at - first);
     }
 };
 
@@ -165,7 +121,6 @@ struct Probs<float, SPLIT> {
     f32x16 v;
     __device__ __forceinline__ void set(const f32x16& s) { v = s; }
 };
-constexpr float kMoveAt = 65536.f;
 
 // Logits (without the scale) of the block whose K lies at `k`.
 template <typename T>
@@ -281,31 +236,6 @@ __device__ __forceinline__ void block_values(Rows<T>& w, lds_char* v, const Prob
     }
 }
 
-// fp32 values as sums of three bf16 values, x = h + m + l: each takes the next eight significant bits,
-// cut, not rounded, so that the sum is exact and h does not overflow.  Products of two such sums leave out
-// m l, l m and l l, at most 2^-21 of the product and 2^-23 on the average.
-struct Planes {
-    bf16x8 h, m, l;
-};
-__device__ __forceinline__ Planes split8(const float (&x)[8]) {
-    u32x4 h, m, l;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        uint32_t a[2], b[2], c[2];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const float v = x[2 * j + e];
-            a[e] = __float_as_uint(v) & 0xffff0000u;
-            const float r = v - __uint_as_float(a[e]);
-            b[e] = __float_as_uint(r) & 0xffff0000u;
-            c[e] = __float_as_uint(r - __uint_as_float(b[e]));
-        }
-        h[j] = __builtin_amdgcn_perm(a[1], a[0], 0x07060302u);   // the upper halves
-        m[j] = __builtin_amdgcn_perm(b[1], b[0], 0x07060302u);
-        l[j] = __builtin_amdgcn_perm(c[1], c[0], 0x07060302u);
-    }
-    return Planes{__builtin_bit_cast(bf16x8, h), __builtin_bit_cast(bf16x8, m), __builtin_bit_cast(bf16x8, l)};
-}
 __device__ __forceinline__ f32x16 mfma_planes(const Planes& a, const Planes& b, f32x16 c) {
     c = mfma_bf16(a.m, b.m, c);
     c = mfma_bf16(a.l, b.h, c);
@@ -414,21 +344,6 @@ __device__ __forceinline__ void add_odd_values(const AttendArgs& a, Rows<T>& w, 
                 __builtin_amdgcn_sched_barrier(0);
             }
     }
-}
-
-// Factor 1 / l of a row and its log-sum-exp from (m, l).  No key seen, or only
-// logits of -inf: zeros and -inf.  A reference of +inf stands for an infinite logit: NaN.
-__device__ __forceinline__ void row_result(float m, float l, float* inv, float* lse) {
-    if (m == INFINITY) l = __builtin_nanf("");
-    *inv = l == 0.f ? 0.f : 1.f / l;
-    *lse = l == 0.f ? -INFINITY : (m + __log2f(l)) * kLn2;
-}
-
-// lse, and the accumulator input that the weights' products start from (see k_cache_weight): a row
-// without weights adds none.
-__device__ __forceinline__ void put_lse(const AttendArgs& a, int64_t row, float lse) {
-    a.lse[row] = lse;
-    if (a.off) a.off[row] = lse == -INFINITY ? -INFINITY : lse * (-kLog2e / a.c2);
 }
 
 // A workgroup: RT rows of one key head and sequence over one range of its slots.  Narrow: bound by HBM
@@ -1280,7 +1195,7 @@ __global__ __launch_bounds__(256) void k_cache_weight_rows(AttendArgs a) {
 // let four workgroups share a compute unit; their waves fill each other's waits, and forming the products of
 // one block amid another's powers, or six workgroups with half the rows, gained nothing.
 // ------------------------------------------------------------------------
-template <typename T>
+template <typename T, int CODE>
 __global__ __launch_bounds__(256, 4) void k_cache_weight(AttendArgs a) {
     constexpr bool kBf = sizeof(T) == 2;
     constexpr int kStep = kBf ? 128 : 64, RB = kStep / 64;    // rows per tile, 32-row blocks of a wave
@@ -1369,7 +1284,26 @@ __global__ __launch_bounds__(256, 4) void k_cache_weight(AttendArgs a) {
                        (slot & ((1 << a.c.page_log2) - 1));
     bf16x8 kb[4];
     float kf[kBf ? 1 : 32];
-    if constexpr (kBf) {
+    if constexpr (CODE != CODE_NONE) {
+        // (8-bit codes: code times scale is a bf16 value)
+        const float s = live ? key_scale(a.c.scale[at]) : 0.f;
+        const char* kr = (const char*)a.c.K + at * kD;
+#pragma unroll
+        for (int i = 0; i < (kBf ? 4 : 8); ++i) {
+            if constexpr (kBf) {
+                float x[4], y[4];
+                const uint2 v = live ? *(const uint2*)(kr + 16 * i + 8 * hh) : make_uint2(0u, 0u);
+                values4<CODE>(v.x, s, x);
+                values4<CODE>(v.y, s, y);
+                kb[i] = pack_bf16x8(x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]);
+            } else {
+                float x[4];
+                values4<CODE>(live ? *(const uint32_t*)(kr + 8 * i + 4 * hh) : 0u, s, x);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) kf[4 * i + e] = x[e];
+            }
+        }
+    } else if constexpr (kBf) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             kb[i] = zero_bf16x8();
@@ -1471,8 +1405,8 @@ void attend_plan(AttendArgs* a) {
     // both 34; 200 over 20,000, 4,400 each, 49 and 41; 1,374 over themselves, 1,850 each in 1.3 rounds, 37 and
     // 29.  fp32, whose wide kernel has the faster products: 64 over 20,000 56 and 57, 90 over 20,000 80 and
     // 61, 200 over 600 22 and 18; 90 over 300 13.3 and 15.8.)
-    double items = work_items(32, false);
-    a->wide = rows > 64 && (!bf || items * a->c.max_len > 512. * (items > 512 ? 1500 : 2500));
+    double items = work_items(a->c.code ? attend_rows(*a) : 32, false);
+    a->wide = !a->c.code && rows > 64 && (!bf || items * a->c.max_len > 512. * (items > 512 ? 1500 : 2500));
     if (a->wide) items = work_items(attend_rows(*a), true);
     // An estimate that ranks divisions into ns ranges, in us where the card is lightly loaded (large calls, which HBM or
     // all SIMDs at once bound, take up to three times as long: 50 for 167 us of tokens over 137,400 slots, 153
@@ -1503,6 +1437,7 @@ void attend_plan(AttendArgs* a) {
 
 // Rows per workgroup.
 int attend_rows(const AttendArgs& a) {
+    if (a.c.code) return (int64_t)a.c.max_q * a.G <= 16 ? 16 : 32;
     if (a.c.dtype == DT_BF16) return a.wide ? Geo<bf16, true>::RT : Geo<bf16, false>::RT;
     return a.wide ? Geo<float, true>::RT : Geo<float, false>::RT;
 }
@@ -1524,24 +1459,38 @@ size_t attend_logits(const AttendArgs& a) {
 }
 
 template <typename T>
-static void attend_go(const AttendArgs& a, hipStream_t st) {
-    const int64_t grid = ((int64_t)a.c.B * a.c.Hkv * a.nsplit + 7) / 8 * 8 * a.row_tiles;
-    if (a.wide)
-        hipLaunchKernelGGL((k_cache_attend<T, true>), dim3(grid), dim3(64 * Geo<T, true>::NW), 0, st, a);
-    else
-        hipLaunchKernelGGL((k_cache_attend<T, false>), dim3(grid), dim3(256), 0, st, a);
+static void join_go(const AttendArgs& a, hipStream_t st) {
     const int64_t rows = (int64_t)a.c.max_q * a.Hq;
     if (a.nsplit > kFew)
         hipLaunchKernelGGL((k_cache_join<T, true>), dim3((rows + 3) / 4, a.c.B), dim3(256), 0, st, a);
     else if (a.nsplit > 1)
         hipLaunchKernelGGL((k_cache_join<T, false>), dim3((rows + 15) / 16, a.c.B), dim3(256), 0, st, a);
+}
+
+template <typename T, int CODE>
+static void weights_go(const AttendArgs& a, hipStream_t st) {
     if (!a.weight_out || a.c.max_len == 0) return;
     const unsigned bh = a.c.B * a.c.Hkv;
     if (a.logits) {
         hipLaunchKernelGGL(k_cache_weight_rows, dim3((a.c.max_len + 1023) / 1024, bh), dim3(256), 0, st, a);
     } else {
-        hipLaunchKernelGGL(k_cache_weight<T>, dim3((a.c.max_len + 63) / 64, bh), dim3(256), 0, st, a);
+        hipLaunchKernelGGL((k_cache_weight<T, CODE>), dim3((a.c.max_len + 63) / 64, bh), dim3(256), 0, st, a);
     }
+}
+
+template <typename T>
+static void attend_go(const AttendArgs& a, hipStream_t st) {
+    const int64_t grid = ((int64_t)a.c.B * a.c.Hkv * a.nsplit + 7) / 8 * 8 * a.row_tiles;
+    if (a.c.code)
+        launch_cache8_attend(a, st);
+    else if (a.wide)
+        hipLaunchKernelGGL((k_cache_attend<T, true>), dim3(grid), dim3(64 * Geo<T, true>::NW), 0, st, a);
+    else
+        hipLaunchKernelGGL((k_cache_attend<T, false>), dim3(grid), dim3(256), 0, st, a);
+    join_go<T>(a, st);
+    if (a.c.code == CODE_E4M3) weights_go<T, CODE_E4M3>(a, st);
+    else if (a.c.code == CODE_INT8) weights_go<T, CODE_INT8>(a, st);
+    else weights_go<T, CODE_NONE>(a, st);
 }
 
 void launch_cache_attend(const AttendArgs& a, hipStream_t st) {

@@ -1,0 +1,83 @@
+// Caches of 8-bit codes: quantisation and its inverse.
+//
+// A row of 64 features (K or V of a slot and head) is code * scale, int8 codes of at most 127 or fp8 (e4m3,
+// at most 448), the scale the smallest power of two that keeps the row's largest value within them, at least 2^-100.
+// A power of two costs int8 up to one of its bits, and e4m3 none; with it, code * scale has at most eight significant bits: it is
+// a bf16 value, so the products of a bf16 cache take it without another rounding, and the quantisation's division
+// is exact.  A row that holds a NaN or an infinity gets the scale NaN: whoever reads it sees that.
+#pragma once
+
+#include "rotary_device.hpp"
+
+namespace vp {
+
+// Scale of a row whose largest magnitude has the bits `top` (of the fp32 value), and its inverse (0 for NaN).
+template <int CODE>
+__device__ __forceinline__ float code_scale(uint32_t top, float* inv) {
+    // 448 = 1.75 2^8, 127 = 1.984375 2^6
+    const int lead = CODE == CODE_E4M3 ? 8 : 6;
+    const uint32_t most = CODE == CODE_E4M3 ? 0x600000u : 0x7e0000u;
+    int e = (int)(top >> 23) - 127 - lead + ((top & 0x7fffffu) > most);
+    e = e < -100 ? -100 : e;
+    const bool odd = top >= 0x7f800000u;
+    *inv = odd ? 0.f : __uint_as_float((uint32_t)(127 - e) << 23);
+    return odd ? __builtin_nanf("") : __uint_as_float((uint32_t)(e + 127) << 23);
+}
+
+// Four codes of values that a scale has brought into range, the first in the lowest byte.
+template <int CODE>
+__device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d) {
+    if constexpr (CODE == CODE_E4M3) {
+        int v = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+        return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, v, true);
+    } else {
+        const uint32_t x = (uint32_t)(int)__builtin_rintf(a) & 255u, y = (uint32_t)(int)__builtin_rintf(b) & 255u;
+        const uint32_t z = (uint32_t)(int)__builtin_rintf(c) & 255u, w = (uint32_t)(int)__builtin_rintf(d);
+        return x | y << 8 | z << 16 | w << 24;
+    }
+}
+
+// A code's value (without scale) in bf16, exactly: features 0, 1 and 2, 3 of four.
+template <int CODE>
+__device__ __forceinline__ void decode4(uint32_t x, uint32_t* lo, uint32_t* hi) {
+    if constexpr (CODE == CODE_E4M3) {
+        *lo = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)x, 1.f, false));
+        *hi = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)x, 1.f, true));
+    } else {
+        const bf16x2 a = {(bf16)(float)(int8_t)x, (bf16)(float)(int8_t)(x >> 8)};
+        const bf16x2 b = {(bf16)(float)(int8_t)(x >> 16), (bf16)(float)(int8_t)(x >> 24)};
+        *lo = __builtin_bit_cast(uint32_t, a);
+        *hi = __builtin_bit_cast(uint32_t, b);
+    }
+}
+template <int CODE>
+__device__ __forceinline__ bf16x8 decode8(uint32_t x, uint32_t y) {
+    u32x4 v;
+    uint32_t a, b;
+    decode4<CODE>(x, &a, &b);
+    v[0] = a, v[1] = b;
+    decode4<CODE>(y, &a, &b);
+    v[2] = a, v[3] = b;
+    return __builtin_bit_cast(bf16x8, v);
+}
+// Code times scale in fp32.
+template <int CODE>
+__device__ __forceinline__ void values4(uint32_t x, float s, float (&f)[4]) {
+    if constexpr (CODE == CODE_E4M3) {
+        uint32_t a, b;
+        decode4<CODE>(x, &a, &b);
+        f[0] = __uint_as_float(a << 16) * s;
+        f[1] = __uint_as_float(a & 0xffff0000u) * s;
+        f[2] = __uint_as_float(b << 16) * s;
+        f[3] = __uint_as_float(b & 0xffff0000u) * s;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f[e] = (float)(int8_t)(x >> (8 * e)) * s;
+    }
+}
+
+// A slot's two scales.
+__device__ __forceinline__ float key_scale(uint32_t s) { return __uint_as_float(s << 16); }
+__device__ __forceinline__ float value_scale(uint32_t s) { return __uint_as_float(s & 0xffff0000u); }
+
+}  // namespace vp

@@ -24,7 +24,11 @@ struct CacheArgs {
     const int32_t* seen;     // [B], append and eviction only
     const int32_t* q_start;  // [B + 1]
     int B, T, max_q, max_len;
+    int code;                // CODE_*: of K and V; `dtype` is then that of the rows
+    uint32_t* scale;         // with codes: [npages, Hkv, page] of (K's, V's) bf16 scales, K's in the lower half
 };
+
+enum { CODE_NONE = 0, CODE_E4M3 = 1, CODE_INT8 = 2 };
 
 struct AttendArgs {
     CacheArgs c;
@@ -57,6 +61,13 @@ struct RotArgs {
     const uint64_t* freq;    // [dim / 2]
     int dim, axes, layout;   // layout 0: interleaved, 1: half
     float mag, sign;
+};
+
+struct NormArgs;
+struct ReadArgs {
+    CacheArgs c;
+    int out_dtype;
+    void *Ko, *Vo;           // [T, Hkv, 64]
 };
 
 struct EvictArgs {
@@ -97,6 +108,16 @@ __device__ __forceinline__ int cache_visible(const CacheSeq& s, int causal, int 
 void launch_rotary(int dtype, const void* x, int64_t x_stride, void* y, int64_t y_stride, int T,
                    int H, const RotArgs& r, hipStream_t st);
 void launch_cache_append(const AppendArgs& a, const RotArgs& r, hipStream_t st);
+void launch_norm_rotary(int dtype, const void* x, int64_t x_stride, void* y, int64_t y_stride, int T,
+                        int H, const NormArgs& nm, const RotArgs& r, hipStream_t st);
+size_t norm_grad_part_bytes(int T, int H, int per_head);
+void launch_norm_rotary_grad(int dtype, const void* x, int64_t x_stride, const void* g, int64_t g_stride,
+                             void* dx, float* dgain, float* dbias, int T, int H, const NormArgs& nm,
+                             const RotArgs& r, float* part, hipStream_t st);
+void launch_cache_append8(const AppendArgs& a, const NormArgs& qn, const NormArgs& kn, const RotArgs& r,
+                          hipStream_t st);
+void launch_cache_read(const ReadArgs& a, hipStream_t st);
+void launch_cache8_attend(const AttendArgs& a, hipStream_t st);
 void attend_plan(AttendArgs* a);
 int attend_rows(const AttendArgs& a);
 size_t attend_part_rows(const AttendArgs& a);

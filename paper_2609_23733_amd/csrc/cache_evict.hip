@@ -497,6 +497,26 @@ __global__ __launch_bounds__(256) void k_evict_move(EvictArgs a, EvictWs w) {
     }
 }
 
+// The same for 8-bit codes: four threads for K's 64 bytes, four for V's.
+__global__ __launch_bounds__(256) void k_evict_move8(EvictArgs a, EvictWs w) {
+    const int bh = blockIdx.y, hk = bh % a.c.Hkv, b = bh / a.c.Hkv;
+    const int n = w.left[bh], kbn = w.kbn[bh], moves = n - kbn;
+    if (blockIdx.x == 0 && hk == 0 && threadIdx.x == 0) a.length_out[b] = n;
+    const int c = threadIdx.x & 7;
+    char* rows = (char*)(c < 4 ? a.c.K : a.c.V) + (c & 3) * 16;
+    for (int j = blockIdx.x * 32 + (threadIdx.x >> 3); j < moves; j += gridDim.x * 32) {
+        const int s = w.mover[(int64_t)bh * w.cap + kbn + j], d = w.hole[(int64_t)bh * w.cap + j];
+        const int64_t src = slot_at(a.c, b, hk, s), dst = slot_at(a.c, b, hk, d);
+        if (src < 0 || dst < 0) continue;
+        *(u32x4*)(rows + dst * kD) = *(const u32x4*)(rows + src * kD);
+        if (c == 0) {
+            a.weight_out[dst] = a.c.weight[src];
+            a.stamp_out[dst] = a.c.stamp[src];
+            a.c.scale[dst] = a.c.scale[src];
+        }
+    }
+}
+
 void launch_cache_evict(const EvictArgs& a, hipStream_t st) {
     EvictWs w = evict_layout(a.c.B, a.c.Hkv, a.c.max_len, a.ws, nullptr);
     const int bh = a.c.B * a.c.Hkv;
@@ -517,7 +537,9 @@ void launch_cache_evict(const EvictArgs& a, hipStream_t st) {
     most = most < 1 ? 1 : most < a.keep ? most : a.keep;
     int64_t gx = (most + 31) / 32, cap = 8192 / bh + 1;
     if (gx > cap) gx = cap;
-    if (a.c.dtype == DT_BF16)
+    if (a.c.code)
+        hipLaunchKernelGGL(k_evict_move8, dim3(gx, bh), dim3(256), 0, st, a, w);
+    else if (a.c.dtype == DT_BF16)
         hipLaunchKernelGGL(k_evict_move<bf16>, dim3(gx, bh), dim3(256), 0, st, a, w);
     else
         hipLaunchKernelGGL(k_evict_move<float>, dim3(gx, bh), dim3(256), 0, st, a, w);

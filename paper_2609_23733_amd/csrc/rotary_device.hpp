@@ -1,0 +1,221 @@
+// Rotary positions: what the kernels that turn heads' features share.
+#pragma once
+
+#include "cache_device.hpp"
+
+namespace vp {
+
+template <typename T>
+struct Vec4 {
+    typedef T type __attribute__((__vector_size__(4 * sizeof(T))));
+};
+
+// Stores that pass the caches by (NT), for outputs larger than these: 43,968 tokens of 16 heads
+// 50 -> 44 us.
+template <bool NT, typename V>
+__device__ __forceinline__ void put(V* p, V v) {
+    if constexpr (NT) __builtin_nontemporal_store(v, p);
+    else *p = v;
+}
+
+// Eight features in a row, at a 16-byte boundary: 16 bytes at a time.
+template <bool NT, typename T>
+__device__ __forceinline__ void put8(T* p, typename Vec4<T>::type a, typename Vec4<T>::type b) {
+    if constexpr (sizeof(T) == 2) {
+        typedef T V8 __attribute__((__vector_size__(16)));
+        put<NT>((V8*)p, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+    } else {
+        put<NT>((typename Vec4<T>::type*)p, a);
+        put<NT>((typename Vec4<T>::type*)(p + 4), b);
+    }
+}
+
+// Sine and cosine of a fraction of a revolution, 32 bits: the nearest quarter turn from the top bits,
+// the rest, |x| <= pi / 4, by the Taylor series to x^9 and x^10 (errors 2e-9 and 2e-9 there).
+__device__ __forceinline__ void sincos_turn(uint32_t t, float* sn, float* cs) {
+    const uint32_t q = (t + 0x20000000u) >> 30;
+    const float x = (float)(int32_t)(t - (q << 30)) * (1.57079632679489662f / 1073741824.f), x2 = x * x;
+    float s = fmaf(x2, 1.f / 362880.f, -1.f / 5040.f);
+    s = fmaf(x2, s, 1.f / 120.f);
+    s = fmaf(x2, s, -1.f / 6.f);
+    s = fmaf(x2 * s, x, x);
+    float c = fmaf(x2, -1.f / 3628800.f, 1.f / 40320.f);
+    c = fmaf(x2, c, -1.f / 720.f);
+    c = fmaf(x2, c, 1.f / 24.f);
+    c = fmaf(x2, c, -0.5f);
+    c = fmaf(x2, c, 1.f);
+    const float a = q & 1 ? c : s, b = q & 1 ? s : c;
+    *sn = __uint_as_float(__float_as_uint(a) ^ ((q & 2) << 30));
+    *cs = __uint_as_float(__float_as_uint(b) ^ (((q + 1) & 2) << 30));
+}
+
+// Sum, and largest value, of the eight lanes that share a head's row.
+template <int CTRL>
+__device__ __forceinline__ int lane_of(int x) { return __builtin_amdgcn_update_dpp(0, x, CTRL, 0xf, 0xf, true); }
+__device__ __forceinline__ float sum8(float x) {
+    x += __builtin_bit_cast(float, lane_of<0xb1>(__builtin_bit_cast(int, x)));    // lane ^ 1
+    x += __builtin_bit_cast(float, lane_of<0x4e>(__builtin_bit_cast(int, x)));    // lane ^ 2
+    return x + __builtin_bit_cast(float, lane_of<0x141>(__builtin_bit_cast(int, x)));   // 7 - lane: the other four
+}
+__device__ __forceinline__ uint32_t max8(uint32_t x) {
+    x = max(x, (uint32_t)lane_of<0xb1>((int)x));
+    x = max(x, (uint32_t)lane_of<0x4e>((int)x));
+    return max(x, (uint32_t)lane_of<0x141>((int)x));
+}
+
+// Eight features of a head's row in one thread (chunk c of eight): pairs 4 c .. 4 c + 3 of those that are
+// turned, f[2 e] and f[2 e + 1] the pair's two; past the turned features two neighbours.  VEC: pairs per
+// section in fours, so that a thread's features are two runs of four, or one of eight.
+template <typename T, bool INTER, bool VEC>
+struct HeadTurn {
+    float co[4], si[4];
+    int lo, hi;                             // VEC: first features of the runs
+    int i0[VEC ? 1 : 4], i1[VEC ? 1 : 4];   // features of a pair
+    __device__ __forceinline__ void places(const RotArgs& r, int c) {
+        const int n = r.dim / r.axes / 2;
+        lo = 8 * c;
+        hi = lo + 4;
+        if constexpr (VEC) {
+            if (!INTER && 8 * c < r.dim) {
+                const int a = 4 * c / n;
+                lo = 2 * a * n + 4 * c - a * n;
+                hi = lo + n;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int p = 4 * c + e;
+                i0[e] = 2 * p;
+                i1[e] = 2 * p + 1;
+                if (!INTER && p < r.dim / 2) {
+                    const int a = p / n;
+                    i0[e] = 2 * a * n + p - a * n;
+                    i1[e] = i0[e] + n;
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void angles(const RotArgs& r, int64_t t, int c) {
+        const int n = r.dim / r.axes / 2;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            co[e] = 1.f;
+            si[e] = 0.f;
+            const int p = 4 * c + e;
+            if (p >= r.dim / 2) continue;
+            const uint64_t turn = (uint64_t)(int64_t)r.pos[t * r.axes + p / n] * r.freq[p];
+            float s, k;
+            sincos_turn((uint32_t)(turn >> 32), &s, &k);
+            co[e] = k * r.mag;
+            si[e] = s * r.mag;
+        }
+    }
+    template <typename U>
+    __device__ __forceinline__ void load(const U* x, float (&f)[8]) const {
+        typedef typename Vec4<U>::type V;
+        if constexpr (VEC) {
+            struct Run {
+                V a, b;
+            };
+            Run v;
+            if constexpr (INTER) {
+                v = *(const Run*)(x + lo);
+            } else {
+                v.a = *(const V*)(x + lo);
+                v.b = *(const V*)(x + hi);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                f[INTER ? e : 2 * e] = (float)v.a[e];
+                f[INTER ? 4 + e : 2 * e + 1] = (float)v.b[e];
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) f[2 * e] = (float)x[i0[e]], f[2 * e + 1] = (float)x[i1[e]];
+        }
+    }
+    template <bool NT>
+    __device__ __forceinline__ void store(T* y, const float (&f)[8]) const {
+        typedef typename Vec4<T>::type V;
+        if constexpr (VEC) {
+            V a, b;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                a[e] = (T)f[INTER ? e : 2 * e];
+                b[e] = (T)f[INTER ? 4 + e : 2 * e + 1];
+            }
+            if constexpr (INTER) {
+                put8<NT>(y + lo, a, b);
+            } else {
+                put<NT>((V*)(y + lo), a);
+                put<NT>((V*)(y + hi), b);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[i0[e]] = (T)f[2 * e], y[i1[e]] = (T)f[2 * e + 1];
+        }
+    }
+    __device__ __forceinline__ void turn(float (&f)[8]) const {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float a = f[2 * e], b = f[2 * e + 1];
+            f[2 * e] = a * co[e] - b * si[e];
+            f[2 * e + 1] = b * co[e] + a * si[e];
+        }
+    }
+    __device__ __forceinline__ void turn_back(float (&f)[8]) const {   // the transpose
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float a = f[2 * e], b = f[2 * e + 1];
+            f[2 * e] = a * co[e] + b * si[e];
+            f[2 * e + 1] = b * co[e] - a * si[e];
+        }
+    }
+};
+
+// The norm of a head's row over its 64 features: n = (x - mean) / sqrt(var + eps) (layer) or x / sqrt(mean x^2 +
+// eps), then n gain + bias.  Mean, then the mean square of what is left: no difference of large sums.
+struct NormArgs {
+    const float *gain, *bias;   // may be null; [64], or [heads, 64]
+    int on, layer, per_head;
+    float eps;
+};
+__device__ __forceinline__ float normalise(const NormArgs& nm, float (&f)[8]) {
+    if (nm.layer) {
+        const float mean = sum8(((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]))) * (1.f / kD);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) f[k] -= mean;
+    }
+    float s = 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) s = fmaf(f[k], f[k], s);
+    const float r = 1.f / sqrtf(sum8(s) * (1.f / kD) + nm.eps);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) f[k] *= r;
+    return r;
+}
+// A thread's eight gains and biases.
+struct Affine {
+    float gain[8], bias[8];
+    template <typename Turn>
+    __device__ __forceinline__ void set(const NormArgs& nm, const Turn& w, int h) {
+        const int at = nm.per_head ? h * kD : 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) gain[k] = 1.f, bias[k] = 0.f;
+        if (nm.gain) w.load(nm.gain + at, gain);
+        if (nm.bias) w.load(nm.bias + at, bias);
+    }
+};
+
+// Whether a rotation's pairs come in fours (HeadTurn's VEC).
+inline bool pairs_in_fours(const RotArgs& r) { return r.dim / r.axes / 2 % 4 == 0; }
+
+// Threads (of eight) per token: one per head while that leaves compute units idle, fewer, each
+// reusing its sines over more heads, when tokens alone make `threads` of them.
+inline int head_split(int64_t tokens, int heads, int64_t threads) {
+    int hs = 1;
+    while (hs < heads && tokens * 8 * hs < threads) hs *= 2;
+    return hs < heads ? hs : heads;
+}
+
+}  // namespace vp

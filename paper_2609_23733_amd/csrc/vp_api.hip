@@ -11,6 +11,7 @@
 
 #include "../../include/vggt_prime.h"
 #include "cache_device.hpp"
+#include "rotary_device.hpp"
 #include "vp_internal.hpp"
 
 namespace {
@@ -828,9 +829,9 @@ bool stride_ok(int64_t stride, int32_t heads, vp_dtype dt) {
            stride <= (1 << 23);
 }
 
-vp_status check_cache(const vp_cache* c, const vp_cache_batch* b, bool chunk, vp::CacheArgs* a) {
+vp_status check_cache(const vp_cache* c, const vp_cache_batch* b, bool chunk, vp::CacheArgs* a, bool codes = false) {
     if (!c || !b) return VP_ERR_INVALID_ARG;
-    if (c->dtype != VP_F32 && c->dtype != VP_BF16) return VP_ERR_INVALID_ARG;
+    if (!codes && c->dtype != VP_F32 && c->dtype != VP_BF16) return VP_ERR_INVALID_ARG;
     if (!c->K || !c->V || !aligned16(c->K) || !aligned16(c->V) || !aligned4(c->weight) ||
         !aligned4(c->stamp) || c->npages < 1 || c->Hkv < 1 || c->page < 1)
         return VP_ERR_INVALID_ARG;
@@ -859,6 +860,37 @@ vp_status check_cache(const vp_cache* c, const vp_cache_batch* b, bool chunk, vp
     return VP_OK;
 }
 
+// A cache of codes, or a plain one with `rows` its own type.
+vp_status check_cache8(const vp_cache8* c, const vp_cache_batch* b, bool chunk, vp::CacheArgs* a) {
+    if (!c) return VP_ERR_INVALID_ARG;
+    const bool codes = c->cache.dtype == VP_E4M3 || c->cache.dtype == VP_INT8;
+    if (c->rows != VP_F32 && c->rows != VP_BF16) return VP_ERR_INVALID_ARG;
+    if (codes ? !c->scale || !aligned16(c->scale) : c->cache.dtype != c->rows || c->scale) return VP_ERR_INVALID_ARG;
+    vp_status st = check_cache(&c->cache, b, chunk, a, codes);
+    if (st != VP_OK) return st;
+    a->dtype = c->rows;
+    if (codes) {
+        a->code = c->cache.dtype == VP_E4M3 ? vp::CODE_E4M3 : vp::CODE_INT8;
+        a->scale = (uint32_t*)c->scale;
+    }
+    return VP_OK;
+}
+
+vp_status check_norm(const vp_head_norm* n, vp::NormArgs* a) {
+    memset(a, 0, sizeof(*a));
+    if (!n) return VP_OK;
+    if ((n->kind != VP_NORM_LAYER && n->kind != VP_NORM_RMS) || !aligned16(n->gain) || !aligned16(n->bias) ||
+        !(n->eps >= 0) || !isfinite(n->eps) || (n->per_head != 0 && n->per_head != 1))
+        return VP_ERR_INVALID_ARG;
+    a->gain = n->gain;
+    a->bias = n->bias;
+    a->on = 1;
+    a->layer = n->kind == VP_NORM_LAYER;
+    a->per_head = n->per_head;
+    a->eps = n->eps == 0.f ? 1e-6f : n->eps;
+    return VP_OK;
+}
+
 bool heads_ok(int32_t Hq, int32_t Hkv) { return Hq >= Hkv && Hq % Hkv == 0; }
 
 // `tokens`: there are any, so positions have to be given.
@@ -883,15 +915,15 @@ vp_status check_rotary(const vp_rotary_spec* r, bool transpose, bool tokens, vp:
     return VP_OK;
 }
 
-vp_status attend_args(const vp_cache* cache, const vp_cache_batch* batch, int32_t Hq,
+vp_status attend_args(const vp_cache* cache, const vp_cache8* cache8, const vp_cache_batch* batch, int32_t Hq,
                       vp::AttendArgs* a) {
     memset(a, 0, sizeof(*a));
-    vp_status st = check_cache(cache, batch, true, &a->c);
+    vp_status st = cache ? check_cache(cache, batch, true, &a->c) : check_cache8(cache8, batch, true, &a->c);
     if (st != VP_OK) return st;
-    if (Hq < 1 || !heads_ok(Hq, cache->Hkv)) return VP_ERR_INVALID_ARG;
+    if (Hq < 1 || !heads_ok(Hq, a->c.Hkv)) return VP_ERR_INVALID_ARG;
     if (Hq > kMaxCacheHeads) return VP_ERR_UNSUPPORTED;
     a->Hq = Hq;
-    a->G = Hq / cache->Hkv;
+    a->G = Hq / a->c.Hkv;
     vp::attend_plan(a);
     // a launch has fewer than 2^32 threads, 2^24 workgroups: of the attention, the join and the weights
     if (((int64_t)a->c.B * a->c.Hkv * a->nsplit + 8) * a->row_tiles >= 1 << 24 ||
@@ -987,33 +1019,40 @@ vp_status vp_cache_append(const vp_cache* cache, const vp_cache_batch* batch, in
 
 size_t vp_cache_attend_workspace_bytes(const vp_cache* cache, const vp_cache_batch* batch, int32_t Hq) {
     vp::AttendArgs a;
-    return attend_args(cache, batch, Hq, &a) == VP_OK ? attend_ws(a) : 0;
+    return cache && attend_args(cache, nullptr, batch, Hq, &a) == VP_OK ? attend_ws(a) : 0;
 }
 
-vp_status vp_cache_attend_plan(const vp_cache* cache, const vp_cache_batch* batch, int32_t Hq,
-                               vp_cache_plan* plan) {
+size_t vp_cache8_attend_workspace_bytes(const vp_cache8* cache, const vp_cache_batch* batch, int32_t Hq) {
     vp::AttendArgs a;
-    vp_status st = attend_args(cache, batch, Hq, &a);
+    return attend_args(nullptr, cache, batch, Hq, &a) == VP_OK ? attend_ws(a) : 0;
+}
+
+namespace {
+
+vp_status plan_of(const vp_cache* cache, const vp_cache8* cache8, const vp_cache_batch* batch, int32_t Hq,
+                  vp_cache_plan* plan) {
+    vp::AttendArgs a;
+    vp_status st = attend_args(cache, cache8, batch, Hq, &a);
     if (st != VP_OK) return st;
     if (!plan) return VP_ERR_INVALID_ARG;
     *plan = {a.wide, vp::attend_rows(a), a.row_tiles, a.nsplit, a.chunk, vp::attend_logits(a) ? 1 : 0};
     return VP_OK;
 }
 
-vp_status vp_cache_attend(const vp_cache* cache, const vp_cache_batch* batch, int32_t Hq,
-                          const void* Q, int64_t q_stride, int32_t causal, float scale, void* O,
-                          float* lse, float* weight_out, void* ws, size_t ws_bytes, void* stream) {
+vp_status attend_of(const char* name, const vp_cache* cache, const vp_cache8* cache8, const vp_cache_batch* batch,
+                    int32_t Hq, const void* Q, int64_t q_stride, int32_t causal, float scale, void* O, float* lse,
+                    float* weight_out, void* ws, size_t ws_bytes, void* stream) {
     vp::AttendArgs a;
-    vp_status st = attend_args(cache, batch, Hq, &a);
+    vp_status st = attend_args(cache, cache8, batch, Hq, &a);
     if (st != VP_OK) return st;
     // (the weights' offsets are lse / scale, the logits' factor scale log2 e: both in fp32's range)
     if (!(scale == 0.f || (scale >= 0x1p-100f && scale <= 0x1p100f))) return VP_ERR_INVALID_ARG;
-    if (weight_out && (!cache->weight || !aligned4(weight_out))) return VP_ERR_INVALID_ARG;
+    if (weight_out && (!a.c.weight || !aligned4(weight_out))) return VP_ERR_INVALID_ARG;
     if (!ws || ((uintptr_t)ws & (kAlign - 1))) return VP_ERR_INVALID_ARG;
     if (ws_bytes < attend_ws(a)) return VP_ERR_WORKSPACE;
     if (batch->T == 0 || batch->max_q == 0) return VP_OK;
     if (!Q || !O || !lse || !aligned16(Q) || !aligned16(O) || !aligned4(lse) ||
-        !stride_ok(q_stride, Hq, cache->dtype) || (weight_out && Q == O))
+        !stride_ok(q_stride, Hq, (vp_dtype)a.c.dtype) || (weight_out && Q == O))
         return VP_ERR_INVALID_ARG;
     a.Q = Q;
     a.q_stride = q_stride;
@@ -1032,7 +1071,54 @@ vp_status vp_cache_attend(const vp_cache* cache, const vp_cache_batch* batch, in
     }
     (void)hipGetLastError();
     vp::launch_cache_attend(a, (hipStream_t)stream);
-    return hip_status("vp_cache_attend");
+    return hip_status(name);
+}
+
+vp_status evict_of(const char* name, const vp_cache* cache, const vp_cache8* cache8, const vp_cache_batch* batch,
+                   int32_t keep, int32_t sink, int32_t recent, float* weight_out, int32_t* stamp_out,
+                   int32_t* length_out, void* ws, size_t ws_bytes, void* stream) {
+    vp::EvictArgs a;
+    memset(&a, 0, sizeof(a));
+    vp_status st = cache ? check_cache(cache, batch, false, &a.c) : check_cache8(cache8, batch, false, &a.c);
+    if (st != VP_OK) return st;
+    if (!a.c.weight || !a.c.stamp || !batch->seen || !weight_out || !stamp_out || !length_out ||
+        !aligned4(weight_out) || !aligned4(stamp_out) || !aligned4(length_out) || keep < 1 || sink < 0 ||
+        recent < 0)
+        return VP_ERR_INVALID_ARG;
+    if (!ws || ((uintptr_t)ws & (kAlign - 1))) return VP_ERR_INVALID_ARG;
+    if (ws_bytes < vp_cache_evict_workspace_bytes(batch->B, a.c.Hkv, batch->max_len))
+        return VP_ERR_WORKSPACE;
+    a.keep = keep; a.sink = sink; a.recent = recent;
+    a.weight_out = weight_out; a.stamp_out = stamp_out; a.length_out = length_out;
+    a.ws = ws;
+    (void)hipGetLastError();
+    vp::launch_cache_evict(a, (hipStream_t)stream);
+    return hip_status(name);
+}
+
+}  // namespace
+
+vp_status vp_cache_attend_plan(const vp_cache* cache, const vp_cache_batch* batch, int32_t Hq,
+                               vp_cache_plan* plan) {
+    return cache ? plan_of(cache, nullptr, batch, Hq, plan) : VP_ERR_INVALID_ARG;
+}
+vp_status vp_cache8_attend_plan(const vp_cache8* cache, const vp_cache_batch* batch, int32_t Hq,
+                                vp_cache_plan* plan) {
+    return plan_of(nullptr, cache, batch, Hq, plan);
+}
+
+vp_status vp_cache_attend(const vp_cache* cache, const vp_cache_batch* batch, int32_t Hq,
+                          const void* Q, int64_t q_stride, int32_t causal, float scale, void* O,
+                          float* lse, float* weight_out, void* ws, size_t ws_bytes, void* stream) {
+    if (!cache) return VP_ERR_INVALID_ARG;
+    return attend_of("vp_cache_attend", cache, nullptr, batch, Hq, Q, q_stride, causal, scale, O, lse, weight_out, ws,
+                     ws_bytes, stream);
+}
+vp_status vp_cache8_attend(const vp_cache8* cache, const vp_cache_batch* batch, int32_t Hq,
+                           const void* Q, int64_t q_stride, int32_t causal, float scale, void* O,
+                           float* lse, float* weight_out, void* ws, size_t ws_bytes, void* stream) {
+    return attend_of("vp_cache8_attend", nullptr, cache, batch, Hq, Q, q_stride, causal, scale, O, lse, weight_out, ws,
+                     ws_bytes, stream);
 }
 
 size_t vp_cache_evict_workspace_bytes(int32_t B, int32_t Hkv, int32_t max_len) {
@@ -1045,21 +1131,115 @@ size_t vp_cache_evict_workspace_bytes(int32_t B, int32_t Hkv, int32_t max_len) {
 vp_status vp_cache_evict(const vp_cache* cache, const vp_cache_batch* batch, int32_t keep,
                          int32_t sink, int32_t recent, float* weight_out, int32_t* stamp_out,
                          int32_t* length_out, void* ws, size_t ws_bytes, void* stream) {
-    vp::EvictArgs a;
+    if (!cache) return VP_ERR_INVALID_ARG;
+    return evict_of("vp_cache_evict", cache, nullptr, batch, keep, sink, recent, weight_out, stamp_out, length_out, ws,
+                    ws_bytes, stream);
+}
+vp_status vp_cache8_evict(const vp_cache8* cache, const vp_cache_batch* batch, int32_t keep,
+                          int32_t sink, int32_t recent, float* weight_out, int32_t* stamp_out,
+                          int32_t* length_out, void* ws, size_t ws_bytes, void* stream) {
+    return evict_of("vp_cache8_evict", nullptr, cache, batch, keep, sink, recent, weight_out, stamp_out, length_out,
+                    ws, ws_bytes, stream);
+}
+
+vp_status vp_cache8_append(const vp_cache8* cache, const vp_cache_batch* batch, int32_t Hq,
+                           const void* Q, int64_t q_stride, const void* K, int64_t k_stride,
+                           const void* V, int64_t v_stride, const vp_head_norm* q_norm,
+                           const vp_head_norm* k_norm, const vp_rotary_spec* rot, void* Q_out, void* stream) {
+    vp::AppendArgs a;
     memset(&a, 0, sizeof(a));
-    vp_status st = check_cache(cache, batch, false, &a.c);
+    vp::RotArgs r;
+    vp::NormArgs qn, kn;
+    vp_status st = check_cache8(cache, batch, true, &a.c);
+    if (st == VP_OK) st = check_rotary(rot, false, batch->T > 0, &r);
+    if (st == VP_OK) st = check_norm(q_norm, &qn);
+    if (st == VP_OK) st = check_norm(k_norm, &kn);
     if (st != VP_OK) return st;
-    if (!cache->weight || !cache->stamp || !batch->seen || !weight_out || !stamp_out || !length_out ||
-        !aligned4(weight_out) || !aligned4(stamp_out) || !aligned4(length_out) || keep < 1 || sink < 0 ||
-        recent < 0)
+    const vp_dtype rows = cache->rows;
+    const int32_t Hkv = a.c.Hkv;
+    if (Q && (Hq < 1 || !heads_ok(Hq, Hkv))) return VP_ERR_INVALID_ARG;
+    if (Q && Hq > kMaxCacheHeads) return VP_ERR_UNSUPPORTED;
+    if (a.c.stamp && !batch->seen) return VP_ERR_INVALID_ARG;
+    if (batch->T == 0 || batch->max_q == 0) return VP_OK;
+    if (!K || !V || !aligned16(K) || !aligned16(V) || !stride_ok(k_stride, Hkv, rows) || !stride_ok(v_stride, Hkv, rows))
         return VP_ERR_INVALID_ARG;
-    if (!ws || ((uintptr_t)ws & (kAlign - 1))) return VP_ERR_INVALID_ARG;
-    if (ws_bytes < vp_cache_evict_workspace_bytes(batch->B, cache->Hkv, batch->max_len))
-        return VP_ERR_WORKSPACE;
-    a.keep = keep; a.sink = sink; a.recent = recent;
-    a.weight_out = weight_out; a.stamp_out = stamp_out; a.length_out = length_out;
-    a.ws = ws;
+    if (Q && (!Q_out || !aligned16(Q) || !aligned16(Q_out) || !stride_ok(q_stride, Hq, rows) ||
+              (Q == Q_out && q_stride != (int64_t)Hq * VP_HEAD_DIM)))
+        return VP_ERR_INVALID_ARG;
+    a.Hq = Q ? Hq : 0;
+    a.Q = Q; a.Kn = K; a.Vn = V; a.Qo = Q_out;
+    a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride;
     (void)hipGetLastError();
-    vp::launch_cache_evict(a, (hipStream_t)stream);
-    return hip_status("vp_cache_evict");
+    vp::launch_cache_append8(a, qn, kn, r, (hipStream_t)stream);
+    return hip_status("vp_cache8_append");
+}
+
+vp_status vp_cache8_read(const vp_cache8* cache, const vp_cache_batch* batch, vp_dtype dtype, void* K_out,
+                         void* V_out, void* stream) {
+    vp::ReadArgs a;
+    memset(&a, 0, sizeof(a));
+    vp_status st = check_cache8(cache, batch, true, &a.c);
+    if (st != VP_OK) return st;
+    if (dtype != VP_F32 && dtype != VP_BF16) return VP_ERR_INVALID_ARG;
+    if (batch->T == 0 || batch->max_q == 0) return VP_OK;
+    if (!K_out || !V_out || !aligned16(K_out) || !aligned16(V_out) || K_out == V_out) return VP_ERR_INVALID_ARG;
+    a.out_dtype = dtype == VP_BF16 ? 1 : 0;
+    a.Ko = K_out;
+    a.Vo = V_out;
+    (void)hipGetLastError();
+    vp::launch_cache_read(a, (hipStream_t)stream);
+    return hip_status("vp_cache8_read");
+}
+
+vp_status vp_norm_rotary(const vp_head_norm* norm, const vp_rotary_spec* rot, vp_dtype dtype, int32_t T, int32_t H,
+                         const void* x, int64_t x_stride, void* y, int64_t y_stride, void* stream) {
+    vp::RotArgs r;
+    vp::NormArgs n;
+    if (!norm) return VP_ERR_INVALID_ARG;
+    vp_status st = check_norm(norm, &n);
+    if (st == VP_OK) st = check_rotary(rot, false, T > 0, &r);
+    if (st != VP_OK) return st;
+    if (dtype != VP_F32 && dtype != VP_BF16) return VP_ERR_INVALID_ARG;
+    if (T < 0 || H < 1) return VP_ERR_INVALID_ARG;
+    if (T > kMaxTokens || H > kMaxCacheHeads) return VP_ERR_UNSUPPORTED;
+    if (T == 0) return VP_OK;
+    if (!x || !y || !aligned16(x) || !aligned16(y) || !stride_ok(x_stride, H, dtype) ||
+        !stride_ok(y_stride, H, dtype) || (x == y && x_stride != y_stride))
+        return VP_ERR_INVALID_ARG;
+    (void)hipGetLastError();
+    vp::launch_norm_rotary(dtype == VP_BF16 ? 1 : 0, x, x_stride, y, y_stride, T, H, n, r, (hipStream_t)stream);
+    return hip_status("vp_norm_rotary");
+}
+
+size_t vp_norm_rotary_grad_workspace_bytes(int32_t T, int32_t H, int32_t per_head) {
+    if (T < 0 || T > kMaxTokens || H < 1 || H > kMaxCacheHeads || (per_head != 0 && per_head != 1)) return 0;
+    return align_up(vp::norm_grad_part_bytes(T, H, per_head));
+}
+
+vp_status vp_norm_rotary_grad(const vp_head_norm* norm, const vp_rotary_spec* rot, vp_dtype dtype, int32_t T, int32_t H,
+                              const void* x, int64_t x_stride, const void* g, int64_t g_stride, void* dx, float* dgain,
+                              float* dbias, void* ws, size_t ws_bytes, void* stream) {
+    vp::RotArgs r;
+    vp::NormArgs n;
+    if (!norm) return VP_ERR_INVALID_ARG;
+    vp_status st = check_norm(norm, &n);
+    if (st == VP_OK) st = check_rotary(rot, false, T > 0, &r);
+    if (st != VP_OK) return st;
+    if (dtype != VP_F32 && dtype != VP_BF16) return VP_ERR_INVALID_ARG;
+    if (T < 0 || H < 1) return VP_ERR_INVALID_ARG;
+    if (T > kMaxTokens || H > kMaxCacheHeads) return VP_ERR_UNSUPPORTED;
+    if (!aligned4(dgain) || !aligned4(dbias)) return VP_ERR_INVALID_ARG;
+    if (T > 0 && (!x || !g || !aligned16(x) || !aligned16(g) || !aligned16(dx) || !stride_ok(x_stride, H, dtype) ||
+                  !stride_ok(g_stride, H, dtype) || dx == x || dx == g))
+        return VP_ERR_INVALID_ARG;
+    if (dgain || dbias) {
+        if (!ws || ((uintptr_t)ws & (kAlign - 1))) return VP_ERR_INVALID_ARG;
+        if (ws_bytes < vp_norm_rotary_grad_workspace_bytes(T, H, n.per_head)) return VP_ERR_WORKSPACE;
+    } else if (!dx || T == 0) {
+        return VP_OK;
+    }
+    (void)hipGetLastError();
+    vp::launch_norm_rotary_grad(dtype == VP_BF16 ? 1 : 0, x, x_stride, g, g_stride, dx, dgain, dbias, T, H, n, r,
+                                (float*)ws, (hipStream_t)stream);
+    return hip_status("vp_norm_rotary_grad");
 }

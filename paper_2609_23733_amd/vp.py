@@ -18,7 +18,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libvggtprime.so")
 
 VP_OK, VP_ERR_INVALID_ARG, VP_ERR_UNSUPPORTED, VP_ERR_WORKSPACE, VP_ERR_HIP = range(5)
-VP_F32, VP_BF16 = 0, 1
+VP_F32, VP_BF16, VP_E4M3, VP_INT8 = range(4)
+NORM_LAYER, NORM_RMS = 0, 1
 MODE_MEAN, MODE_SURR, MODE_FULL = 0, 1, 2
 RULE_THRESHOLD, RULE_ARGMAX, RULE_THRESHOLD_BINARY, RULE_ARGMAX_BINARY = 0, 1, 2, 3
 POOL_GATED, POOL_MEAN = 0, 1
@@ -37,7 +38,10 @@ EXPORTS = ("vp_workspace_bytes", "vp_router_score", "vp_router_score_noalloc",
            "vp_tome_workspace_bytes", "vp_tome_plan", "vp_tome_merge", "vp_tome_merge_qkv",
            "vp_tome_unmerge", "vp_rotary_frequencies", "vp_rotary", "vp_cache_append",
            "vp_cache_attend_workspace_bytes", "vp_cache_attend_plan", "vp_cache_attend",
-           "vp_cache_evict_workspace_bytes", "vp_cache_evict")
+           "vp_cache_evict_workspace_bytes", "vp_cache_evict", "vp_norm_rotary",
+           "vp_norm_rotary_grad_workspace_bytes", "vp_norm_rotary_grad", "vp_cache8_append",
+           "vp_cache8_attend_workspace_bytes", "vp_cache8_attend_plan", "vp_cache8_attend",
+           "vp_cache8_evict", "vp_cache8_read")
 TOME_SPECIAL = 5   # special tokens per view (camera + registers), never merged
 MODEL_DIM = MAX_HEADS * HEAD_DIM
 BLOCK_VECS = ("ln1_w", "ln1_b", "b_qkv", "b_o", "ls1", "ln2_w", "ln2_b", "b_fc1", "b_fc2", "ls2")
@@ -80,6 +84,15 @@ class vp_cache(ctypes.Structure):
     _fields_ = [("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("weight", ctypes.c_void_p),
                 ("stamp", ctypes.c_void_p), ("npages", ctypes.c_int64), ("page", ctypes.c_int32),
                 ("Hkv", ctypes.c_int32), ("d", ctypes.c_int32), ("dtype", ctypes.c_int)]
+
+
+class vp_cache8(ctypes.Structure):
+    _fields_ = [("cache", vp_cache), ("scale", ctypes.c_void_p), ("rows", ctypes.c_int)]
+
+
+class vp_head_norm(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int), ("gain", ctypes.c_void_p), ("bias", ctypes.c_void_p),
+                ("per_head", ctypes.c_int32), ("eps", ctypes.c_float)]
 
 
 class vp_cache_batch(ctypes.Structure):
@@ -171,7 +184,21 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.vp_cache_evict_workspace_bytes.argtypes = [i32, i32, i32]
     lib.vp_cache_evict_workspace_bytes.restype = ctypes.c_size_t
     lib.vp_cache_evict.argtypes = [cch, cba, i32, i32, i32, P, P, P, P, ctypes.c_size_t, P]
+    c8, hnp, szt = ctypes.POINTER(vp_cache8), ctypes.POINTER(vp_head_norm), ctypes.c_size_t
+    lib.vp_norm_rotary.argtypes = [hnp, rsp, ctypes.c_int, i32, i32, P, i64, P, i64, P]
+    lib.vp_norm_rotary_grad_workspace_bytes.argtypes = [i32, i32, i32]
+    lib.vp_norm_rotary_grad_workspace_bytes.restype = szt
+    lib.vp_norm_rotary_grad.argtypes = [hnp, rsp, ctypes.c_int, i32, i32, P, i64, P, i64, P, P, P, P, szt, P]
+    lib.vp_cache8_append.argtypes = [c8, cba, i32, P, i64, P, i64, P, i64, hnp, hnp, rsp, P, P]
+    lib.vp_cache8_attend_workspace_bytes.argtypes = [c8, cba, i32]
+    lib.vp_cache8_attend_workspace_bytes.restype = szt
+    lib.vp_cache8_attend_plan.argtypes = [c8, cba, i32, ctypes.POINTER(vp_cache_plan)]
+    lib.vp_cache8_attend.argtypes = [c8, cba, i32, P, i64, i32, f32, P, P, P, P, szt, P]
+    lib.vp_cache8_evict.argtypes = [c8, cba, i32, i32, i32, P, P, P, P, szt, P]
+    lib.vp_cache8_read.argtypes = [c8, cba, ctypes.c_int, P, P, P]
     for f in ("vp_rotary_frequencies", "vp_rotary", "vp_cache_append", "vp_cache_attend_plan",
+              "vp_norm_rotary", "vp_norm_rotary_grad", "vp_cache8_append", "vp_cache8_attend_plan",
+              "vp_cache8_attend", "vp_cache8_evict", "vp_cache8_read",
               "vp_cache_attend", "vp_cache_evict"):
         getattr(lib, f).restype = ctypes.c_int
     for f in ("vp_router_score", "vp_router_score_noalloc", "vp_router_logits", "vp_assign_heads",
