@@ -159,16 +159,17 @@ struct HeadTurn {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const float a = f[2 * e], b = f[2 * e + 1];
-            f[2 * e] = a * co[e] - b * si[e];
-            f[2 * e + 1] = b * co[e] + a * si[e];
+            // (fused by hand, so that every kernel rounds alike)
+            f[2 * e] = fmaf(a, co[e], -(b * si[e]));
+            f[2 * e + 1] = fmaf(b, co[e], a * si[e]);
         }
     }
     __device__ __forceinline__ void turn_back(float (&f)[8]) const {   // the transpose
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const float a = f[2 * e], b = f[2 * e + 1];
-            f[2 * e] = a * co[e] + b * si[e];
-            f[2 * e + 1] = b * co[e] - a * si[e];
+            f[2 * e] = fmaf(a, co[e], b * si[e]);
+            f[2 * e + 1] = fmaf(b, co[e], -(a * si[e]));
         }
     }
 };
@@ -189,7 +190,7 @@ __device__ __forceinline__ float normalise(const NormArgs& nm, float (&f)[8]) {
     float s = 0.f;
 #pragma unroll
     for (int k = 0; k < 8; ++k) s = fmaf(f[k], f[k], s);
-    const float r = 1.f / sqrtf(sum8(s) * (1.f / kD) + nm.eps);
+    const float r = 1.f / sqrtf(fmaf(sum8(s), 1.f / kD, nm.eps));
 #pragma unroll
     for (int k = 0; k < 8; ++k) f[k] *= r;
     return r;
