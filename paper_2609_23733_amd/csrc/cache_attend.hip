@@ -300,7 +300,7 @@ __device__ __forceinline__ bool clean_values(lds_char* v, int rows, int k, int e
 // Values that are not finite in slots [k0, k1) of a tile seen in part, which clean_values() took
 // out, for the rows that see them.  Rare: slot by slot from memory, logits by plain sums, few loads
 // at a time (this must not set the kernel's register count).
-template <typename T>
+template <typename T, int CODE>
 __device__ __forceinline__ void add_odd_values(const AttendArgs& a, Rows<T>& w, int b, int hk, int k0, int k1,
                                                int lane) {
     const int hh = lane >> 5;
@@ -311,8 +311,19 @@ __device__ __forceinline__ void add_odd_values(const AttendArgs& a, Rows<T>& w, 
         const int64_t at = ((((int64_t)page * a.c.Hkv + hk) << a.c.page_log2) +
                             (k & ((1 << a.c.page_log2) - 1))) * kD;
         const T *kr = (const T*)a.c.K + at, *vr = (const T*)a.c.V + at;
-        float x = 0.f;
-        if constexpr (Rows<T>::kBf) {
+        float x = 0.f, vs = 0.f;
+        if constexpr (CODE != CODE_NONE) {
+            const uint32_t sc = a.c.scale[at / kD];
+            vs = value_scale(sc);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                float f[4];
+                values4<CODE>(*(const uint32_t*)((const char*)a.c.K + at + 16 * (i >> 1) + 8 * hh + 4 * (i & 1)), key_scale(sc), f);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x = fmaf((float)(T)f[e], (float)w.qb[i >> 1][4 * (i & 1) + e], x);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        } else if constexpr (Rows<T>::kBf) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const bf16x8 kv = load_bf16x8((const bf16*)kr + 16 * i + 8 * hh);
@@ -336,9 +347,14 @@ __device__ __forceinline__ void add_odd_values(const AttendArgs& a, Rows<T>& w, 
         for (int m = 0; m < 2; ++m)
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
+                float f[4];
+                if constexpr (CODE != CODE_NONE)
+                    values4<CODE>(*(const uint32_t*)((const char*)a.c.V + at + 32 * m + 8 * g + 4 * hh), vs, f);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float v = (float)vr[32 * m + 8 * g + 4 * hh + e];
+                    float v;
+                    if constexpr (CODE != CODE_NONE) v = (float)(T)f[e];
+                    else v = (float)vr[32 * m + 8 * g + 4 * hh + e];
                     if (sees && !(fabsf(v) <= 3.4028235e38f)) w.o[m][4 * g + e] += p * v;
                 }
                 __builtin_amdgcn_sched_barrier(0);
@@ -352,9 +368,14 @@ __device__ __forceinline__ void add_odd_values(const AttendArgs& a, Rows<T>& w, 
 // 16 heads, bf16: 260 us, 950 TFLOP/s, the SIMDs' cycles 58 % in vector instructions and 43 % in MFMAs;
 // kernel alone, after some 40 passes: the first ones run at lower clocks, 280-350.  fp32, three prompts of
 // 8.6 GFLOP: 63 us).
-template <typename T, bool WIDE>
+//
+// CODE: K and V are 8-bit codes (wide bf16 rows only).  Tiles are the same in LDS, code times scale as bf16 values; they come through
+// registers: a wave loads a tile's 16 slots two tiles ahead and writes them, decoded, one ahead.
+template <typename T, bool WIDE, int CODE>
 __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(AttendArgs a) {
     typedef Geo<T, WIDE> G;
+    constexpr bool kCode = CODE != CODE_NONE;
+    static_assert(!kCode || (WIDE && G::kBf), "codes: wide bf16 rows");
     __shared__ __attribute__((aligned(1024))) char smem[G::kLds];
     const int tid = threadIdx.x, lane = tid & 63, l31 = lane & 31, hh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -461,10 +482,57 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(Att
                 issue_unit(t, unit, part & 1, unit_page(t, unit));
             }
         };
-        auto issue_first = [&]() {
+        bool odd = false;
+        // Codes: lane's 16 of slot lane / 4 of the wave's 16, and the slot's scales.
+        u32x4 kc, vc;
+        uint32_t sc = 0;
+        auto fetch_codes = [&](int t) {
+            const int k = unit_slot(t, wave);
+            const int64_t at = (((int64_t)pw.page(k >> a.c.page_log2, lane) * a.c.Hkv + hk) << a.c.page_log2) + (k & page_mask);
+            kc = *(const u32x4*)((const char*)a.c.K + at * kD + lane * 16);
+            vc = *(const u32x4*)((const char*)a.c.V + at * kD + lane * 16);
+            sc = a.c.scale[at + (lane >> 2)];
+        };
+        auto put_codes = [&](int t) {
+            const int r = lane >> 2, pc = 2 * (lane & 3);
+            lds_char* tile = ring + (t % G::NST) * G::kTile + (16 * wave + r) * 128;
+            typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+            u32x4 k[2], v[2];
+            decode16<CODE>(kc, key_scale(sc), k);
+            decode16<CODE>(vc, value_scale(sc), v);
+            const int k0 = c0 + t * G::TK, slot = k0 + 16 * wave;
+            if (!pw.sane || k0 + G::TK > seen_by_all) {
+                // (as clean_values() does to tiles that are copied)
+                const int at = slot >> a.c.page_log2;
+                const bool live = slot + r < c1 && (pw.sane || (at <= pw.last && pw.valid(pw.row[at])));
+                bool any = false;
 #pragma unroll
-            for (int t = 0; t < G::AHEAD; ++t)
-                if (t < nt) issue(t);
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        uint32_t x = v[i][j];
+                        const bool lo = (x & 0x7f80u) == 0x7f80u, hi = (x & 0x7f800000u) == 0x7f800000u;
+                        any = any || (live && (lo || hi));
+                        v[i][j] = !live ? 0u : x & (lo ? 0xffff0000u : 0xffffffffu) & (hi ? 0xffffu : 0xffffffffu);
+                    }
+                odd |= __builtin_amdgcn_ballot_w64(any) != 0;
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                *(lds_u32x4*)(tile + (((pc + i) ^ (r >> 1)) << 4)) = k[i];
+                *(lds_u32x4*)(tile + G::kTileV + (((pc + i) ^ (2 * (r & 3))) << 4)) = v[i];
+            }
+        };
+        auto issue_first = [&]() {
+            if constexpr (kCode) {
+                fetch_codes(0);
+                put_codes(0);
+                if (nt > 1) fetch_codes(1);
+            } else {
+#pragma unroll
+                for (int t = 0; t < G::AHEAD; ++t)
+                    if (t < nt) issue(t);
+            }
         };
         if constexpr (!WIDE || G::kBf) issue_first();
         // Groups of 16 slots of the tile at k0 that exist (all, unless the table is wrong).
@@ -480,10 +548,20 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(Att
             }
             return units;
         };
-        bool odd = false;
         // Tile t has come: its copies, and where it is seen in part its values are cleaned by the wave
         // that copied them.  Then (wide) all waves are past the tile whose place the next copies take.
         auto arrive = [&](int t) {
+            if constexpr (kCode) {
+                // (this wave's part of tile t is written; after the barrier all are, and no wave is at work on a
+                // tile before t - 1, so the next one's place is free)
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                __builtin_amdgcn_s_barrier();
+                if (t + 1 < nt) {
+                    put_codes(t + 1);
+                    if (t + 2 < nt) fetch_codes(t + 2);
+                }
+                return;
+            }
             const int more = nt - 1 - t, k0 = c0 + (tfirst + t * tstep) * G::TK;
             lds_char* tile = ring + (t % G::NST) * G::kTile;
             if constexpr (WIDE) {
@@ -909,7 +987,7 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(Att
                 if (!pw.sane || k0 + G::TK > seen_by_all)
 #pragma unroll
                     for (int nb = 0; nb < G::NB; ++nb)
-                        add_odd_values<T>(a, w[nb], b, hk, k0, k0 + G::TK < c1 ? k0 + G::TK : c1, lane);
+                        add_odd_values<T, CODE>(a, w[nb], b, hk, k0, k0 + G::TK < c1 ? k0 + G::TK : c1, lane);
             }
     }
 #pragma unroll
@@ -1405,8 +1483,9 @@ void attend_plan(AttendArgs* a) {
     // both 34; 200 over 20,000, 4,400 each, 49 and 41; 1,374 over themselves, 1,850 each in 1.3 rounds, 37 and
     // 29.  fp32, whose wide kernel has the faster products: 64 over 20,000 56 and 57, 90 over 20,000 80 and
     // 61, 200 over 600 22 and 18; 90 over 300 13.3 and 15.8.)
+    a->wide = 0;
     double items = work_items(a->c.code ? attend_rows(*a) : 32, false);
-    a->wide = !a->c.code && rows > 64 && (!bf || items * a->c.max_len > 512. * (items > 512 ? 1500 : 2500));
+    a->wide = (bf || !a->c.code) && rows > 64 && (!bf || items * a->c.max_len > 512. * (items > 512 ? 1500 : 2500));
     if (a->wide) items = work_items(attend_rows(*a), true);
     // An estimate that ranks divisions into ns ranges, in us where the card is lightly loaded (large calls, which HBM or
     // all SIMDs at once bound, take up to three times as long: 50 for 167 us of tokens over 137,400 slots, 153
@@ -1437,7 +1516,7 @@ void attend_plan(AttendArgs* a) {
 
 // Rows per workgroup.
 int attend_rows(const AttendArgs& a) {
-    if (a.c.code) return (int64_t)a.c.max_q * a.G <= 16 ? 16 : 32;
+    if (a.c.code && !a.wide) return (int64_t)a.c.max_q * a.G <= 16 ? 16 : 32;
     if (a.c.dtype == DT_BF16) return a.wide ? Geo<bf16, true>::RT : Geo<bf16, false>::RT;
     return a.wide ? Geo<float, true>::RT : Geo<float, false>::RT;
 }
@@ -1481,12 +1560,20 @@ static void weights_go(const AttendArgs& a, hipStream_t st) {
 template <typename T>
 static void attend_go(const AttendArgs& a, hipStream_t st) {
     const int64_t grid = ((int64_t)a.c.B * a.c.Hkv * a.nsplit + 7) / 8 * 8 * a.row_tiles;
-    if (a.c.code)
+    if (a.c.code && !a.wide) {
         launch_cache8_attend(a, st);
-    else if (a.wide)
-        hipLaunchKernelGGL((k_cache_attend<T, true>), dim3(grid), dim3(64 * Geo<T, true>::NW), 0, st, a);
-    else
-        hipLaunchKernelGGL((k_cache_attend<T, false>), dim3(grid), dim3(256), 0, st, a);
+    } else if (a.c.code) {
+        if constexpr (sizeof(T) == 2) {
+            if (a.c.code == CODE_E4M3)
+                hipLaunchKernelGGL((k_cache_attend<T, true, CODE_E4M3>), dim3(grid), dim3(64 * Geo<T, true>::NW), 0, st, a);
+            else
+                hipLaunchKernelGGL((k_cache_attend<T, true, CODE_INT8>), dim3(grid), dim3(64 * Geo<T, true>::NW), 0, st, a);
+        }
+    } else if (a.wide) {
+        hipLaunchKernelGGL((k_cache_attend<T, true, CODE_NONE>), dim3(grid), dim3(64 * Geo<T, true>::NW), 0, st, a);
+    } else {
+        hipLaunchKernelGGL((k_cache_attend<T, false, CODE_NONE>), dim3(grid), dim3(256), 0, st, a);
+    }
     join_go<T>(a, st);
     if (a.c.code == CODE_E4M3) weights_go<T, CODE_E4M3>(a, st);
     else if (a.c.code == CODE_INT8) weights_go<T, CODE_INT8>(a, st);

@@ -76,6 +76,32 @@ __device__ __forceinline__ void values4(uint32_t x, float s, float (&f)[4]) {
     }
 }
 
+// Sixteen codes times their scale as bf16 values.  e4m3 with a power of two: the conversion scales by itself (by the
+// exponent alone, so other scales take the product, and its rounding).
+template <int CODE>
+__device__ __forceinline__ void decode16(const u32x4& x, float s, u32x4 (&v)[2]) {
+    if constexpr (CODE == CODE_E4M3) {
+        const uint32_t b = __float_as_uint(s);
+        const bool plain = (b & 0x807fffffu) == 0 && b != 0 && b < 0x7f800000u;
+        if (__builtin_amdgcn_ballot_w64(!plain) == 0) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                v[j >> 1][2 * (j & 1)] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)x[j], s, false));
+                v[j >> 1][2 * (j & 1) + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)x[j], s, true));
+            }
+            return;
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        float f[4];
+        values4<CODE>(x[j], s, f);
+        const bf16x2 a = {(bf16)f[0], (bf16)f[1]}, b = {(bf16)f[2], (bf16)f[3]};
+        v[j >> 1][2 * (j & 1)] = __builtin_bit_cast(uint32_t, a);
+        v[j >> 1][2 * (j & 1) + 1] = __builtin_bit_cast(uint32_t, b);
+    }
+}
+
 // A slot's two scales.
 __device__ __forceinline__ float key_scale(uint32_t s) { return __uint_as_float(s << 16); }
 __device__ __forceinline__ float value_scale(uint32_t s) { return __uint_as_float(s & 0xffff0000u); }

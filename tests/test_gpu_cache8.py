@@ -353,6 +353,73 @@ def test_attend_values_of_any_size(cache, rows, vstd):  # noqa: F811
     check(cache, pool, normal(17, (20, 2, 64), rows, 3.0), [20], True, 0)
 
 
+WIDE = [
+    # lens, chunks, Hq, Hkv, page, kind, causal
+    ([1374], [1374], 16, 16, 64, "e4m3", True), ([3000, 2000, 700, 50], [1100, 900, 300, 0], 8, 4, 32, "int8", True),
+    ([3300, 90, 2000], [1500, 77, 900], 12, 4, 16, "e4m3", True), ([10000, 300], [260, 17], 16, 4, 64, "int8", False),
+    ([2500], [2000], 64, 16, 16, "int8", True), ([2400, 1300], [1300, 1300], 16, 8, 16, "e4m3", True),
+    ([9001], [500], 16, 2, 128, "e4m3", False),
+]
+
+
+@pytest.mark.parametrize("junk", ["nan", "bits"])
+@pytest.mark.parametrize("lens,qs,Hq,Hkv,page,kind,causal", WIDE)
+def test_attend_wide(cache, lens, qs, Hq, Hkv, page, kind, causal, junk):  # noqa: F811
+    log("attend8 wide %s %s Hq=%d Hkv=%d page=%d %s causal=%d %s" % (lens, qs, Hq, Hkv, page, kind, causal, junk))
+    pool = Pool8(cache, lens, Hkv, page, kind, seed=100 + sum(lens), junk=junk)
+    check(cache, pool, normal(7, (sum(qs), Hq, 64), BF), qs, causal, 1)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_attend_wide_odd(cache, kind):  # noqa: F811
+    """Whole-view calls with what is rare: scales of NaN in the chunk, missing pages, logits that rise late, values near
+    the largest."""
+    log("attend8 wide, odd contents %s" % kind)
+    n, q = 4000, 1500
+    Q = normal(9, (q, 16, 64), BF)
+    pool = Pool8(cache, [n], 2, 32, kind, seed=33)
+    odd_scales(pool, n)
+    check(cache, pool, Q, [q], True, 1)
+    pool = Pool8(cache, [n], 2, 32, kind, seed=34)
+    check(cache, pool, Q, [q], True, 1, gone=[s for p in (0, 3, 70, 124) for s in range(32 * p, 32 * p + 32) if s < n])
+    pool = Pool8(cache, [n], 2, 32, kind, seed=35, std=3.0)
+    k = pool.k[0].clone()
+    k[2500:] *= 8
+    pool.put(0, k, pool.v[0])
+    check(cache, pool, normal(10, (q, 16, 64), BF, 3.0), [q], False, 1)
+    pool = Pool8(cache, [n], 2, 32, kind, seed=36)
+    pool.put(0, pool.k[0], torch.clamp(pool.v[0], -4, 4) * 2e37)
+    check(cache, pool, Q, [q], True, 1)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("q", [5, 1500])
+def test_attend_scales_of_other_origin(cache, kind, q):  # noqa: F811
+    """Scales that are no powers of two: within another bf16 rounding of every value (2^-8) and key (2^-8 of a
+    logit's absolute sum X) where rows are many."""
+    log("attend8 other scales %s q=%d" % (kind, q))
+    n = 9000
+    pool = Pool8(cache, [n], 2, 64, kind, seed=38)
+    p, s = pool.at(0, n)
+    for j, have in ((0, pool.k), (1, pool.v)):
+        f = (1 + torch.rand(n, 2, generator=gen(40 + j))).to(BF)
+        code = (pool.K if j == 0 else pool.V)[p, :, s]
+        sc = (pool.scale[p, :, s, j].float() * f.float()).to(BF)
+        pool.scale[p, :, s, j] = sc
+        have[0] = codes64.decode64(code, sc.double(), kind)
+    Q = normal(9, (q, 4, 64), BF)
+    pc, batch = pool.cuda(), pool.batch([q])
+    assert cache.attend_plan(pc, batch, 4, q).shared == (q > 64)
+    O, lse = cache.attend(pc, batch, Q.cuda(), False)
+    for h in range(4):
+        one = torch.ones(q, n, dtype=torch.bool, device="cuda")
+        ro, rl, _, A, X = whole64(Q[:, h].cuda(), pool.k[0][:, h // 2].cuda(), pool.v[0][:, h // 2].cuda(), one, 0.125)
+        shift = 2.0 ** -8 * X + (64 * X + n / 16 + 16 + rl.abs()) * U       # of a logit
+        assert ((lse[:, h].double() - rl).abs() <= 2 * shift).all()
+        tol = (2 * (torch.exp(2 * shift) - 1))[:, None] * A + 2.0 ** -7 * A
+        assert ((O[:, h].double() - ro).abs() <= tol + 2.0 ** -8 * (ro.abs() + tol)).all()
+
+
 def test_attend_logits_of_minus_infinity(cache):  # noqa: F811
     """Keys of huge scale against fitting queries: weight 0; a row with no other logit gives zeros."""
     log("attend8 -inf logits")
