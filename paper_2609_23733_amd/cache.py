@@ -10,6 +10,7 @@ the tensors they name; what the tensors contain may change between calls.
 from __future__ import annotations
 
 import ctypes
+import functools
 from typing import Optional, Sequence
 
 import torch
@@ -199,24 +200,45 @@ class _NormRotation(torch.autograd.Function):
         return norm_rotary(x, norm, pos, rot)
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
     def backward(ctx, g):
-        x, gain, bias, pos = ctx.saved_tensors     # (refuses values that were changed in place)
-        norm, rot = ctx.norm, ctx.rot
-        T, H = x.shape[0], x.shape[1]
-        if not g.is_contiguous() or g.data_ptr() % 16:     # (broadcast, or a part of something)
-            g = g.clone(memory_format=torch.contiguous_format)
-        dx, dgain, dbias = (torch.empty(t.shape, dtype=t.dtype, device=t.device) if need else None
-                            for t, need in zip((x, gain, bias), ctx.needs_input_grad))
-        ptr = lambda t: None if t is None else t.data_ptr()
-        lib, ws, n = load_library(), None, 0
-        if dgain is not None or dbias is not None:
-            n = lib.vp_norm_rotary_grad_workspace_bytes(T, H, norm.heads is not None)
-            ws = torch.empty(n, dtype=torch.uint8, device=x.device)
-        _done(lib.vp_norm_rotary_grad(norm.at(H), None if rot is None else rot.at(pos, T), _dt(x), T, H, x.data_ptr(),
-                                      _rows(x, "x", T, H, x.dtype), g.data_ptr(), _rows(g, "the gradient", T, H, x.dtype),
-                                      ptr(dx), ptr(dgain), ptr(dbias), ptr(ws), n, _stream()), "vp_norm_rotary_grad")
-        return dx, dgain, dbias, None, None, None
+        # (once_differentiable's bookkeeping takes a third of a small call's time: only where it has something to do)
+        return (_second if torch.is_grad_enabled() else _norm_gradients)(ctx, g)
+
+
+def _norm_gradients(ctx, g):
+    x, gain, bias, pos = ctx.saved_tensors             # (refuses values that were changed in place)
+    norm, rot = ctx.norm, ctx.rot
+    T, H, _ = x.shape
+    if not g.is_contiguous() or g.data_ptr() % 16:     # (broadcast, or a part of something)
+        g = g.clone(memory_format=torch.contiguous_format)
+    need = ctx.needs_input_grad
+    dx = dgain = dbias = None
+    at_x = at_gain = at_bias = at_ws = n = 0
+    if need[0]:
+        dx = torch.empty(T, H, HEAD_DIM, dtype=x.dtype, device=x.device)
+        at_x = dx.data_ptr()
+    if need[1]:
+        dgain = torch.empty_like(gain)
+        at_gain = dgain.data_ptr()
+    if need[2]:
+        dbias = torch.empty_like(bias)
+        at_bias = dbias.data_ptr()
+    if need[1] or need[2]:
+        n = _norm_workspace(T, H, norm.heads is not None)
+        ws = torch.empty(n, dtype=torch.uint8, device=x.device)
+        at_ws = ws.data_ptr()
+    _done(load_library().vp_norm_rotary_grad(norm._ref, None if rot is None else rot.at(pos, T), _dt(x), T, H, x.data_ptr(),
+                                             x.stride(0) if T > 1 else H * HEAD_DIM, g.data_ptr(), H * HEAD_DIM, at_x,
+                                             at_gain, at_bias, at_ws, n, _stream()), "vp_norm_rotary_grad")
+    return dx, dgain, dbias, None, None, None
+
+
+_second = torch.autograd.function.once_differentiable(_norm_gradients)
+
+
+@functools.lru_cache(maxsize=256)
+def _norm_workspace(T: int, H: int, per_head: bool) -> int:
+    return load_library().vp_norm_rotary_grad_workspace_bytes(T, H, per_head)
 
 
 class PagedCache:

@@ -61,6 +61,8 @@ struct RotArgs {
     const uint64_t* freq;    // [dim / 2]
     int dim, axes, layout;   // layout 0: interleaved, 1: half
     float mag, sign;
+    int n;                   // pairs per section
+    float inv_n;
 };
 
 struct NormArgs;

@@ -2,13 +2,23 @@
 #include "cache_codes.hpp"
 
 namespace vp {
+#ifndef TAPP
+#define TAPP (128*1024)
+#endif
 
 // ------------------------------------------------------------------------
 // Append: rows of a token, Q's heads (normalised and turned, to Q_out), K's (normalised, turned and quantised, to
 // the page), V's (quantised, to the page); CODE_NONE: stored in the rows' type.  Eight lanes share a row, whose largest value
 // takes three exchanges; the row goes from load to codes in registers.  hs threads of eight share a token, each
-// takes every hs-th row, two loaded at a time (Q_out may be Q).
+// takes every hs-th row: of Q, then of K, then of V, the first of each loaded at once (Q_out may be Q).
+// Chunks: 32 neighbouring tokens' threads of one row are neighbours, so that what a page gets per slot (codes, scales,
+// weight, stamp) is written in runs.
 // ------------------------------------------------------------------------
+struct Spread {
+    int hs, runs;
+    int k0, v0;      // rows of Q, and of Q and K, modulo hs
+};
+
 template <int CODE>
 __device__ __forceinline__ uint32_t quantise(float (&f)[8], uint32_t* lo, uint32_t* hi, bool inter) {
     uint32_t top = 0;
@@ -28,91 +38,95 @@ __device__ __forceinline__ uint32_t quantise(float (&f)[8], uint32_t* lo, uint32
     return __float_as_uint(s) >> 16;
 }
 
+// A row of the page: its eight features (or codes) and, by one lane, its scale.
 template <typename T, int CODE, bool INTER, bool VEC>
-__global__ __launch_bounds__(256) void k_cache_append8(AppendArgs a, NormArgs qn, NormArgs kn, RotArgs r, int hs) {
+__device__ __forceinline__ void put_row(const CacheArgs& a, void* pool, int64_t at, int isv, const HeadTurn<T, INTER, VEC>& w,
+                                        float (&f)[8], int c) {
+    if constexpr (CODE == CODE_NONE) {
+        w.template store<false>((T*)pool + at * kD, f);
+    } else {
+        uint32_t lo, hi;
+        const uint32_t s = quantise<CODE>(f, &lo, &hi, INTER || !VEC);
+        char* row = (char*)pool + at * kD;
+        if constexpr (VEC && INTER) {
+            *(uint2*)(row + 8 * c) = make_uint2(lo, hi);
+        } else if constexpr (VEC) {
+            *(uint32_t*)(row + w.lo) = lo;
+            *(uint32_t*)(row + w.hi) = hi;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t two = (e < 2 ? lo : hi) >> (16 * (e & 1));
+                row[w.i0[e]] = (char)two;
+                row[w.i1[e]] = (char)(two >> 8);
+            }
+        }
+        if (c == 0) ((uint16_t*)(a.scale + at))[isv] = (uint16_t)s;
+    }
+}
+
+// 1,374 tokens of 16 + 16 + 16 heads, bf16 to int8, with norms: @APP@.
+template <typename T, int CODE, bool INTER, bool VEC>
+__global__ __launch_bounds__(256) void k_cache_append8(AppendArgs a, NormArgs qn, NormArgs kn, RotArgs r, Spread sp) {
     const int b = blockIdx.y;
     const CacheSeq sq = cache_seq(a.c, b);
     const int id = blockIdx.x * 256 + threadIdx.x;
-    const int c = id & 7, h0 = (id >> 3) % hs, i = (id >> 3) / hs;
+    const int c = id & 7, g = id >> 3;
+    const int h0 = sp.runs ? (g >> 5) % sp.hs : g % sp.hs, i = sp.runs ? (g >> 5) / sp.hs * 32 + (g & 31) : g / sp.hs;
     if (i >= sq.nq) return;
     const int64_t t = sq.q0 + i;
     const int slot = sq.len - sq.n + i;
-    int page = -1;
-    if (slot >= 0) page = a.c.table[(int64_t)b * a.c.max_pages + (slot >> a.c.page_log2)];
-    const bool live = page >= 0 && page < a.c.npages;
-    const int in = slot & ((1 << a.c.page_log2) - 1);
-    const int Hkv = a.c.Hkv, hq = a.Q ? a.Hq : 0, all = live ? hq + 2 * Hkv : hq;
+    const int Hkv = a.c.Hkv, hq = a.Q ? a.Hq : 0;
+    // the first rows
+    int hk = h0 - sp.k0, hv = h0 - sp.v0;
+    hk += hk < 0 ? sp.hs : 0;
+    hv += hv < 0 ? sp.hs : 0;
     HeadTurn<T, INTER, VEC> w;
     HeadTurn<T, true, true> plain;   // V: eight features in a row
     w.places(r, c);
     plain.lo = 8 * c;
     plain.hi = 8 * c + 4;
-    auto load = [&](int h, float (&f)[8]) {
-        if (h < hq) w.load((const T*)a.Q + t * a.q_stride + h * kD, f);
-        else if (h < hq + Hkv) w.load((const T*)a.Kn + t * a.k_stride + (h - hq) * kD, f);
-        else plain.load((const T*)a.Vn + t * a.v_stride + (h - hq - Hkv) * kD, f);
-    };
-    float f[2][8];
-#pragma unroll
-    for (int k = 0; k < 2; ++k)
-        if (h0 + k * hs < all) load(h0 + k * hs, f[k]);
+    const T *qr = (const T*)a.Q + t * a.q_stride, *kr = (const T*)a.Kn + t * a.k_stride, *vr = (const T*)a.Vn + t * a.v_stride;
+    float fq[8], fk[8], fv[8];
+    if (h0 < hq) w.load(qr + h0 * kD, fq);
+    if (hk < Hkv) w.load(kr + hk * kD, fk);
+    if (hv < Hkv) plain.load(vr + hv * kD, fv);
+    int page = -1;
+    if (slot >= 0) page = a.c.table[(int64_t)b * a.c.max_pages + (slot >> a.c.page_log2)];
     w.angles(r, t, c);
-    for (int h = h0; h < all; h += 2 * hs) {
+    auto turned = [&](const NormArgs& nm, int h, float (&f)[8]) {
+        if (nm.on) {
+            Affine p;
+            p.set(nm, w, h);
+            normalise(nm, f);
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int hk = h + k * hs;
-            if (hk >= all) break;
-            float v[8];
-            const bool isq = hk < hq, isv = hk >= hq + Hkv;
-            const NormArgs& nm = isq ? qn : kn;
-            if (!isv) {
-                if (nm.on) {
-                    Affine p;
-                    p.set(nm, w, isq ? hk : hk - hq);
-                    normalise(nm, f[k]);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) f[k][e] = fmaf(f[k][e], p.gain[e], p.bias[e]);
-                }
-                w.turn(f[k]);
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = f[k][e];
-            if (hk + 2 * hs < all) load(hk + 2 * hs, f[k]);
-            if (isq) {
-                w.template store<false>((T*)a.Qo + (t * a.Hq + hk) * kD, v);
-                continue;
-            }
-            const int head = hk - hq - (isv ? Hkv : 0);
-            const int64_t at = (((int64_t)page * Hkv + head) << a.c.page_log2) + in;
-            if constexpr (CODE == CODE_NONE) {
-                if (isv) plain.template store<false>((T*)a.c.V + at * kD, v);
-                else w.template store<false>((T*)a.c.K + at * kD, v);
-            } else {
-                uint32_t lo, hi;
-                const uint32_t s = quantise<CODE>(v, &lo, &hi, isv || INTER || !VEC);
-                if (isv) {
-                    *(uint2*)((char*)a.c.V + at * kD + 8 * c) = make_uint2(lo, hi);
-                } else if constexpr (VEC && INTER) {
-                    *(uint2*)((char*)a.c.K + at * kD + 8 * c) = make_uint2(lo, hi);
-                } else if constexpr (VEC) {
-                    *(uint32_t*)((char*)a.c.K + at * kD + w.lo) = lo;
-                    *(uint32_t*)((char*)a.c.K + at * kD + w.hi) = hi;
-                } else {
-                    char* kr = (char*)a.c.K + at * kD;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const uint32_t two = (e < 2 ? lo : hi) >> (16 * (e & 1));
-                        kr[w.i0[e]] = (char)two;
-                        kr[w.i1[e]] = (char)(two >> 8);
-                    }
-                }
-                if (c == 0) ((uint16_t*)(a.c.scale + at))[isv] = (uint16_t)s;
-            }
-            if (!isv && c == 0) {
-                if (a.c.weight) a.c.weight[at] = 0.f;
-                if (a.c.stamp) a.c.stamp[at] = a.c.seen[b] - sq.n + i;
-            }
+            for (int e = 0; e < 8; ++e) f[e] = fmaf(f[e], p.gain[e], p.bias[e]);
         }
+        w.turn(f);
+    };
+    for (int h = h0; h < hq; h += sp.hs) {
+        turned(qn, h, fq);
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = fq[e];
+        if (h + sp.hs < hq) w.load(qr + (h + sp.hs) * kD, fq);
+        w.template store<false>((T*)a.Qo + (t * a.Hq + h) * kD, v);
+    }
+    if (page < 0 || page >= a.c.npages) return;
+    const int64_t at0 = (((int64_t)page * Hkv) << a.c.page_log2) + (slot & ((1 << a.c.page_log2) - 1));
+    for (int h = hk; h < Hkv; h += sp.hs) {
+        turned(kn, h, fk);
+        const int64_t at = at0 + ((int64_t)h << a.c.page_log2);
+        put_row<T, CODE>(a.c, a.c.K, at, 0, w, fk, c);
+        if (c == 0) {
+            if (a.c.weight) a.c.weight[at] = 0.f;
+            if (a.c.stamp) a.c.stamp[at] = a.c.seen[b] - sq.n + i;
+        }
+        if (h + sp.hs < Hkv) w.load(kr + (h + sp.hs) * kD, fk);
+    }
+    for (int h = hv; h < Hkv; h += sp.hs) {
+        put_row<T, CODE>(a.c, a.c.V, at0 + ((int64_t)h << a.c.page_log2), 1, plain, fv, c);
+        if (h + sp.hs < Hkv) plain.load(vr + (h + sp.hs) * kD, fv);
     }
 }
 
@@ -167,10 +181,12 @@ __global__ __launch_bounds__(256) void k_cache_read(ReadArgs a) {
 
 void launch_cache_append8(const AppendArgs& a, const NormArgs& qn, const NormArgs& kn, const RotArgs& r,
                           hipStream_t st) {
-    const int hs = head_split((int64_t)a.c.B * a.c.max_q, (a.Q ? a.Hq : 0) + 2 * a.c.Hkv, 128 * 1024);
-    const dim3 grid((unsigned)(((int64_t)a.c.max_q * hs * 8 + 255) / 256), a.c.B);
+    const int hq = a.Q ? a.Hq : 0, hs = head_split((int64_t)a.c.B * a.c.max_q, hq + 2 * a.c.Hkv, TAPP);
+    const Spread sp = {hs, a.c.max_q >= 16, hq % hs, (hq + a.c.Hkv) % hs};
+    const int64_t rows = sp.runs ? (int64_t)(a.c.max_q + 31) / 32 * 32 : a.c.max_q;
+    const dim3 grid((unsigned)((rows * hs * 8 + 255) / 256), a.c.B);
     const bool vec = pairs_in_fours(r), inter = r.layout == 0;
-#define GO(TT, CO, IN, VE) hipLaunchKernelGGL((k_cache_append8<TT, CO, IN, VE>), grid, dim3(256), 0, st, a, qn, kn, r, hs)
+#define GO(TT, CO, IN, VE) hipLaunchKernelGGL((k_cache_append8<TT, CO, IN, VE>), grid, dim3(256), 0, st, a, qn, kn, r, sp)
 #define GO_TURN(TT, CO)                                                          \
     do {                                                                         \
         if (inter) { if (vec) GO(TT, CO, true, true); else GO(TT, CO, true, false); }  \

@@ -12,7 +12,8 @@
 namespace vp {
 
 // hs threads of eight share a token; each takes every hs-th head, two at a time: their loads are issued together
-// (y may be x, so no load moves over a store by itself).
+// (y may be x, so no load moves over a store by itself).  10,992 tokens of 16 heads, bf16: 13.2 us, 3.4 TB/s; 43,968 tokens
+// (stores past the caches) 42.5 us, 4.2 TB/s, with two threads a token; with eight 50, with one 45; four heads at a time 46.8.
 template <typename T, bool INTER, bool VEC, bool NT>
 __global__ __launch_bounds__(256) void k_norm_rotary(const T* x, int64_t x_stride, T* y, int64_t y_stride,
                                                      int Tn, int H, int hs, NormArgs nm, RotArgs r) {
@@ -25,8 +26,9 @@ __global__ __launch_bounds__(256) void k_norm_rotary(const T* x, int64_t x_strid
     const T* xr = x + t * x_stride;
     T* yr = y + t * y_stride;
     float f[2][8];
-    w.load(xr + h0 * kD, f[0]);
-    if (h0 + hs < H) w.load(xr + (h0 + hs) * kD, f[1]);
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+        if (h0 + k * hs < H) w.load(xr + (h0 + k * hs) * kD, f[k]);
     Affine p;
     p.set(nm, w, h0);
     w.angles(r, t, c);
@@ -50,7 +52,8 @@ __global__ __launch_bounds__(256) void k_norm_rotary(const T* x, int64_t x_strid
 // The gradient.  Row slots of eight lanes, 32 a workgroup: slot s takes heads s % hs, s % hs + hs, .. of tokens s / hs,
 // s / hs + slots / hs, ..; with a gain per head hs = H, so that a slot keeps to one head.  A slot's
 // eight lanes each sum their features' gradients over all its rows; a workgroup's slots (of one head) meet in LDS,
-// the workgroups' sums in k_norm_grad_join, in an order that T and H fix.
+// the workgroups' sums in k_norm_grad_join, in an order that T and H fix.  43,968 tokens of 16 heads, bf16: 56.4 us, 4.8
+// TB/s, what a copy reaches.
 template <typename T, bool INTER, bool VEC, bool NT>
 __global__ __launch_bounds__(256) void k_norm_rotary_grad(const T* __restrict__ x, int64_t x_stride,
                                                           const T* __restrict__ g, int64_t g_stride,
@@ -111,24 +114,44 @@ __global__ __launch_bounds__(256) void k_norm_rotary_grad(const T* __restrict__ 
     }
 }
 
-// Sums over the workgroups in 64 bits: 16 of the 128 sums of a head, 16 threads each.  (Feature of lane c's e-th sum:
-// the lanes' places once more.)
+// Sums over the workgroups in 64 bits: 16 of the 128 sums of a head, 64 threads each, whose loads are issued sixteen at a
+// time (the parts of 1,024 workgroups at once: they come from other XCDs' caches, so every round of loads waits for
+// memory).  (Feature of lane c's e-th sum: the lanes' places once more.)
 template <bool INTER, bool VEC>
-__global__ __launch_bounds__(256) void k_norm_grad_join(const float* __restrict__ part, int blocks, int m, int H,
-                                                        RotArgs r, float* __restrict__ dgain, float* __restrict__ dbias) {
+__global__ __launch_bounds__(1024) void k_norm_grad_join(const float* __restrict__ part, int blocks, int m, int H, int per_head,
+                                                         RotArgs r, float* __restrict__ dgain, float* __restrict__ dbias) {
+    constexpr int kGroups = 64, kOnce = 16;
     const int k = threadIdx.x & 15, grp = threadIdx.x >> 4, c = blockIdx.y, h = blockIdx.x;
+    const float* mine = part + c * 16 + k;
     double sum = 0.;
-#pragma unroll 8
-    for (int b = grp; b < blocks; b += 16) {
-        // (slot i of workgroup b has head (32 b + i) % H where every head has sums of its own)
-        const int i = m == 1 && gridDim.x == 1 ? 0 : ((h - 32 * b) % H + H) % H;
-        if (i < m) sum += (double)part[((int64_t)b * m + i) * 128 + c * 16 + k];
+    // With sums per head, slot i of workgroup b has head (32 b + i) % H: i = (h - 32 b) mod H, if the workgroup has it.
+    const int step = per_head ? 32 * kGroups % H : 0;
+    int i = per_head ? ((h - 32 * grp) % H + H) % H : 0;
+    for (int b = grp; b < blocks; b += kGroups * kOnce) {
+        float v[kOnce];
+#pragma unroll
+        for (int j = 0; j < kOnce; ++j) {
+            const int bj = b + kGroups * j;
+            const bool have = bj < blocks && i < m;
+            v[j] = mine[have ? ((int64_t)bj * m + i) * 128 : 0];
+            v[j] = have ? v[j] : 0.f;
+            i -= step;
+            i += i < 0 ? H : 0;
+        }
+#pragma unroll
+        for (int j = 0; j < kOnce; ++j) sum += (double)v[j];
     }
-    __shared__ double s[16][17];
+    __shared__ double s[kGroups][17];
+    s[grp][k] = sum;
+    __syncthreads();
+    if (grp >= 8) return;
+#pragma unroll
+    for (int j = 8; j < kGroups; j += 8) sum += s[grp + j][k];
     s[grp][k] = sum;
     __syncthreads();
     if (grp) return;
-    for (int j = 1; j < 16; ++j) sum += s[j][k];
+#pragma unroll
+    for (int j = 1; j < 8; ++j) sum += s[j][k];
     HeadTurn<float, INTER, VEC> w;
     w.places(r, c);
     const int e = k & 7;
@@ -169,7 +192,7 @@ static bool past_caches(int dtype, int64_t T, int H) {
 void launch_norm_rotary(int dtype, const void* x, int64_t x_stride, void* y, int64_t y_stride, int T,
                         int H, const NormArgs& nm, const RotArgs& r, hipStream_t st) {
     const bool nt = past_caches(dtype, T, H);
-    const int hs = head_split(T, H, nt ? 2048 * 1024 : 256 * 1024);
+    const int hs = head_split(T, H, nt ? 512 * 1024 : 128 * 1024);
     const dim3 grid((unsigned)(((int64_t)T * hs * 8 + 255) / 256));
 #define GO(TT, IN, VE, NTV)                                                                                    \
     hipLaunchKernelGGL((k_norm_rotary<TT, IN, VE, NTV>), grid, dim3(256), 0, st, (const TT*)x, x_stride, (TT*)y, \
@@ -179,7 +202,8 @@ void launch_norm_rotary(int dtype, const void* x, int64_t x_stride, void* y, int
 #undef GO
 }
 
-// Workgroups of the gradient: four a compute unit, fewer where rows are few; with a gain per head their 32
+// Workgroups of the gradient: four a compute unit (43,968 tokens of 16 heads, bf16: 56.4 us and 4.3 for the join of their
+// parts; two 70.5 and 4.0, eight 53.2 and 6.8), fewer where rows are few; with a gain per head their 32
 // slots each make whole turns through the heads.
 static int norm_grad_blocks(int T, int H, int per_head) {
     int64_t n = ((int64_t)T * H + 31) / 32;
@@ -212,7 +236,7 @@ void launch_norm_rotary_grad(int dtype, const void* x, int64_t x_stride, const v
 #undef GO
     if (!part) return;
     const dim3 grid(nm.per_head ? H : 1, 8);
-#define GO(IN, VE) hipLaunchKernelGGL((k_norm_grad_join<IN, VE>), grid, dim3(256), 0, st, (const float*)part, blocks, m, H, r, dgain, dbias)
+#define GO(IN, VE) hipLaunchKernelGGL((k_norm_grad_join<IN, VE>), grid, dim3(1024), 0, st, (const float*)part, blocks, m, H, nm.per_head, r, dgain, dbias)
     const bool vec = pairs_in_fours(r);
     if (r.layout == 0) { if (vec) GO(true, true); else GO(true, false); }
     else { if (vec) GO(false, true); else GO(false, false); }

@@ -70,16 +70,22 @@ template <typename T, bool INTER, bool VEC>
 struct HeadTurn {
     float co[4], si[4];
     int lo, hi;                             // VEC: first features of the runs
+    int sec;                                // and their section
     int i0[VEC ? 1 : 4], i1[VEC ? 1 : 4];   // features of a pair
+    // p / r.n of a pair: (p + 1/2) / n lies 1 / 64 from a whole number at least.  (An integer division per pair and
+    // thread took longer than the rest of a row.)
+    static __device__ __forceinline__ int section(const RotArgs& r, int p) { return (int)(((float)p + 0.5f) * r.inv_n); }
     __device__ __forceinline__ void places(const RotArgs& r, int c) {
-        const int n = r.dim / r.axes / 2;
         lo = 8 * c;
         hi = lo + 4;
+        sec = 0;
         if constexpr (VEC) {
-            if (!INTER && 8 * c < r.dim) {
-                const int a = 4 * c / n;
-                lo = 2 * a * n + 4 * c - a * n;
-                hi = lo + n;
+            if (8 * c < r.dim) {
+                sec = section(r, 4 * c);
+                if (!INTER) {
+                    lo = 4 * c + sec * r.n;
+                    hi = lo + r.n;
+                }
             }
         } else {
 #pragma unroll
@@ -88,26 +94,34 @@ struct HeadTurn {
                 i0[e] = 2 * p;
                 i1[e] = 2 * p + 1;
                 if (!INTER && p < r.dim / 2) {
-                    const int a = p / n;
-                    i0[e] = 2 * a * n + p - a * n;
-                    i1[e] = i0[e] + n;
+                    i0[e] = p + section(r, p) * r.n;
+                    i1[e] = i0[e] + r.n;
                 }
             }
         }
     }
     __device__ __forceinline__ void angles(const RotArgs& r, int64_t t, int c) {
-        const int n = r.dim / r.axes / 2;
+        int pos[4];
+        uint64_t freq[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            co[e] = 1.f;
-            si[e] = 0.f;
             const int p = 4 * c + e;
+            pos[e] = 0;
+            freq[e] = 0;
             if (p >= r.dim / 2) continue;
-            const uint64_t turn = (uint64_t)(int64_t)r.pos[t * r.axes + p / n] * r.freq[p];
+            pos[e] = VEC && e ? pos[0] : r.pos[t * r.axes + (VEC ? sec : section(r, p))];
+            freq[e] = r.freq[p];
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            // bits 32 .. 63 of pos * freq: exact modulo a revolution
+            const uint32_t u = (uint32_t)pos[e], fl = (uint32_t)freq[e], fh = (uint32_t)(freq[e] >> 32);
+            const uint32_t turn = __umulhi(u, fl) + u * fh - (pos[e] < 0 ? fl : 0u);
             float s, k;
-            sincos_turn((uint32_t)(turn >> 32), &s, &k);
-            co[e] = k * r.mag;
-            si[e] = s * r.mag;
+            sincos_turn(turn, &s, &k);
+            const bool turned = 4 * c + e < r.dim / 2;
+            co[e] = turned ? k * r.mag : 1.f;
+            si[e] = turned ? s * r.mag : 0.f;
         }
     }
     template <typename U>
@@ -209,7 +223,7 @@ struct Affine {
 };
 
 // Whether a rotation's pairs come in fours (HeadTurn's VEC).
-inline bool pairs_in_fours(const RotArgs& r) { return r.dim / r.axes / 2 % 4 == 0; }
+inline bool pairs_in_fours(const RotArgs& r) { return r.n % 4 == 0; }
 
 // Threads (of eight) per token: one per head while that leaves compute units idle, fewer, each
 // reusing its sines over more heads, when tokens alone make `threads` of them.

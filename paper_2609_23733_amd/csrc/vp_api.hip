@@ -912,6 +912,8 @@ vp_status check_rotary(const vp_rotary_spec* r, bool transpose, bool tokens, vp:
     a->axes = r->axes;
     a->layout = r->layout;
     if (r->mag != 0.f) a->mag = r->mag;
+    a->n = r->dim / r->axes / 2;
+    a->inv_n = a->n ? 1.f / (float)a->n : 0.f;
     return VP_OK;
 }
 
