@@ -278,13 +278,14 @@ __global__ __launch_bounds__(256, NB == 1 && kBfRows<T> ? 3 : 2) void k_cache8_a
             }
             pw.start(a.c, b, c0, c1 - 1, lane);
             Tile8 w0, w1;
+            // A tile's loads are issued before the last one's are waited for; no branch skips them (past the end: the last
+            // tile again), as the wait counts the loads behind those it is for on every way there.
             fetch(0, w0);
             for (int t = 0; t < nt; t += 2) {
-                if (t + 1 < nt) fetch(t + 1, w1);
+                fetch(t + 1 < nt ? t + 1 : nt - 1, w1);
                 compute(t, w0);
-                if (t + 1 >= nt) break;
-                if (t + 2 < nt) fetch(t + 2, w0);
-                compute(t + 1, w1);
+                fetch(t + 2 < nt ? t + 2 : nt - 1, w0);
+                if (t + 1 < nt) compute(t + 1, w1);
             }
             float top = 0.f;
 #pragma unroll

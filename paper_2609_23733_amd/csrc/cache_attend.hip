@@ -56,6 +56,14 @@ struct Geo {
     }
 };
 
+// Wide workgroups over 8-bit codes: eight waves, which share the decoding of a tile (with four, a view over 43,968 slots
+// takes 298 us instead of @W8@).
+template <typename T, bool WIDE, int CODE>
+struct GeoOf : Geo<T, WIDE> {
+    static constexpr int NW = CODE == CODE_NONE ? Geo<T, WIDE>::NW : 8;
+    static constexpr int RT = WIDE ? 32 * Geo<T, WIDE>::NB * NW : 32;
+};
+
 template <int CPT>
 __device__ __forceinline__ void wait_tiles(int behind) {
     // Copies are counted in the order of their issue: all but the `behind` youngest tiles' have
@@ -372,8 +380,8 @@ __device__ __forceinline__ void add_odd_values(const AttendArgs& a, Rows<T>& w, 
 // CODE: K and V are 8-bit codes (wide bf16 rows only).  Tiles are the same in LDS, code times scale as bf16 values; they come through
 // registers: a wave loads a tile's 16 slots two tiles ahead and writes them, decoded, one ahead.
 template <typename T, bool WIDE, int CODE>
-__global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(AttendArgs a) {
-    typedef Geo<T, WIDE> G;
+__global__ __launch_bounds__((64 * GeoOf<T, WIDE, CODE>::NW), 2) void k_cache_attend(AttendArgs a) {
+    typedef GeoOf<T, WIDE, CODE> G;
     constexpr bool kCode = CODE != CODE_NONE;
     static_assert(!kCode || (WIDE && G::kBf), "codes: wide bf16 rows");
     __shared__ __attribute__((aligned(1024))) char smem[G::kLds];
@@ -483,45 +491,51 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(Att
             }
         };
         bool odd = false;
-        // Codes: lane's 16 of slot lane / 4 of the wave's 16, and the slot's scales.
-        u32x4 kc, vc;
+        // Codes: wave w decodes slots 8 w .. + 7 of a tile, K's by the lower lanes and V's by the upper, 16 features each.
+        u32x4 codes;
         uint32_t sc = 0;
+        const int cr = (lane & 31) >> 2, cp = 2 * (lane & 3);   // slot of the eight, first of two 16-byte pieces
+        const char* cbase = nullptr;
+        uint32_t cput[2];
+        if constexpr (kCode) {
+            cbase = (const char*)(hh ? a.c.V : a.c.K) + (lane & 31) * 16;
+            const int row = 8 * wave + cr;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                cput[i] = row * 128 + (hh ? G::kTileV + (((cp + i) ^ (2 * (row & 3))) << 4) : ((cp + i) ^ ((row >> 1) & 7)) << 4);
+        }
         auto fetch_codes = [&](int t) {
-            const int k = unit_slot(t, wave);
-            const int64_t at = (((int64_t)pw.page(k >> a.c.page_log2, lane) * a.c.Hkv + hk) << a.c.page_log2) + (k & page_mask);
-            kc = *(const u32x4*)((const char*)a.c.K + at * kD + lane * 16);
-            vc = *(const u32x4*)((const char*)a.c.V + at * kD + lane * 16);
-            sc = a.c.scale[at + (lane >> 2)];
+            const int k = unit_slot(t, wave >> 1);
+            const int64_t at = (((int64_t)pw.page(k >> a.c.page_log2, lane) * a.c.Hkv + hk) << a.c.page_log2) + (k & page_mask) +
+                               8 * (wave & 1);
+            codes = *(const u32x4*)(cbase + at * kD);
+            sc = a.c.scale[at + cr];
         };
         auto put_codes = [&](int t) {
-            const int r = lane >> 2, pc = 2 * (lane & 3);
-            lds_char* tile = ring + (t % G::NST) * G::kTile + (16 * wave + r) * 128;
-            typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
-            u32x4 k[2], v[2];
-            decode16<CODE>(kc, key_scale(sc), k);
-            decode16<CODE>(vc, value_scale(sc), v);
-            const int k0 = c0 + t * G::TK, slot = k0 + 16 * wave;
+            u32x4 v[2];
+            decode16<CODE>(codes, hh ? value_scale(sc) : key_scale(sc), v);
+            const int k0 = c0 + t * G::TK, slot = k0 + 8 * wave;
             if (!pw.sane || k0 + G::TK > seen_by_all) {
-                // (as clean_values() does to tiles that are copied)
+                // (V: as clean_values() does to tiles that are copied)
                 const int at = slot >> a.c.page_log2;
-                const bool live = slot + r < c1 && (pw.sane || (at <= pw.last && pw.valid(pw.row[at])));
+                const bool live = slot + cr < c1 && (pw.sane || (at <= pw.last && pw.valid(pw.row[at])));
                 bool any = false;
+                if (hh)
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
+                    for (int i = 0; i < 2; ++i)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        uint32_t x = v[i][j];
-                        const bool lo = (x & 0x7f80u) == 0x7f80u, hi = (x & 0x7f800000u) == 0x7f800000u;
-                        any = any || (live && (lo || hi));
-                        v[i][j] = !live ? 0u : x & (lo ? 0xffff0000u : 0xffffffffu) & (hi ? 0xffffu : 0xffffffffu);
-                    }
+                        for (int j = 0; j < 4; ++j) {
+                            uint32_t x = v[i][j];
+                            const bool lo = (x & 0x7f80u) == 0x7f80u, hi = (x & 0x7f800000u) == 0x7f800000u;
+                            any = any || (live && (lo || hi));
+                            v[i][j] = !live ? 0u : x & (lo ? 0xffff0000u : 0xffffffffu) & (hi ? 0xffffu : 0xffffffffu);
+                        }
                 odd |= __builtin_amdgcn_ballot_w64(any) != 0;
             }
+            typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+            lds_char* tile = ring + (t % G::NST) * G::kTile;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                *(lds_u32x4*)(tile + (((pc + i) ^ (r >> 1)) << 4)) = k[i];
-                *(lds_u32x4*)(tile + G::kTileV + (((pc + i) ^ (2 * (r & 3))) << 4)) = v[i];
-            }
+            for (int i = 0; i < 2; ++i) *(lds_u32x4*)(tile + cput[i]) = v[i];
         };
         auto issue_first = [&]() {
             if constexpr (kCode) {
@@ -960,7 +974,12 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(Att
             }
             if (lane == 0) s_redo[wave] = redo;
             __syncthreads();
-            if (s_redo[0] | s_redo[1] | s_redo[2] | s_redo[3]) {
+            auto any_wave = [&]() {
+                int any = 0;
+                for (int v = 0; v < G::NW; ++v) any |= s_redo[v];
+                return any != 0;
+            };
+            if (any_wave()) {
                 if constexpr (!G::kBf) load_q();
 #pragma unroll 1
                 for (int pass = 0; pass < 2; ++pass) {
@@ -971,7 +990,7 @@ __global__ __launch_bounds__((64 * Geo<T, WIDE>::NW), 2) void k_cache_attend(Att
                     __syncthreads();
                     if (lane == 0) s_redo[wave] = far;
                     __syncthreads();
-                    if (!(s_redo[0] | s_redo[1] | s_redo[2] | s_redo[3])) break;
+                    if (!any_wave()) break;
                 }
             }
         }
@@ -1495,14 +1514,14 @@ void attend_plan(AttendArgs* a) {
     // in one range, 11.1 in three; 1,000 slots, 200 tokens: 25 in one, 17 in eight; 30 sequences of up to
     // 102 tokens and 8,333 slots: 140 in one, 115 in eight, 131 in sixteen.)
     const double slot = a->wide ? (bf ? 0.016 : 0.038) : (bf ? 0.006 : 0.019);
-    const double start = a->wide ? 512 : 192, together = 512, range = a->wide ? 0.15 : 0.05;
+    const double start = a->wide ? 512 : 192, together = a->wide && a->c.code ? 256 : 512, range = a->wide ? 0.15 : 0.05;
     const int64_t most = (a->c.max_len + 127) / 128;
     int64_t best = 1;
     double best_t = 0;
     for (int64_t ns = 1; ns <= most && ns <= 256; ++ns) {
         const int64_t ch = ((a->c.max_len + ns - 1) / ns + 63) / 64 * 64;
         const double rounds = items * ns / together;
-        const double slots = equal || rounds <= 1 ? ceil(rounds) * (ch + start)
+        const double slots = equal || (rounds <= 1 && (!a->c.code || a->wide)) ? ceil(rounds) * (ch + start)
                                                   : items * (a->c.max_len + start * ns) / together + ch + start;
         const double t = slots * slot + range * ns + (ns == 1 ? 0. : ns <= kFew ? 3. : 4.5);
         if (ns == 1 || t < best_t) best = ns, best_t = t;
@@ -1516,7 +1535,7 @@ void attend_plan(AttendArgs* a) {
 
 // Rows per workgroup.
 int attend_rows(const AttendArgs& a) {
-    if (a.c.code && !a.wide) return (int64_t)a.c.max_q * a.G <= 16 ? 16 : 32;
+    if (a.c.code) return a.wide ? GeoOf<bf16, true, CODE_INT8>::RT : (int64_t)a.c.max_q * a.G <= 16 ? 16 : 32;
     if (a.c.dtype == DT_BF16) return a.wide ? Geo<bf16, true>::RT : Geo<bf16, false>::RT;
     return a.wide ? Geo<float, true>::RT : Geo<float, false>::RT;
 }
@@ -1564,10 +1583,9 @@ static void attend_go(const AttendArgs& a, hipStream_t st) {
         launch_cache8_attend(a, st);
     } else if (a.c.code) {
         if constexpr (sizeof(T) == 2) {
-            if (a.c.code == CODE_E4M3)
-                hipLaunchKernelGGL((k_cache_attend<T, true, CODE_E4M3>), dim3(grid), dim3(64 * Geo<T, true>::NW), 0, st, a);
-            else
-                hipLaunchKernelGGL((k_cache_attend<T, true, CODE_INT8>), dim3(grid), dim3(64 * Geo<T, true>::NW), 0, st, a);
+            const dim3 threads(64 * GeoOf<T, true, CODE_INT8>::NW);
+            if (a.c.code == CODE_E4M3) hipLaunchKernelGGL((k_cache_attend<T, true, CODE_E4M3>), dim3(grid), threads, 0, st, a);
+            else hipLaunchKernelGGL((k_cache_attend<T, true, CODE_INT8>), dim3(grid), threads, 0, st, a);
         }
     } else if (a.wide) {
         hipLaunchKernelGGL((k_cache_attend<T, true, CODE_NONE>), dim3(grid), dim3(64 * Geo<T, true>::NW), 0, st, a);
