@@ -518,8 +518,8 @@ vp_status vp_cache_evict(const vp_cache *cache, const vp_cache_batch *batch, int
  *   RMS    n = x / sqrt(mean x^2 + eps)
  *   y = R (n gain + bias),  R the rotation by the token's positions (rot may be NULL: none).
  * gain and bias: device fp32, 16-byte aligned, [64] for all heads or with per_head [H, 64]; either may be
- * NULL (1, 0).  eps >= 0; 1e-6 when 0.  A row whose mean square leaves fp32's range gives its limit (gain times
- * zero, plus the bias). */
+ * NULL (1, 0).  eps >= 0; 1e-6 when 0.  A row whose squares' sum leaves fp32's range gives the
+ * bias, or NaN where its sum does. */
 typedef enum { VP_NORM_LAYER = 0, VP_NORM_RMS = 1 } vp_norm_kind;
 typedef struct {
     vp_norm_kind kind;

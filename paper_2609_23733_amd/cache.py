@@ -39,6 +39,14 @@ def _done(code: int, where: str):
         raise VPError(code, where)
 
 
+def _here(*tensors):
+    """Refuses tensors that are not on the current device, whose stream the call goes to."""
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise ValueError("a tensor is on %s, the current device is %d" % (t.device, dev))
+
+
 def _rows(t: torch.Tensor, name: str, T: int, H: int, dtype) -> int:
     """Checks a [T, H, 64] tensor whose tokens may lie apart; returns their distance."""
     try:
@@ -173,7 +181,8 @@ class HeadNorm:
 def norm_rotary(x, norm: HeadNorm, pos=None, rot: Optional[Rotary] = None, out: Optional[torch.Tensor] = None):
     """x [T, H, 64], every head's row normalised and turned by its token's position, in one pass (without
     `rot` only normalised).  `out` may be x.  Where x, gain or bias require gradients they get them (no `out`
-    then)."""
+    then).  As with every operator of torch's: while a training step is captured into a graph, no eager graph of
+    the same leaves may be alive."""
     if (rot is None) != (pos is None):
         raise ValueError("a rotation needs positions" if pos is None else "positions need a rotation (rot)")
     if torch.is_grad_enabled() and (x.requires_grad or (norm.gain is not None and norm.gain.requires_grad) or
@@ -187,6 +196,7 @@ def norm_rotary(x, norm: HeadNorm, pos=None, rot: Optional[Rotary] = None, out: 
     if out is None:
         out = torch.empty(T, H, HEAD_DIM, dtype=x.dtype, device=x.device)
     ys = _rows(out, "out", T, H, x.dtype)
+    _here(x, out, norm.gain, norm.bias, pos)
     _done(load_library().vp_norm_rotary(norm.at(H), None if rot is None else rot.at(pos, T), _dt(x), T, H, x.data_ptr(), xs,
                                         out.data_ptr(), ys, _stream()), "vp_norm_rotary")
     return out
@@ -338,6 +348,8 @@ def append(pc: PagedCache, batch: Batch, Q, K, V, pos=None, rot: Optional[Rotary
         raise ValueError("a rotation needs positions" if pos is None else "positions need a rotation (rot)")
     turn = None if rot is None else rot.at(pos, T)
     if pc.codes or q_norm is not None or k_norm is not None:
+        _here(pc.K, K, V, Q, pos)
+    if pc.codes or q_norm is not None or k_norm is not None:
         _done(load_library().vp_cache8_append(pc._ref8, batch._for(T), Hq, q, qs, K.data_ptr(), ks, V.data_ptr(), vs,
                                               None if q_norm is None or Q is None else q_norm.at(Hq),
                                               None if k_norm is None else k_norm.at(Hkv), turn, qo, _stream()),
@@ -360,6 +372,7 @@ def read(pc: PagedCache, batch: Batch, T: int, dtype: Optional[torch.dtype] = No
     new = lambda: torch.zeros(T, pc.Hkv, HEAD_DIM, dtype=dtype, device=pc.K.device)
     K_out, V_out = new() if K_out is None else K_out, new() if V_out is None else V_out
     shape = (T, pc.Hkv, HEAD_DIM)
+    _here(pc.K, K_out, V_out)
     _done(load_library().vp_cache8_read(pc._ref8, batch._for(T), vp.VP_BF16 if dtype is torch.bfloat16 else vp.VP_F32,
                                         _whole(K_out, "K_out", shape, dtype), _whole(V_out, "V_out", shape, dtype),
                                         _stream()), "vp_cache8_read")
@@ -394,6 +407,8 @@ def attend(pc: PagedCache, batch: Batch, Q, causal: bool = True, scale: float = 
     if lse is None:
         lse = torch.empty(T, Hq, dtype=torch.float32, device=Q.device)
     o, ls, wo = _whole(O, "O", (T, Hq, HEAD_DIM), dt), _whole(lse, "lse", (T, Hq), torch.float32), None
+    if pc.codes:
+        _here(pc.K, Q)
     if weight_out is not None:
         if pc.weight is None:
             raise ValueError("the cache has no weights")

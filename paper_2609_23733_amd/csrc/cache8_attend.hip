@@ -213,11 +213,11 @@ __global__ __launch_bounds__(256, NB == 1 && kBfRows<T> ? 3 : 2) void k_cache8_a
             }
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
+                const int left = vis[nb] - k0 - 4 * g;
+                auto sees = [&](int j) { return 16 * (j >> 2) + (j & 3) < left && ((units >> (j >> 2)) & 1); };
                 if (partial) {
-                    const int left = vis[nb] - k0 - 4 * g;
 #pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        x[nb][j] = 16 * (j >> 2) + (j & 3) < left && ((units >> (j >> 2)) & 1) ? x[nb][j] : -INFINITY;
+                    for (int j = 0; j < 8; ++j) x[nb][j] = sees(j) ? x[nb][j] : -INFINITY;
                 }
                 if (logits[nb])
 #pragma unroll
@@ -250,9 +250,10 @@ __global__ __launch_bounds__(256, NB == 1 && kBfRows<T> ? 3 : 2) void k_cache8_a
                 }
                 l[nb] += sum;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float pv = p[j] * vs[j];
-                    p[j] = partial && x[nb][j] == -INFINITY ? 0.f : pv;   // (no value of an unseen slot)
+                for (int j = 0; j < 8; ++j) p[j] *= vs[j];
+                if (partial) {   // (an unseen slot's scale may be anything)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) p[j] = sees(j) ? p[j] : 0.f;
                 }
                 Parts<kP> pb;
                 pb.set(p);

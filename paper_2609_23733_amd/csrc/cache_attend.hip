@@ -1502,10 +1502,6 @@ void attend_plan(AttendArgs* a) {
     // both 34; 200 over 20,000, 4,400 each, 49 and 41; 1,374 over themselves, 1,850 each in 1.3 rounds, 37 and
     // 29.  fp32, whose wide kernel has the faster products: 64 over 20,000 56 and 57, 90 over 20,000 80 and
     // 61, 200 over 600 22 and 18; 90 over 300 13.3 and 15.8.)
-    a->wide = 0;
-    double items = work_items(a->c.code ? attend_rows(*a) : 32, false);
-    a->wide = (bf || !a->c.code) && rows > 64 && (!bf || items * a->c.max_len > 512. * (items > 512 ? 1500 : 2500));
-    if (a->wide) items = work_items(attend_rows(*a), true);
     // An estimate that ranks divisions into ns ranges, in us where the card is lightly loaded (large calls, which HBM or
     // all SIMDs at once bound, take up to three times as long: 50 for 167 us of tokens over 137,400 slots, 153
     // for 260 of a view over 43,968): the slots of a workgroup and its start, in units of slots, times the rounds of
@@ -1513,18 +1509,48 @@ void attend_plan(AttendArgs* a) {
     // launch, and what it reads per range.  (300 slots, a token, bf16: 8.3 us
     // in one range, 11.1 in three; 1,000 slots, 200 tokens: 25 in one, 17 in eight; 30 sequences of up to
     // 102 tokens and 8,333 slots: 140 in one, 115 in eight, 131 in sixteen.)
-    const double slot = a->wide ? (bf ? 0.016 : 0.038) : (bf ? 0.006 : 0.019);
-    const double start = a->wide ? 512 : 192, together = a->wide && a->c.code ? 256 : 512, range = a->wide ? 0.15 : 0.05;
     const int64_t most = (a->c.max_len + 127) / 128;
     int64_t best = 1;
-    double best_t = 0;
-    for (int64_t ns = 1; ns <= most && ns <= 256; ++ns) {
-        const int64_t ch = ((a->c.max_len + ns - 1) / ns + 63) / 64 * 64;
-        const double rounds = items * ns / together;
-        const double slots = equal || (rounds <= 1 && (!a->c.code || a->wide)) ? ceil(rounds) * (ch + start)
-                                                  : items * (a->c.max_len + start * ns) / together + ch + start;
-        const double t = slots * slot + range * ns + (ns == 1 ? 0. : ns <= kFew ? 3. : 4.5);
-        if (ns == 1 || t < best_t) best = ns, best_t = t;
+    auto divide = [&](double items, double slot, double start, double together, double range, bool one_round) {
+        double best_t = 0;
+        for (int64_t ns = 1; ns <= most && ns <= 256; ++ns) {
+            const int64_t ch = ((a->c.max_len + ns - 1) / ns + 63) / 64 * 64;
+            const double rounds = items * ns / together;
+            const double slots = equal || (rounds <= 1 && one_round) ? ceil(rounds) * (ch + start)
+                                                                     : items * (a->c.max_len + start * ns) / together + ch + start;
+            const double t = slots * slot + range * ns + (ns == 1 ? 0. : ns <= kFew ? 3. : 4.5);
+            if (ns == 1 || t < best_t) best = ns, best_t = t;
+        }
+        return best_t;
+    };
+    a->wide = 0;
+    if (!a->c.code) {
+        double items = work_items(32, false);
+        a->wide = rows > 64 && (!bf || items * a->c.max_len > 512. * (items > 512 ? 1500 : 2500));
+        if (a->wide) items = work_items(attend_rows(*a), true);
+        divide(items, a->wide ? (bf ? 0.016 : 0.038) : (bf ? 0.006 : 0.019), a->wide ? 512 : 192, 512, a->wide ? 0.15 : 0.05, true);
+    } else {
+        // 8-bit codes: narrow workgroups, which each decode what they read, by all the work if ragged (31 tokens of four key
+        // heads, ragged to 10,992 slots: 31 us in the six ranges of one round, 28 in eight, 27 in eleven); wide ones, whose
+        // time per slot grows with the waves that have rows, and of which a compute unit has one.  The shorter estimate
+        // decides, in us: 16 heads, 1,000 tokens over 1,000 slots 22 narrow, 29 wide; 400 over 5,000 46 and 34; 90 over 20,000 41
+        // and 36; 40 over 20,000 31 and 34.  Ragged batches whose rows would fill less than a quarter of the wide
+        // tiles stay narrow (30 sequences of up to 102 tokens and 8,333 slots: 73 and 91).
+        const double t = divide(work_items(attend_rows(*a), false), rows <= 16 ? 0.008 : bf ? 0.017 : 0.03, 192, 512, 0.05, false);
+        const int64_t narrow = best;
+        const int waves = (int)std::min<int64_t>(8, (rows + 63) / 64);
+        if (bf && rows > 64) {
+            a->wide = 1;
+            const int rt = attend_rows(*a);
+            const double items = work_items(rt, true);
+            const double tiles = a->row_tiles + (equal ? (double)others * a->row_tiles : std::min((double)others * a->row_tiles, (double)(rest * a->G) / rt + others));
+            a->wide = divide(items, 0.01 + 0.0024 * waves, 600, 256, 0.15, true) < t &&
+                      (equal || (double)a->c.T * a->G >= 0.25 * tiles * rt);
+        }
+        if (!a->wide) {
+            work_items(attend_rows(*a), false);
+            best = narrow;
+        }
     }
     a->chunk = (int)(((a->c.max_len + best - 1) / best + 63) / 64 * 64);
     if (a->chunk < 64) a->chunk = 64;

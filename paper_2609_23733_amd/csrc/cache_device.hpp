@@ -116,6 +116,9 @@ size_t norm_grad_part_bytes(int T, int H, int per_head);
 void launch_norm_rotary_grad(int dtype, const void* x, int64_t x_stride, const void* g, int64_t g_stride,
                              void* dx, float* dgain, float* dbias, int T, int H, const NormArgs& nm,
                              const RotArgs& r, float* part, hipStream_t st);
+// Fewer than 2^32 threads, 2^24 workgroups, in the launch.
+bool append8_fits(const AppendArgs& a);
+bool read_fits(const ReadArgs& a);
 void launch_cache_append8(const AppendArgs& a, const NormArgs& qn, const NormArgs& kn, const RotArgs& r,
                           hipStream_t st);
 void launch_cache_read(const ReadArgs& a, hipStream_t st);

@@ -1171,6 +1171,7 @@ vp_status vp_cache8_append(const vp_cache8* cache, const vp_cache_batch* batch, 
     a.Hq = Q ? Hq : 0;
     a.Q = Q; a.Kn = K; a.Vn = V; a.Qo = Q_out;
     a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride;
+    if (!vp::append8_fits(a)) return VP_ERR_UNSUPPORTED;
     (void)hipGetLastError();
     vp::launch_cache_append8(a, qn, kn, r, (hipStream_t)stream);
     return hip_status("vp_cache8_append");
@@ -1188,6 +1189,7 @@ vp_status vp_cache8_read(const vp_cache8* cache, const vp_cache_batch* batch, vp
     a.out_dtype = dtype == VP_BF16 ? 1 : 0;
     a.Ko = K_out;
     a.Vo = V_out;
+    if (!vp::read_fits(a)) return VP_ERR_UNSUPPORTED;
     (void)hipGetLastError();
     vp::launch_cache_read(a, (hipStream_t)stream);
     return hip_status("vp_cache8_read");

@@ -100,6 +100,8 @@ def test_bad_calls(lib):
     for kw in (dict(keep=0), dict(sink=-1), dict(wo=None), dict(ws=FAKE + 8)):
         assert evict(lib, c, b, **kw) == 1, kw
     assert evict(lib, c, b, n=0) == 3
+    many = batch(B=4000, T=1 << 23, max_q=1 << 23, max_len=640)       # 2^32 threads and more
+    assert append(lib, c, many) == 2 and read(lib, c, many) == 2 and attend(lib, c, many) == 2
     empty = batch(T=0, max_q=0)
     assert attend(lib, c, empty) == 0 and append(lib, c, empty) == 0 and read(lib, c, empty) == 0
 

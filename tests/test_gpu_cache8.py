@@ -599,6 +599,27 @@ def test_stream_layer(cache, kind, rows):  # noqa: F811
         assert (O.float() - P).abs().max() <= (2.0 ** -6 if rows == BF else 1e-4) * max(1.0, P.abs().max().item()), step
 
 
+def test_other_devices(cache, monkeypatch):  # noqa: F811
+    """Tensors that are not on the current device are refused (the current device's number is what is changed here)."""
+    K, V = (torch.zeros(4, 2, 16, 64, dtype=torch.int8, device="cuda") for _ in range(2))
+    pc = cache.PagedCache(K, V, scale=torch.ones(4, 2, 16, 2, dtype=BF, device="cuda"))
+    batch = cache.Batch(i32([[0]]), i32([5]), i32([0, 2]), 2, 5)
+    rows = normal(1, (2, 2, 64), BF).cuda()
+    n = cache.HeadNorm("rms")
+    ws = cache.attend_workspace(pc, batch, 2, 2)
+    k, v = torch.empty_like(rows), torch.empty_like(rows)
+    calls = [lambda: cache.append(pc, batch, rows, rows, rows, Q_out=k), lambda: cache.read(pc, batch, 2, K_out=k, V_out=v),
+             lambda: cache.norm_rotary(rows, n, out=k), lambda: cache.attend(pc, batch, rows, O=k, ws=ws)]
+    for call in calls:
+        call()
+    real = torch.cuda.current_device()
+    with monkeypatch.context() as m:
+        m.setattr(torch.cuda, "current_device", lambda: real + 1)
+        for call in calls:
+            with pytest.raises(ValueError, match="device"):
+                call()
+
+
 def test_refusals(cache):  # noqa: F811
     mk = lambda *s, dtype=torch.int8: torch.zeros(*s, dtype=dtype, device="cuda")
     K, V, s = mk(4, 2, 16, 64), mk(4, 2, 16, 64), mk(4, 2, 16, 2, dtype=BF)
