@@ -392,11 +392,24 @@ __global__ __launch_bounds__((64 * GeoOf<T, WIDE, CODE>::NW), 2) void k_cache_at
     // those past the end of short sequences, which have nothing to do, come last and in a row, and
     // each turns the heads by five, so that no sequence meets the same XCD and shader engine every time
     // (ranges of a head one after the other: 32 ragged sequences, 8 ranges, 49 us; so: 31).
-    const int turn = (blockIdx.x >> 3) / a.row_tiles, rt = (blockIdx.x >> 3) - turn * a.row_tiles;
-    const int x = turn * 8 + (blockIdx.x & 7), heads = a.c.B * a.c.Hkv;
-    const int split = x / heads;
+    const int heads = a.c.B * a.c.Hkv;
+    int turn = (blockIdx.x >> 3) / a.row_tiles, rt = (blockIdx.x >> 3) - turn * a.row_tiles;
+    int x = turn * 8 + (blockIdx.x & 7), split = x / heads, y = (x - split * heads + 5 * split) % heads;
+    if constexpr (kCode) {
+        // Codes, one workgroup per compute unit: a row tile of everything before the next, so that the last one, which may
+        // have few rows, comes last; and all ranges of a sequence one after the other, as the compute units that an
+        // XCD's workgroups go to follow from their numbers (with those of a long sequence always every fourth, 149 us
+        // for 82), turned by three from tile to tile.  Ragged: six sequences of up to 700 tokens over 20,000 slots 103 us, 167 in the other
+        // order; 16 of up to 400 over 3,000 62 and 81.
+        const int turns = (heads * a.nsplit + 7) >> 3;
+        rt = (blockIdx.x >> 3) / turns;
+        x = ((blockIdx.x >> 3) - rt * turns + 3 * rt) % turns * 8 + (blockIdx.x & 7);
+        const int per = a.c.Hkv * a.nsplit, b8 = x / per;
+        split = x < heads * a.nsplit ? (x - b8 * per) / a.c.Hkv : a.nsplit;
+        y = b8 * a.c.Hkv + (x - b8 * per) % a.c.Hkv;
+    }
     if (split >= a.nsplit) return;
-    const int y = (x - split * heads + 5 * split) % heads, hk = y % a.c.Hkv, b = y / a.c.Hkv;
+    const int hk = y % a.c.Hkv, b = y / a.c.Hkv;
 
     const CacheSeq sq = cache_seq(a.c, b);
     const int nrows = sq.nq * a.G, row0 = rt * G::RT + (WIDE ? wave * 32 * G::NB : 0);
@@ -1511,13 +1524,17 @@ void attend_plan(AttendArgs* a) {
     // 102 tokens and 8,333 slots: 140 in one, 115 in eight, 131 in sixteen.)
     const int64_t most = (a->c.max_len + 127) / 128;
     int64_t best = 1;
-    auto divide = [&](double items, double slot, double start, double together, double range, bool one_round) {
+    // `whole`: workgroups per range; `share`: of all the work, what the estimate of it counts
+    auto divide = [&](double items, double whole, double slot, double start, double together, double range, bool one_round,
+                      double share) {
         double best_t = 0;
         for (int64_t ns = 1; ns <= most && ns <= 256; ++ns) {
             const int64_t ch = ((a->c.max_len + ns - 1) / ns + 63) / 64 * 64;
-            const double rounds = items * ns / together;
-            const double slots = equal || (rounds <= 1 && one_round) ? ceil(rounds) * (ch + start)
-                                                                     : items * (a->c.max_len + start * ns) / together + ch + start;
+            double slots = ceil(items * ns / together) * (ch + start);
+            if (!equal) {
+                const double all = share * (items * (a->c.max_len + start * ns) / together + ch + start);
+                slots = one_round && whole * ns <= together ? std::min<double>(ch + start, all) : all;
+            }
             const double t = slots * slot + range * ns + (ns == 1 ? 0. : ns <= kFew ? 3. : 4.5);
             if (ns == 1 || t < best_t) best = ns, best_t = t;
         }
@@ -1528,24 +1545,32 @@ void attend_plan(AttendArgs* a) {
         double items = work_items(32, false);
         a->wide = rows > 64 && (!bf || items * a->c.max_len > 512. * (items > 512 ? 1500 : 2500));
         if (a->wide) items = work_items(attend_rows(*a), true);
-        divide(items, a->wide ? (bf ? 0.016 : 0.038) : (bf ? 0.006 : 0.019), a->wide ? 512 : 192, 512, a->wide ? 0.15 : 0.05, true);
+        divide(items, items, a->wide ? (bf ? 0.016 : 0.038) : (bf ? 0.006 : 0.019), a->wide ? 512 : 192, 512,
+               a->wide ? 0.15 : 0.05, true, 1);
     } else {
         // 8-bit codes: narrow workgroups, which each decode what they read, by all the work if ragged (31 tokens of four key
         // heads, ragged to 10,992 slots: 31 us in the six ranges of one round, 28 in eight, 27 in eleven); wide ones, whose
         // time per slot grows with the waves that have rows, and of which a compute unit has one.  The shorter estimate
         // decides, in us: 16 heads, 1,000 tokens over 1,000 slots 22 narrow, 29 wide; 400 over 5,000 46 and 34; 90 over 20,000 41
-        // and 36; 40 over 20,000 31 and 34.  Ragged batches whose rows would fill less than a quarter of the wide
-        // tiles stay narrow (30 sequences of up to 102 tokens and 8,333 slots: 73 and 91).
-        const double t = divide(work_items(attend_rows(*a), false), rows <= 16 ? 0.008 : bf ? 0.017 : 0.03, 192, 512, 0.05, false);
+        // and 36; 40 over 20,000 31 and 34; ragged to 400 tokens over 3,000 slots, 16 sequences, 81 and 62.  Ragged batches
+        // whose rows would fill less than a seventh of the wide tiles stay narrow (30 sequences of up to 102 tokens and 8,333
+        // slots: 73 and 91).
+        double t = divide(work_items(attend_rows(*a), false), 0, rows <= 16 ? 0.008 : bf ? 0.017 : 0.03, 192, 512, 0.05, false, 1);
+        if (!equal) t *= 0.8;   // (the others' lengths are less than assumed more often than not)
         const int64_t narrow = best;
-        const int waves = (int)std::min<int64_t>(8, (rows + 63) / 64);
         if (bf && rows > 64) {
             a->wide = 1;
             const int rt = attend_rows(*a);
-            const double items = work_items(rt, true);
-            const double tiles = a->row_tiles + (equal ? (double)others * a->row_tiles : std::min((double)others * a->row_tiles, (double)(rest * a->G) / rt + others));
-            a->wide = divide(items, 0.01 + 0.0024 * waves, 600, 256, 0.15, true) < t &&
-                      (equal || (double)a->c.T * a->G >= 0.25 * tiles * rt);
+            // us per slot of a tile of n rows
+            auto slot = [](double n) { return 0.01 + 0.0024 * std::min(8., ceil(n / 64)); };
+            const double items = work_items(rt, true), one = slot((double)rows);
+            // Row tiles, of few rows as their share of `one`: the largest sequence's and the others'.
+            const double own = a->row_tiles == 1 ? 1 : (double)(rows / rt) + (rows % rt ? slot((double)(rows % rt)) / one : 0);
+            const double few = others ? slot((double)rest * a->G / others) / one : 0;
+            const double whole = own + std::min(others * own, (a->row_tiles > 1 ? (double)rest * a->G / rt : 0) + others * few);
+            const double tiles = a->row_tiles + std::min((double)others * a->row_tiles, (double)rest * a->G / rt + others);
+            a->wide = divide(items, a->c.Hkv * whole, one, 600, 256, 0.15, true, 0.6) < t &&
+                      (equal || (double)a->c.T * a->G >= 0.15 * tiles * rt);
         }
         if (!a->wide) {
             work_items(attend_rows(*a), false);
