@@ -39,12 +39,16 @@ def _done(code: int, where: str):
         raise VPError(code, where)
 
 
-def _here(*tensors):
-    """Refuses tensors that are not on the current device, whose stream the call goes to."""
-    dev = torch.cuda.current_device()
+_device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+
+
+def _here(*tensors) -> int:
+    """The current device's current stream; refuses tensors that are elsewhere."""
+    dev = _device()
     for t in tensors:
         if t is not None and t.get_device() != dev:
             raise ValueError("a tensor is on %s, the current device is %d" % (t.device, dev))
+    return _raw_stream(dev)
 
 
 def _rows(t: torch.Tensor, name: str, T: int, H: int, dtype) -> int:
@@ -163,9 +167,12 @@ class HeadNorm:
                 raise ValueError("%s must be [%d] or [heads, %d]" % (name, HEAD_DIM, HEAD_DIM))
             if t.data_ptr() % 16:
                 raise ValueError("%s must start at a multiple of 16 bytes" % name)
+        if gain is not None and bias is not None and gain.device != bias.device:
+            raise ValueError("gain and bias are on different devices")
         if not 0 < eps < float("inf"):
             raise ValueError("eps must be positive")
         self.kind, self.gain, self.bias, self.eps = kind, gain, bias, float(eps)
+        self.tensor = bias if gain is None else gain       # (for its device)
         self.heads = shape[0] if shape is not None and len(shape) == 2 else None
         ptr = lambda t: None if t is None else t.data_ptr()
         self._c = vp.vp_head_norm(_NORMS[kind], ptr(gain), ptr(bias), self.heads is not None, self.eps)
@@ -196,9 +203,8 @@ def norm_rotary(x, norm: HeadNorm, pos=None, rot: Optional[Rotary] = None, out: 
     if out is None:
         out = torch.empty(T, H, HEAD_DIM, dtype=x.dtype, device=x.device)
     ys = _rows(out, "out", T, H, x.dtype)
-    _here(x, out, norm.gain, norm.bias, pos)
     _done(load_library().vp_norm_rotary(norm.at(H), None if rot is None else rot.at(pos, T), _dt(x), T, H, x.data_ptr(), xs,
-                                        out.data_ptr(), ys, _stream()), "vp_norm_rotary")
+                                        out.data_ptr(), ys, _here(x, out, norm.tensor, pos)), "vp_norm_rotary")
     return out
 
 
@@ -348,11 +354,10 @@ def append(pc: PagedCache, batch: Batch, Q, K, V, pos=None, rot: Optional[Rotary
         raise ValueError("a rotation needs positions" if pos is None else "positions need a rotation (rot)")
     turn = None if rot is None else rot.at(pos, T)
     if pc.codes or q_norm is not None or k_norm is not None:
-        _here(pc.K, K, V, Q, pos)
-    if pc.codes or q_norm is not None or k_norm is not None:
+        st = _here(pc.K, K, V, Q, pos, q_norm and q_norm.tensor, k_norm and k_norm.tensor)
         _done(load_library().vp_cache8_append(pc._ref8, batch._for(T), Hq, q, qs, K.data_ptr(), ks, V.data_ptr(), vs,
                                               None if q_norm is None or Q is None else q_norm.at(Hq),
-                                              None if k_norm is None else k_norm.at(Hkv), turn, qo, _stream()),
+                                              None if k_norm is None else k_norm.at(Hkv), turn, qo, st),
               "vp_cache8_append")
     else:
         _done(load_library().vp_cache_append(pc._ref, batch._for(T), Hq, q, qs, K.data_ptr(), ks, V.data_ptr(), vs,
@@ -372,10 +377,10 @@ def read(pc: PagedCache, batch: Batch, T: int, dtype: Optional[torch.dtype] = No
     new = lambda: torch.zeros(T, pc.Hkv, HEAD_DIM, dtype=dtype, device=pc.K.device)
     K_out, V_out = new() if K_out is None else K_out, new() if V_out is None else V_out
     shape = (T, pc.Hkv, HEAD_DIM)
-    _here(pc.K, K_out, V_out)
+    st = _here(pc.K, K_out, V_out)
     _done(load_library().vp_cache8_read(pc._ref8, batch._for(T), vp.VP_BF16 if dtype is torch.bfloat16 else vp.VP_F32,
                                         _whole(K_out, "K_out", shape, dtype), _whole(V_out, "V_out", shape, dtype),
-                                        _stream()), "vp_cache8_read")
+                                        st), "vp_cache8_read")
     return K_out, V_out
 
 

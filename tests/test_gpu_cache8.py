@@ -599,6 +599,38 @@ def test_stream_layer(cache, kind, rows):  # noqa: F811
         assert (O.float() - P).abs().max() <= (2.0 ** -6 if rows == BF else 1e-4) * max(1.0, P.abs().max().item()), step
 
 
+@pytest.mark.parametrize("kind", KINDS)
+def test_stream_example(cache, kind):  # noqa: F811
+    """examples/stream_views.py over codes: three small views through a block; the attention of every view against 64 bits
+    over the values that the codes of all views' keys and values stand for (tolerance of test_gpu_cache.py's)."""
+    log("stream example %s" % kind)
+    import importlib.util
+    import os
+    from paper_2609_23733_amd import synth
+    at = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "stream_views.py")
+    spec = importlib.util.spec_from_file_location("stream_views", at)
+    ex = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(ex)
+    P = 90
+    outs = ex.main(3, 10 * P, P, kind)
+    w = {k: v.cuda() for k, v in synth.make_block_weights((1, 0)).items()}
+    pos = torch.from_numpy(synth.token_positions(1, P)).cuda()
+    ws = torch.empty(vp.block_workspace_bytes(1, P), dtype=torch.uint8, device="cuda")
+    ks, vs = [], []
+    for v in range(3):
+        X = synth.make_block_input(1, P, (1, v), device="cuda")
+        Q, K, V = (t.cpu() for t in vp.block_qkv(X, pos, w, 1, P, ws))
+        ks.append(codes64.quantise64(K.double(), kind)[2]), vs.append(codes64.quantise64(V.double(), kind)[2])
+        K, V = torch.cat(ks), torch.cat(vs)
+        Y = torch.empty(P, 16, 64, dtype=BF)
+        every = torch.ones(P, K.shape[0], dtype=torch.bool)
+        for h in range(16):
+            Y[:, h] = whole64(Q[:, h], K[:, h], V[:, h], every, 0.125)[0].to(BF)
+        ref = vp.block_out(X, Y.cuda(), w, 1, P, ws).float()
+        err = (outs[v].float() - ref).abs().max().item()
+        assert err <= 2.0 ** -5 * ref.abs().max().item(), (v, err)
+
+
 def test_other_devices(cache, monkeypatch):  # noqa: F811
     """Tensors that are not on the current device are refused (the current device's number is what is changed here)."""
     K, V = (torch.zeros(4, 2, 16, 64, dtype=torch.int8, device="cuda") for _ in range(2))
@@ -612,9 +644,9 @@ def test_other_devices(cache, monkeypatch):  # noqa: F811
              lambda: cache.norm_rotary(rows, n, out=k), lambda: cache.attend(pc, batch, rows, O=k, ws=ws)]
     for call in calls:
         call()
-    real = torch.cuda.current_device()
+    real = cache._device()
     with monkeypatch.context() as m:
-        m.setattr(torch.cuda, "current_device", lambda: real + 1)
+        m.setattr(cache, "_device", lambda: real + 1)
         for call in calls:
             with pytest.raises(ValueError, match="device"):
                 call()
