@@ -554,7 +554,7 @@ vp_status vp_norm_rotary_grad(const vp_head_norm *norm, const vp_rotary_spec *ro
  *
  * Append writes the smallest power of two, from 2^-100 on, for which the row's largest magnitude is at most 127 or 448
  * of it, and codes rounded to nearest, ties to even: an error of at most half a step, scale / 2 (INT8) or
- * 2^-4 of the value and scale 2^-10 (E4M3).  A row with a NaN or an infinity gets scale NaN and codes 0.  Codes and
+ * 2^-4 of the value and scale 2^-10 (E4M3), but for values that would round to 2^128: they get the code below.  A row with a NaN or an infinity gets scale NaN and codes 0.  Codes and
  * scales of other origin are taken as they are: scales other than powers of two cost calls of many rows another rounding, of
  * code times scale to bf16. */
 typedef struct {

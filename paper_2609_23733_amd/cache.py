@@ -157,9 +157,16 @@ class HeadNorm:
 
     def __init__(self, kind: str = "layer", gain: Optional[torch.Tensor] = None,
                  bias: Optional[torch.Tensor] = None, eps: float = 1e-6):
-        shape = None
-        for t, name in ((gain, "gain"), (bias, "bias")):
+        if not 0 < eps < float("inf"):
+            raise ValueError("eps must be positive")
+        self.kind, self.gain, self.bias, self.eps = kind, gain, bias, float(eps)
+        self._bind()
+
+    def _bind(self):
+        shape, at = None, []
+        for t, name in ((self.gain, "gain"), (self.bias, "bias")):
             if t is None:
+                at.append(0)
                 continue
             _need(t, name, shape, torch.float32)
             shape = tuple(t.shape)
@@ -167,19 +174,19 @@ class HeadNorm:
                 raise ValueError("%s must be [%d] or [heads, %d]" % (name, HEAD_DIM, HEAD_DIM))
             if t.data_ptr() % 16:
                 raise ValueError("%s must start at a multiple of 16 bytes" % name)
-        if gain is not None and bias is not None and gain.device != bias.device:
+            at.append(t.data_ptr())
+        if self.gain is not None and self.bias is not None and self.gain.device != self.bias.device:
             raise ValueError("gain and bias are on different devices")
-        if not 0 < eps < float("inf"):
-            raise ValueError("eps must be positive")
-        self.kind, self.gain, self.bias, self.eps = kind, gain, bias, float(eps)
-        self.tensor = bias if gain is None else gain       # (for its device)
+        self.tensor = self.bias if self.gain is None else self.gain       # (for its device)
         self.heads = shape[0] if shape is not None and len(shape) == 2 else None
-        ptr = lambda t: None if t is None else t.data_ptr()
-        self._c = vp.vp_head_norm(_NORMS[kind], ptr(gain), ptr(bias), self.heads is not None, self.eps)
-        self._ref = ctypes.byref(self._c)
+        self._at = tuple(at)
+        self._ref = ctypes.byref(vp.vp_head_norm(_NORMS[self.kind], *at, self.heads is not None, self.eps))
 
     def at(self, H: int):
         """The C argument for rows of H heads."""
+        gain, bias = self.gain, self.bias
+        if self._at != (0 if gain is None else gain.data_ptr(), 0 if bias is None else bias.data_ptr()):
+            self._bind()                # (a parameter whose storage was exchanged)
         if self.heads is not None and self.heads != H:
             raise ValueError("a norm of %d heads for %d" % (self.heads, H))
         return self._ref
@@ -243,7 +250,7 @@ def _norm_gradients(ctx, g):
         n = _norm_workspace(T, H, norm.heads is not None)
         ws = torch.empty(n, dtype=torch.uint8, device=x.device)
         at_ws = ws.data_ptr()
-    _done(load_library().vp_norm_rotary_grad(norm._ref, None if rot is None else rot.at(pos, T), _dt(x), T, H, x.data_ptr(),
+    _done(load_library().vp_norm_rotary_grad(norm.at(H), None if rot is None else rot.at(pos, T), _dt(x), T, H, x.data_ptr(),
                                              x.stride(0) if T > 1 else H * HEAD_DIM, g.data_ptr(), H * HEAD_DIM, at_x,
                                              at_gain, at_bias, at_ws, n, _stream()), "vp_norm_rotary_grad")
     return dx, dgain, dbias, None, None, None

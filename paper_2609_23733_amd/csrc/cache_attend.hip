@@ -56,8 +56,8 @@ struct Geo {
     }
 };
 
-// Wide workgroups over 8-bit codes: eight waves, which share the decoding of a tile (with four, a view over 43,968 slots
-// takes 298 us instead of @W8@).
+// Wide workgroups over 8-bit codes: eight waves, which share the decoding of a tile (1,374 tokens over 43,968 slots of 16
+// heads, e4m3: 273 us, with four waves 298; kernel alone, among other calls 258, 960 TFLOP/s, as over a bf16 cache).
 template <typename T, bool WIDE, int CODE>
 struct GeoOf : Geo<T, WIDE> {
     static constexpr int NW = CODE == CODE_NONE ? Geo<T, WIDE>::NW : 8;

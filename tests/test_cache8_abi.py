@@ -175,5 +175,9 @@ def test_reference_codes(kind):
         again = (x / s[:, None]).to(torch.float8_e4m3fn).double() * s[:, None]
         near = (x / s[:, None]).float().double() == x / s[:, None]       # (torch rounds through fp32)
         assert torch.equal(again[near], v[near])
+    big = torch.tensor([[f * 2.0 ** 127] + [1e38] * 63 for f in (1.0, 1.74, 1.76, 1.98, 1.99, 1.9999999)], dtype=torch.float64)
+    v = codes64.quantise64(big, kind)[2]
+    # (below 2^128 at most a step: 16 times 2^120, or 2^122)
+    assert (v.abs() < 2.0 ** 128).all() and ((v - big).abs() <= 2.0 ** (124 if kind == "e4m3" else 122)).all()
     code, s, v = codes64.quantise64(torch.tensor([[0.0] * 64, [math.inf] + [1.0] * 63, [math.nan] * 64]), kind)
     assert s[0] == 2.0 ** -100 and (v[0] == 0).all() and torch.isnan(s[1:]).all() and torch.isnan(v[1:]).all()

@@ -174,8 +174,8 @@ def test_plain_caches_with_norms(cache, dtype):  # noqa: F811
     ref = cache.rotary(Q, pos, rot).cpu().double()
     assert ((only_k.cpu().double() - ref).abs() <= 2 * rot_tol(Q.cpu(), ref, 1.0, dtype)).all()
     assert cache.append(pc, batch, None, K, V, pos, rot, k_norm=kn) is None
-    f32 = cache.read(pc, batch, 42, F32)[0]
-    assert torch.equal(f32, k.float())
+    for other in (F32, BF):
+        assert torch.equal(cache.read(pc, batch, 42, other)[0], k.to(other))
     same = Q.clone()
     assert torch.equal(cache.append(pc, batch, same, K, V, pos, rot, Q_out=same, q_norm=qn, k_norm=kn), q)
 
@@ -197,6 +197,9 @@ def test_rows_at_the_ends(cache, kind):  # noqa: F811
     V[8, 0] = torch.nextafter(V[7, 0], torch.tensor(math.inf))
     V[9, 0, :] = torch.arange(64) / 2 + 0.5         # ties
     V[9, 0, 0] = top
+    V[10:14] = torch.tensor([1.74, 1.76, 1.98, 1.99])[:, None, None] * 2.0 ** 127 * torch.linspace(-1, 1, 64)
+    V[14] = torch.finfo(F32).max
+    V[15] = torch.finfo(BF).max
     cache.append(pc, batch, None, torch.zeros(64, 1, 64, device="cuda"), V.cuda())
     code, s, v = codes64.quantise64(V.double(), kind)
     p, at = pool.at(0, 64)

@@ -233,6 +233,25 @@ def test_refusals(cache):  # noqa: F811
         y.sum().backward()
 
 
+def test_parameters_whose_storage_changes(cache):  # noqa: F811
+    """A gain that gets other memory after the norm was made (as moving a module does) is read from there."""
+    x = normal(1, (5, 4, 64), F32).cuda()
+    gain = torch.nn.Parameter(torch.ones(64, device="cuda"))
+    norm = cache.HeadNorm("rms", gain)
+    one = cache.norm_rotary(x, norm).detach()
+    gain.data = torch.full((4, 64), 2.0, device="cuda")
+    two = cache.norm_rotary(x, norm)
+    assert torch.equal(two.detach(), 2 * one) and norm.heads == 4
+    two.sum().backward()
+    assert gain.grad.shape == (4, 64)
+    gain.data = torch.ones(3, 64, device="cuda")
+    with pytest.raises(ValueError, match="heads"):
+        cache.norm_rotary(x, norm)
+    gain.data = torch.ones(32, device="cuda")
+    with pytest.raises(ValueError):
+        cache.norm_rotary(x, norm)
+
+
 def test_rows_that_are_not_finite_or_tiny(cache):  # noqa: F811
     """A NaN or an infinity stays in its row; rows of zeros give the bias, of equal values (layer) too."""
     x = normal(3, (40, 3, 64), F32)
