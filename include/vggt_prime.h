@@ -564,7 +564,8 @@ typedef struct {
 } vp_cache8;
 
 /* Append as vp_cache_append, with norms of Q's and K's heads before the rotation (q_norm and k_norm may be NULL: none), and
- * K and V quantised on their way, from fp32. */
+ * K and V quantised on their way: K's norm and rotation are in fp64 for that, so that its codes are those of the exact
+ * rows but for features within 1e-9 of a border between two codes. */
 vp_status vp_cache8_append(const vp_cache8 *cache, const vp_cache_batch *batch, int32_t Hq,
                            const void *Q, int64_t q_stride, const void *K, int64_t k_stride,
                            const void *V, int64_t v_stride, const vp_head_norm *q_norm,

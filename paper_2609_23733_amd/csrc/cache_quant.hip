@@ -10,7 +10,61 @@ namespace vp {
 // takes every hs-th row: of Q, then of K, then of V, the first of each loaded at once (Q_out may be Q).
 // Chunks: 32 neighbouring tokens' threads of one row are neighbours, so that what a page gets per slot (codes, scales,
 // weight, stamp) is written in runs.
+//
+// K is normalised and turned in fp64: a row's code follows from its side of a border between two codes, which fp32's
+// errors put a few features of a view's 1.4 million on the wrong one of (8.3 us in fp32, 10.0 so).
 // ------------------------------------------------------------------------
+// d in fp32, cut, the last bit set if anything was cut off: on d's side of every border between codes (fp32 rounding
+// might put it on the border itself).
+__device__ __forceinline__ float beside(double d) {
+    uint32_t lo = (uint32_t)__double2loint(d);
+    lo = (lo & 0xe0000000u) | (lo & 0x1fffffffu ? 0x20000000u : 0u);
+    return (float)__hiloint2double(__double2hiint(d), (int)lo);
+}
+
+template <typename Turn>
+struct Row64 {
+    double co[4], si[4];
+    __device__ __forceinline__ void angles(const Turn& w, const RotArgs& r, int64_t t, int c) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            co[e] = 1.;
+            si[e] = 0.;
+            const int p = 4 * c + e;
+            if (p >= r.dim / 2) continue;
+            sincos_turn64((uint64_t)(int64_t)r.pos[t * r.axes + Turn::section(r, p)] * r.freq[p], &si[e], &co[e]);
+            co[e] *= (double)r.mag;
+            si[e] *= (double)r.mag;
+        }
+    }
+    __device__ __forceinline__ void turned(const NormArgs& nm, const Turn& w, int h, float (&f)[8]) const {
+        double v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = (double)f[e];
+        if (nm.on) {
+            Affine p;
+            p.set(nm, w, h);
+            if (nm.layer) {
+                const double mean = sum8(((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]))) * (1. / kD);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] -= mean;
+            }
+            double s = 0.;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s = fma(v[e], v[e], s);
+            const double inv = rsqrt(fma(sum8(s), 1. / kD, (double)nm.eps));
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = fma(v[e] * inv, (double)p.gain[e], (double)p.bias[e]);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const double a = v[2 * e], b = v[2 * e + 1];
+            f[2 * e] = beside(fma(a, co[e], -(b * si[e])));
+            f[2 * e + 1] = beside(fma(b, co[e], a * si[e]));
+        }
+    }
+};
+
 struct Spread {
     int hs, runs;
     int k0, v0;      // rows of Q, and of Q and K, modulo hs
@@ -66,7 +120,7 @@ __device__ __forceinline__ void put_row(const CacheArgs& a, void* pool, int64_t 
     }
 }
 
-// 1,374 tokens of 16 + 16 + 16 heads, bf16 to int8, with norms: 8.4 us, 20 MB (15.2 with
+// 1,374 tokens of 16 + 16 + 16 heads, bf16 to int8, with norms: 10.0 us, 20 MB (in fp32 8.3; 15.2 with
 // the three kinds of row in one loop, whose arrays the compiler kept in memory).
 template <typename T, int CODE, bool INTER, bool VEC>
 __global__ __launch_bounds__(256) void k_cache_append8(AppendArgs a, NormArgs qn, NormArgs kn, RotArgs r, Spread sp) {
@@ -95,7 +149,14 @@ __global__ __launch_bounds__(256) void k_cache_append8(AppendArgs a, NormArgs qn
     if (hv < Hkv) plain.load(vr + hv * kD, fv);
     int page = -1;
     if (slot >= 0) page = a.c.table[(int64_t)b * a.c.max_pages + (slot >> a.c.page_log2)];
-    w.angles(r, t, c);
+    Row64<HeadTurn<T, INTER, VEC>> w64;
+    if constexpr (CODE != CODE_NONE) {
+        if (h0 < hq || hk < Hkv) w64.angles(w, r, t, c);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w.co[e] = (float)w64.co[e], w.si[e] = (float)w64.si[e];
+    } else {
+        w.angles(r, t, c);
+    }
     auto turned = [&](const NormArgs& nm, int h, float (&f)[8]) {
         if (nm.on) {
             Affine p;
@@ -117,7 +178,8 @@ __global__ __launch_bounds__(256) void k_cache_append8(AppendArgs a, NormArgs qn
     if (page < 0 || page >= a.c.npages) return;
     const int64_t at0 = (((int64_t)page * Hkv) << a.c.page_log2) + (slot & ((1 << a.c.page_log2) - 1));
     for (int h = hk; h < Hkv; h += sp.hs) {
-        turned(kn, h, fk);
+        if constexpr (CODE != CODE_NONE) w64.turned(kn, w, h, fk);
+        else turned(kn, h, fk);
         const int64_t at = at0 + ((int64_t)h << a.c.page_log2);
         put_row<T, CODE>(a.c, a.c.K, at, 0, w, fk, c);
         if (c == 0) {
@@ -182,7 +244,7 @@ __global__ __launch_bounds__(256) void k_cache_read(ReadArgs a) {
 
 // ------------------------------------------------------------------ launchers
 
-// A view of 1,374 tokens: 16 threads of eight per token 8.4 us; 8 9.7, 32 9.4, one for each of the 48 rows 10.0.
+// A view of 1,374 tokens (K in fp32): 16 threads of eight per token 8.4 us; 8 9.7, 32 9.4, one for each of the 48 rows 10.0.
 static Spread append8_spread(const AppendArgs& a) {
     const int hq = a.Q ? a.Hq : 0, hs = head_split((int64_t)a.c.B * a.c.max_q, hq + 2 * a.c.Hkv, 128 * 1024);
     return Spread{hs, a.c.max_q >= 16, hq % hs, (hq + a.c.Hkv) % hs};

@@ -2,8 +2,8 @@
 back, attention with its weights, eviction, and the stream layer that runs them.
 
 Tolerances (set before the first run).  Codes are exact: V's have to be those of the definition; K's, quantised from the
-normalised and turned row that the kernel has in fp32 (error t of test_gpu_head_norm.py), lie within half a
-step of the scale in use plus t, and the scale is the definition's for a largest value within t.  Attention: those of
+normalised and turned row that the kernel has in fp64, lie within half a step of the scale in use (plus the t that
+test_gpu_head_norm.py has for fp32) and are the definition's where that is no near tie; scales likewise.  Attention: those of
 test_gpu_cache.py over the values that the codes stand for, as code times scale is exact; the kernel's two products by
 scales add two roundings, within the 16 u of E."""
 import math
@@ -133,6 +133,13 @@ def test_append_and_read(cache, lens, qs, Hq, Hkv, page, kind, rows, norm, gain,
         held = codes64.decode64(hK[p, :, s], ks, kind)
         step = codes64.step64((y.abs() + ty) / ks[..., None], kind) * ks[..., None]
         assert ((held - y).abs() <= step / 2 + ty).all(), b
+        # the definition's code, but within 1e-6 of a step of a border (fp64 rows are off by less than 1e-9)
+        _, s64, want = codes64.quantise64(y, kind)
+        top = big / (codes64.LARGEST[kind] * s64)
+        assert (ks == s64)[(top < 1 - 1e-9) & (top > 0.5 + 1e-9)].all(), b
+        place = y.abs() / (codes64.step64(y / s64[..., None], kind) * s64[..., None])
+        clear = ((place - place.floor() - 0.5).abs() > 1e-6) & (ks == s64)[..., None]
+        assert torch.equal(held[clear], want[clear]) and (m == 0 or clear.double().mean() > 0.99), b
         assert (hW[p, :, s] == 0).all()
         assert torch.equal(hStamp[p, :, s], (n + 11 - m + torch.arange(m, dtype=torch.int32))[:, None].expand(m, Hkv))
         before[0][p, :, s], before[1][p, :, s], before[2][p, :, s] = hK[p, :, s], hV[p, :, s], hS[p, :, s]
