@@ -151,22 +151,30 @@ class _Rotation(torch.autograd.Function):
         return rotary(g, pos, ctx.rot, None, not ctx.transpose), None, None, None
 
 
+def _memory(gain, bias):
+    """Where gain and bias lie, and their sizes."""
+    a, n = (0, 0) if gain is None else (gain.data_ptr(), gain.numel())
+    return (a, n, 0, 0) if bias is None else (a, n, bias.data_ptr(), bias.numel())
+
+
 class HeadNorm:
     """The norm of a head's row over its 64 features: kind "layer" (mean and variance) or "rms" (mean
-    square), with gain and bias fp32 [64], or [H, 64] for a norm per head, or None (see vp_head_norm)."""
+    square), with gain and bias fp32 [64], or [H, 64] for a norm per head, or None (see vp_head_norm).  Gain and bias
+    may be exchanged later; kind and eps may not."""
 
     def __init__(self, kind: str = "layer", gain: Optional[torch.Tensor] = None,
                  bias: Optional[torch.Tensor] = None, eps: float = 1e-6):
-        if not 0 < eps < float("inf"):
+        if not 0 < ctypes.c_float(eps).value < float("inf"):
             raise ValueError("eps must be positive")
-        self.kind, self.gain, self.bias, self.eps = kind, gain, bias, float(eps)
+        self._kind, self.gain, self.bias, self._eps = kind, gain, bias, float(eps)
         self._bind()
 
+    kind, eps = property(lambda self: self._kind), property(lambda self: self._eps)
+
     def _bind(self):
-        shape, at = None, []
+        shape = None
         for t, name in ((self.gain, "gain"), (self.bias, "bias")):
             if t is None:
-                at.append(0)
                 continue
             _need(t, name, shape, torch.float32)
             shape = tuple(t.shape)
@@ -174,18 +182,16 @@ class HeadNorm:
                 raise ValueError("%s must be [%d] or [heads, %d]" % (name, HEAD_DIM, HEAD_DIM))
             if t.data_ptr() % 16:
                 raise ValueError("%s must start at a multiple of 16 bytes" % name)
-            at.append(t.data_ptr())
         if self.gain is not None and self.bias is not None and self.gain.device != self.bias.device:
             raise ValueError("gain and bias are on different devices")
         self.tensor = self.bias if self.gain is None else self.gain       # (for its device)
         self.heads = shape[0] if shape is not None and len(shape) == 2 else None
-        self._at = tuple(at)
-        self._ref = ctypes.byref(vp.vp_head_norm(_NORMS[self.kind], *at, self.heads is not None, self.eps))
+        self._at = at = _memory(self.gain, self.bias)
+        self._ref = ctypes.byref(vp.vp_head_norm(_NORMS[self._kind], at[0], at[2], self.heads is not None, self._eps))
 
     def at(self, H: int):
         """The C argument for rows of H heads."""
-        gain, bias = self.gain, self.bias
-        if self._at != (0 if gain is None else gain.data_ptr(), 0 if bias is None else bias.data_ptr()):
+        if self._at != _memory(self.gain, self.bias):
             self._bind()                # (a parameter whose storage was exchanged)
         if self.heads is not None and self.heads != H:
             raise ValueError("a norm of %d heads for %d" % (self.heads, H))
@@ -231,6 +237,8 @@ class _NormRotation(torch.autograd.Function):
 def _norm_gradients(ctx, g):
     x, gain, bias, pos = ctx.saved_tensors             # (refuses values that were changed in place)
     norm, rot = ctx.norm, ctx.rot
+    if norm._at != _memory(gain, bias):                # (it got others, or the graph kept copies)
+        norm = HeadNorm(norm.kind, gain, bias, norm.eps)
     T, H, _ = x.shape
     if not g.is_contiguous() or g.data_ptr() % 16:     # (broadcast, or a part of something)
         g = g.clone(memory_format=torch.contiguous_format)
@@ -250,7 +258,7 @@ def _norm_gradients(ctx, g):
         n = _norm_workspace(T, H, norm.heads is not None)
         ws = torch.empty(n, dtype=torch.uint8, device=x.device)
         at_ws = ws.data_ptr()
-    _done(load_library().vp_norm_rotary_grad(norm.at(H), None if rot is None else rot.at(pos, T), _dt(x), T, H, x.data_ptr(),
+    _done(load_library().vp_norm_rotary_grad(norm._ref, None if rot is None else rot.at(pos, T), _dt(x), T, H, x.data_ptr(),
                                              x.stride(0) if T > 1 else H * HEAD_DIM, g.data_ptr(), H * HEAD_DIM, at_x,
                                              at_gain, at_bias, at_ws, n, _stream()), "vp_norm_rotary_grad")
     return dx, dgain, dbias, None, None, None
@@ -284,6 +292,8 @@ class PagedCache:
         if stamp is not None:
             _need(stamp, "stamp", K.shape[:3], torch.int32)
         self.codes = K.dtype in _CODES
+        if self.codes and any(t is not None and t.device != K.device for t in (V, weight, stamp, scale)):
+            raise ValueError("the cache's tensors are on different devices")
         if self.codes:
             if scale is None:
                 raise ValueError("a cache of codes needs scales")
@@ -361,7 +371,7 @@ def append(pc: PagedCache, batch: Batch, Q, K, V, pos=None, rot: Optional[Rotary
         raise ValueError("a rotation needs positions" if pos is None else "positions need a rotation (rot)")
     turn = None if rot is None else rot.at(pos, T)
     if pc.codes or q_norm is not None or k_norm is not None:
-        st = _here(pc.K, K, V, Q, pos, q_norm and q_norm.tensor, k_norm and k_norm.tensor)
+        st = _here(pc.K, K, V, Q, Q_out, pos, q_norm and q_norm.tensor, k_norm and k_norm.tensor, batch.table)
         _done(load_library().vp_cache8_append(pc._ref8, batch._for(T), Hq, q, qs, K.data_ptr(), ks, V.data_ptr(), vs,
                                               None if q_norm is None or Q is None else q_norm.at(Hq),
                                               None if k_norm is None else k_norm.at(Hkv), turn, qo, st),
@@ -384,7 +394,7 @@ def read(pc: PagedCache, batch: Batch, T: int, dtype: Optional[torch.dtype] = No
     new = lambda: torch.zeros(T, pc.Hkv, HEAD_DIM, dtype=dtype, device=pc.K.device)
     K_out, V_out = new() if K_out is None else K_out, new() if V_out is None else V_out
     shape = (T, pc.Hkv, HEAD_DIM)
-    st = _here(pc.K, K_out, V_out)
+    st = _here(pc.K, K_out, V_out, batch.table)
     _done(load_library().vp_cache8_read(pc._ref8, batch._for(T), vp.VP_BF16 if dtype is torch.bfloat16 else vp.VP_F32,
                                         _whole(K_out, "K_out", shape, dtype), _whole(V_out, "V_out", shape, dtype),
                                         st), "vp_cache8_read")
@@ -420,7 +430,7 @@ def attend(pc: PagedCache, batch: Batch, Q, causal: bool = True, scale: float = 
         lse = torch.empty(T, Hq, dtype=torch.float32, device=Q.device)
     o, ls, wo = _whole(O, "O", (T, Hq, HEAD_DIM), dt), _whole(lse, "lse", (T, Hq), torch.float32), None
     if pc.codes:
-        _here(pc.K, Q)
+        _here(pc.K, Q, O, lse, weight_out, ws, batch.table)
     if weight_out is not None:
         if pc.weight is None:
             raise ValueError("the cache has no weights")
@@ -461,6 +471,8 @@ def evict(pc: PagedCache, table, length, seen, keep: int, max_len: int, sink: in
     if ws is None:
         ws = evict_workspace(pc, B, max_len)
     w, n = _work(ws)
+    if pc.codes:
+        _here(pc.K, table, length, seen, weight_out, stamp_out, length_out, ws)
     c = vp.vp_cache_batch(table.data_ptr(), length.data_ptr(), seen.data_ptr(), None, B, pages, 0, 0,
                           int(max_len))
     _done(pc._call("evict")(pc._ref, ctypes.byref(c), int(keep), int(sink), int(recent), wo, so, lo, w, n, _stream()),

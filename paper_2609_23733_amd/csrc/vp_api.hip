@@ -1232,7 +1232,7 @@ vp_status vp_norm_rotary_grad(const vp_head_norm* norm, const vp_rotary_spec* ro
     if (dtype != VP_F32 && dtype != VP_BF16) return VP_ERR_INVALID_ARG;
     if (T < 0 || H < 1) return VP_ERR_INVALID_ARG;
     if (T > kMaxTokens || H > kMaxCacheHeads) return VP_ERR_UNSUPPORTED;
-    if (!aligned4(dgain) || !aligned4(dbias)) return VP_ERR_INVALID_ARG;
+    if (!aligned4(dgain) || !aligned4(dbias) || (dgain && dgain == dbias)) return VP_ERR_INVALID_ARG;
     if (T > 0 && (!x || !g || !aligned16(x) || !aligned16(g) || !aligned16(dx) || !stride_ok(x_stride, H, dtype) ||
                   !stride_ok(g_stride, H, dtype) || dx == x || dx == g))
         return VP_ERR_INVALID_ARG;

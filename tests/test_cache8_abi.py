@@ -110,7 +110,7 @@ def test_bad_norms(lib):
     def fwd(n=norm(), rot=spec(), dtype=vp.VP_BF16, T=3, H=4, x=FAKE, xs=256, y=FAKE2, ys=256):
         return lib.vp_norm_rotary(None if n is None else R(n), None if rot is None else R(rot), dtype, T, H, x, xs, y, ys, None)
 
-    def grad(n=norm(), rot=spec(), dtype=vp.VP_BF16, T=3, H=4, x=FAKE, xs=256, g=FAKE, gs=256, dx=FAKE2, dg=FAKE, db=FAKE,
+    def grad(n=norm(), rot=spec(), dtype=vp.VP_BF16, T=3, H=4, x=FAKE, xs=256, g=FAKE, gs=256, dx=FAKE2, dg=FAKE, db=FAKE + 1024,
              ws=FAKE, n_ws=1 << 30):
         return lib.vp_norm_rotary_grad(None if n is None else R(n), R(rot), dtype, T, H, x, xs, g, gs, dx, dg, db, ws, n_ws, None)
 
@@ -123,7 +123,7 @@ def test_bad_norms(lib):
     for kw in (dict(y=None), dict(ys=128), dict(y=FAKE, ys=512)):
         assert fwd(**kw) == 1, kw
     for kw, code in [(dict(g=None), 1), (dict(gs=255), 1), (dict(dx=FAKE), 1), (dict(dx=FAKE_ODD), 1), (dict(dg=FAKE_ODD), 1),
-                     (dict(db=FAKE_ODD), 1), (dict(ws=None), 1), (dict(ws=FAKE + 8), 1), (dict(n_ws=0), 3)]:
+                     (dict(db=FAKE_ODD), 1), (dict(db=FAKE), 1), (dict(ws=None), 1), (dict(ws=FAKE + 8), 1), (dict(n_ws=0), 3)]:
         assert grad(**kw) == code, kw
     assert fwd(T=0) == 0 and grad(dx=None, dg=None, db=None, ws=None, n_ws=0) == 0
     size = lib.vp_norm_rotary_grad_workspace_bytes
@@ -148,7 +148,7 @@ def test_python_refusals():
         cache.HeadNorm("layer", t)
     with pytest.raises(KeyError):
         cache.HeadNorm("batch")
-    for eps in (0.0, -1.0, float("nan"), float("inf")):
+    for eps in (0.0, -1.0, float("nan"), float("inf"), 1e-50, 1e39):
         with pytest.raises(ValueError, match="eps"):
             cache.HeadNorm("rms", eps=eps)
     n = cache.HeadNorm("rms")

@@ -647,11 +647,13 @@ def test_other_devices(cache, monkeypatch):  # noqa: F811
     pc = cache.PagedCache(K, V, scale=torch.ones(4, 2, 16, 2, dtype=BF, device="cuda"))
     batch = cache.Batch(i32([[0]]), i32([5]), i32([0, 2]), 2, 5)
     rows = normal(1, (2, 2, 64), BF).cuda()
+    full = cache.PagedCache.empty(4, 2, 16, torch.int8)
     n = cache.HeadNorm("rms")
     ws = cache.attend_workspace(pc, batch, 2, 2)
     k, v = torch.empty_like(rows), torch.empty_like(rows)
     calls = [lambda: cache.append(pc, batch, rows, rows, rows, Q_out=k), lambda: cache.read(pc, batch, 2, K_out=k, V_out=v),
-             lambda: cache.norm_rotary(rows, n, out=k), lambda: cache.attend(pc, batch, rows, O=k, ws=ws)]
+             lambda: cache.norm_rotary(rows, n, out=k), lambda: cache.attend(pc, batch, rows, O=k, ws=ws),
+             lambda: cache.evict(full, batch.table, batch.length, i32([5]), 4, 5)]
     for call in calls:
         call()
     real = cache._device()

@@ -252,6 +252,44 @@ def test_parameters_whose_storage_changes(cache):  # noqa: F811
         cache.norm_rotary(x, norm)
 
 
+def test_parameters_exchanged_before_the_gradient(cache):  # noqa: F811
+    """A graph's gradients are of the gain and bias of its forward pass, whatever the norm holds by then."""
+    rot = cache.Rotary.make(64)
+    pos = torch.arange(9, dtype=torch.int32, device="cuda")[:, None]
+    x = normal(1, (9, 4, 64), F32).cuda().requires_grad_()
+    leaf = lambda s, *sh: (1 + normal(s, sh, F32).cuda()).requires_grad_()
+    ga, bi, g = leaf(2, 4, 64), leaf(3, 4, 64), normal(4, (9, 4, 64), F32).cuda()
+    step = lambda n: cache.norm_rotary(x, n, pos, rot)
+    want = torch.autograd.grad(step(cache.HeadNorm("layer", ga, bi)), [x, ga, bi], g)
+    same = lambda d: all(torch.equal(p, q) for p, q in zip(d, want))
+    norm = cache.HeadNorm("layer", ga, bi)
+    y = step(norm)
+    norm.gain, norm.bias = leaf(5, 4, 64), None
+    other = step(norm)
+    assert same(torch.autograd.grad(y, [x, ga, bi], g))
+    assert not torch.equal(torch.autograd.grad(other, [x], g)[0], want[0])
+    # other sizes at the same address
+    norm = cache.HeadNorm("layer", ga, bi)
+    y = step(norm)
+    norm.gain, norm.bias = ga.detach()[0], bi.detach()[0]
+    one = step(norm).detach()
+    assert torch.equal(one, step(cache.HeadNorm("layer", ga.detach()[0].clone(), bi.detach()[0].clone())).detach())
+    assert same(torch.autograd.grad(y, [x, ga, bi], g))
+    norm.gain, norm.bias = ga.detach()[:3], bi.detach()[:3]
+    with pytest.raises(ValueError, match="heads"):
+        step(norm)
+    # copies that the graph kept on the host
+    norm = cache.HeadNorm("layer", ga, bi)
+    with torch.autograd.graph.save_on_cpu():
+        y = step(norm)
+    with torch.no_grad():
+        ga.add_(1.0)
+    assert same(torch.autograd.grad(y, [x, ga, bi], g))
+    for name in ("kind", "eps"):
+        with pytest.raises(AttributeError):
+            setattr(norm, name, 1)
+
+
 def test_rows_that_are_not_finite_or_tiny(cache):  # noqa: F811
     """A NaN or an infinity stays in its row; rows of zeros give the bias, of equal values (layer) too."""
     x = normal(3, (40, 3, 64), F32)
