@@ -927,8 +927,9 @@ vp_status attend_args(const vp_cache* cache, const vp_cache8* cache8, const vp_c
     a->Hq = Hq;
     a->G = Hq / a->c.Hkv;
     vp::attend_plan(a);
-    // a launch has fewer than 2^32 threads, 2^24 workgroups: of the attention, the join and the weights
-    if (((int64_t)a->c.B * a->c.Hkv * a->nsplit + 8) * a->row_tiles >= 1 << 24 ||
+    // a launch has fewer than 2^32 threads, 2^24 workgroups (2^23 of the 512 threads that share decoded tiles): of the
+    // attention, the join and the weights
+    if (((int64_t)a->c.B * a->c.Hkv * a->nsplit + 8) * a->row_tiles >= (a->wide && a->c.code ? 1 << 23 : 1 << 24) ||
         (a->nsplit > 1 && (int64_t)a->c.max_q * Hq >= 1 << 26) || a->c.max_len > (1 << 30) - 64)
         return VP_ERR_UNSUPPORTED;
     return VP_OK;

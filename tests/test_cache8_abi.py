@@ -102,6 +102,12 @@ def test_bad_calls(lib):
     assert evict(lib, c, b, n=0) == 3
     many = batch(B=4000, T=1 << 23, max_q=1 << 23, max_len=640)       # 2^32 threads and more
     assert append(lib, c, many) == 2 and read(lib, c, many) == 2 and attend(lib, c, many) == 2
+    # workgroups of 512 threads: 2^23 of them are too many
+    wide, plan = coded(Hkv=64, page=4096, npages=1 << 30), vp.vp_cache_plan()
+    for B, code in ((500, 0), (600, 2)):
+        b2 = batch(B=B, T=72, max_q=72, max_len=69100000, max_pages=17000)
+        assert lib.vp_cache8_attend_plan(R(wide), R(b2), 128, R(plan)) == code, B
+        assert plan.shared == 1 and plan.ranges == 256 and plan.row_tiles == 1
     empty = batch(T=0, max_q=0)
     assert attend(lib, c, empty) == 0 and append(lib, c, empty) == 0 and read(lib, c, empty) == 0
 
