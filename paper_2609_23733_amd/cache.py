@@ -171,6 +171,9 @@ class HeadNorm:
 
     kind, eps = property(lambda self: self._kind), property(lambda self: self._eps)
 
+    def __reduce__(self):               # (copied and pickled as what it is made of, parameters with their module's)
+        return HeadNorm, (self._kind, self.gain, self.bias, self._eps)
+
     def _bind(self):
         shape = None
         for t, name in ((self.gain, "gain"), (self.bias, "bias")):

@@ -8,6 +8,9 @@ e_z = |gain| e_h + u Z, the two means by e_z + 12 u Z and N e_z + e_n Z + 12 u N
     |dx| is off by r ((2 + N^2) e_z + (2 N + 1) e_n Z + 32 u Z (1 + N^2)) + |dx| (12 u S r + 20 u).
 Sums over R rows: each term by e_h N + max |h| e_n + u, and (64 + R / 256) u of the absolute sum for the chains of a
 slot (R / 256 rows at most: 32 slots of 8 workgroups or more) and of a workgroup.  bf16 outputs: 2^-8 of the value more."""
+import copy
+import pickle
+
 import numpy as np
 import pytest
 import torch
@@ -250,6 +253,25 @@ def test_parameters_whose_storage_changes(cache):  # noqa: F811
     gain.data = torch.ones(32, device="cuda")
     with pytest.raises(ValueError):
         cache.norm_rotary(x, norm)
+
+
+def test_copies(cache):  # noqa: F811
+    """A copied module's norm has the copy's parameters."""
+    class Heads(torch.nn.Module):
+        def __init__(self):
+            super().__init__()
+            self.gain = torch.nn.Parameter(torch.full((64,), 2.0, device="cuda"))
+            self.norm = cache.HeadNorm("rms", self.gain, None, 1e-5)
+
+    one = Heads()
+    two = copy.deepcopy(one)
+    assert two.norm.gain is two.gain and two.gain is not one.gain and (two.norm.kind, two.norm.eps) == ("rms", 1e-5)
+    x = normal(1, (5, 4, 64), F32).cuda()
+    with torch.no_grad():
+        two.gain.fill_(4.0)
+        assert torch.equal(cache.norm_rotary(x, two.norm), 2 * cache.norm_rotary(x, one.norm))
+        back = pickle.loads(pickle.dumps(cache.HeadNorm("layer", torch.ones(4, 64, device="cuda"))))
+        assert torch.equal(cache.norm_rotary(x, back), cache.norm_rotary(x, cache.HeadNorm("layer")))
 
 
 def test_parameters_exchanged_before_the_gradient(cache):  # noqa: F811
