@@ -220,7 +220,8 @@ def norm_rotary(x, norm: HeadNorm, pos=None, rot: Optional[Rotary] = None, out: 
         out = torch.empty(T, H, HEAD_DIM, dtype=x.dtype, device=x.device)
     ys = _rows(out, "out", T, H, x.dtype)
     _done(load_library().vp_norm_rotary(norm.at(H), None if rot is None else rot.at(pos, T), _dt(x), T, H, x.data_ptr(), xs,
-                                        out.data_ptr(), ys, _here(x, out, norm.tensor, pos)), "vp_norm_rotary")
+                                        out.data_ptr(), ys, _here(x, out, norm.tensor, pos, rot and rot.freq)),
+          "vp_norm_rotary")
     return out
 
 
@@ -374,7 +375,8 @@ def append(pc: PagedCache, batch: Batch, Q, K, V, pos=None, rot: Optional[Rotary
         raise ValueError("a rotation needs positions" if pos is None else "positions need a rotation (rot)")
     turn = None if rot is None else rot.at(pos, T)
     if pc.codes or q_norm is not None or k_norm is not None:
-        st = _here(pc.K, K, V, Q, Q_out, pos, q_norm and q_norm.tensor, k_norm and k_norm.tensor, batch.table)
+        st = _here(pc.K, K, V, Q, Q_out, pos, rot and rot.freq, q_norm and q_norm.tensor, k_norm and k_norm.tensor,
+                   batch.table)
         _done(load_library().vp_cache8_append(pc._ref8, batch._for(T), Hq, q, qs, K.data_ptr(), ks, V.data_ptr(), vs,
                                               None if q_norm is None or Q is None else q_norm.at(Hq),
                                               None if k_norm is None else k_norm.at(Hkv), turn, qo, st),

@@ -656,6 +656,12 @@ def test_other_devices(cache, monkeypatch):  # noqa: F811
              lambda: cache.evict(full, batch.table, batch.length, i32([5]), 4, 5)]
     for call in calls:
         call()
+    # (frequencies elsewhere: what a Rotary made while another device was the current one has)
+    rot, pos = cache.Rotary.make(64), torch.zeros(2, 1, dtype=torch.int32, device="cuda")
+    rot.freq = rot.freq.cpu()
+    for call in (lambda: cache.norm_rotary(rows, n, pos, rot), lambda: cache.append(pc, batch, rows, rows, rows, pos, rot)):
+        with pytest.raises(ValueError, match="device"):
+            call()
     real = cache._device()
     with monkeypatch.context() as m:
         m.setattr(cache, "_device", lambda: real + 1)
