@@ -400,7 +400,7 @@ __global__ __launch_bounds__((64 * GeoOf<T, WIDE, CODE>::NW), 2) void k_cache_at
         // have few rows, comes last; and all ranges of a sequence one after the other, as the compute units that an
         // XCD's workgroups go to follow from their numbers (with those of a long sequence always every fourth, 149 us
         // for 82), turned by three from tile to tile.  Ragged: six sequences of up to 700 tokens over 20,000 slots 103 us, 167 in the other
-        // order; 16 of up to 400 over 3,000 62 and 81.
+        // order; 16 of up to 400 over 3,000 62 and 81 (both before few rows were spread over the SIMDs).
         const int turns = (heads * a.nsplit + 7) >> 3;
         rt = (blockIdx.x >> 3) / turns;
         x = ((blockIdx.x >> 3) - rt * turns + 3 * rt) % turns * 8 + (blockIdx.x & 7);
@@ -412,8 +412,12 @@ __global__ __launch_bounds__((64 * GeoOf<T, WIDE, CODE>::NW), 2) void k_cache_at
     const int hk = y % a.c.Hkv, b = y / a.c.Hkv;
 
     const CacheSeq sq = cache_seq(a.c, b);
-    const int nrows = sq.nq * a.G, row0 = rt * G::RT + (WIDE ? wave * 32 * G::NB : 0);
+    const int nrows = sq.nq * a.G;
     if (rt * G::RT >= nrows) return;
+    // A tile of few rows: one group of rows for each of four waves (a SIMD each), the other sees nothing.  (16 sequences of up
+    // to 400 tokens over 3,000 slots 76 -> 69 us.  200 rows as seven waves' groups, two waves a SIMD: 37 -> 44.)
+    const bool slim = kCode && nrows - rt * G::RT <= 16 * G::NW;
+    const int wave_rows = slim ? 32 : 32 * G::NB, row0 = rt * G::RT + (WIDE ? wave * wave_rows : 0);
     const int tile_last = rt * G::RT + G::RT - 1 < nrows ? rt * G::RT + G::RT - 1 : nrows - 1;
     const int klim = cache_visible(sq, a.causal, tile_last / a.G);
     const int c0 = split * a.chunk, c1 = c0 + a.chunk < klim ? c0 + a.chunk : klim;
@@ -429,7 +433,7 @@ __global__ __launch_bounds__((64 * GeoOf<T, WIDE, CODE>::NW), 2) void k_cache_at
         int r = row0 + 32 * nb + l31;
         r = r < nrows ? r : nrows - 1;
         const int i = r / a.G, head = hk * a.G + r - i * a.G;
-        w[nb].vis = cache_visible(sq, a.causal, i);
+        w[nb].vis = kCode && nb && slim ? 0 : cache_visible(sq, a.causal, i);
         w[nb].m = -INFINITY;
         w[nb].l = 0.f;
         w[nb].o[0] = w[nb].o[1] = zero_f32x16();
@@ -453,7 +457,7 @@ __global__ __launch_bounds__((64 * GeoOf<T, WIDE, CODE>::NW), 2) void k_cache_at
         }
     };
     if constexpr (!WIDE || G::kBf) load_q();
-    const int wave_last = row0 + 32 * G::NB - 1 < nrows ? row0 + 32 * G::NB - 1 : nrows - 1;
+    const int wave_last = row0 + wave_rows - 1 < nrows ? row0 + wave_rows - 1 : nrows - 1;
     const int wlim = alive ? cache_visible(sq, a.causal, wave_last / a.G) : 0;
     // slots of this range that every row of the workgroup sees
     const int all = cache_visible(sq, a.causal, rt * G::RT / a.G), seen_by_all = all < c1 ? all : c1;
@@ -687,22 +691,23 @@ __global__ __launch_bounds__((64 * GeoOf<T, WIDE, CODE>::NW), 2) void k_cache_at
             };
             typedef f32x16 Logits[G::NB];
             typedef Probs<T, G::kSplit> BlockP[G::NB];
-            auto half = [&](auto mask, Logits& s, int k0, Logits& sn, lds_char* k, lds_char* v, lds_char* v_next,
+            auto half = [&](auto mask, auto width, Logits& s, int k0, Logits& sn, lds_char* k, lds_char* v, lds_char* v_next,
                             const BlockP& pv, BlockP& pn) {
+                constexpr int NB = decltype(width)::value;
                 if constexpr (decltype(mask)::value)
 #pragma unroll
-                    for (int nb = 0; nb < G::NB; ++nb) block_mask<T>(w[nb], k0, ~0u, lane, s[nb]);
+                    for (int nb = 0; nb < NB; ++nb) block_mask<T>(w[nb], k0, ~0u, lane, s[nb]);
                 constexpr int kOf[8] = {4, 5, 6, 0, 1, 2, 3, 7};   // 0-3: logits, 4-7: values
                 bf16x8 f[8] = {ahead[0], ahead[1], ahead[2]};
                 // Two logits at a time, in three steps an MFMA apart so that none waits for the last:
                 // the exponent, its power, the sum and the rounding.
                 auto exponent = [&](int u) {
 #pragma unroll
-                    for (int r = 2 * (u / G::NB); r < 2 * (u / G::NB) + 2; ++r)
-                        s[u % G::NB][r] = fmaf(s[u % G::NB][r], a.c2, -ref[u % G::NB]);
+                    for (int r = 2 * (u / NB); r < 2 * (u / NB) + 2; ++r)
+                        s[u % NB][r] = fmaf(s[u % NB][r], a.c2, -ref[u % NB]);
                 };
                 auto add = [&](int u) {
-                    const int nb = u % G::NB, i = u / G::NB;
+                    const int nb = u % NB, i = u / NB;
                     sum[nb][(2 * i) & 3] += s[nb][2 * i];
                     sum[nb][(2 * i + 1) & 3] += s[nb][2 * i + 1];
                     pn[nb].v[i >> 2][(2 * i) & 7] = (bf16)s[nb][2 * i];
@@ -710,8 +715,8 @@ __global__ __launch_bounds__((64 * GeoOf<T, WIDE, CODE>::NW), 2) void k_cache_at
                 };
                 exponent(0);
 #pragma unroll
-                for (int u = 0; u < 8 * G::NB; ++u) {
-                    const int i = u / G::NB, nb = u % G::NB, n = kOf[i];
+                for (int u = 0; u < 8 * NB; ++u) {
+                    const int i = u / NB, nb = u % NB, n = kOf[i];
                     if (nb == 0) {
                         if (i < 5) f[i + 3] = kOf[i + 3] < 4 ? key_at(k, kOf[i + 3]) : value_at(v, kOf[i + 3] - 4);
                         else ahead[i - 5] = value_at(v_next, i - 5);
@@ -719,13 +724,13 @@ __global__ __launch_bounds__((64 * GeoOf<T, WIDE, CODE>::NW), 2) void k_cache_at
                     Rows<T>& x = w[nb];
                     if (n < 4) sn[nb] = mfma_bf16(f[i], x.qb[n], n ? sn[nb] : zero_f32x16());
                     else x.o[n & 1] = mfma_bf16(f[i], pv[nb].v[(n - 4) >> 1], x.o[n & 1]);
-                    if (u + 1 < 8 * G::NB) exponent(u + 1);
+                    if (u + 1 < 8 * NB) exponent(u + 1);
                     s[nb][2 * i] = exp2f_fast(s[nb][2 * i]);
                     s[nb][2 * i + 1] = exp2f_fast(s[nb][2 * i + 1]);
                     if (u > 0) add(u - 1);
                     __builtin_amdgcn_sched_barrier(0);
                 }
-                add(8 * G::NB - 1);
+                add(8 * NB - 1);
             };
             auto probs = [&](Logits& s, int k0, BlockP& p) {
 #pragma unroll
@@ -739,11 +744,11 @@ __global__ __launch_bounds__((64 * GeoOf<T, WIDE, CODE>::NW), 2) void k_cache_at
                     p[nb].set(s[nb]);
                 }
             };
-            auto body = [&](auto mask, int t) {   // second block of tile t, first of tile t + 1
+            auto body = [&](auto mask, auto width, int t) {   // second block of tile t, first of tile t + 1
                 lds_char *cur = tile_at(t), *next = tile_at(t + 1);
                 const int k0 = c0 + t * G::TK;
-                half(mask, s1, k0 + 32, s0, next, cur + G::kTileV, cur + G::kTileV + G::kBlock, p0, p1);
-                half(mask, s0, k0 + 64, s1, next + G::kBlock, cur + G::kTileV + G::kBlock, next + G::kTileV, p1, p0);
+                half(mask, width, s1, k0 + 32, s0, next, cur + G::kTileV, cur + G::kTileV + G::kBlock, p0, p1);
+                half(mask, width, s0, k0 + 64, s1, next + G::kBlock, cur + G::kTileV + G::kBlock, next + G::kTileV, p1, p0);
             };
             arrive(0);
             if (alive && pw.sane) {
@@ -765,17 +770,24 @@ __global__ __launch_bounds__((64 * GeoOf<T, WIDE, CODE>::NW), 2) void k_cache_at
 #pragma unroll
                 for (int i = 0; i < 3; ++i) ahead[i] = value_at(tile_at(0) + G::kTileV, i);
                 int t = 0;
+                typedef std::integral_constant<int, G::NB> All;
+                if (kCode && slim)
+                    for (; t + 1 < nt; ++t) {
+                        arrive(t + 1);
+                        body(std::true_type(), std::integral_constant<int, 1>(), t);
+                    }
                 for (; t + 1 < nt && t + 1 < tfull; ++t) {
                     arrive(t + 1);
-                    body(std::false_type(), t);
+                    body(std::false_type(), All(), t);
                 }
                 for (; t + 1 < nt; ++t) {
                     arrive(t + 1);
-                    body(std::true_type(), t);
+                    body(std::true_type(), All(), t);
                 }
                 probs(s1, c0 + t * G::TK + 32, p1);
 #pragma unroll
                 for (int nb = 0; nb < G::NB; ++nb) {
+                    if (kCode && nb && slim) break;
                     block_values<T, G::kSplit>(w[nb], tile_at(t) + G::kTileV, p0[nb], false, lane);
                     block_values<T, G::kSplit>(w[nb], tile_at(t) + G::kTileV + G::kBlock, p1[nb], false, lane);
                     w[nb].l = (sum[nb][0] + sum[nb][1]) + (sum[nb][2] + sum[nb][3]);
@@ -1030,7 +1042,7 @@ __global__ __launch_bounds__((64 * GeoOf<T, WIDE, CODE>::NW), 2) void k_cache_at
     if constexpr (WIDE) {
 #pragma unroll
         for (int nb = 0; nb < G::NB; ++nb) {
-            if (row0 + 32 * nb + l31 >= nrows) return;
+            if ((kCode && nb && slim) || row0 + 32 * nb + l31 >= nrows) return;
             float inv, lse;
             row_result(w[nb].m, w[nb].l, &inv, &lse);
             if (inv == 0.f) w[nb].o[0] = w[nb].o[1] = zero_f32x16();   // no weight on any values

@@ -403,6 +403,42 @@ def test_attend_wide_odd(cache, kind):  # noqa: F811
 
 
 @pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("q", [513, 545, 640, 641])
+def test_attend_wide_few_rows(cache, kind, q):  # noqa: F811
+    """A last tile of 1, 33, 128 and 129 rows; sequences that are no more than that; what is rare in such tiles."""
+    log("attend8 wide, few rows %s q=%d" % (kind, q))
+    n, lens, qs = 7000, [7000, 300, 64, 1], [q, q - 512, 1, 0]
+    pool = Pool8(cache, lens, 8, 32, kind, seed=41, junk="bits")
+    check(cache, pool, normal(9, (sum(qs), 8, 64), BF), qs, True, 1)
+    Q = normal(10, (q, 8, 64), BF)
+    pool = Pool8(cache, [n], 8, 32, kind, seed=42)
+    odd_scales(pool, n)
+    check(cache, pool, Q, [q], True, 1)
+    pool = Pool8(cache, [n], 8, 32, kind, seed=43)
+    check(cache, pool, Q, [q], False, 1, gone=[s for p in (0, 3, 70, 124) for s in range(32 * p, 32 * p + 32) if s < n])
+    pool = Pool8(cache, [n], 8, 32, kind, seed=44, std=3.0)
+    k = pool.k[0].clone()
+    k[2500:] *= 8
+    pool.put(0, k, torch.clamp(pool.v[0], -4, 4) * 2e37)
+    Q = normal(11, (q, 8, 64), BF, 3.0).cuda()
+    pc, batch = pool.cuda(), pool.batch([q])
+    assert cache.attend_plan(pc, batch, 8, q).shared == 1
+    O, lse = cache.attend(pc, batch, Q, True)
+    # The tolerance of test_gpu_cache.py and what underflow takes: a power below 2^-126 counts as 0 in the products, and the
+    # powers' sum is 1 at least (the reference is one of the row's logits, and grows with them), so each of n slots loses at
+    # most 2^-126 of the largest |v|, below 2^126 here: n, where most results are of the size of 1e37.
+    sees = torch.arange(n, device="cuda") < (n - q + torch.arange(q, device="cuda") + 1)[:, None]
+    for h in range(8):
+        v = pool.v[0][:, h].cuda()
+        ro, rl, _, A, X = whole64(Q[:, h], pool.k[0][:, h].cuda(), v, sees, 0.125)
+        E = (64 * X + n / 16 + 16 + rl.abs()) * U
+        tol = (2 * E[:, None] * A + n * 2.0 ** -126 * v.abs().max()).cpu().numpy()
+        tol = torch.from_numpy(bf16_tol(tol, A.cpu().numpy(), ro.cpu().numpy())).cuda()
+        assert ((O[:, h].double() - ro).abs() <= tol).all(), h
+        assert ((lse[:, h].double() - rl).abs() <= 2 * E + 2 * U * rl.abs()).all(), h
+
+
+@pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("q", [5, 1500])
 def test_attend_scales_of_other_origin(cache, kind, q):  # noqa: F811
     """Scales that are no powers of two: within another bf16 rounding of every value (2^-8) and key (2^-8 of a
