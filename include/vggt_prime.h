@@ -574,8 +574,8 @@ vp_status vp_cache8_append(const vp_cache8 *cache, const vp_cache_batch *batch, 
 
 /* Attend as vp_cache_attend (arguments, workspace, plan, weights, rows that see nothing) over code times scale; O and Q in
  * `rows`.  A NaN in a slot's value (its scale, or an E4M3 code) makes results of rows that see the slot NaN, at
- * least in its feature, and reaches no other row.  bf16 rows: probabilities as sums of two bf16 values, rounded to
- * bf16 in calls of many rows over many slots (vp_cache_plan's `shared`).  fp32 rows: exact products, fp32 sums; a
+ * least in its feature, and reaches no other row.  bf16 rows: probabilities as sums of two bf16 values, or in calls of many
+ * rows over many slots (vp_cache_plan's `shared`) as fp16 values, within 2^-11, where that range does.  fp32 rows: exact products, fp32 sums; a
  * row of Q with an infinity gives NaN. */
 size_t vp_cache8_attend_workspace_bytes(const vp_cache8 *cache, const vp_cache_batch *batch,
                                         int32_t Hq);

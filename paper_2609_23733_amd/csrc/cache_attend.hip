@@ -129,6 +129,20 @@ struct Probs<float, SPLIT> {
     f32x16 v;
     __device__ __forceinline__ void set(const f32x16& s) { v = s; }
 };
+// In fp16, for values that are there in fp16, too (wide workgroups over 8-bit codes): within 2^-11 of each at the cost of a
+// single bf16 value, but for probabilities below 2^-14, whose step is 2^-24 (errors of 1.66e-3 of the result, with
+// single bf16 values 2.33e-3; a view over 43,968 slots 265 -> 274 us, for the range that settle() watches).
+struct HalfProbs {
+    f16x8 v[2];
+    __device__ __forceinline__ void set(const f32x16& s) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i >> 3][i & 7] = (f16)s[i];
+    }
+};
+__device__ __forceinline__ f32x16 mfma_value(bf16x8 f, bf16x8 p, f32x16 c) { return mfma_bf16(f, p, c); }
+__device__ __forceinline__ f32x16 mfma_value(bf16x8 f, f16x8 p, f32x16 c) {
+    return mfma_f16(__builtin_bit_cast(f16x8, f), p, c);
+}
 
 // Logits (without the scale) of the block whose K lies at `k`.
 template <typename T>
@@ -218,6 +232,14 @@ __device__ __forceinline__ bf16x8 tr_read(lds_char* a) {
 
 // O^T += V^T P^T of the block whose V lies at `v`.  `rest`: with the second parts of split probabilities
 // (which an infinite value would turn into NaN).
+__device__ __forceinline__ void block_values(Rows<bf16>& w, lds_char* v, const HalfProbs& p, int lane) {
+    const int hh = lane >> 5, i16 = lane & 15, dq = (lane >> 4) & 1;
+    const int v0 = (8 * hh + (i16 >> 2)) * 128 + (((2 * dq + ((i16 & 3) >> 1)) ^ (2 * (i16 >> 2))) << 4) + (i16 & 1) * 8;
+#pragma unroll
+    for (int st = 0; st < 2; ++st)
+#pragma unroll
+        for (int m = 0; m < 2; ++m) w.o[m] = mfma_value(tr_read(v + (v0 ^ (m << 6)) + st * 2048), p.v[st], w.o[m]);
+}
 template <typename T, bool SPLIT>
 __device__ __forceinline__ void block_values(Rows<T>& w, lds_char* v, const Probs<T, SPLIT>& p, bool rest, int lane) {
     const int l31 = lane & 31, hh = lane >> 5;
@@ -377,12 +399,15 @@ __device__ __forceinline__ void add_odd_values(const AttendArgs& a, Rows<T>& w, 
 // kernel alone, after some 40 passes: the first ones run at lower clocks, 280-350.  fp32, three prompts of
 // 8.6 GFLOP: 63 us).
 //
-// CODE: K and V are 8-bit codes (wide bf16 rows only).  Tiles are the same in LDS, code times scale as bf16 values; they come through
-// registers: a wave loads a tile's 16 slots two tiles ahead and writes them, decoded, one ahead.
+// CODE: K and V are 8-bit codes (wide bf16 rows only).  Tiles lie in LDS as bf16 ones do, K as bf16 values, V as fp16 ones; they come
+// through registers: a wave loads a tile's 16 slots two tiles ahead and writes them, decoded, one ahead.
 template <typename T, bool WIDE, int CODE>
 __global__ __launch_bounds__((64 * GeoOf<T, WIDE, CODE>::NW), 2) void k_cache_attend(AttendArgs a) {
     typedef GeoOf<T, WIDE, CODE> G;
     constexpr bool kCode = CODE != CODE_NONE;
+    constexpr bool kSplit = G::kSplit || kCode;                                 // where references may move
+    typedef std::conditional_t<kCode, HalfProbs, Probs<T, G::kSplit>> WideP;    // where they stay
+    constexpr float kLift = kCode ? 10.f : 0.f;    // probabilities of a row's first block are 2^kLift at most
     static_assert(!kCode || (WIDE && G::kBf), "codes: wide bf16 rows");
     __shared__ __attribute__((aligned(1024))) char smem[G::kLds];
     const int tid = threadIdx.x, lane = tid & 63, l31 = lane & 31, hh = lane >> 5;
@@ -508,46 +533,93 @@ __global__ __launch_bounds__((64 * GeoOf<T, WIDE, CODE>::NW), 2) void k_cache_at
             }
         };
         bool odd = false;
-        // Codes: wave w decodes slots 8 w .. + 7 of a tile, K's by the lower lanes and V's by the upper, 16 features each.
+        // Codes: waves 0 .. 3 decode 16 slots of a tile's K each, waves 4 .. 7 of its V, a lane 16 features.
+        // K as bf16 values.  V, while `halves`, in fp16 and 2^-vexp of itself, where a slot's scale is 2^-kDown (e4m3's least code is
+        // 2^-9, fp16's least number 2^-24) to 2^kUp times 2^vexp (2^6 448, and up to twice that with a scale that is no power of two,
+        // lies below 65,504).  Elsewhere (`far` past kUp + kDown) the range is done again over bf16 values.
+        constexpr int kUp = 6, kDown = 15;
         u32x4 codes;
         uint32_t sc = 0;
-        const int cr = (lane & 31) >> 2, cp = 2 * (lane & 3);   // slot of the eight, first of two 16-byte pieces
+        const bool isv = wave >= 4;
+        const int cr = lane >> 2, cp = 2 * (lane & 3);   // slot of the 16, first of two 16-byte pieces
         const char* cbase = nullptr;
         uint32_t cput[2];
+        bool halves = kCode;
+        int vexp = 0;
+        int far = -1;                                    // largest scale of V so far: 2^(far - kDown + vexp)
         if constexpr (kCode) {
-            cbase = (const char*)(hh ? a.c.V : a.c.K) + (lane & 31) * 16;
-            const int row = 8 * wave + cr;
+            cbase = (const char*)(isv ? a.c.V : a.c.K) + (lane & 3) * 16;
+            const int row = 16 * (wave & 3) + cr;
 #pragma unroll
             for (int i = 0; i < 2; ++i)
-                cput[i] = row * 128 + (hh ? G::kTileV + (((cp + i) ^ (2 * (row & 3))) << 4) : ((cp + i) ^ ((row >> 1) & 7)) << 4);
+                cput[i] = row * 128 + (isv ? G::kTileV + (((cp + i) ^ (2 * (row & 3))) << 4) : ((cp + i) ^ ((row >> 1) & 7)) << 4);
         }
         auto fetch_codes = [&](int t) {
-            const int k = unit_slot(t, wave >> 1);
-            const int64_t at = (((int64_t)pw.page(k >> a.c.page_log2, lane) * a.c.Hkv + hk) << a.c.page_log2) + (k & page_mask) +
-                               8 * (wave & 1);
+            const int k = unit_slot(t, wave & 3);
+            const int64_t at = (((int64_t)pw.page(k >> a.c.page_log2, lane) * a.c.Hkv + hk) << a.c.page_log2) + (k & page_mask) + cr;
             codes = *(const u32x4*)(cbase + at * kD);
-            sc = a.c.scale[at + cr];
+            sc = a.c.scale[at];
+        };
+        // 2^vexp: 8 times the first tile's largest finite scale of V, so that later ones may be 2^9 times as large, or 2^-12.
+        auto first_scale = [&]() {
+            int id = 0;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int p = unit_page(0, u);
+                if (lane >> 4 == u) id = p;
+            }
+            const int k = c0 + lane < c1 ? c0 + lane : c1 - 1;
+            // (slots past the end: the last one; a unit past the last one has its page)
+            const int64_t at = (((int64_t)id * a.c.Hkv + hk) << a.c.page_log2) + (k & page_mask);
+            uint32_t b = (a.c.scale[at] >> 16) & 0x7fffu;
+            b = b < 0x7f80u ? b : 0u;
+#pragma unroll
+            for (int o = 32; o >= 1; o >>= 1) b = max(b, (uint32_t)__shfl_xor((int)b, o));
+            vexp = __builtin_amdgcn_readfirstlane((int)(b >> 7)) - 127 + 3;
         };
         auto put_codes = [&](int t) {
             u32x4 v[2];
-            decode16<CODE>(codes, hh ? value_scale(sc) : key_scale(sc), v);
-            const int k0 = c0 + t * G::TK, slot = k0 + 8 * wave;
-            if (!pw.sane || k0 + G::TK > seen_by_all) {
-                // (V: as clean_values() does to tiles that are copied)
-                const int at = slot >> a.c.page_log2;
-                const bool live = slot + cr < c1 && (pw.sane || (at <= pw.last && pw.valid(pw.row[at])));
-                bool any = false;
-                if (hh)
+            const int k0 = c0 + t * G::TK, slot = k0 + 16 * (wave & 3);
+            if (isv) {
+                // Slots past the end or on no page may hold anything: zeros.
+                const bool part = !pw.sane || k0 + G::TK > seen_by_all;
+                if (part) {
+                    const int at = slot >> a.c.page_log2;
+                    const bool live = slot + cr < c1 && (pw.sane || (at <= pw.last && pw.valid(pw.row[at])));
+                    if (!live) codes = u32x4{0u, 0u, 0u, 0u}, sc = 0u;
+                }
+                if (halves) {
+                    const float f = __builtin_amdgcn_ldexpf(value_scale(sc), -vexp);
+                    const int d = (int)(sc >> 23) - (127 + vexp - kDown);   // (a negative scale: past kUp)
+                    if (__builtin_amdgcn_ballot_w64((uint32_t)d > kUp + kDown || (CODE == CODE_E4M3 && (sc & 0x7f0000u)))) {
+                        uint32_t any = (codes[0] | codes[1]) | (codes[2] | codes[3]);
+                        if (CODE == CODE_E4M3) any &= 0x7f7f7f7fu;
+                        const int e = (int)(sc >> 23 & 255u), de = e - (127 + vexp - kDown);
+                        if (any && e != 255) far = max(far, (uint32_t)de <= kUp + kDown ? de : kUp + kDown + 1);
+                        decode16_half<CODE, false>(codes, f, v);
+                    } else {
+                        far = max(far, d);
+                        decode16_half<CODE, true>(codes, f, v);
+                    }
+                } else {
+                    decode16<CODE>(codes, value_scale(sc), v);
+                }
+                if (part) {   // (as clean_values() does to tiles that are copied)
+                    const uint32_t inf = halves ? 0x7c00u : 0x7f80u;
+                    bool any = false;
 #pragma unroll
                     for (int i = 0; i < 2; ++i)
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
                             uint32_t x = v[i][j];
-                            const bool lo = (x & 0x7f80u) == 0x7f80u, hi = (x & 0x7f800000u) == 0x7f800000u;
-                            any = any || (live && (lo || hi));
-                            v[i][j] = !live ? 0u : x & (lo ? 0xffff0000u : 0xffffffffu) & (hi ? 0xffffu : 0xffffffffu);
+                            const bool lo = (x & inf) == inf, hi = (x & inf << 16) == inf << 16;
+                            any = any || lo || hi;
+                            v[i][j] = x & (lo ? 0xffff0000u : 0xffffffffu) & (hi ? 0xffffu : 0xffffffffu);
                         }
-                odd |= __builtin_amdgcn_ballot_w64(any) != 0;
+                    odd |= __builtin_amdgcn_ballot_w64(any) != 0;
+                }
+            } else {
+                decode16<CODE>(codes, key_scale(sc), v);
             }
             typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
             lds_char* tile = ring + (t % G::NST) * G::kTile;
@@ -557,6 +629,7 @@ __global__ __launch_bounds__((64 * GeoOf<T, WIDE, CODE>::NW), 2) void k_cache_at
         auto issue_first = [&]() {
             if constexpr (kCode) {
                 fetch_codes(0);
+                if (halves) first_scale();
                 put_codes(0);
                 if (nt > 1) fetch_codes(1);
             } else {
@@ -633,10 +706,10 @@ __global__ __launch_bounds__((64 * GeoOf<T, WIDE, CODE>::NW), 2) void k_cache_at
                     for (int j = 0; j < G::TK / 32; ++j)
 #pragma unroll
                         for (int nb = 0; nb < G::NB; ++nb) {
-                            Probs<T, G::kSplit> p;
-                            block_probs<T, G::kSplit>(w[nb], tile + j * G::kBlock, a.c2, k0 + 32 * j, partial, units >> (2 * j),
+                            Probs<T, kSplit> p;
+                            block_probs<T, kSplit>(w[nb], tile + j * G::kBlock, a.c2, k0 + 32 * j, partial, units >> (2 * j),
                                            lane, logits, p);
-                            block_values<T, G::kSplit>(w[nb], tile + G::kTileV + j * G::kBlock, p, rest, lane);
+                            block_values<T, kSplit>(w[nb], tile + G::kTileV + j * G::kBlock, p, rest, lane);
                         }
             }
         };
@@ -671,7 +744,7 @@ __global__ __launch_bounds__((64 * GeoOf<T, WIDE, CODE>::NW), 2) void k_cache_at
             // first block had none, or values are huge), the workgroup does its range again carefully.
             const int tfull = pw.sane ? (seen_by_all - c0) / G::TK : 0;   // tiles all rows see
             f32x16 s0[G::NB], s1[G::NB];
-            Probs<T, G::kSplit> p0[G::NB], p1[G::NB];
+            WideP p0[G::NB], p1[G::NB];
             float ref[G::NB], sum[G::NB][4] = {};
             // Half a tile: eight operands from LDS, each for the MFMAs of the row groups and followed by the
             // vector instructions of two of a group's 16 logits; they are read three ahead.  The first three are values, of a tile
@@ -690,9 +763,36 @@ __global__ __launch_bounds__((64 * GeoOf<T, WIDE, CODE>::NW), 2) void k_cache_at
                 return *(lds_frag*)(k + (a0 ^ (i << 5)));
             };
             typedef f32x16 Logits[G::NB];
-            typedef Probs<T, G::kSplit> BlockP[G::NB];
+            typedef WideP BlockP[G::NB];
+            typedef std::conditional_t<kCode, f16, bf16> P16;
+            // Codes: a block's sums into l, and where one comes near fp16's largest value, references raised so that it is 2^kLift.
+            // (s: the block's powers still.)
+            auto settle = [&](auto width, Logits& s, BlockP& p) __attribute__((always_inline)) {
+                constexpr int NB = decltype(width)::value;
+                float tot[NB], top = 0.f;
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                    tot[nb] = (sum[nb][0] + sum[nb][1]) + (sum[nb][2] + sum[nb][3]);
+                    w[nb].l += tot[nb];
+                    top = maximum(top, tot[nb]);
+                }
+                if (!__builtin_amdgcn_ballot_w64(!(top < 65504.f))) return;
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                    const float both = maximum(tot[nb], __shfl_xor(tot[nb], 32));
+                    int k = (int)(__float_as_uint(both) >> 23) - 127 - (int)kLift;
+                    k = k > 0 && k < 120 ? k : 0;   // (further, or no number: seen by l in the end)
+                    const float f = __uint_as_float((uint32_t)(127 - k) << 23);
+                    w[nb].l *= f;
+                    w[nb].m += (float)k;
+                    ref[nb] += (float)k;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) w[nb].o[0][r] *= f, w[nb].o[1][r] *= f, s[nb][r] *= f;
+                    p[nb].set(s[nb]);
+                }
+            };
             auto half = [&](auto mask, auto width, Logits& s, int k0, Logits& sn, lds_char* k, lds_char* v, lds_char* v_next,
-                            const BlockP& pv, BlockP& pn) {
+                            const BlockP& pv, BlockP& pn) __attribute__((always_inline)) {
                 constexpr int NB = decltype(width)::value;
                 if constexpr (decltype(mask)::value)
 #pragma unroll
@@ -708,10 +808,15 @@ __global__ __launch_bounds__((64 * GeoOf<T, WIDE, CODE>::NW), 2) void k_cache_at
                 };
                 auto add = [&](int u) {
                     const int nb = u % NB, i = u / NB;
-                    sum[nb][(2 * i) & 3] += s[nb][2 * i];
-                    sum[nb][(2 * i + 1) & 3] += s[nb][2 * i + 1];
-                    pn[nb].v[i >> 2][(2 * i) & 7] = (bf16)s[nb][2 * i];
-                    pn[nb].v[i >> 2][(2 * i + 1) & 7] = (bf16)s[nb][2 * i + 1];
+                    if (kCode && i < 2) {
+                        sum[nb][2 * i] = s[nb][2 * i];
+                        sum[nb][2 * i + 1] = s[nb][2 * i + 1];
+                    } else {
+                        sum[nb][(2 * i) & 3] += s[nb][2 * i];
+                        sum[nb][(2 * i + 1) & 3] += s[nb][2 * i + 1];
+                    }
+                    pn[nb].v[i >> 2][(2 * i) & 7] = (P16)s[nb][2 * i];
+                    pn[nb].v[i >> 2][(2 * i + 1) & 7] = (P16)s[nb][2 * i + 1];
                 };
                 exponent(0);
 #pragma unroll
@@ -723,7 +828,7 @@ __global__ __launch_bounds__((64 * GeoOf<T, WIDE, CODE>::NW), 2) void k_cache_at
                     }
                     Rows<T>& x = w[nb];
                     if (n < 4) sn[nb] = mfma_bf16(f[i], x.qb[n], n ? sn[nb] : zero_f32x16());
-                    else x.o[n & 1] = mfma_bf16(f[i], pv[nb].v[(n - 4) >> 1], x.o[n & 1]);
+                    else x.o[n & 1] = mfma_value(f[i], pv[nb].v[(n - 4) >> 1], x.o[n & 1]);
                     if (u + 1 < 8 * NB) exponent(u + 1);
                     s[nb][2 * i] = exp2f_fast(s[nb][2 * i]);
                     s[nb][2 * i + 1] = exp2f_fast(s[nb][2 * i + 1]);
@@ -731,11 +836,15 @@ __global__ __launch_bounds__((64 * GeoOf<T, WIDE, CODE>::NW), 2) void k_cache_at
                     __builtin_amdgcn_sched_barrier(0);
                 }
                 add(8 * NB - 1);
+                if constexpr (kCode) settle(width, s, pn);
             };
-            auto probs = [&](Logits& s, int k0, BlockP& p) {
+            auto probs = [&](Logits& s, int k0, BlockP& p) __attribute__((always_inline)) {
 #pragma unroll
                 for (int nb = 0; nb < G::NB; ++nb) {
                     block_mask<T>(w[nb], k0, ~0u, lane, s[nb]);
+                    if (kCode)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) sum[nb][j] = 0.f;
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
                         s[nb][r] = exp2f_fast(fmaf(s[nb][r], a.c2, -ref[nb]));
@@ -743,8 +852,9 @@ __global__ __launch_bounds__((64 * GeoOf<T, WIDE, CODE>::NW), 2) void k_cache_at
                     }
                     p[nb].set(s[nb]);
                 }
+                if constexpr (kCode) settle(std::integral_constant<int, G::NB>(), s, p);
             };
-            auto body = [&](auto mask, auto width, int t) {   // second block of tile t, first of tile t + 1
+            auto body = [&](auto mask, auto width, int t) __attribute__((always_inline)) {   // second block of tile t, first of tile t + 1
                 lds_char *cur = tile_at(t), *next = tile_at(t + 1);
                 const int k0 = c0 + t * G::TK;
                 half(mask, width, s1, k0 + 32, s0, next, cur + G::kTileV, cur + G::kTileV + G::kBlock, p0, p1);
@@ -762,7 +872,7 @@ __global__ __launch_bounds__((64 * GeoOf<T, WIDE, CODE>::NW), 2) void k_cache_at
                     for (int r = 0; r < 16; r += 2) top = maximum(maximum(top, s[r]), s[r + 1]);
                     const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false,
                                                                     false);
-                    w[nb].m = maximum(__uint_as_float(x[0]), __uint_as_float(x[1])) * a.c2;
+                    w[nb].m = maximum(__uint_as_float(x[0]), __uint_as_float(x[1])) * a.c2 - kLift;
                     ref[nb] = w[nb].m == -INFINITY ? 0.f : w[nb].m;
                     s1[nb] = block_logits<T>(w[nb], tile_at(0) + G::kBlock, lane);
                 }
@@ -784,16 +894,55 @@ __global__ __launch_bounds__((64 * GeoOf<T, WIDE, CODE>::NW), 2) void k_cache_at
                     arrive(t + 1);
                     body(std::true_type(), All(), t);
                 }
-                probs(s1, c0 + t * G::TK + 32, p1);
+                if constexpr (kCode) {   // (block by block: a reference that rises takes the results so far along)
 #pragma unroll
-                for (int nb = 0; nb < G::NB; ++nb) {
-                    if (kCode && nb && slim) break;
-                    block_values<T, G::kSplit>(w[nb], tile_at(t) + G::kTileV, p0[nb], false, lane);
-                    block_values<T, G::kSplit>(w[nb], tile_at(t) + G::kTileV + G::kBlock, p1[nb], false, lane);
-                    w[nb].l = (sum[nb][0] + sum[nb][1]) + (sum[nb][2] + sum[nb][3]);
+                    for (int nb = 0; nb < G::NB; ++nb)
+                        if (!(nb && slim)) block_values(w[nb], tile_at(t) + G::kTileV, p0[nb], lane);
+                    probs(s1, c0 + t * G::TK + 32, p1);
+#pragma unroll
+                    for (int nb = 0; nb < G::NB; ++nb)
+                        if (!(nb && slim)) block_values(w[nb], tile_at(t) + G::kTileV + G::kBlock, p1[nb], lane);
+                } else {
+                    probs(s1, c0 + t * G::TK + 32, p1);
+#pragma unroll
+                    for (int nb = 0; nb < G::NB; ++nb) {
+                        block_values<T, G::kSplit>(w[nb], tile_at(t) + G::kTileV, p0[nb], false, lane);
+                        block_values<T, G::kSplit>(w[nb], tile_at(t) + G::kTileV + G::kBlock, p1[nb], false, lane);
+                        w[nb].l = (sum[nb][0] + sum[nb][1]) + (sum[nb][2] + sum[nb][3]);
+                    }
                 }
             } else {
                 for (int t = 1; t < nt; ++t) arrive(t);
+            }
+            if constexpr (kCode) {
+                // What is off by fp16's range.  A scale out of its bounds.  Sums past fp32's range, rows whose first
+                // logits were -inf alone.  Probabilities below 2^-14 are off by 2^-25 at most: n slots together by no more than 2^-8
+                // of a row's largest result (each apart, of as much / sqrt(n)), if that is 2^-17 n times the largest value.  A first slot
+                // without values of its own may so have 98 % of the weight of 9,000 slots.
+                __shared__ int s_far[G::NW];
+#pragma unroll
+                for (int o = 32; o >= 1; o >>= 1) far = max(far, __shfl_xor(far, o));
+                if (lane == 0) s_far[wave] = far;
+                __syncthreads();
+                for (int v = 4; v < G::NW; ++v) far = max(far, s_far[v]);
+                redo = far > kUp + kDown;
+                const float most = far < 0 ? 0.f : __builtin_amdgcn_ldexpf(CODE == CODE_E4M3 ? 448.f : 128.f, far - kDown);
+                if (alive)
+#pragma unroll
+                    for (int nb = 0; nb < G::NB; ++nb) {
+                        const int n = (w[nb].vis < c1 ? w[nb].vis : c1) - c0;
+                        float top = 0.f;
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) top = maximum(maximum(top, fabsf(w[nb].o[0][r])), fabsf(w[nb].o[1][r]));
+                        top = maximum(top, __shfl_xor(top, 32));
+                        redo = redo || __builtin_amdgcn_ballot_w64(n > 0 && !(top >= (float)n * most * 0x1p-17f));
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) {
+                            w[nb].o[0][r] = __builtin_amdgcn_ldexpf(w[nb].o[0][r], vexp);
+                            w[nb].o[1][r] = __builtin_amdgcn_ldexpf(w[nb].o[1][r], vexp);
+                        }
+                    }
+                halves = false;
             }
         } else if constexpr (WIDE) {
             // fp32: six bf16 MFMAs for every eight fp32 ones, of which each takes 16 times its share.  K and
@@ -1010,7 +1159,7 @@ __global__ __launch_bounds__((64 * GeoOf<T, WIDE, CODE>::NW), 2) void k_cache_at
                 for (int pass = 0; pass < 2; ++pass) {
                     restart(pass > 0);
                     issue_first();
-                    careful(false);
+                    careful(kCode && pass == 0);
                     const bool far = overflown();
                     __syncthreads();
                     if (lane == 0) s_redo[wave] = far;

@@ -109,6 +109,25 @@ __device__ __forceinline__ void decode16(const u32x4& x, float s, u32x4 (&v)[2])
     }
 }
 
+// The same in fp16, exact for code times scale within its range.  POWER: the scale is a power of two.
+template <int CODE, bool POWER>
+__device__ __forceinline__ void decode16_half(const u32x4& x, float s, u32x4 (&v)[2]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        f16x2 a, b;
+        if constexpr (CODE == CODE_E4M3 && POWER) {
+            a = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)x[j], s, false));
+            b = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)x[j], s, true));
+        } else {
+            float f[4];
+            values4<CODE>(x[j], s, f);
+            a = f16x2{(f16)f[0], (f16)f[1]}, b = f16x2{(f16)f[2], (f16)f[3]};
+        }
+        v[j >> 1][2 * (j & 1)] = __builtin_bit_cast(uint32_t, a);
+        v[j >> 1][2 * (j & 1) + 1] = __builtin_bit_cast(uint32_t, b);
+    }
+}
+
 // A slot's two scales.
 __device__ __forceinline__ float key_scale(uint32_t s) { return __uint_as_float(s << 16); }
 __device__ __forceinline__ float value_scale(uint32_t s) { return __uint_as_float(s & 0xffff0000u); }

@@ -736,3 +736,93 @@ def test_refusals(cache):  # noqa: F811
         cache.append(pc, batch, rows.to(BF), rows.to(BF), rows.to(BF), k_norm=cache.HeadNorm("rms", torch.ones(3, 64, device="cuda")))
     with pytest.raises(TypeError):
         cache.StreamLayer(1, 10, 10, 2, dtype=torch.float16)
+
+
+# ------------------------------------------------------------------ precision of many rows
+
+def check_rms(cache, pool, Q, n, q, causal, below=0.0):  # noqa: F811
+    """Mean squares over the call: of the errors no more than what two roundings leave, in units of a row's largest output
+    (so that rows of small outputs count as others do).  The output's own, to bf16, is taken from the reference itself.
+    Probabilities of more than 2^-14 of the largest in fp16 or finer: off by 2^-11 of themselves, each apart, so by a third of that squared
+    on the average, and an output by sum p^2 v^2 times it (single bf16 values: 2^-8 for 2^-11); logits, each
+    apart, by 64 u X, sums by (n / 16 + 16 + |lse|) u of the output.  `below`: what smaller probabilities may take, together, of a row's
+    largest output.  1 % for the sample, some 300,000 values, whose root of the mean square varies by 0.2 %."""
+    Hq, Hkv = Q.shape[1], pool.k[0].shape[1]
+    pc, batch = pool.cuda(), pool.batch([q])
+    assert cache.attend_plan(pc, batch, Hq, q).shared == 1
+    O, lse = cache.attend(pc, batch, Q.cuda(), causal)
+    see = n - q + torch.arange(q, device="cuda") + 1 if causal else torch.full((q,), n, device="cuda")
+    sees = torch.arange(n, device="cuda") < see[:, None]
+    err = own = rest = 0.0
+    for h in range(Hq):
+        k, v = (t[0][:, h * Hkv // Hq].cuda() for t in (pool.k, pool.v))
+        ro, rl, p, A, X = whole64(Q[:, h].cuda(), k, v, sees, 0.125)
+        E = (64 * X + n / 16 + 16 + rl.abs()) * U
+        assert ((lse[:, h].double() - rl).abs() <= 2 * E).all(), h
+        unit = ro.abs().amax(dim=1, keepdim=True)
+        top = v.abs().max()                                   # (squares stay in range)
+        term = torch.sqrt((p * p) @ (v / top) ** 2) * top * (2.0 ** -11 / 3 ** 0.5 + 64 * X[:, None] * U)
+        term += 2 * ro.abs() * (n / 16 + 16 + rl.abs())[:, None] * U + below * unit
+        mean = lambda e: ((e / unit) ** 2).mean().item() / Hq
+        err, own, rest = err + mean(O[:, h].double() - ro), own + mean(ro.to(BF).double() - ro), rest + mean(term)
+    got, most = math.sqrt(err), math.sqrt(own) + math.sqrt(rest)
+    log("errors %.2e of a row's largest output, at most %.2e + %.2e" % (got, math.sqrt(own), math.sqrt(rest)))
+    assert got <= 1.01 * most
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("q,causal", [(700, False), (520, True)])
+def test_attend_wide_precision(cache, kind, q, causal):  # noqa: F811
+    """Outputs of many rows are as exact as those of few: their own rounding, and little more."""
+    log("attend8 wide precision %s q=%d" % (kind, q))
+    n = 6000
+    pool = Pool8(cache, [n], 4, 32, kind, seed=61, junk="bits")
+    check_rms(cache, pool, normal(62, (q, 8, 64), BF), n, q, causal)
+
+
+RISE = [
+    # logit of the first slot, of slot 3,001, values of the first slot, of the first 64, exponents of the others
+    (16.0, 0.0, 0.0, 1.0, 0), (40.0, 0.0, 0.0, 1.0, 0), (0.0, 13.0, 1.0, 1.0, 0), (0.0, 30.0, 1.0, 1.0, 0), (20.0, 45.0, 0.0, 1.0, 0),
+    (0.0, 0.0, 0.0, 0.0, 0), (0.0, 0.0, 1.0, 1.0, 30), (16.0, 0.0, 0.0, 2.0 ** -40, 8), (9.0, 12.0, 0.0, 2.0 ** 20, 0),
+    (0.0, 0.0, 1.0, 2.0 ** -9, 0), (0.0, 0.0, 1.0, 2.0 ** -11, 0), (0.0, 0.0, 1.0, 2.0 ** 12, 1),
+]
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("q", [700, 520])
+@pytest.mark.parametrize("first,later,v0,v64,spread", RISE)
+def test_attend_wide_precision_of_uneven_slots(cache, kind, q, first, later, v0, v64, spread):  # noqa: F811
+    """The same where one slot has most of the weight, early or late, with values or without, and where values
+    differ by many powers of two from slot to slot."""
+    log("attend8 wide precision %s q=%d %s" % (kind, q, (first, later, v0, v64, spread)))
+    n = 6000
+    pool = Pool8(cache, [n], 4, 32, kind, seed=63)
+    k, v = normal(64, (n, 4, 64), F32), normal(65, (n, 4, 64), F32)
+    Q = normal(66, (q, 8, 64), BF)
+    Q[..., 0] = 8.0
+    k[..., 0] = 0.0
+    for at, x in ((0, first), (3000, later)):
+        if x:
+            k[at], k[at, :, 0] = 0.0, x          # (a logit of x with every query)
+    v *= torch.exp2(torch.randint(-spread, spread + 1, (n, 1, 1), generator=gen(67)).float())
+    v[:64] *= v64
+    v[0] *= v0
+    pool.put(0, k, v)
+    check_rms(cache, pool, Q, n, q, False, 2.0 ** -10)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("up", [-40, 8, 9, 10, 11, 12, 13, 40])
+def test_attend_wide_precision_of_the_last_slots(cache, kind, up):  # noqa: F811
+    """The same where the slots of the last tile, which is not full, have larger values than all others, or smaller ones and
+    nearly all of the weight."""
+    log("attend8 wide precision %s, last slots 2^%d" % (kind, up))
+    n, q = 6000, 700
+    pool = Pool8(cache, [n], 4, 32, kind, seed=68)
+    k, v = normal(69, (n, 4, 64), F32), normal(70, (n, 4, 64), F32)
+    v[n - 40:] *= 2.0 ** up
+    Q = normal(71, (q, 8, 64), BF)
+    if up < 0:
+        Q[..., 0], k[..., 0], k[n - 40:, :, 0] = 8.0, 0.0, 50.0
+    pool.put(0, k, v)
+    check_rms(cache, pool, Q, n, q, False, 2.0 ** -10)
