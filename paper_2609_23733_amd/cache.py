@@ -16,7 +16,7 @@ from typing import Optional, Sequence
 import torch
 
 from . import vp
-from .vp import HEAD_DIM, VPError, _check, _dt, _need, _ptr, load_library
+from .vp import HEAD_DIM, VPError, _check, _dt, _need, _ptr, _wrote, load_library
 
 ROT_INTERLEAVED, ROT_HALF = 0, 1
 ROT_SCALE_NONE, ROT_SCALE_LINEAR, ROT_SCALE_PARTS = 0, 1, 2
@@ -128,24 +128,27 @@ def rotary(x, pos, rot: Rotary, out: Optional[torch.Tensor] = None, transpose: b
         return _Rotation.apply(x, pos, rot, transpose)
     T, H = x.shape[0], x.shape[1]
     xs = _rows(x, "x", T, H, x.dtype)
-    if out is None:
+    given = out is not None
+    if not given:
         out = torch.empty(T, H, HEAD_DIM, dtype=x.dtype, device=x.device)
     ys = _rows(out, "out", T, H, x.dtype)
     _done(load_library().vp_rotary(rot.at(pos, T), _dt(x), T, H, x.data_ptr(), xs, out.data_ptr(), ys,
                                    transpose, _stream()), "vp_rotary")
+    if given:
+        _wrote(out)
     return out
 
 
 class _Rotation(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, pos, rot, transpose):
-        ctx.save_for_backward(pos)
+        ctx.save_for_backward(pos, rot.freq)
         ctx.rot, ctx.transpose = rot, bool(transpose)
         return rotary(x, pos, rot, None, transpose)
 
     @staticmethod
     def backward(ctx, g):
-        pos, = ctx.saved_tensors
+        pos, _ = ctx.saved_tensors
         if not g.is_contiguous() or g.data_ptr() % 16:     # (broadcast, or a part of something)
             g = g.clone(memory_format=torch.contiguous_format)
         return rotary(g, pos, ctx.rot, None, not ctx.transpose), None, None, None
@@ -216,19 +219,22 @@ def norm_rotary(x, norm: HeadNorm, pos=None, rot: Optional[Rotary] = None, out: 
         return _NormRotation.apply(x, norm.gain, norm.bias, pos, norm, rot)
     T, H = x.shape[0], x.shape[1]
     xs = _rows(x, "x", T, H, x.dtype)
-    if out is None:
+    given = out is not None
+    if not given:
         out = torch.empty(T, H, HEAD_DIM, dtype=x.dtype, device=x.device)
     ys = _rows(out, "out", T, H, x.dtype)
     _done(load_library().vp_norm_rotary(norm.at(H), None if rot is None else rot.at(pos, T), _dt(x), T, H, x.data_ptr(), xs,
                                         out.data_ptr(), ys, _here(x, out, norm.tensor, pos, rot and rot.freq)),
           "vp_norm_rotary")
+    if given:
+        _wrote(out)
     return out
 
 
 class _NormRotation(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, gain, bias, pos, norm, rot):
-        ctx.save_for_backward(x, gain, bias, pos)
+        ctx.save_for_backward(x, gain, bias, pos, None if rot is None else rot.freq)
         ctx.norm, ctx.rot = norm, rot
         return norm_rotary(x, norm, pos, rot)
 
@@ -239,7 +245,7 @@ class _NormRotation(torch.autograd.Function):
 
 
 def _norm_gradients(ctx, g):
-    x, gain, bias, pos = ctx.saved_tensors             # (refuses values that were changed in place)
+    x, gain, bias, pos, _ = ctx.saved_tensors          # (refuses values that were changed in place)
     norm, rot = ctx.norm, ctx.rot
     if norm._at != _memory(gain, bias):                # (it got others, or the graph kept copies)
         norm = HeadNorm(norm.kind, gain, bias, norm.eps)
@@ -315,6 +321,7 @@ class PagedCache:
         self._c8 = vp.vp_cache8(self._c, ptr(scale), vp.VP_BF16 if self.dtype is torch.bfloat16 else vp.VP_F32)
         self._ref8 = ctypes.byref(self._c8)
         self._ref = self._ref8 if self.codes else ctypes.byref(self._c)
+        self._pool = [t for t in (K, V, weight, stamp, scale) if t is not None]
 
     def _call(self, name: str):
         """The library's call for this cache."""
@@ -365,6 +372,7 @@ def append(pc: PagedCache, batch: Batch, Q, K, V, pos=None, rot: Optional[Rotary
     T, Hkv, dt = K.shape[0], pc.Hkv, pc.dtype
     ks, vs = _rows(K, "K", T, Hkv, dt), _rows(V, "V", T, Hkv, dt)
     Hq = qs = q = qo = 0
+    given = Q is not None and Q_out is not None
     if Q is not None:
         Hq = Q.shape[1]
         qs, q = _rows(Q, "Q", T, Hq, dt), Q.data_ptr()
@@ -384,6 +392,7 @@ def append(pc: PagedCache, batch: Batch, Q, K, V, pos=None, rot: Optional[Rotary
     else:
         _done(load_library().vp_cache_append(pc._ref, batch._for(T), Hq, q, qs, K.data_ptr(), ks, V.data_ptr(), vs,
                                              turn, qo, _stream()), "vp_cache_append")
+    _wrote(*pc._pool, Q_out if given else None)
     return Q_out if Q is not None else None
 
 
@@ -397,12 +406,14 @@ def read(pc: PagedCache, batch: Batch, T: int, dtype: Optional[torch.dtype] = No
         raise ValueError("rows are read in bf16 or fp32")
     # (zeros: rows past the last sequence's are left as they are)
     new = lambda: torch.zeros(T, pc.Hkv, HEAD_DIM, dtype=dtype, device=pc.K.device)
+    given = K_out, V_out
     K_out, V_out = new() if K_out is None else K_out, new() if V_out is None else V_out
     shape = (T, pc.Hkv, HEAD_DIM)
     st = _here(pc.K, K_out, V_out, batch.table)
     _done(load_library().vp_cache8_read(pc._ref8, batch._for(T), vp.VP_BF16 if dtype is torch.bfloat16 else vp.VP_F32,
                                         _whole(K_out, "K_out", shape, dtype), _whole(V_out, "V_out", shape, dtype),
                                         st), "vp_cache8_read")
+    _wrote(*given)
     return K_out, V_out
 
 
@@ -429,6 +440,7 @@ def attend(pc: PagedCache, batch: Batch, Q, causal: bool = True, scale: float = 
     T, Hq, _ = Q.shape
     dt = pc.dtype
     qs = _rows(Q, "Q", T, Hq, dt)
+    given = O, lse, weight_out
     if O is None:
         O = torch.empty(T, Hq, HEAD_DIM, dtype=dt, device=Q.device)
     if lse is None:
@@ -445,6 +457,7 @@ def attend(pc: PagedCache, batch: Batch, Q, causal: bool = True, scale: float = 
     w, n = _work(ws)
     _done(pc._call("attend")(pc._ref, batch._for(T), Hq, Q.data_ptr(), qs, causal, scale, o, ls, wo, w, n, _stream()),
           "vp_cache_attend")
+    _wrote(*given)
     return O, lse
 
 
@@ -482,6 +495,7 @@ def evict(pc: PagedCache, table, length, seen, keep: int, max_len: int, sink: in
                           int(max_len))
     _done(pc._call("evict")(pc._ref, ctypes.byref(c), int(keep), int(sink), int(recent), wo, so, lo, w, n, _stream()),
           "vp_cache_evict")
+    _wrote(weight_out, stamp_out, length_out, pc.K, pc.V, pc.scale)
     return length_out
 
 

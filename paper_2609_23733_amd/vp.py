@@ -237,6 +237,12 @@ def _dt(t: torch.Tensor) -> int:
     raise TypeError("unsupported dtype %s" % t.dtype)
 
 
+def _wrote(*tensors):
+    """After a call that wrote the caller's tensors through their addresses: autograd's versions of them go up, as
+    after torch's own in-place operations, so that a backward pass that had saved one refuses."""
+    torch._C._increment_version([t for t in tensors if t is not None])
+
+
 def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
 
@@ -318,6 +324,7 @@ def router_score(Q, K, V, W, U, w, S: int, P: int, ws: torch.Tensor, scale: floa
                                           ctypes.byref(rw), ctypes.byref(st), _ptr(ws),
                                           ws.numel() * ws.element_size(), _stream()),
            "vp_router_score")
+    _wrote(*vars(out).values())
     return out
 
 
@@ -343,6 +350,7 @@ def router_score_noalloc(Q, K, V, W, U, w, S: int, P: int, scale: float = 0.0,
                                                   ctypes.byref(rw), ctypes.byref(st),
                                                   _stream()),
            "vp_router_score_noalloc")
+    _wrote(*vars(out).values())
     return out
 
 
@@ -358,6 +366,7 @@ def router_logits(u, Wr, br, out: Optional[torch.Tensor] = None) -> torch.Tensor
     _need(out, "logits", (H, 3), torch.float32)
     _check(load_library().vp_router_logits(_ptr(u), _ptr(Wr), _ptr(br), H, Din, 3, _dt(Wr),
                                            _ptr(out), _stream()), "vp_router_logits")
+    _wrote(out)
     return out
 
 
@@ -376,6 +385,7 @@ def assign_heads(scores, rule: int, tau_low: float = TAU_LOW, tau_high: float = 
     _check(load_library().vp_assign_heads(_ptr(scores), H, M, int(rule), float(tau_low),
                                           float(tau_high), _ptr(modes), _ptr(buckets),
                                           _stream()), "vp_assign_heads")
+    _wrote(modes, buckets)
     return modes, buckets
 
 
@@ -425,6 +435,7 @@ def routed_global_attention(Q, K, V, modes, buckets, state: RouterState,
         ctypes.byref(shp), _ptr(Q), _ptr(K), _ptr(V), _ptr(modes), _ptr(buckets),
         ctypes.byref(st), ctypes.byref(sw), _ptr(Y), _dt(Y), _ptr(ws),
         ws.numel() * ws.element_size(), _stream()), "vp_routed_global_attention")
+    _wrote(Y)
     return Y
 
 
@@ -450,6 +461,7 @@ def full_head_attention(Q, K, V, buckets, S: int, P: int, ws: torch.Tensor, Y: t
                                                  _ptr(buckets), _ptr(Y), _dt(Y), _ptr(ws),
                                                  ws.numel() * ws.element_size(), _stream()),
            "vp_full_head_attention")
+    _wrote(Y)
 
 
 def linear_heads(V, modes, state: RouterState, surr, S: int, P: int, Y: torch.Tensor,
@@ -472,6 +484,7 @@ def linear_heads(V, modes, state: RouterState, surr, S: int, P: int, Y: torch.Te
                                           _ptr(modes), ctypes.byref(st), ctypes.byref(sw),
                                           _ptr(Y), _dt(Y), _ptr(ws), nws, _stream()),
            "vp_linear_heads")
+    _wrote(Y)
 
 
 class RoutedLayer:
@@ -604,6 +617,7 @@ def block_qkv(X, pos, w, S: int, P: int, ws: torch.Tensor, Q=None, K=None, V=Non
                                        _ptr(out[0]), _ptr(out[1]), _ptr(out[2]), _ptr(ws),
                                        ws.numel() * ws.element_size(), _stream()),
            "vp_block_qkv")
+    _wrote(*out)
     return tuple(out)
 
 
@@ -623,6 +637,7 @@ def block_out(X, Y, w, S: int, P: int, ws: torch.Tensor, X_out=None):
     _check(load_library().vp_block_out(ctypes.byref(shp), _ptr(X), _ptr(Y), ctypes.byref(bw),
                                        _ptr(X_out), _ptr(ws), ws.numel() * ws.element_size(),
                                        _stream()), "vp_block_out")
+    _wrote(X_out)
     return X_out
 
 
@@ -787,6 +802,7 @@ def tome_plan(K, plan: TomePlan) -> TomePlan:
                                        int(plan.nspecial), _ptr(plan.row), _ptr(plan.row_start),
                                        _ptr(plan.members), _ptr(plan.best), _ptr(plan.score),
                                        _ptr(plan.ws), plan.ws.numel(), _stream()), "vp_tome_plan")
+    _wrote(plan.row, plan.row_start, plan.members, plan.best, plan.score)
     return plan
 
 
@@ -801,6 +817,7 @@ def tome_merge(X, plan: TomePlan, out=None):
     _check(load_library().vp_tome_merge(ctypes.byref(shp), _ptr(X), plan.nrows,
                                         _ptr(plan.row_start), _ptr(plan.members), _ptr(out),
                                         _stream()), "vp_tome_merge")
+    _wrote(out)
     return out
 
 
@@ -816,6 +833,7 @@ def tome_merge_qkv(Q, K, V, plan: TomePlan, Qm, Km, Vm):
                                             plan.nrows, _ptr(plan.row_start),
                                             _ptr(plan.members), _ptr(Qm), _ptr(Km), _ptr(Vm),
                                             _stream()), "vp_tome_merge_qkv")
+    _wrote(Qm, Km, Vm)
     return Qm, Km, Vm
 
 
@@ -830,6 +848,7 @@ def tome_unmerge(Ym, plan: TomePlan, out=None):
     _check(load_library().vp_tome_unmerge(ctypes.byref(shp), _ptr(Ym), plan.nrows,
                                           _ptr(plan.row), _ptr(out), _stream()),
            "vp_tome_unmerge")
+    _wrote(out)
     return out
 
 

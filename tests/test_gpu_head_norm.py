@@ -15,7 +15,7 @@ import numpy as np
 import pytest
 import torch
 
-from paper_2609_23733_amd import vp
+from paper_2609_23733_amd import synth, vp
 from test_gpu_cache import BF, BFU, F32, U, _gpu, cache, gen, log, normal, radians, rotate64  # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -361,3 +361,67 @@ def test_graph_of_a_training_step(cache):  # noqa: F811
         torch.cuda.synchronize()
         for a, b in zip(got, step()):
             assert torch.equal(a, b), k
+
+
+def test_saved_inputs_that_the_operators_overwrite(cache):  # noqa: F811
+    """The library writes through addresses; a backward pass that saved what was overwritten refuses, as after torch's
+    own in-place operations."""
+    bf = lambda s, *shape: normal(s, shape, BF).cuda()
+    pos = torch.arange(6, dtype=torch.int32, device="cuda")[:, None]
+    i32 = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    rot, other = cache.Rotary.make(64), cache.HeadNorm("rms")
+    mk = lambda dt: cache.PagedCache.empty(2, 16, 16, dtype=dt)
+    k = bf(2, 6, 16, 64)
+    w = synth.make_block_weights((1, 0))
+    w = {n: t.cuda() for n, t in w.items()}
+    ws = torch.empty(vp.block_workspace_bytes(1, 6), dtype=torch.uint8, device="cuda")
+    X, pos2 = bf(3, 6, 1024), torch.zeros(6, 2, dtype=torch.int32, device="cuda")
+    batch = cache.Batch(i32(0, 1)[None], i32(6), i32(0, 6), 6, 6, i32(6))
+
+    def both(call):
+        return [lambda x, pc=mk(dt): call(pc, x) for dt in (BF, torch.int8)]
+
+    writers = [lambda x: cache.norm_rotary(x, other, out=x), lambda x: cache.rotary(x, pos, rot, out=x)]
+    writers += both(lambda pc, x: cache.append(pc, batch, x, k, k, Q_out=x))
+    writers += both(lambda pc, x: cache.attend(pc, batch, x, O=x))
+    writers += both(lambda pc, x: cache.read(pc, batch, 6, K_out=x))
+    writers += both(lambda pc, x: cache.read(pc, batch, 6, V_out=x))
+    writers += [lambda x, i=i: vp.block_qkv(X, pos2, w, 1, 6, ws, *[x if j == i else None for j in range(3)]) for i in range(3)]
+    writers += [lambda x: vp.block_out(X, k, w, 1, 6, ws, X_out=x.view(6, 1024))]
+    for n, write in enumerate(writers):
+        gain = torch.ones(64, device="cuda").requires_grad_()
+        x = bf(1, 6, 16, 64)
+        y = cache.norm_rotary(x, cache.HeadNorm("rms", gain), pos, rot)
+        with torch.no_grad():
+            write(x)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.sum().backward()
+        log("writer %d" % n)
+    # positions and frequencies, which the gradient needs as the forward pass had them
+    for call in (lambda x: cache.norm_rotary(x, cache.HeadNorm("rms"), pos, rot), lambda x: cache.rotary(x, pos, rot)):
+        for t in (pos, rot.freq):
+            x = bf(1, 6, 16, 64).requires_grad_()
+            y = call(x)
+            t.add_(1)
+            with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+                y.sum().backward()
+    # what the cache's own tensors are saved for
+    for dt in (F32, torch.int8):
+        pc = cache.PagedCache.empty(2, 16, 16, dtype=dt, rows=F32)
+        for name in ("K", "V", "weight", "stamp", "scale"):
+            t = getattr(pc, name)
+            if t is None:
+                continue
+            before = t._version
+            cache.append(pc, batch, None, k.float(), k.float())
+            assert t._version > before, name
+            before = t._version
+            cache.evict(pc, batch.table, i32(6), i32(6), 3, 6)
+            assert t._version > before, name
+        before = pc.weight._version
+        cache.attend(pc, batch, k.float(), weight_out=pc.weight)
+        assert pc.weight._version > before
+        lse = torch.empty(6, 16, device="cuda")
+        before = lse._version
+        cache.attend(pc, batch, k.float(), lse=lse)
+        assert lse._version > before
