@@ -322,6 +322,7 @@ class PagedCache:
         self._ref8 = ctypes.byref(self._c8)
         self._ref = self._ref8 if self.codes else ctypes.byref(self._c)
         self._pool = [t for t in (K, V, weight, stamp, scale) if t is not None]
+        self._where = [K] + [t for t in self._pool if t.get_device() != K.get_device()]   # (as Batch's)
 
     def _call(self, name: str):
         """The library's call for this cache."""
@@ -356,6 +357,8 @@ class Batch:
             _need(seen, "seen", (self.B,), torch.int32)
         self.table, self.length, self.q_start, self.seen = table, length, q_start, seen
         self.max_q, self.max_len = int(max_q), int(max_len)
+        # (to check their device by: the table, and what is not with it)
+        self._where = [table] + [t for t in (length, q_start, seen) if t is not None and t.get_device() != table.get_device()]
         self._first = (table.data_ptr(), length.data_ptr(), None if seen is None else seen.data_ptr(),
                        q_start.data_ptr(), self.B, self.max_pages)
 
@@ -383,12 +386,13 @@ def append(pc: PagedCache, batch: Batch, Q, K, V, pos=None, rot: Optional[Rotary
         raise ValueError("a rotation needs positions" if pos is None else "positions need a rotation (rot)")
     turn = None if rot is None else rot.at(pos, T)
     if pc.codes or q_norm is not None or k_norm is not None:
-        st = _here(pc.K, K, V, Q, Q_out, pos, rot and rot.freq, q_norm and q_norm.tensor, k_norm and k_norm.tensor,
-                   batch.table)
+        # (a norm's tensor is the one in use after `at`)
+        qn = None if q_norm is None or Q is None else q_norm.at(Hq)
+        kn = None if k_norm is None else k_norm.at(Hkv)
+        st = _here(*pc._where, K, V, Q, Q_out, pos, rot and rot.freq, q_norm and q_norm.tensor, k_norm and k_norm.tensor,
+                   *batch._where)
         _done(load_library().vp_cache8_append(pc._ref8, batch._for(T), Hq, q, qs, K.data_ptr(), ks, V.data_ptr(), vs,
-                                              None if q_norm is None or Q is None else q_norm.at(Hq),
-                                              None if k_norm is None else k_norm.at(Hkv), turn, qo, st),
-              "vp_cache8_append")
+                                              qn, kn, turn, qo, st), "vp_cache8_append")
     else:
         _done(load_library().vp_cache_append(pc._ref, batch._for(T), Hq, q, qs, K.data_ptr(), ks, V.data_ptr(), vs,
                                              turn, qo, _stream()), "vp_cache_append")
@@ -409,7 +413,7 @@ def read(pc: PagedCache, batch: Batch, T: int, dtype: Optional[torch.dtype] = No
     given = K_out, V_out
     K_out, V_out = new() if K_out is None else K_out, new() if V_out is None else V_out
     shape = (T, pc.Hkv, HEAD_DIM)
-    st = _here(pc.K, K_out, V_out, batch.table)
+    st = _here(*pc._where, K_out, V_out, *batch._where)
     _done(load_library().vp_cache8_read(pc._ref8, batch._for(T), vp.VP_BF16 if dtype is torch.bfloat16 else vp.VP_F32,
                                         _whole(K_out, "K_out", shape, dtype), _whole(V_out, "V_out", shape, dtype),
                                         st), "vp_cache8_read")
@@ -447,7 +451,7 @@ def attend(pc: PagedCache, batch: Batch, Q, causal: bool = True, scale: float = 
         lse = torch.empty(T, Hq, dtype=torch.float32, device=Q.device)
     o, ls, wo = _whole(O, "O", (T, Hq, HEAD_DIM), dt), _whole(lse, "lse", (T, Hq), torch.float32), None
     if pc.codes:
-        _here(pc.K, Q, O, lse, weight_out, ws, batch.table)
+        _here(pc.K, Q, O, lse, weight_out, ws, *batch._where)
     if weight_out is not None:
         if pc.weight is None:
             raise ValueError("the cache has no weights")

@@ -826,3 +826,45 @@ def test_attend_wide_precision_of_the_last_slots(cache, kind, up):  # noqa: F811
         Q[..., 0], k[..., 0], k[n - 40:, :, 0] = 8.0, 0.0, 50.0
     pool.put(0, k, v)
     check_rms(cache, pool, Q, n, q, False, 2.0 ** -10)
+
+
+class Elsewhere(torch.Tensor):
+    """A tensor that says to be on the next device."""
+
+    def get_device(self):
+        return torch.cuda.current_device() + 1
+
+
+def test_batches_and_norms_of_other_devices(cache):  # noqa: F811
+    """Every tensor of a batch, and a norm's gain or bias as exchanged, are looked at before a call passes them on."""
+    there = lambda t: t.as_subclass(Elsewhere)
+    pc = cache.PagedCache.empty(4, 2, 16, torch.int8)
+    rows = normal(1, (2, 2, 64), BF).cuda()
+    own = [i32([[0]]), i32([5]), i32([0, 2]), i32([5])]
+    mk = lambda *t: cache.Batch(*t[:3], 2, 5, t[3])
+    calls = [lambda b: cache.append(pc, b, rows, rows, rows), lambda b: cache.read(pc, b, 2),
+             lambda b: cache.attend(pc, b, rows)]
+    for call in calls:
+        call(mk(*own))
+        for i in range(4):
+            with pytest.raises(ValueError, match="device"):
+                call(mk(*[there(t) if i == j else t for j, t in enumerate(own)]))
+    for plain in (pc, cache.PagedCache.empty(4, 2, 16)):
+        for which in ("q_norm", "k_norm"):
+            for name in ("gain", "bias"):
+                n = cache.HeadNorm("rms", **{name: torch.ones(64, device="cuda")})
+                call = lambda: cache.append(plain, mk(*own), rows, rows, rows, **{which: n})
+                call()
+                setattr(n, name, there(torch.ones(64, device="cuda")))
+                with pytest.raises(ValueError, match="device"):
+                    call()
+    # a plain cache's tensors, in the calls that it shares with codes
+    full = cache.PagedCache.empty(4, 2, 16)
+    for i in range(1, 4):
+        t = [full.K, full.V, full.weight, full.stamp]
+        t[i] = there(t[i])
+        odd = cache.PagedCache(*t)
+        for call in (lambda: cache.append(odd, mk(*own), rows, rows, rows, q_norm=cache.HeadNorm("rms")),
+                     lambda: cache.read(odd, mk(*own), 2)):
+            with pytest.raises(ValueError, match="device"):
+                call()
