@@ -14,6 +14,7 @@ import functools
 from typing import Optional, Sequence
 
 import torch
+from torch.autograd import forward_ad
 
 from . import vp
 from .vp import HEAD_DIM, VPError, _check, _dt, _need, _ptr, _wrote, load_library
@@ -49,6 +50,14 @@ def _here(*tensors) -> int:
         if t is not None and t.get_device() != dev:
             raise ValueError("a tensor is on %s, the current device is %d" % (t.device, dev))
     return _raw_stream(dev)
+
+
+def _no_tangents(*tensors):
+    """Refuses dual tensors (forward-mode derivatives), whose tangents a call through addresses would lose."""
+    if forward_ad._current_level >= 0:
+        for t in tensors:
+            if t is not None and forward_ad.unpack_dual(t).tangent is not None:
+                raise ValueError("forward-mode derivatives are not available (unpack_dual gives a tensor without)")
 
 
 def _rows(t: torch.Tensor, name: str, T: int, H: int, dtype) -> int:
@@ -126,6 +135,7 @@ def rotary(x, pos, rot: Rotary, out: Optional[torch.Tensor] = None, transpose: b
         if out is not None:
             raise ValueError("out would not be part of the gradient's graph")
         return _Rotation.apply(x, pos, rot, transpose)
+    _no_tangents(x, out)
     T, H = x.shape[0], x.shape[1]
     xs = _rows(x, "x", T, H, x.dtype)
     given = out is not None
@@ -217,6 +227,7 @@ def norm_rotary(x, norm: HeadNorm, pos=None, rot: Optional[Rotary] = None, out: 
         if out is not None:
             raise ValueError("out would not be part of the gradient's graph")
         return _NormRotation.apply(x, norm.gain, norm.bias, pos, norm, rot)
+    _no_tangents(x, norm.gain, norm.bias, out)
     T, H = x.shape[0], x.shape[1]
     xs = _rows(x, "x", T, H, x.dtype)
     given = out is not None
@@ -246,6 +257,7 @@ class _NormRotation(torch.autograd.Function):
 
 def _norm_gradients(ctx, g):
     x, gain, bias, pos, _ = ctx.saved_tensors          # (refuses values that were changed in place)
+    _no_tangents(g)
     norm, rot = ctx.norm, ctx.rot
     if norm._at != _memory(gain, bias):                # (it got others, or the graph kept copies)
         norm = HeadNorm(norm.kind, gain, bias, norm.eps)

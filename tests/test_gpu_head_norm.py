@@ -425,3 +425,34 @@ def test_saved_inputs_that_the_operators_overwrite(cache):  # noqa: F811
         before = lse._version
         cache.attend(pc, batch, k.float(), lse=lse)
         assert lse._version > before
+
+
+def test_forward_mode_is_refused(cache):  # noqa: F811
+    """Dual tensors, with and without requires_grad: nothing computes their tangents."""
+    from torch.autograd import forward_ad
+    pos = torch.arange(6, dtype=torch.int32, device="cuda")[:, None]
+    rot, norm = cache.Rotary.make(64), cache.HeadNorm("rms", torch.ones(64, device="cuda"))
+    x = normal(1, (6, 4, 64), F32).cuda()
+    calls = [lambda x, n: cache.norm_rotary(x, n, pos, rot), lambda x, n: cache.norm_rotary(x, n),
+             lambda x, n: cache.norm_rotary(x, n, out=torch.empty_like(x)), lambda x, n: cache.rotary(x, pos, rot)]
+    for call in calls:
+        with forward_ad.dual_level():
+            call(x, norm)                                     # (no dual among them)
+            for leaf in (x, x.clone().requires_grad_()):
+                with pytest.raises((ValueError, RuntimeError, NotImplementedError)):
+                    call(forward_ad.make_dual(leaf, torch.ones_like(x)), norm)
+            with torch.no_grad(), pytest.raises(ValueError, match="forward-mode"):
+                call(forward_ad.make_dual(x, torch.ones_like(x)), norm)
+        call(x, norm)
+    with forward_ad.dual_level():
+        for name in ("gain", "bias"):
+            t = torch.ones(64, device="cuda")
+            with pytest.raises(ValueError, match="forward-mode"):
+                cache.norm_rotary(x, cache.HeadNorm("layer", **{name: forward_ad.make_dual(t, t)}))
+    # a dual gradient that comes back to the operators
+    for call in calls[:2] + calls[3:]:
+        leaf = x.clone().requires_grad_()
+        y = call(leaf, norm)
+        with forward_ad.dual_level():
+            with pytest.raises(ValueError, match="forward-mode"):
+                torch.autograd.grad(y, leaf, forward_ad.make_dual(torch.ones_like(x), x))
