@@ -41,6 +41,7 @@ def _done(code: int, where: str):
 
 
 _device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+_grad_enabled = torch.is_grad_enabled
 
 
 def _here(*tensors) -> int:
@@ -54,10 +55,19 @@ def _here(*tensors) -> int:
 
 def _no_tangents(*tensors):
     """Refuses dual tensors (forward-mode derivatives), whose tangents a call through addresses would lose."""
-    if forward_ad._current_level >= 0:
+    for t in tensors:
+        if t is not None and forward_ad.unpack_dual(t).tangent is not None:
+            raise ValueError("forward-mode derivatives are not available (unpack_dual gives a tensor without)")
+
+
+def _no_gradients(*tensors):
+    """Refuses tensors that require gradients, in calls that have none to give."""
+    if _grad_enabled():
         for t in tensors:
-            if t is not None and forward_ad.unpack_dual(t).tangent is not None:
-                raise ValueError("forward-mode derivatives are not available (unpack_dual gives a tensor without)")
+            if t is not None and t.requires_grad:
+                raise ValueError("the cache's operators have no gradients: call them under torch.no_grad (norm_rotary alone has some)")
+    if forward_ad._current_level >= 0:
+        _no_tangents(*tensors)
 
 
 def _rows(t: torch.Tensor, name: str, T: int, H: int, dtype) -> int:
@@ -135,7 +145,8 @@ def rotary(x, pos, rot: Rotary, out: Optional[torch.Tensor] = None, transpose: b
         if out is not None:
             raise ValueError("out would not be part of the gradient's graph")
         return _Rotation.apply(x, pos, rot, transpose)
-    _no_tangents(x, out)
+    if forward_ad._current_level >= 0:
+        _no_tangents(x, out)
     T, H = x.shape[0], x.shape[1]
     xs = _rows(x, "x", T, H, x.dtype)
     given = out is not None
@@ -227,7 +238,8 @@ def norm_rotary(x, norm: HeadNorm, pos=None, rot: Optional[Rotary] = None, out: 
         if out is not None:
             raise ValueError("out would not be part of the gradient's graph")
         return _NormRotation.apply(x, norm.gain, norm.bias, pos, norm, rot)
-    _no_tangents(x, norm.gain, norm.bias, out)
+    if forward_ad._current_level >= 0:
+        _no_tangents(x, norm.gain, norm.bias, out)
     T, H = x.shape[0], x.shape[1]
     xs = _rows(x, "x", T, H, x.dtype)
     given = out is not None
@@ -257,7 +269,8 @@ class _NormRotation(torch.autograd.Function):
 
 def _norm_gradients(ctx, g):
     x, gain, bias, pos, _ = ctx.saved_tensors          # (refuses values that were changed in place)
-    _no_tangents(g)
+    if forward_ad._current_level >= 0:
+        _no_tangents(g)
     norm, rot = ctx.norm, ctx.rot
     if norm._at != _memory(gain, bias):                # (it got others, or the graph kept copies)
         norm = HeadNorm(norm.kind, gain, bias, norm.eps)
@@ -383,24 +396,30 @@ def append(pc: PagedCache, batch: Batch, Q, K, V, pos=None, rot: Optional[Rotary
            k_norm: Optional[HeadNorm] = None):
     """New tokens into the cache: K [T, Hkv, 64] rotated, V as it is; returns the rotated Q [T, Hq,
     64] (None without Q).  With q_norm or k_norm Q's or K's heads are normalised before the rotation.  A cache
-    of codes gets them quantised."""
+    of codes gets them quantised.  There are no gradients: with norms or codes, rows, gains and biases that require them are
+    refused, but under torch.no_grad."""
     T, Hkv, dt = K.shape[0], pc.Hkv, pc.dtype
     ks, vs = _rows(K, "K", T, Hkv, dt), _rows(V, "V", T, Hkv, dt)
     Hq = qs = q = qo = 0
-    given = Q is not None and Q_out is not None
+    given = ()
     if Q is not None:
         Hq = Q.shape[1]
         qs, q = _rows(Q, "Q", T, Hq, dt), Q.data_ptr()
         if Q_out is None:
             Q_out = torch.empty(T, Hq, HEAD_DIM, dtype=dt, device=Q.device)
+        else:
+            given = (Q_out,)
         qo = _whole(Q_out, "Q_out", (T, Hq, HEAD_DIM), dt)
     if (rot is None) != (pos is None):
         raise ValueError("a rotation needs positions" if pos is None else "positions need a rotation (rot)")
     turn = None if rot is None else rot.at(pos, T)
     if pc.codes or q_norm is not None or k_norm is not None:
-        # (a norm's tensor is the one in use after `at`)
-        qn = None if q_norm is None or Q is None else q_norm.at(Hq)
-        kn = None if k_norm is None else k_norm.at(Hkv)
+        qn = qg = qb = kn = kg = kb = None
+        if q_norm is not None and Q is not None:
+            qn, qg, qb = q_norm.at(Hq), q_norm.gain, q_norm.bias       # (as they are after `at`)
+        if k_norm is not None:
+            kn, kg, kb = k_norm.at(Hkv), k_norm.gain, k_norm.bias
+        _no_gradients(K, V, Q, Q_out, qg, qb, kg, kb)
         st = _here(*pc._where, K, V, Q, Q_out, pos, rot and rot.freq, q_norm and q_norm.tensor, k_norm and k_norm.tensor,
                    *batch._where)
         _done(load_library().vp_cache8_append(pc._ref8, batch._for(T), Hq, q, qs, K.data_ptr(), ks, V.data_ptr(), vs,
@@ -408,7 +427,7 @@ def append(pc: PagedCache, batch: Batch, Q, K, V, pos=None, rot: Optional[Rotary
     else:
         _done(load_library().vp_cache_append(pc._ref, batch._for(T), Hq, q, qs, K.data_ptr(), ks, V.data_ptr(), vs,
                                              turn, qo, _stream()), "vp_cache_append")
-    _wrote(*pc._pool, Q_out if given else None)
+    _wrote(*pc._pool, *given)
     return Q_out if Q is not None else None
 
 
@@ -422,14 +441,17 @@ def read(pc: PagedCache, batch: Batch, T: int, dtype: Optional[torch.dtype] = No
         raise ValueError("rows are read in bf16 or fp32")
     # (zeros: rows past the last sequence's are left as they are)
     new = lambda: torch.zeros(T, pc.Hkv, HEAD_DIM, dtype=dtype, device=pc.K.device)
-    given = K_out, V_out
+    K_given, V_given = K_out is not None, V_out is not None
     K_out, V_out = new() if K_out is None else K_out, new() if V_out is None else V_out
     shape = (T, pc.Hkv, HEAD_DIM)
+    if K_given or V_given:
+        _no_gradients(K_out, V_out)
     st = _here(*pc._where, K_out, V_out, *batch._where)
     _done(load_library().vp_cache8_read(pc._ref8, batch._for(T), vp.VP_BF16 if dtype is torch.bfloat16 else vp.VP_F32,
                                         _whole(K_out, "K_out", shape, dtype), _whole(V_out, "V_out", shape, dtype),
                                         st), "vp_cache8_read")
-    _wrote(*given)
+    if K_given or V_given:
+        _wrote(K_out, V_out)
     return K_out, V_out
 
 
@@ -452,18 +474,22 @@ def attend(pc: PagedCache, batch: Batch, Q, causal: bool = True, scale: float = 
            weight_out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
     """Attention of the new tokens' queries Q [T, Hq, 64] over their sequences' slots: (O [T, Hq,
     64], lse [T, Hq] fp32).  With `weight_out` (it may be pc.weight) the attention weights of
-    the call are added to the slots they fall on."""
+    the call are added to the slots they fall on.  There are no gradients: over codes, a Q that requires them is refused, but
+    under torch.no_grad."""
     T, Hq, _ = Q.shape
     dt = pc.dtype
     qs = _rows(Q, "Q", T, Hq, dt)
-    given = O, lse, weight_out
+    given = O is not None or lse is not None
     if O is None:
         O = torch.empty(T, Hq, HEAD_DIM, dtype=dt, device=Q.device)
     if lse is None:
         lse = torch.empty(T, Hq, dtype=torch.float32, device=Q.device)
     o, ls, wo = _whole(O, "O", (T, Hq, HEAD_DIM), dt), _whole(lse, "lse", (T, Hq), torch.float32), None
     if pc.codes:
-        _here(pc.K, Q, O, lse, weight_out, ws, *batch._where)
+        _no_gradients(Q, O, lse, weight_out)
+        st = _here(pc.K, Q, O, lse, weight_out, ws, *batch._where)
+    else:
+        st = _stream()
     if weight_out is not None:
         if pc.weight is None:
             raise ValueError("the cache has no weights")
@@ -471,9 +497,12 @@ def attend(pc: PagedCache, batch: Batch, Q, causal: bool = True, scale: float = 
     if ws is None:
         ws = attend_workspace(pc, batch, Hq, T)
     w, n = _work(ws)
-    _done(pc._call("attend")(pc._ref, batch._for(T), Hq, Q.data_ptr(), qs, causal, scale, o, ls, wo, w, n, _stream()),
+    _done(pc._call("attend")(pc._ref, batch._for(T), Hq, Q.data_ptr(), qs, causal, scale, o, ls, wo, w, n, st),
           "vp_cache_attend")
-    _wrote(*given)
+    if weight_out is not None:
+        _wrote(O, lse, weight_out)
+    elif given:
+        _wrote(O, lse)
     return O, lse
 
 
@@ -511,7 +540,7 @@ def evict(pc: PagedCache, table, length, seen, keep: int, max_len: int, sink: in
                           int(max_len))
     _done(pc._call("evict")(pc._ref, ctypes.byref(c), int(keep), int(sink), int(recent), wo, so, lo, w, n, _stream()),
           "vp_cache_evict")
-    _wrote(weight_out, stamp_out, length_out, pc.K, pc.V, pc.scale)
+    _wrote(weight_out, stamp_out, length_out, *pc._pool)
     return length_out
 
 
@@ -526,6 +555,8 @@ class StreamLayer:
     it.  `rot`: positions given to step() are applied to Q and K; `q_norm`, `k_norm`: norms of their heads
     before.  `dtype`: of the cache; torch.float8_e4m3fn or torch.int8 for 8-bit codes, `rows` (bf16 when not
     given) then of Q, K, V and O.
+
+    There are no gradients; with norms or codes, rows and parameters that require them are refused, but under torch.no_grad.
 
     A step is enqueued on the current stream without waiting for it.  Its chunks' starts and bounds
     are the host's, so a captured step would repeat those of the capture."""

@@ -237,10 +237,13 @@ def _dt(t: torch.Tensor) -> int:
     raise TypeError("unsupported dtype %s" % t.dtype)
 
 
+_raise_versions = torch._C._increment_version
+
+
 def _wrote(*tensors):
     """After a call that wrote the caller's tensors through their addresses: autograd's versions of them go up, as
     after torch's own in-place operations, so that a backward pass that had saved one refuses."""
-    torch._C._increment_version([t for t in tensors if t is not None])
+    _raise_versions(tensors)
 
 
 def _ptr(t: Optional[torch.Tensor]):
@@ -802,7 +805,7 @@ def tome_plan(K, plan: TomePlan) -> TomePlan:
                                        int(plan.nspecial), _ptr(plan.row), _ptr(plan.row_start),
                                        _ptr(plan.members), _ptr(plan.best), _ptr(plan.score),
                                        _ptr(plan.ws), plan.ws.numel(), _stream()), "vp_tome_plan")
-    _wrote(plan.row, plan.row_start, plan.members, plan.best, plan.score)
+    _wrote(*(t for t in (plan.row, plan.row_start, plan.members, plan.best, plan.score) if t is not None))
     return plan
 
 

@@ -868,3 +868,35 @@ def test_batches_and_norms_of_other_devices(cache):  # noqa: F811
                      lambda: cache.read(odd, mk(*own), 2)):
             with pytest.raises(ValueError, match="device"):
                 call()
+
+
+def test_gradients_are_refused(cache):  # noqa: F811
+    """Calls that have no gradients to give, with something that requires them: refused, where a graph would be
+    expected; taken under no_grad.  The plain cache's own calls take them as ever."""
+    own = (i32([[0]]), i32([5]), i32([0, 2]), 2, 5, i32([5]))
+    batch = cache.Batch(*own)
+    rows, leaf = normal(1, (2, 2, 64), BF).cuda(), normal(1, (2, 2, 64), BF).cuda().requires_grad_()
+    codes, plain = cache.PagedCache.empty(4, 2, 16, torch.int8), cache.PagedCache.empty(4, 2, 16)
+    one = torch.ones(64, device="cuda")
+    gain, bias = cache.HeadNorm("rms", one.clone().requires_grad_()), cache.HeadNorm("rms", one, one.clone().requires_grad_())
+    calls = [lambda x=x: cache.append(codes, batch, *x) for x in ((leaf, rows, rows), (rows, leaf, rows), (rows, rows, leaf))]
+    calls += [lambda pc=pc, n=n, w=w: cache.append(pc, batch, rows, rows, rows, **{w: n})
+              for pc in (codes, plain) for n in (gain, bias) for w in ("q_norm", "k_norm")]
+    calls += [lambda: cache.append(plain, batch, leaf, rows, rows, q_norm=cache.HeadNorm("rms")),
+              lambda: cache.append(codes, batch, rows, rows, rows, Q_out=leaf.detach().clone().requires_grad_()),
+              lambda: cache.attend(codes, batch, leaf), lambda: cache.attend(codes, batch, rows, O=leaf.detach().clone().requires_grad_()),
+              lambda: cache.read(codes, batch, 2, K_out=leaf.detach().clone().requires_grad_()),
+              lambda: cache.StreamLayer(1, 10, 10, 2, q_norm=gain).step(rows, rows, rows),
+              lambda: cache.StreamLayer(1, 10, 10, 2, dtype=torch.int8).step(leaf, rows, rows)]
+    for call in calls:
+        with pytest.raises(ValueError, match="no_grad"):
+            call()
+        with torch.no_grad():
+            call()
+    for call in (lambda: cache.append(plain, batch, leaf, leaf, leaf), lambda: cache.attend(plain, batch, leaf)[0]):
+        assert not call().requires_grad
+    with torch.autograd.forward_ad.dual_level():
+        dual = torch.autograd.forward_ad.make_dual(rows, rows)
+        for call in (lambda: cache.append(codes, batch, rows, dual, rows), lambda: cache.attend(codes, batch, dual)):
+            with pytest.raises(ValueError, match="forward-mode"):
+                call()
