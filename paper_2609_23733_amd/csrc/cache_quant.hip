@@ -25,7 +25,7 @@ __device__ __forceinline__ float beside(double d) {
 template <typename Turn>
 struct Row64 {
     double co[4], si[4];
-    __device__ __forceinline__ void angles(const Turn& w, const RotArgs& r, int64_t t, int c) {
+    __device__ __forceinline__ void angles(const RotArgs& r, int64_t t, int c) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             co[e] = 1.;
@@ -59,8 +59,9 @@ struct Row64 {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const double a = v[2 * e], b = v[2 * e + 1];
-            f[2 * e] = beside(fma(a, co[e], -(b * si[e])));
-            f[2 * e + 1] = beside(fma(b, co[e], a * si[e]));
+            const bool turn = e < w.pairs;
+            f[2 * e] = beside(turn ? fma(a, co[e], -(b * si[e])) : a);
+            f[2 * e + 1] = beside(turn ? fma(b, co[e], a * si[e]) : b);
         }
     }
 };
@@ -151,7 +152,7 @@ __global__ __launch_bounds__(256) void k_cache_append8(AppendArgs a, NormArgs qn
     if (slot >= 0) page = a.c.table[(int64_t)b * a.c.max_pages + (slot >> a.c.page_log2)];
     Row64<HeadTurn<T, INTER, VEC>> w64;
     if constexpr (CODE != CODE_NONE) {
-        if (h0 < hq || hk < Hkv) w64.angles(w, r, t, c);
+        if (h0 < hq || hk < Hkv) w64.angles(r, t, c);
 #pragma unroll
         for (int e = 0; e < 4; ++e) w.co[e] = (float)w64.co[e], w.si[e] = (float)w64.si[e];
     } else {

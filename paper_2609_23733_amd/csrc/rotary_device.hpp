@@ -101,6 +101,7 @@ __device__ __forceinline__ uint32_t max8(uint32_t x) {
 template <typename T, bool INTER, bool VEC>
 struct HeadTurn {
     float co[4], si[4];
+    int pairs;                              // of the four: turned (the first)
     int lo, hi;                             // VEC: first features of the runs
     int sec;                                // and their section
     int i0[VEC ? 1 : 4], i1[VEC ? 1 : 4];   // features of a pair
@@ -111,6 +112,7 @@ struct HeadTurn {
         lo = 8 * c;
         hi = lo + 4;
         sec = 0;
+        pairs = r.dim / 2 - 4 * c;
         if constexpr (VEC) {
             if (8 * c < r.dim) {
                 sec = section(r, 4 * c);
@@ -201,9 +203,12 @@ struct HeadTurn {
             for (int e = 0; e < 4; ++e) y[i0[e]] = (T)f[2 * e], y[i1[e]] = (T)f[2 * e + 1];
         }
     }
+    // (Features that are not turned stay as they are: an infinity times a sine of 0 would reach its neighbour.)
     __device__ __forceinline__ void turn(float (&f)[8]) const {
+        if (VEC && pairs <= 0) return;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
+            if (!VEC && e >= pairs) break;
             const float a = f[2 * e], b = f[2 * e + 1];
             // (fused by hand, so that every kernel rounds alike)
             f[2 * e] = fmaf(a, co[e], -(b * si[e]));
@@ -211,8 +216,10 @@ struct HeadTurn {
         }
     }
     __device__ __forceinline__ void turn_back(float (&f)[8]) const {   // the transpose
+        if (VEC && pairs <= 0) return;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
+            if (!VEC && e >= pairs) break;
             const float a = f[2 * e], b = f[2 * e + 1];
             f[2 * e] = fmaf(a, co[e], b * si[e]);
             f[2 * e + 1] = fmaf(b, co[e], -(a * si[e]));

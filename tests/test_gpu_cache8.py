@@ -900,3 +900,29 @@ def test_gradients_are_refused(cache):  # noqa: F811
         for call in (lambda: cache.append(codes, batch, rows, dual, rows), lambda: cache.attend(codes, batch, dual)):
             with pytest.raises(ValueError, match="forward-mode"):
                 call()
+
+
+@pytest.mark.parametrize("rows", [BF, F32])
+@pytest.mark.parametrize("dim,axes,layout", [(None, 1, "half"), (32, 1, "half"), (32, 2, "interleaved"), (10, 1, "half"), (10, 1, "interleaved")])
+def test_features_that_are_not_turned(cache, rows, dim, axes, layout):  # noqa: F811
+    """Without a norm they pass unchanged, as in the plain append: an infinity or a NaN stays in its feature."""
+    T = 40
+    pos = torch.randint(-1000, 1000, (T, axes), generator=gen(1)).to(torch.int32).cuda()
+    turn = (None, None) if dim is None else (pos, cache.Rotary.make(dim, 100.0, axes, layout))
+    Q, K, V = (normal(s, (T, h, 64), rows) for s, h in ((2, 4), (3, 2), (4, 2)))
+    for x in (Q, K):
+        x[3, 1, 63], x[5, 0, 40], x[6, 1, 33], x[7, 0, 62] = math.inf, -math.inf, math.nan, math.inf
+    Q, K, V = Q.cuda(), K.cuda(), V.cuda()
+    batch = cache.Batch(i32([[0, 1, 2]]), i32([T]), i32([0, T]), T, T, i32([T]))
+    plain = cache.PagedCache.empty(3, 2, 16, rows)
+    want = cache.append(plain, batch, Q, K, V, *turn)
+    # (the turned features: the compiler fuses either product of a pair)
+    same = lambda a, b: torch.allclose(a.float(), b.float(), rtol=2.0 ** -7 if rows == BF else 1e-5, atol=1e-5, equal_nan=True)
+    codes = cache.PagedCache.empty(3, 2, 16, torch.int8, rows=rows)
+    assert same(cache.append(codes, batch, Q, K, V, *turn), want)
+    norm = cache.HeadNorm("rms")
+    other = cache.PagedCache.empty(3, 2, 16, rows)
+    assert same(cache.append(other, batch, Q, K, V, *turn, k_norm=norm), want)
+    cache.append(other, batch, Q, K, V, *turn, q_norm=norm)
+    for a, b in zip(cache.read(other, batch, T), cache.read(plain, batch, T)):
+        assert same(a, b)

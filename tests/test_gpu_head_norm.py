@@ -456,3 +456,22 @@ def test_forward_mode_is_refused(cache):  # noqa: F811
         with forward_ad.dual_level():
             with pytest.raises(ValueError, match="forward-mode"):
                 torch.autograd.grad(y, leaf, forward_ad.make_dual(torch.ones_like(x), x))
+
+
+@pytest.mark.parametrize("dim", [None, 32, 10])
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+def test_infinities_past_the_turned_features(cache, dim, layout):  # noqa: F811
+    """A bias, or a gradient, that is infinite in a feature that is not turned stays in it."""
+    pos = torch.arange(7, dtype=torch.int32, device="cuda")[:, None]
+    turn = () if dim is None else (pos, cache.Rotary.make(dim, layout=layout))
+    bias = torch.zeros(64)
+    bias[63], bias[40] = float("inf"), float("-inf")
+    norm = cache.HeadNorm("layer", None, bias.cuda().requires_grad_())
+    x, g = normal(1, (7, 3, 64), F32).cuda(), normal(2, (7, 3, 64), F32)
+    g[2, 1, 62] = float("inf")
+    y = cache.norm_rotary(x, norm, *turn)
+    odd = torch.zeros(64, dtype=torch.bool)
+    odd[63] = odd[40] = True
+    assert torch.equal(torch.isinf(y.cpu()), odd.expand(7, 3, 64)) and not torch.isnan(y).any()
+    d, = torch.autograd.grad(y, norm.bias, g.cuda())
+    assert torch.isposinf(d[62]) and torch.isfinite(d).sum() == 63
