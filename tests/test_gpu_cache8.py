@@ -926,3 +926,84 @@ def test_features_that_are_not_turned(cache, rows, dim, axes, layout):  # noqa: 
     cache.append(other, batch, Q, K, V, *turn, q_norm=norm)
     for a, b in zip(cache.read(other, batch, T), cache.read(plain, batch, T)):
         assert same(a, b)
+
+
+@pytest.mark.parametrize("where", ["chunk", "before"])
+def test_attend_wide_codes_of_nan(cache, where):  # noqa: F811
+    """e4m3 NaN codes by the kernel of many rows: in the chunk, where some rows see their slots and others do not, and before
+    it, where all do.  Features without one are right wherever the row's logits are numbers."""
+    log("attend8 wide, NaN codes %s" % where)
+    n, q = 4000, 1500
+    pool = Pool8(cache, [n], 4, 32, "e4m3", seed=45)
+    Q = normal(46, (q, 16, 64), BF)
+    p, s = pool.at(0, n)
+    end = n if where == "chunk" else n - q
+    kn, v1, v2 = end - 3, end - 9, end - 400
+    pool.K[p[kn], 1, s[kn], 9] = 255
+    pool.V[p[v1], 0, s[v1], 5], pool.V[p[v2], 2, s[v2], 33] = 127, 255
+    pc, batch = pool.cuda(), pool.batch([q])
+    assert cache.attend_plan(pc, batch, 16, q).shared == 1
+    O, lse = (t.double() for t in cache.attend(pc, batch, Q.cuda(), True))
+    see = n - q + torch.arange(q, device="cuda") + 1
+    sees = torch.arange(n, device="cuda") < see[:, None]
+    for h in range(16):
+        k, v = pool.k[0][:, h // 4].cuda(), pool.v[0][:, h // 4].cuda()
+        ro, rl, _, A, X = whole64(Q[:, h].cuda(), k, v, sees, 0.125)
+        E = (64 * X + n / 16 + 16 + rl.abs()) * U
+        tol = torch.from_numpy(bf16_tol((2 * E[:, None] * A).cpu().numpy(), A.cpu().numpy(), ro.cpu().numpy())).cuda()
+        nan = torch.zeros(q, 64, dtype=torch.bool, device="cuda")
+        lost = torch.zeros(q, dtype=torch.bool, device="cuda")
+        for hk, at, f in ((0, v1, 5), (2, v2, 33)):
+            if h // 4 == hk:
+                nan[:, f] = see > at
+        if h // 4 == 1:
+            lost = see > kn
+            nan[lost] = True
+        assert torch.equal(torch.isnan(O[:, h]), nan), h
+        assert ((O[:, h] - ro).abs() <= tol)[~nan].all(), h
+        assert torch.equal(torch.isnan(lse[:, h]), lost) and ((lse[:, h] - rl).abs() <= 2 * E)[~lost].all(), h
+
+
+@pytest.mark.parametrize("rows", [BF, F32])
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("q", [1, 5, 90])
+def test_weights_over_pages_that_do_not_exist(cache, rows, kind, q):  # noqa: F811
+    """Logits kept (one and five tokens) and formed again: slots on missing pages keep their weights, the others get theirs."""
+    log("attend8 weights, bad pages %s %s q=%d" % (rows, kind, q))
+    n = 4700
+    gone = [s for p in (2, 17, 42) for s in range(16 * p, 16 * p + 16)]
+    pool = Pool8(cache, [n], 1, 16, kind, seed=35, rows=rows)
+    pc, batch = pool.cuda(), pool.batch([q])
+    assert cache.attend_plan(pc, batch, 2, q).logits_kept == (q < 90)
+    check(cache, pool, normal(13, (q, 2, 64), rows), [q], True, 0, gone=gone)
+
+
+def test_another_stream_and_workspace(cache):  # noqa: F811
+    """The same step on the default stream and, at the same time, on two others with workspaces and caches of their own."""
+    log("cache8 streams")
+    rot, norm = cache.Rotary.make(64), cache.HeadNorm("rms", 1 + normal(9, (64,), F32).cuda())
+    pos = torch.tensor([[1999], [899]], dtype=torch.int32, device="cuda")
+    steps = []
+    for k in range(3):
+        pool = Pool8(cache, [2000, 900], 2, 16, "e4m3", seed=41)
+        pc, batch = pool.cuda(), pool.batch([1, 1], seen=[2000, 900])
+        Q, K, V = (normal(i, (2, h, 64), BF).cuda() for i, h in ((1, 8), (2, 2), (3, 2)))
+        steps.append((pool, pc, batch, Q, K, V, cache.attend_workspace(pc, batch, 8, 2).fill_(255)))
+
+    def run(pool, pc, batch, Q, K, V, ws):
+        out = []
+        for _ in range(20):
+            q = cache.append(pc, batch, Q, K, V, pos, rot, q_norm=norm, k_norm=norm)
+            O, lse = cache.attend(pc, batch, q, True, weight_out=pool.gW, ws=ws)
+            out += [O, lse, *cache.read(pc, batch, 2)]
+        return out + [pool.gW]
+
+    torch.cuda.synchronize()
+    outs = []
+    streams = [torch.cuda.current_stream(), torch.cuda.Stream(), torch.cuda.Stream()]
+    for st, args in zip(streams, steps):
+        with torch.cuda.stream(st):
+            outs.append(run(*args))
+    torch.cuda.synchronize()
+    for other in outs[1:]:
+        assert len(other) == len(outs[0]) and all(torch.equal(a, b) for a, b in zip(outs[0], other))
