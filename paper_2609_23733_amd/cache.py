@@ -176,9 +176,9 @@ class _Rotation(torch.autograd.Function):
 
 
 def _memory(gain, bias):
-    """Where gain and bias lie, and their sizes."""
-    a, n = (0, 0) if gain is None else (gain.data_ptr(), gain.numel())
-    return (a, n, 0, 0) if bias is None else (a, n, bias.data_ptr(), bias.numel())
+    """Where gain and bias lie, and how: what the kernels read changes with any of these."""
+    return (gain is not None and (gain.data_ptr(), gain.numel(), gain.stride(), gain.dtype),
+            bias is not None and (bias.data_ptr(), bias.numel(), bias.stride(), bias.dtype))
 
 
 class HeadNorm:
@@ -213,8 +213,10 @@ class HeadNorm:
             raise ValueError("gain and bias are on different devices")
         self.tensor = self.bias if self.gain is None else self.gain       # (for its device)
         self.heads = shape[0] if shape is not None and len(shape) == 2 else None
-        self._at = at = _memory(self.gain, self.bias)
-        self._ref = ctypes.byref(vp.vp_head_norm(_NORMS[self._kind], at[0], at[2], self.heads is not None, self._eps))
+        self._at = _memory(self.gain, self.bias)
+        ptr = lambda t: None if t is None else t.data_ptr()
+        self._ref = ctypes.byref(vp.vp_head_norm(_NORMS[self._kind], ptr(self.gain), ptr(self.bias), self.heads is not None,
+                                                 self._eps))
 
     def at(self, H: int):
         """The C argument for rows of H heads."""

@@ -475,3 +475,28 @@ def test_infinities_past_the_turned_features(cache, dim, layout):  # noqa: F811
     assert torch.equal(torch.isinf(y.cpu()), odd.expand(7, 3, 64)) and not torch.isnan(y).any()
     d, = torch.autograd.grad(y, norm.bias, g.cuda())
     assert torch.isposinf(d[62]) and torch.isfinite(d).sum() == 63
+
+
+def test_parameters_exchanged_for_others_at_their_address(cache):  # noqa: F811
+    """Of as many elements, but of another shape, other strides or another type."""
+    x = normal(1, (5, 4, 64), F32).cuda()
+    G = (1 + normal(2, (64, 64), F32)).cuda()
+    fresh = lambda g: cache.norm_rotary(x, cache.HeadNorm("rms", g))
+    norm = cache.HeadNorm("rms", G[:1])
+    with pytest.raises(ValueError, match="heads"):
+        cache.norm_rotary(x, norm)                            # (one head's gain)
+    norm.gain = G[0]
+    assert torch.equal(cache.norm_rotary(x, norm), fresh(G[0].clone()))
+    norm.gain = G[:1]
+    with pytest.raises(ValueError, match="heads"):
+        cache.norm_rotary(x, norm)
+    for bad in (G[:, 0], G[0].view(torch.int32)):
+        norm = cache.HeadNorm("rms", G[0])
+        norm.gain = bad
+        with pytest.raises(ValueError):
+            cache.norm_rotary(x, norm)
+        norm.gain, norm.bias = G[0], bad
+        with pytest.raises(ValueError):
+            cache.norm_rotary(x, norm)
+        norm.bias = None
+        assert torch.equal(cache.norm_rotary(x, norm), fresh(G[0].clone()))
