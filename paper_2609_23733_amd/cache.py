@@ -388,9 +388,14 @@ class Batch:
         self._where = [table] + [t for t in (length, q_start, seen) if t is not None and t.get_device() != table.get_device()]
         self._first = (table.data_ptr(), length.data_ptr(), None if seen is None else seen.data_ptr(),
                        q_start.data_ptr(), self.B, self.max_pages)
+        self._last = (None, None)
 
     def _for(self, T: int):
-        return ctypes.byref(vp.vp_cache_batch(*self._first, T, self.max_q, self.max_len))
+        """The C argument for calls of T rows."""
+        sizes, last = (T, self.max_q, self.max_len), self._last
+        if last[0] != sizes:            # (made once for the calls of a step: a microsecond each)
+            self._last = last = (sizes, ctypes.byref(vp.vp_cache_batch(*self._first, *sizes)))
+        return last[1]
 
 
 def append(pc: PagedCache, batch: Batch, Q, K, V, pos=None, rot: Optional[Rotary] = None,
