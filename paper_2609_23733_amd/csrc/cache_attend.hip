@@ -64,6 +64,16 @@ struct GeoOf : Geo<T, WIDE> {
     static constexpr int RT = WIDE ? 32 * Geo<T, WIDE>::NB * NW : 32;
 };
 
+// Largest of the lanes' numbers of BITS bits, uniform: bit by bit, without the latency of exchanges.
+template <int BITS>
+__device__ __forceinline__ int top_of_wave(int x) {
+    int r = 0;
+#pragma unroll
+    for (int b = BITS - 1; b >= 0; --b)
+        if (__builtin_amdgcn_ballot_w64(x >= r + (1 << b))) r += 1 << b;
+    return r;
+}
+
 template <int CPT>
 __device__ __forceinline__ void wait_tiles(int behind) {
     // Copies are counted in the order of their issue: all but the `behind` youngest tiles' have
@@ -131,7 +141,7 @@ struct Probs<float, SPLIT> {
 };
 // In fp16, for values that are there in fp16, too (wide workgroups over 8-bit codes): within 2^-11 of each at the cost of a
 // single bf16 value, but for probabilities below 2^-14, whose step is 2^-24 (errors of 1.66e-3 of the result, with
-// single bf16 values 2.33e-3; a view over 43,968 slots 265 -> 274 us, for the range that settle() watches).
+// single bf16 values 2.33e-3; a view over 43,968 slots 265 -> 274 us, for the range that totals() watches).
 struct HalfProbs {
     f16x8 v[2];
     __device__ __forceinline__ void set(const f32x16& s) {
@@ -538,6 +548,7 @@ __global__ __launch_bounds__((64 * GeoOf<T, WIDE, CODE>::NW), 2) void k_cache_at
         // 2^-9, fp16's least number 2^-24) to 2^kUp times 2^vexp (2^6 448, and up to twice that with a scale that is no power of two,
         // lies below 65,504).  Elsewhere (`far` past kUp + kDown) the range is done again over bf16 values.
         constexpr int kUp = 6, kDown = 15;
+        __shared__ int s_range[kCode ? 2 * G::NW : 1];   // per wave: far + 1, 31 - what its rows allow for it
         u32x4 codes;
         uint32_t sc = 0;
         const bool isv = wave >= 4;
@@ -571,11 +582,8 @@ __global__ __launch_bounds__((64 * GeoOf<T, WIDE, CODE>::NW), 2) void k_cache_at
             const int k = c0 + lane < c1 ? c0 + lane : c1 - 1;
             // (slots past the end: the last one; a unit past the last one has its page)
             const int64_t at = (((int64_t)id * a.c.Hkv + hk) << a.c.page_log2) + (k & page_mask);
-            uint32_t b = (a.c.scale[at] >> 16) & 0x7fffu;
-            b = b < 0x7f80u ? b : 0u;
-#pragma unroll
-            for (int o = 32; o >= 1; o >>= 1) b = max(b, (uint32_t)__shfl_xor((int)b, o));
-            vexp = __builtin_amdgcn_readfirstlane((int)(b >> 7)) - 127 + 3;
+            const int e = (int)(a.c.scale[at] >> 23 & 255u);
+            vexp = top_of_wave<8>(e < 255 ? e : 0) - 127 + 3;
         };
         auto put_codes = [&](int t) {
             u32x4 v[2];
@@ -767,16 +775,19 @@ __global__ __launch_bounds__((64 * GeoOf<T, WIDE, CODE>::NW), 2) void k_cache_at
             typedef std::conditional_t<kCode, f16, bf16> P16;
             // Codes: a block's sums into l, and where one comes near fp16's largest value, references raised so that it is 2^kLift.
             // (s: the block's powers still.)
-            auto settle = [&](auto width, Logits& s, BlockP& p) __attribute__((always_inline)) {
+            auto totals = [&](auto width, float (&tot)[G::NB]) __attribute__((always_inline)) {
                 constexpr int NB = decltype(width)::value;
-                float tot[NB], top = 0.f;
+                float top = 0.f;
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) {
                     tot[nb] = (sum[nb][0] + sum[nb][1]) + (sum[nb][2] + sum[nb][3]);
                     w[nb].l += tot[nb];
                     top = maximum(top, tot[nb]);
                 }
-                if (!__builtin_amdgcn_ballot_w64(!(top < 65504.f))) return;
+                return __builtin_amdgcn_ballot_w64(!(top < 65504.f)) != 0;
+            };
+            auto raise = [&](auto width, Logits& s, const float (&tot)[G::NB], BlockP& p) __attribute__((always_inline)) {
+                constexpr int NB = decltype(width)::value;
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) {
                     const float both = maximum(tot[nb], __shfl_xor(tot[nb], 32));
@@ -818,9 +829,21 @@ __global__ __launch_bounds__((64 * GeoOf<T, WIDE, CODE>::NW), 2) void k_cache_at
                     pn[nb].v[i >> 2][(2 * i) & 7] = (P16)s[nb][2 * i];
                     pn[nb].v[i >> 2][(2 * i + 1) & 7] = (P16)s[nb][2 * i + 1];
                 };
-                exponent(0);
+                auto power = [&](int u) {
+                    const int nb = u % NB, i = u / NB;
+                    s[nb][2 * i] = exp2f_fast(s[nb][2 * i]);
+                    s[nb][2 * i + 1] = exp2f_fast(s[nb][2 * i + 1]);
+                };
+                // Units (two logits) whose powers come before slot u of the 8 NB: one each; codes: all before the last, whose MFMA hides
+                // a part of the totals.
+                constexpr int kSlots = 8 * NB, kBusy = kCode ? kSlots - 1 : kSlots;
+                auto units = [](int u) { return u >= kBusy ? kSlots : (u * kSlots + kBusy - 1) / kBusy; };
+                float tot[G::NB];
+                bool near = false;
 #pragma unroll
-                for (int u = 0; u < 8 * NB; ++u) {
+                for (int u = 0; u < units(1); ++u) exponent(u);
+#pragma unroll
+                for (int u = 0; u < kSlots; ++u) {
                     const int i = u / NB, nb = u % NB, n = kOf[i];
                     if (nb == 0) {
                         if (i < 5) f[i + 3] = kOf[i + 3] < 4 ? key_at(k, kOf[i + 3]) : value_at(v, kOf[i + 3] - 4);
@@ -829,14 +852,20 @@ __global__ __launch_bounds__((64 * GeoOf<T, WIDE, CODE>::NW), 2) void k_cache_at
                     Rows<T>& x = w[nb];
                     if (n < 4) sn[nb] = mfma_bf16(f[i], x.qb[n], n ? sn[nb] : zero_f32x16());
                     else x.o[n & 1] = mfma_value(f[i], pv[nb].v[(n - 4) >> 1], x.o[n & 1]);
-                    if (u + 1 < 8 * NB) exponent(u + 1);
-                    s[nb][2 * i] = exp2f_fast(s[nb][2 * i]);
-                    s[nb][2 * i + 1] = exp2f_fast(s[nb][2 * i + 1]);
-                    if (u > 0) add(u - 1);
+#pragma unroll
+                    for (int a = units(u + 1); a < units(u + 2); ++a) exponent(a);
+#pragma unroll
+                    for (int a = units(u); a < units(u + 1); ++a) power(a);
+#pragma unroll
+                    for (int a = u > 0 ? units(u - 1) : 0; a < units(u); ++a) add(a);
+                    if (kCode && u == kSlots - 1) near = totals(width, tot);
                     __builtin_amdgcn_sched_barrier(0);
                 }
-                add(8 * NB - 1);
-                if constexpr (kCode) settle(width, s, pn);
+                if constexpr (kCode) {
+                    if (__builtin_expect(near, 0)) raise(width, s, tot, pn);
+                } else {
+                    add(kSlots - 1);
+                }
             };
             auto probs = [&](Logits& s, int k0, BlockP& p) __attribute__((always_inline)) {
 #pragma unroll
@@ -852,7 +881,11 @@ __global__ __launch_bounds__((64 * GeoOf<T, WIDE, CODE>::NW), 2) void k_cache_at
                     }
                     p[nb].set(s[nb]);
                 }
-                if constexpr (kCode) settle(std::integral_constant<int, G::NB>(), s, p);
+                if constexpr (kCode) {
+                    const std::integral_constant<int, G::NB> width;
+                    float tot[G::NB];
+                    if (__builtin_expect(totals(width, tot), 0)) raise(width, s, tot, p);
+                }
             };
             auto body = [&](auto mask, auto width, int t) __attribute__((always_inline)) {   // second block of tile t, first of tile t + 1
                 lds_char *cur = tile_at(t), *next = tile_at(t + 1);
@@ -915,18 +948,11 @@ __global__ __launch_bounds__((64 * GeoOf<T, WIDE, CODE>::NW), 2) void k_cache_at
                 for (int t = 1; t < nt; ++t) arrive(t);
             }
             if constexpr (kCode) {
-                // What is off by fp16's range.  A scale out of its bounds.  Sums past fp32's range, rows whose first
-                // logits were -inf alone.  Probabilities below 2^-14 are off by 2^-25 at most: n slots together by no more than 2^-8
-                // of a row's largest result (each apart, of as much / sqrt(n)), if that is 2^-17 n times the largest value.  A first slot
-                // without values of its own may so have 98 % of the weight of 9,000 slots.
-                __shared__ int s_far[G::NW];
-#pragma unroll
-                for (int o = 32; o >= 1; o >>= 1) far = max(far, __shfl_xor(far, o));
-                if (lane == 0) s_far[wave] = far;
-                __syncthreads();
-                for (int v = 4; v < G::NW; ++v) far = max(far, s_far[v]);
-                redo = far > kUp + kDown;
-                const float most = far < 0 ? 0.f : __builtin_amdgcn_ldexpf(CODE == CODE_E4M3 ? 448.f : 128.f, far - kDown);
+                // What fp16's range does not hold is done again.  Scales out of their bounds.  Results or sums past fp32's range, rows
+                // whose first logits were -inf alone.  Probabilities below 2^-14 are off by 2^-25 at most: n slots together by no
+                // more than 2^-8 of a row's largest result (each apart, of as much / sqrt(n)), if that is 2^-17 n times the largest value.
+                // A first slot without values of its own may so have 98 % of the weight of 9,000 slots.
+                int room = 31;   // largest `far` that the rows allow
                 if (alive)
 #pragma unroll
                     for (int nb = 0; nb < G::NB; ++nb) {
@@ -935,13 +961,18 @@ __global__ __launch_bounds__((64 * GeoOf<T, WIDE, CODE>::NW), 2) void k_cache_at
 #pragma unroll
                         for (int r = 0; r < 16; ++r) top = maximum(maximum(top, fabsf(w[nb].o[0][r])), fabsf(w[nb].o[1][r]));
                         top = maximum(top, __shfl_xor(top, 32));
-                        redo = redo || __builtin_amdgcn_ballot_w64(n > 0 && !(top >= (float)n * most * 0x1p-17f));
+                        const float q = top / ((float)n * (CODE == CODE_E4M3 ? 448.f : 128.f) * 0x1p-17f);
+                        int here = max(-1, kDown - 127 + (int)(__float_as_uint(q) >> 23));
+                        if (!(__builtin_amdgcn_ldexpf(top, vexp) <= 3.4028235e38f)) here = -2;
+                        if (n > 0) room = min(room, here);
 #pragma unroll
                         for (int r = 0; r < 16; ++r) {
                             w[nb].o[0][r] = __builtin_amdgcn_ldexpf(w[nb].o[0][r], vexp);
                             w[nb].o[1][r] = __builtin_amdgcn_ldexpf(w[nb].o[1][r], vexp);
                         }
                     }
+                const int f = top_of_wave<5>(far + 1), l = top_of_wave<6>(31 - room);
+                if (lane == 0) s_range[wave] = f, s_range[G::NW + wave] = l;
                 halves = false;
             }
         } else if constexpr (WIDE) {
@@ -1138,7 +1169,7 @@ __global__ __launch_bounds__((64 * GeoOf<T, WIDE, CODE>::NW), 2) void k_cache_at
         }
         if constexpr (WIDE) {
             __shared__ int s_redo[G::NW];
-            redo = redo || !pw.sane || overflown();
+            redo = redo || !pw.sane || (!kCode && overflown());
             if (alive) {
                 bool far = false;
 #pragma unroll
@@ -1153,7 +1184,13 @@ __global__ __launch_bounds__((64 * GeoOf<T, WIDE, CODE>::NW), 2) void k_cache_at
                 for (int v = 0; v < G::NW; ++v) any |= s_redo[v];
                 return any != 0;
             };
-            if (any_wave()) {
+            bool again = any_wave();
+            if constexpr (kCode) {
+                int f = 0, l = 0;
+                for (int v = 0; v < G::NW; ++v) f = max(f, s_range[v]), l = max(l, s_range[G::NW + v]);
+                again = again || f - 1 > kUp + kDown || f - 1 > 31 - l;
+            }
+            if (again) {
                 if constexpr (!G::kBf) load_q();
 #pragma unroll 1
                 for (int pass = 0; pass < 2; ++pass) {
