@@ -57,7 +57,8 @@ struct Geo {
 };
 
 // Wide workgroups over 8-bit codes: eight waves, which share the decoding of a tile (1,374 tokens over 43,968 slots of 16
-// heads, e4m3: 273 us, with four waves 298; kernel alone, among other calls 258, 960 TFLOP/s, as over a bf16 cache).
+// heads, e4m3, with bf16 probabilities: 273 us, with four waves 298; as they are now 279, of which the kernel takes 271, 920
+// TFLOP/s, over a bf16 cache 260).
 template <typename T, bool WIDE, int CODE>
 struct GeoOf : Geo<T, WIDE> {
     static constexpr int NW = CODE == CODE_NONE ? Geo<T, WIDE>::NW : 8;
@@ -141,7 +142,8 @@ struct Probs<float, SPLIT> {
 };
 // In fp16, for values that are there in fp16, too (wide workgroups over 8-bit codes): within 2^-11 of each at the cost of a
 // single bf16 value, but for probabilities below 2^-14, whose step is 2^-24 (errors of 1.66e-3 of the result, with
-// single bf16 values 2.33e-3; a view over 43,968 slots 265 -> 274 us, for the range that totals() watches).
+// single bf16 values 2.33e-3; a view over 43,968 slots 266 -> 279 us, 16 ragged sequences of up to 400 tokens over 3,000 slots 69 ->
+// 75, for the sums of every block that totals() looks at).
 struct HalfProbs {
     f16x8 v[2];
     __device__ __forceinline__ void set(const f32x16& s) {
@@ -434,8 +436,8 @@ __global__ __launch_bounds__((64 * GeoOf<T, WIDE, CODE>::NW), 2) void k_cache_at
         // Codes, one workgroup per compute unit: a row tile of everything before the next, so that the last one, which may
         // have few rows, comes last; and all ranges of a sequence one after the other, as the compute units that an
         // XCD's workgroups go to follow from their numbers (with those of a long sequence always every fourth, 149 us
-        // for 82), turned by three from tile to tile.  Ragged: six sequences of up to 700 tokens over 20,000 slots 103 us, 167 in the other
-        // order; 16 of up to 400 over 3,000 62 and 81 (both before few rows were spread over the SIMDs).
+        // for 82), turned by three from tile to tile.  Ragged, 16 heads: six sequences of up to 700 tokens over 20,000 slots, four
+        // key heads, 135 us, in the order of the other caches 170; 16 of up to 400 over 3,000, 16 key heads, 75 and 92.
         const int turns = (heads * a.nsplit + 7) >> 3;
         rt = (blockIdx.x >> 3) / turns;
         x = ((blockIdx.x >> 3) - rt * turns + 3 * rt) % turns * 8 + (blockIdx.x & 7);
@@ -449,8 +451,8 @@ __global__ __launch_bounds__((64 * GeoOf<T, WIDE, CODE>::NW), 2) void k_cache_at
     const CacheSeq sq = cache_seq(a.c, b);
     const int nrows = sq.nq * a.G;
     if (rt * G::RT >= nrows) return;
-    // A tile of few rows: one group of rows for each of four waves (a SIMD each), the other sees nothing.  (16 sequences of up
-    // to 400 tokens over 3,000 slots 76 -> 69 us.  200 rows as seven waves' groups, two waves a SIMD: 37 -> 44.)
+    // A tile of few rows: one group of rows for each of four waves (a SIMD each), the other sees nothing.  (The 16 sequences
+    // above 82 -> 75 us.  200 rows as seven waves' groups, two waves a SIMD: 37 -> 44.)
     const bool slim = kCode && nrows - rt * G::RT <= 16 * G::NW;
     const int wave_rows = slim ? 32 : 32 * G::NB, row0 = rt * G::RT + (WIDE ? wave * wave_rows : 0);
     const int tile_last = rt * G::RT + G::RT - 1 < nrows ? rt * G::RT + G::RT - 1 : nrows - 1;
@@ -1749,10 +1751,13 @@ void attend_plan(AttendArgs* a) {
         // 8-bit codes: narrow workgroups, which each decode what they read, by all the work if ragged (31 tokens of four key
         // heads, ragged to 10,992 slots: 31 us in the six ranges of one round, 28 in eight, 27 in eleven); wide ones, whose
         // time per slot grows with the waves that have rows, and of which a compute unit has one.  The shorter estimate
-        // decides, in us: 16 heads, 1,000 tokens over 1,000 slots 22 narrow, 29 wide; 400 over 5,000 46 and 34; 90 over 20,000 41
-        // and 36; 40 over 20,000 31 and 34; ragged to 400 tokens over 3,000 slots, 16 sequences, 81 and 62.  Ragged batches
+        // decides, in us: 16 heads, 1,000 tokens over 1,000 slots 22 narrow, 33 wide; 400 over 5,000 42 and 37; 90 over 20,000 37
+        // and 36; 200 over 3,000 22 and 24; ragged to 400 tokens over 3,000 slots, 16 sequences, 81 and 75.  Ragged batches
         // whose rows would fill less than a seventh of the wide tiles stay narrow (30 sequences of up to 102 tokens and 8,333
-        // slots: 73 and 91).
+        // slots: 75 and 96).  What the lengths are is guessed: 0.6 of the work that the wide tiles' bounds allow, and 0.8 of
+        // the narrow estimate.  Of 44 random batches (2 to 32 sequences, of up to 70 to 1,374 tokens and 300 to 30,000 slots, 2 to
+        // 16 key heads) the picks take 1.06 of the better kernel's time on the average, narrow alone 1.31, wide alone 1.08; with
+        // 1 for the 0.8 1.05, with 1 for the 0.6 1.06, without the seventh 1.05: these decide near ties.
         double t = divide(work_items(attend_rows(*a), false), 0, rows <= 16 ? 0.008 : bf ? 0.017 : 0.03, 192, 512, 0.05, false, 1);
         if (!equal) t *= 0.8;   // (the others' lengths are less than assumed more often than not)
         const int64_t narrow = best;
