@@ -556,7 +556,7 @@ vp_status vp_norm_rotary_grad(const vp_head_norm *norm, const vp_rotary_spec *ro
  * of it, and codes rounded to nearest, ties to even: an error of at most half a step, scale / 2 (INT8) or
  * 2^-4 of the value and scale 2^-10 (E4M3), but for values that would round to 2^128: they get the code below.  A row with a NaN or an infinity gets scale NaN and codes 0.  Codes and
  * scales of other origin are taken as they are: scales other than powers of two cost calls of many rows another rounding, of
- * code times scale to bf16. */
+ * code times scale to bf16 (values: to fp16 where its range does). */
 typedef struct {
     vp_cache cache;
     void *scale;
@@ -574,9 +574,9 @@ vp_status vp_cache8_append(const vp_cache8 *cache, const vp_cache_batch *batch, 
 
 /* Attend as vp_cache_attend (arguments, workspace, plan, weights, rows that see nothing) over code times scale; O and Q in
  * `rows`.  A NaN in a slot's value (its scale, or an E4M3 code) makes results of rows that see the slot NaN, at
- * least in its feature, and reaches no other row.  bf16 rows: probabilities as sums of two bf16 values, or in calls of many
- * rows over many slots (vp_cache_plan's `shared`) as fp16 values, within 2^-11, where that range does.  fp32 rows: exact products, fp32 sums; a
- * row of Q with an infinity gives NaN. */
+ * least in its feature, and reaches no other row.  bf16 rows: probabilities as sums of two bf16 values (2^-16 of each); in
+ * calls of many rows over many slots (vp_cache_plan's `shared`) in fp16 (2^-11), or as such sums for rows and values that
+ * fp16's range does not hold.  fp32 rows: exact products, fp32 sums; a row of Q with an infinity gives NaN. */
 size_t vp_cache8_attend_workspace_bytes(const vp_cache8 *cache, const vp_cache_batch *batch,
                                         int32_t Hq);
 vp_status vp_cache8_attend_plan(const vp_cache8 *cache, const vp_cache_batch *batch, int32_t Hq,
