@@ -576,7 +576,8 @@ vp_status vp_cache8_append(const vp_cache8 *cache, const vp_cache_batch *batch, 
  * `rows`.  A NaN in a slot's value (its scale, or an E4M3 code) makes results of rows that see the slot NaN, at
  * least in its feature, and reaches no other row.  bf16 rows: probabilities as sums of two bf16 values (2^-16 of each); in
  * calls of many rows over many slots (vp_cache_plan's `shared`) in fp16 (2^-11 of each, or 2^-31 of the row's largest
- * in the range), or as such sums for rows and values that fp16's range does not hold.  fp32 rows: exact products, fp32 sums; a row of Q with an infinity gives NaN. */
+ * in the range), or as such sums for rows and values that fp16's range does not hold.  fp32 rows: exact products, fp32
+ * sums; a row of Q with an infinity gives NaN. */
 size_t vp_cache8_attend_workspace_bytes(const vp_cache8 *cache, const vp_cache_batch *batch,
                                         int32_t Hq);
 vp_status vp_cache8_attend_plan(const vp_cache8 *cache, const vp_cache_batch *batch, int32_t Hq,

@@ -141,9 +141,9 @@ struct Probs<float, SPLIT> {
     __device__ __forceinline__ void set(const f32x16& s) { v = s; }
 };
 // In fp16, for values that are there in fp16, too (wide workgroups over 8-bit codes): within 2^-11 of each at the cost of a
-// single bf16 value, but for probabilities below 2^-14, whose step is 2^-24, where the row's largest is 2^6 or more (errors of 1.66e-3 of the result, with
-// single bf16 values 2.33e-3; a view over 43,968 slots 266 -> 279 us, 16 ragged sequences of up to 400 tokens over 3,000 slots 69 ->
-// 75, for the sums of every block that totals() looks at).
+// single bf16 value, but for probabilities below 2^-14, whose step is 2^-24, where the row's largest is 2^6 or more
+// (errors of 1.66e-3 of the result, with single bf16 values 2.33e-3; a view over 43,968 slots 266 -> 279 us, 16 ragged
+// sequences of up to 400 tokens over 3,000 slots 69 -> 75, for the sums of every block that totals() looks at).
 struct HalfProbs {
     f16x8 v[2];
     __device__ __forceinline__ void set(const f32x16& s) {
